@@ -1,0 +1,540 @@
+"""The serving and training operators around the expert layer, as measurable calls.
+
+Four operators that a Mixture-of-Experts block needs next to the layer itself:
+
+* ``norm``    residual addition and root-mean-square norm, forward (with an
+              MX8 output: e4m3 values, one power-of-two scale per 32) and
+              backward.
+* ``route``   routing from logits: softmax or sigmoid scores, a balance bias
+              that only selects, expert groups, top-k, renormalised gates;
+              forward and backward.
+* ``linear``  the product with a matrix held in MX4 (e2m1 values, one
+              power-of-two scale per 32 along the reduction), from one row on.
+* ``experts`` the expert layer's forward with MX4 weights, on bf16 or MX8
+              activations, from one token to a prefill.
+
+Every case is one call of one of them.  With ``own`` unset `run` computes the
+operator from elementary torch operations in float32; with it set it calls the
+library.  `exact` gives the same outputs from the definitions in float64.
+
+MX8 and MX4 hold blocks of 32 consecutive values x with the smallest power of
+two 2^e for which max|x| <= 448 * 2^e (MX8) or 6 * 2^e (MX4), and x / 2^e
+rounded to the nearest e4m3 (e2m1) value, ties to even.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-6
+# e2m1: code -> value (bit 3 is the sign)
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0)
+
+
+def listed():
+    return [
+        # The norm in front of the layer, a decode step of 16 sequences: latency.
+        dict(name="norm_decode_16", op="norm", back=False, T=16, h=7168, dtype="bf16",
+             residual=True, mx8=True),
+        # The same in a prefill: the residual stream out, the bf16 input of the
+        # router and the MX8 input of the experts.
+        dict(name="norm_prefill_32k", op="norm", back=False, T=32768, h=7168, dtype="bf16",
+             residual=True, mx8=True),
+        # Its gradient in training, an odd number of tokens (workload 3's hidden size).
+        dict(name="norm_backward", op="norm", back=True, T=16385, h=4096, dtype="bf16",
+             residual=True, mx8=False),
+        # A 256-expert router's selection, one decode step: sigmoid scores, balance
+        # bias, 4 of 8 groups.
+        dict(name="route_decode_16", op="route", back=False, T=16, E=256, k=8, score="sigmoid",
+             bias=True, groups=8, top_groups=4, renorm=True, scale=2.5),
+        # The same over the tokens of workload 5.
+        dict(name="route_131k", op="route", back=False, T=131072, E=256, k=8, score="sigmoid",
+             bias=True, groups=8, top_groups=4, renorm=True, scale=2.5),
+        # Softmax gates without renormalisation: every logit has a gradient.
+        dict(name="route_backward", op="route", back=True, T=100003, E=160, k=6, score="softmax",
+             bias=False, groups=1, top_groups=1, renorm=False, scale=1.0),
+        # One token through one projection of workload 4's sizes.
+        dict(name="linear_1", op="linear", T=1, N=4096, K=7168, mx8=False),
+        # A decode batch through workload 3's FC1 (2 F = 28672), MX8 activations.
+        dict(name="linear_batch_48", op="linear", T=48, N=28672, K=4096, mx8=True),
+        # One token through the 32 fine-grained local experts of workload 4.
+        dict(name="experts_decode_1", op="experts", T=1, h=7168, F=2048, E=32, k=8, mx8=False),
+        # A decode batch through them: every expert has rows.
+        dict(name="experts_decode_64", op="experts", T=64, h=7168, F=2048, E=32, k=8, mx8=True),
+        # A short ragged prefill through workload 2's experts, bf16 activations.
+        dict(name="experts_prefill_1027", op="experts", T=1027, h=2048, F=1408, E=16, k=4,
+             mx8=False),
+        # A prefill of workload 4's tokens.
+        dict(name="experts_prefill_8192", op="experts", T=8192, h=7168, F=2048, E=32, k=8,
+             mx8=True),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _log_by(rng, by, lo, hi):
+    return max(lo, _log_int(rng, lo, hi) // by * by)
+
+
+def draw(rng):
+    op = rng.choice(("norm", "route", "linear", "experts", "experts"))
+    if op == "norm":
+        back = rng.random() < 0.4
+        dtype = "f32" if rng.random() < 0.25 else "bf16"
+        return dict(op=op, back=back, T=_log_int(rng, 1, 32768), h=_log_by(rng, 64, 512, 7168),
+                    dtype=dtype, residual=rng.random() < 0.8,
+                    mx8=not back and dtype == "bf16" and rng.random() < 0.6)
+    if op == "route":
+        E = rng.choice((8, 16, 32, 64, 64, 128, 160, 256, 256))
+        groups = rng.choice((1, 4, 8)) if E >= 64 else 1
+        top = rng.randint(groups // 2, groups - 1) if groups > 1 else 1
+        return dict(op=op, back=rng.random() < 0.4, T=_log_int(rng, 1, 131072), E=E,
+                    k=rng.randint(2, min(8, E // 2)), score=rng.choice(("softmax", "sigmoid")),
+                    bias=rng.random() < 0.5, groups=groups, top_groups=top,
+                    renorm=rng.random() < 0.6, scale=rng.choice((1.0, 2.5)))
+    if op == "linear":
+        return dict(op=op, T=_log_int(rng, 1, 600), N=_log_by(rng, 32, 256, 28672),
+                    K=_log_by(rng, 32, 256, 14336), mx8=rng.random() < 0.5)
+    while True:
+        E = rng.choice((8, 16, 32, 32, 64))
+        c = dict(op=op, T=_log_int(rng, 1, 8192), h=_log_by(rng, 64, 512, 7168),
+                 F=_log_by(rng, 64, 256, 4096), E=E, k=rng.randint(1, 8),
+                 mx8=rng.random() < 0.5)
+        # the plain form multiplies every token with every expert
+        slots, size = c["T"] * E * c["F"], E * c["h"] * c["F"]
+        if size <= 5e8 and slots <= 5e8 and slots * c["h"] <= 3e12:
+            return c
+
+
+# ----------------------------------------------------------------- inputs
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed) * 1000003 + 29)
+    return g
+
+
+def _normal(gen, shape, std=1.0, dtype=torch.float32):
+    x = torch.empty(shape, dtype=dtype, device="cuda")
+    flat = x.view(-1)
+    for i in range(0, flat.numel(), 1 << 27):
+        n = min(1 << 27, flat.numel() - i)
+        flat[i:i + n].copy_(torch.randn(n, generator=gen, device="cuda") * std)
+    return x
+
+
+def _mx4_rows(gen, E, N, K):
+    """Row-major MX4 matrices as a checkpoint holds them: codes [E, N, K/2]
+    (value 2 i in the low half of byte i) and scale bytes [E, N, K/32] (2^(s -
+    127)).  The codes are distributed as those of normal weights, of a
+    standard deviation of about 0.02."""
+    # values of a normal block, its largest (about 2.2 sigma) at 6, by 8-bit quantile
+    q = torch.special.ndtri((torch.arange(256, dtype=torch.float64) + 0.5) / 256) * (5.0 / 2.2)
+    mag = torch.tensor(E2M1[:8], dtype=torch.float64)
+    code = (q.abs()[:, None] - mag).abs().argmin(1) + 8 * (q < 0)
+    pair = (code[:, None] * 16 + code).reshape(-1).to(torch.uint8).cuda()
+    codes = torch.empty((E, N, K // 2), dtype=torch.uint8, device="cuda")
+    for e in range(E):
+        codes[e] = pair[torch.randint(0, 65536, (N, K // 2), generator=gen, device="cuda",
+                                      dtype=torch.int32)]
+    scales = torch.randint(119, 122, (E, N, K // 32), generator=gen, device="cuda",
+                           dtype=torch.int32).to(torch.uint8)
+    return codes, scales
+
+
+def _mx8_rows(x):
+    """x [T, h] as MX8: e4m3 bytes [T, h] and scale bytes [T, h/32]."""
+    b = x.float().view(x.shape[0], -1, 32)
+    m, ex = torch.frexp(b.abs().amax(2))
+    e = (ex - 9 + (m > 0.875).int()).clamp(min=-127)
+    q = torch.ldexp(b, -e[..., None]).to(torch.float8_e4m3fn)
+    return q.view(torch.uint8).view(x.shape), (e + 127).to(torch.uint8)
+
+
+def _topk_sorted(v, k):
+    """The k largest of each row, largest first, ties to the lowest index."""
+    v, i = torch.sort(v, dim=1, descending=True, stable=True)
+    return v[:, :k], i[:, :k]
+
+
+def _clear_margin(c, logits, bias):
+    """Rows whose selection and its order no rounding of a score to float32
+    can change: neighbours among the k + 1 largest, and the groups at the
+    boundary, are apart by well over it."""
+    z = logits.double()
+    s = torch.sigmoid(z) if c["score"] == "sigmoid" else torch.softmax(z, 1)
+    s = s + bias.double() if bias is not None else s
+    ok = torch.ones(len(s), dtype=torch.bool, device=s.device)
+    if c["groups"] > 1:
+        per = s.view(len(s), c["groups"], -1)
+        g = per.topk(2, dim=2).values.sum(2)
+        gs = torch.sort(g, dim=1, descending=True).values
+        ok &= gs[:, c["top_groups"] - 1] - gs[:, c["top_groups"]] > 4e-6 * gs[:, 0].abs()
+        keep = g >= gs[:, c["top_groups"] - 1:c["top_groups"]]
+        s = torch.where(keep[..., None], per, -torch.inf).view(len(s), -1)
+    v = torch.sort(s, dim=1, descending=True).values[:, :c["k"] + 1]
+    gap = v[:, :-1] - v[:, 1:]
+    return ok & (gap > 4e-6 * v[:, :1].abs()).all(1)
+
+
+def _logits(c, gen):
+    """Router logits, tokens of different temperature, and the balance bias."""
+    T, E = c["T"], c["E"]
+    bias = _normal(gen, (E,), 0.05) if c["bias"] else None
+    z = _normal(gen, (T, E), 1.0) * (0.5 + 1.5 * torch.rand((T, 1), generator=gen, device="cuda"))
+    for _ in range(50):
+        bad = (~_clear_margin(c, z, bias)).nonzero()[:, 0]
+        if len(bad) == 0:
+            break
+        z[bad] = _normal(gen, (len(bad), E), 1.5)
+    return z, bias
+
+
+def prepare(case, seed):
+    c, gen, dev = case, _gen(seed), "cuda"
+    s = dict(case)
+    if c["op"] == "norm":
+        T, h = c["T"], c["h"]
+        dt = torch.bfloat16 if c["dtype"] == "bf16" else torch.float32
+        s["X"] = _normal(gen, (T, h), 1.0, dt)
+        s["w"] = (1 + _normal(gen, (h,), 0.1)).to(dt)
+        if c["back"]:
+            s["dY"] = _normal(gen, (T, h), 1.0, dt)
+            s["dS"] = _normal(gen, (T, h), 1.0, dt) if c["residual"] else None
+            s["dX"] = torch.empty((T, h), dtype=dt, device=dev)
+            s["dw"] = torch.empty((h,), device=dev)
+            return s
+        s["R"] = _normal(gen, (T, h), 3.0, dt) if c["residual"] else None
+        s["S"] = torch.empty((T, h), dtype=dt, device=dev) if c["residual"] else None
+        s["Y"] = torch.empty((T, h), dtype=dt, device=dev)
+        if c["mx8"]:
+            s["Q"] = torch.empty((T, h), dtype=torch.uint8, device=dev)
+            s["QS"] = torch.empty((T, h // 32), dtype=torch.uint8, device=dev)
+            s["V"] = torch.empty((T, h), dtype=dt, device=dev)
+        return s
+    if c["op"] == "route":
+        T, E, k = c["T"], c["E"], c["k"]
+        s["logits"], s["bias_"] = _logits(c, gen)
+        s["idx"] = torch.empty((T, k), dtype=torch.int32, device=dev)
+        s["gates"] = torch.empty((T, k), device=dev)
+        if c["back"]:
+            s["idx"], _ = _route_plain(c, s["logits"], s["bias_"])
+            s["dgates"] = _normal(gen, (T, k))
+            s["dlogits"] = torch.empty((T, E), device=dev)
+        return s
+    if c["op"] == "linear":
+        T, N, K = c["T"], c["N"], c["K"]
+        X = _normal(gen, (T, K), 1.0, torch.bfloat16)
+        s["X"], s["XS"] = _mx8_rows(X) if c["mx8"] else (X, None)
+        codes, scales = _mx4_rows(gen, 1, N, K)
+        s["Wc"], s["Ws"] = _laid_out(1, N, K, codes, scales) if own else (codes, scales)
+        s["Y"] = torch.empty((T, N), dtype=torch.bfloat16, device=dev)
+        return s
+    T, h, F, E, k = c["T"], c["h"], c["F"], c["E"], c["k"]
+    X = _normal(gen, (T, h), 1.0, torch.bfloat16)
+    s["X"], s["XS"] = _mx8_rows(X) if c["mx8"] else (X, None)
+    # skewed experts: a popularity added to each token's preference
+    z = _normal(gen, (T, E), 1.0) + _normal(gen, (1, E), 0.5)
+    v, i = _topk_sorted(z, k)
+    v = torch.exp(v - v[:, :1])
+    s["idx"], s["gates"] = i.to(torch.int32).contiguous(), (v / v.sum(1, keepdim=True)).contiguous()
+    c1, s1 = _mx4_rows(gen, E, 2 * F, h)
+    c2, s2 = _mx4_rows(gen, E, h, F)
+    s["W1c"], s["W1s"] = _laid_out(E, 2 * F, h, c1, s1) if own else (c1, s1)
+    s["W2c"], s["W2s"] = _laid_out(E, h, F, c2, s2) if own else (c2, s2)
+    s["Yout"] = torch.empty((T, h), dtype=torch.bfloat16, device=dev)
+    return s
+
+
+def _laid_out(E, N, K, codes, scales):
+    """The matrices in the library's order, once per program."""
+    import paper_2511_21431_amd as mf
+    return mf.memfine_mx4_pack(E, N, K, codes, scales)
+
+
+# ------------------------------------------------------------- plain forms
+def _mx8_values(q, s):
+    """float32 values of e4m3 bytes [T, h] with scale bytes [T, h/32]."""
+    b = q.view(torch.float8_e4m3fn).float().view(q.shape[0], -1, 32)
+    return torch.ldexp(b, s.int()[..., None] - 127).view(q.shape)
+
+
+def _mx4_values(codes, scales):
+    """float32 values [..., K] of MX4 codes [..., K/2], scale bytes [..., K/32]."""
+    t = torch.tensor(E2M1, device=codes.device)
+    pairs = torch.stack((t[torch.arange(256, device=codes.device) & 15],
+                         t[torch.arange(256, device=codes.device) >> 4]), 1)
+    v = pairs[codes.int()].view(*scales.shape, 32)
+    return v.mul_(torch.exp2(scales.float() - 127)[..., None]).flatten(-2)
+
+
+def _norm_plain(s):
+    x = s["X"].float()
+    if s["residual"]:
+        # the sum is stored in the residual stream's type, and the norm is of what is stored
+        S = (x + s["R"].float()).to(s["X"].dtype)
+        x = S.float()
+    y = x * torch.rsqrt((x * x).mean(1, keepdim=True) + EPS) * s["w"].float()
+    out = {"Y": y.to(s["X"].dtype)}
+    if s["residual"]:
+        out["S"] = S
+    if s["mx8"]:
+        out["V"] = _mx8_values(*_mx8_rows(y)).to(s["X"].dtype)
+    return out
+
+
+def _norm_back_plain(s):
+    x, dy = s["X"].float(), s["dY"].float()
+    r = torch.rsqrt((x * x).mean(1, keepdim=True) + EPS)
+    n = x * r
+    dn = dy * s["w"].float()
+    dx = r * (dn - n * (dn * n).mean(1, keepdim=True))
+    if s["dS"] is not None:
+        dx = dx + s["dS"].float()
+    return {"dX": dx.to(s["X"].dtype), "dw": (dy * n).sum(0)}
+
+
+def _scores(c, z):
+    if c["score"] == "sigmoid":
+        return 1 / (1 + torch.exp(-z))
+    e = torch.exp(z - z.amax(1, keepdim=True))
+    return e / e.sum(1, keepdim=True)
+
+
+def _route_plain(c, logits, bias):
+    p = _scores(c, logits)
+    v = p + bias if bias is not None else p
+    if c["groups"] > 1:
+        per = v.view(len(v), c["groups"], -1)
+        g = torch.sort(per, dim=2, descending=True).values[..., :2].sum(2)
+        _, gi = _topk_sorted(g, c["top_groups"])
+        keep = (gi[:, :, None] == torch.arange(c["groups"], device=v.device)).any(1)
+        v = torch.where(keep[..., None], per, -torch.inf).view(len(v), -1)
+    _, i = _topk_sorted(v, c["k"])
+    g = torch.gather(p, 1, i)
+    if c["renorm"]:
+        g = g / g.sum(1, keepdim=True)
+    return i.to(torch.int32).contiguous(), g * c["scale"]
+
+
+def _route_back_plain(s):
+    p = _scores(s, s["logits"])
+    i, dg = s["idx"].long(), s["dgates"] * s["scale"]
+    g = torch.gather(p, 1, i)
+    if s["renorm"]:
+        total = g.sum(1, keepdim=True)
+        dg = (dg - (dg * g).sum(1, keepdim=True) / total) / total
+    dp = torch.zeros_like(p).scatter(1, i, dg)
+    if s["score"] == "sigmoid":
+        return dp * p * (1 - p)
+    return p * (dp - (dp * p).sum(1, keepdim=True))
+
+
+def _linear_plain(s):
+    x = _mx8_values(s["X"], s["XS"]) if s["mx8"] else s["X"].float()
+    return (x @ _mx4_values(s["Wc"][0], s["Ws"][0]).T).to(torch.bfloat16)
+
+
+def _swiglu(u, F, mx8):
+    a = u[..., :F] / (1 + torch.exp(-u[..., :F])) * u[..., F:]
+    # MX8 activations: the second product's input is rounded to MX8 as well
+    return _mx8_values(*_mx8_rows(a.reshape(-1, F))).view(a.shape) if mx8 else a
+
+
+def _experts_plain(s):
+    T, h, F, E, k = s["T"], s["h"], s["F"], s["E"], s["k"]
+    x = _mx8_values(s["X"], s["XS"]) if s["mx8"] else s["X"].float()
+    if T * k <= E:  # fewer slots than experts: each slot with its expert's matrices
+        e = s["idx"].long().view(-1)
+        W1, W2 = (_mx4_values(s[a][e], s[b][e]) for a, b in (("W1c", "W1s"), ("W2c", "W2s")))
+        xs = x.repeat_interleave(k, 0)
+        a = _swiglu(torch.bmm(W1, xs[:, :, None]).view(T * k, 2 * F), F, s["mx8"])
+        y = torch.bmm(W2, a[:, :, None]).view(T, k, h)
+        return (y * s["gates"][..., None]).sum(1).to(torch.bfloat16)
+    # all experts on all tokens, the gates zero where a token does not go
+    G = ((s["idx"][..., None] == torch.arange(E, device=x.device)) * s["gates"][..., None]).sum(1)
+    u = x @ _mx4_values(s["W1c"], s["W1s"]).view(E * 2 * F, h).T
+    a = _swiglu(u.view(T, E, 2 * F), F, s["mx8"]) * G[..., None]
+    W2 = _mx4_values(s["W2c"], s["W2s"]).permute(0, 2, 1).reshape(E * F, h)
+    return (a.view(T, E * F) @ W2).to(torch.bfloat16)
+
+
+# --------------------------------------------------------------------- run
+def run(state):
+    s = state
+    if not own:
+        if s["op"] == "norm":
+            return _norm_back_plain(s) if s["back"] else _norm_plain(s)
+        if s["op"] == "route":
+            if s["back"]:
+                return {"dlogits": _route_back_plain(s)}
+            i, g = _route_plain(s, s["logits"], s["bias_"])
+            return {"idx": i, "gates": g}
+        return {"Y": _linear_plain(s) if s["op"] == "linear" else _experts_plain(s)}
+    import paper_2511_21431_amd as mf
+    if s["op"] == "norm" and s["back"]:
+        mf.memfine_norm_bwd(EPS, s["X"], s["w"], s["dY"], s["dX"], s["dw"], dS=s["dS"])
+        return {"dX": s["dX"], "dw": s["dw"]}
+    if s["op"] == "norm":
+        out = {"Y": s["Y"]}
+        mf.memfine_norm_fwd(EPS, s["X"], s["w"], R=s["R"], S=s["S"], Y=s["Y"], Q=s.get("Q"),
+                            QS=s.get("QS"))
+        if s["residual"]:
+            out["S"] = s["S"]
+        if s["mx8"]:
+            mf.memfine_mx8_unpack(s["Q"], s["QS"], s["V"])
+            out["V"] = s["V"]
+        return out
+    if s["op"] == "route":
+        g = mf.make_gating(E=s["E"], k=s["k"], score=s["score"], groups=s["groups"],
+                           top_groups=s["top_groups"], renorm=s["renorm"], scale=s["scale"])
+        if s["back"]:
+            mf.memfine_route_bwd(g, s["logits"], s["idx"], s["dgates"], s["dlogits"])
+            return {"dlogits": s["dlogits"]}
+        mf.memfine_route_fwd(g, s["logits"], s["idx"], s["gates"], bias=s["bias_"])
+        return {"idx": s["idx"], "gates": s["gates"]}
+    if s["op"] == "linear":
+        mf.memfine_linear_mx4(s["N"], s["K"], s["X"], s["Wc"], s["Ws"], s["Y"], XS=s["XS"])
+        return {"Y": s["Y"]}
+    shape = mf.make_shape(s["T"], s["h"], s["F"], s["E"], s["k"], mf.BF16)
+    mf.memfine_moe_fwd_mx4(shape, 1, s["X"], s["idx"], s["gates"], s["W1c"], s["W1s"], s["W2c"],
+                           s["W2s"], s["Yout"], XS=s["XS"])
+    return {"Y": s["Yout"]}
+
+
+def work(case):
+    c = case
+    if c["op"] == "norm":
+        T, h = c["T"], c["h"]
+        n, es = T * h, 2 if c["dtype"] == "bf16" else 4
+        if c["back"]:
+            return {"bytes": es * n * (4 if c["residual"] else 3) + (es + 4) * h, "flops": 10.0 * n}
+        held = es * (4 if c["residual"] else 2) + (1 + 1 / 32 if c["mx8"] else 0)
+        return {"bytes": held * n + es * h, "flops": 6.0 * n}
+    if c["op"] == "route":
+        T, E, k = c["T"], c["E"], c["k"]
+        # the backward of renormalised softmax gates and of sigmoid scores needs the selected
+        # experts' logits alone
+        dense = not c["back"] or (c["score"] == "softmax" and not c["renorm"])
+        logits = T * E if dense else T * k
+        return {"bytes": 4.0 * (logits + (T * E if c["back"] else 0)) + 8.0 * T * k,
+                "flops": 6.0 * T * E}
+    xb = 1 + 1 / 32 if c["mx8"] else 2
+    wb = 0.5 + 1 / 32
+    if c["op"] == "linear":
+        T, N, K = c["T"], c["N"], c["K"]
+        return {"bytes": wb * N * K + xb * T * K + 2.0 * T * N, "flops": 2.0 * T * N * K}
+    T, h, F, E, k = c["T"], c["h"], c["F"], c["E"], c["k"]
+    # experts that have a token, at most
+    used = min(E, T * k)
+    return {"bytes": wb * 3 * used * h * F + (xb + 2) * T * h + 8.0 * T * k,
+            "flops": 6.0 * T * k * h * F}
+
+
+# ------------------------------------------------------- definitions, 64 bits
+def _e4m3_64(v):
+    """float64 v, |v| <= 448, to the nearest e4m3 value, ties to even."""
+    e = torch.frexp(v)[1].double() - 1
+    step = torch.exp2(e.clamp(min=-6) - 3)
+    return torch.round(v / step) * step
+
+
+def _mx8_64(x):
+    b = x.reshape(-1, 32)
+    top = b.abs().amax(1, keepdim=True)
+    e = torch.ceil(torch.log2(top / 448)).clamp(min=-127)
+    e = torch.where(top > 448 * torch.exp2(e), e + 1, e)
+    e = torch.where(top <= 448 * torch.exp2(e - 1), e - 1, e).clamp(min=-127)
+    e = torch.where(top > 0, e, torch.zeros_like(e))
+    return (_e4m3_64(b / torch.exp2(e)) * torch.exp2(e)).reshape(x.shape)
+
+
+def _held_64(q, s):
+    """float64 values of an MX8 tensor from its bits."""
+    b = q.long()
+    ex, man = (b >> 3) & 15, b & 7
+    mag = torch.where(ex > 0, (8 + man).double() * torch.exp2(ex.double() - 10),
+                      man.double() * 2.0 ** -9)
+    v = torch.where(b >= 128, -mag, mag)
+    return v * torch.exp2(s.double() - 127).repeat_interleave(32, -1)
+
+
+def _weights_64(codes, scales):
+    """float64 matrix [N, K] of row-major MX4 codes and scales, from the bits of e2m1."""
+    c = torch.stack((codes & 15, codes >> 4), -1).flatten(-2).long()
+    ex, man = (c >> 1) & 3, c & 1
+    mag = torch.where(ex > 0, (2 + man).double() * torch.exp2(ex.double() - 2), 0.5 * man.double())
+    v = torch.where(c >= 8, -mag, mag)
+    return v * torch.exp2(scales.double() - 127).repeat_interleave(32, -1)
+
+
+def exact(case, seed):
+    """The outputs in float64 (tensors too large for that to be quick: none here)."""
+    global own
+    held, own = own, False  # the row-major weights
+    try:
+        s = prepare(case, seed)
+    finally:
+        own = held
+    d = torch.float64
+    if s["op"] == "norm" and s["back"]:
+        x, dy, w = s["X"].to(d), s["dY"].to(d), s["w"].to(d)
+        h = x.shape[1]
+        ms = x.square().sum(1, keepdim=True) / h + EPS
+        # y_j = w_j x_j ms^(-1/2): d y_j / d x_i = w_j ms^(-1/2) (delta_ij - x_i x_j / (h ms))
+        proj = (dy * w * x).sum(1, keepdim=True) / (h * ms)
+        dx = (dy * w - x * proj) / ms.sqrt()
+        if s["dS"] is not None:
+            dx += s["dS"].to(d)
+        return {"dX": dx, "dw": (dy * x / ms.sqrt()).sum(0)}
+    if s["op"] == "norm":
+        x, out = s["X"].to(d), {}
+        if s["R"] is not None:
+            x = (x + s["R"].to(d))
+            out["S"] = x
+            x = x.to(s["X"].dtype).to(d) if s["X"].dtype == torch.bfloat16 else x.float().to(d)
+        out["Y"] = x / (x.square().mean(1, keepdim=True) + EPS).sqrt() * s["w"].to(d)
+        if s["mx8"]:
+            out["V"] = _mx8_64(out["Y"])
+        return out
+    if s["op"] == "route":
+        z = s["logits"].to(d)
+        p = torch.sigmoid(z) if s["score"] == "sigmoid" else torch.softmax(z, 1)
+        if s["back"]:
+            # by autograd, from the forward's formula on the held selection
+            z = z.clone().requires_grad_()
+            p = torch.sigmoid(z) if s["score"] == "sigmoid" else torch.softmax(z, 1)
+            g = p.gather(1, s["idx"].long())
+            g = s["scale"] * (g / g.sum(1, keepdim=True) if s["renorm"] else g)
+            (dz,) = torch.autograd.grad((g * s["dgates"].to(d)).sum(), z)
+            return {"dlogits": dz}
+        v = p + s["bias_"].to(d) if s["bias_"] is not None else p.clone()
+        if s["groups"] > 1:
+            per = v.view(len(v), s["groups"], -1)
+            two = per.topk(2, dim=2).values.sum(2)
+            drop = torch.ones_like(two, dtype=torch.bool)
+            drop.scatter_(1, two.topk(s["top_groups"], dim=1).indices, False)
+            v = per.masked_fill(drop[..., None], -torch.inf).reshape(len(v), -1)
+        i = v.topk(s["k"], dim=1).indices
+        g = p.gather(1, i)
+        g = s["scale"] * (g / g.sum(1, keepdim=True) if s["renorm"] else g)
+        return {"idx": i.to(torch.int32), "gates": g}
+    x = _held_64(s["X"], s["XS"]) if s["mx8"] else s["X"].to(d)
+    if s["op"] == "linear":
+        return {"Y": x @ _weights_64(s["Wc"][0], s["Ws"][0]).T}
+    F, Y = s["F"], torch.zeros(x.shape, dtype=d, device=x.device)
+    for e in range(s["E"]):
+        t, j = (s["idx"] == e).nonzero(as_tuple=True)
+        if len(t) == 0:
+            continue
+        u = x[t] @ _weights_64(s["W1c"][e], s["W1s"][e]).T
+        a = u[:, :F] * torch.sigmoid(u[:, :F]) * u[:, F:]
+        if s["mx8"]:
+            a = _mx8_64(a)
+        y = a @ _weights_64(s["W2c"][e], s["W2s"][e]).T
+        Y.index_add_(0, t, y * s["gates"][t, j].to(d)[:, None])
+    return {"Y": Y}
