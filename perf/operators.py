@@ -253,7 +253,7 @@ def prepare(case, seed):
 def _laid_out(E, N, K, codes, scales):
     """The matrices in the library's order, once per program."""
     import paper_2511_21431_amd as mf
-    return mf.memfine_mx4_pack(E, N, K, codes, scales)
+    return mf.memfine_mxw_pack(E, N, K, codes, scales)
 
 
 # ------------------------------------------------------------- plain forms
@@ -386,7 +386,7 @@ def run(state):
         if s["residual"]:
             out["S"] = s["S"]
         if s["mx8"]:
-            mf.memfine_mx8_unpack(s["Q"], s["QS"], s["V"])
+            mf.memfine_mx_values(s["Q"], s["QS"], s["V"])
             out["V"] = s["V"]
         return out
     if s["op"] == "route":
@@ -398,10 +398,10 @@ def run(state):
         mf.memfine_route_fwd(g, s["logits"], s["idx"], s["gates"], bias=s["bias_"])
         return {"idx": s["idx"], "gates": s["gates"]}
     if s["op"] == "linear":
-        mf.memfine_linear_mx4(s["N"], s["K"], s["X"], s["Wc"], s["Ws"], s["Y"], XS=s["XS"])
+        mf.memfine_linear_mxw(s["N"], s["K"], s["X"], s["Wc"], s["Ws"], s["Y"], XS=s["XS"])
         return {"Y": s["Y"]}
     shape = mf.make_shape(s["T"], s["h"], s["F"], s["E"], s["k"], mf.BF16)
-    mf.memfine_moe_fwd_mx4(shape, 1, s["X"], s["idx"], s["gates"], s["W1c"], s["W1s"], s["W2c"],
+    mf.memfine_moe_fwd_mxw(shape, 1, s["X"], s["idx"], s["gates"], s["W1c"], s["W1s"], s["W2c"],
                            s["W2s"], s["Yout"], XS=s["XS"])
     return {"Y": s["Yout"]}
 
