@@ -401,6 +401,160 @@ int memfine_router_bwd(const memfine_shape* shape, const void* d_X, const void* 
                        void* d_dX, float* d_dWr, int32_t accumulate_dX, int32_t accumulate_dWr,
                        const memfine_allocator* alloc, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Around the layer: the norm in front of it, routing from logits, and the
+ * layer's forward with 4-bit weights.  Pointers must be 16-byte aligned
+ * (MEMFINE_ERR_INVALID_ARG otherwise, as for a null pointer that is not
+ * optional); T = 0 does nothing but what is said below.
+ *
+ * The MX formats hold blocks of 32 consecutive values of a row and one scale
+ * byte s per block, 2^(s - 127): MX8 has e4m3 values (one byte each), MX4 has
+ * e2m1 values (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; two to a byte,
+ * the first in the low half).  The scale is the smallest power of two, at
+ * least 2^-127, that keeps the block's largest magnitude within 448 (MX8) or 6
+ * (MX4) times it; values are rounded to nearest, ties to even.  A block that
+ * holds a NaN or an infinity gets s = 255, and all its values are NaN.
+ */
+
+/*
+ * Residual addition and root-mean-square norm of T rows of h elements (h a
+ * multiple of 64, at most 16384, else MEMFINE_ERR_UNSUPPORTED; T < 2^31):
+ *   S = X + R            rounded to dtype; without R (null) S is X
+ *   Y = S / sqrt(mean(S^2) + eps) * w
+ *   d_X, d_R  dtype [T, h];   d_w  dtype [h];   eps >= 0
+ *   d_S   dtype [T, h] out, may be null (must be null without R); may be d_X
+ *         or d_R itself
+ *   d_Y   dtype [T, h] out, may be null;
+ *   d_Q, d_QS  uint8 [T, h], [T, h / 32] out: the MX8 form of the unrounded
+ *         Y; both or neither
+ * At least one of d_Y and d_Q is asked for.  fp32 arithmetic.
+ */
+int memfine_norm_fwd(int64_t T, int32_t h, int32_t dtype, float eps, const void* d_X,
+                     const void* d_R, const void* d_w, void* d_S, void* d_Y, uint8_t* d_Q,
+                     uint8_t* d_QS, void* stream);
+
+/*
+ * Its gradient.  With r = 1 / sqrt(mean(X^2) + eps), X the norm's input (the
+ * forward's S):
+ *   dX = r (dY w - X r^2 mean(dY w X)) + dS    dtype [T, h]: the gradient of X
+ *        and, with a residual, of R alike; d_dS (the gradient that reaches S
+ *        from elsewhere) may be null; d_dX may be d_dY or d_dS itself
+ *   dw = sum over rows of dY X r               float [h], added to d_dw when
+ *        accumulate_dw = 1, else overwriting it (T = 0: zeros)
+ * Sums over rows are formed in a fixed order.  Working memory (partial sums of
+ * dw) comes from `alloc` as for the layer's calls.
+ */
+int memfine_norm_bwd(int64_t T, int32_t h, int32_t dtype, float eps, const void* d_X,
+                     const void* d_w, const void* d_dY, const void* d_dS, void* d_dX, float* d_dw,
+                     int32_t accumulate_dw, const memfine_allocator* alloc, void* stream);
+
+/* The values of an MX8 tensor, d_Q [T, h] with d_QS [T, h / 32] (h a multiple
+ * of 32), as d_out, dtype [T, h]: exact in float, and in bf16 unless a value is
+ * below its subnormals. */
+int memfine_mx_values(int64_t T, int32_t h, const uint8_t* d_Q, const uint8_t* d_QS,
+                       int32_t dtype, void* d_out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Routing from logits, for routers other than the renormalised softmax top-k
+ * of memfine_router_fwd.  Per token:
+ *   p_e = softmax over the E experts, or sigmoid, of the logits
+ *   v_e = p_e + bias_e (no bias: p_e); selects, and enters nothing else
+ *   groups > 1: the experts form `groups` runs of E / groups; a group's score
+ *     is the sum of its two largest v (its v, when E = groups), and only
+ *     experts of the top_groups best groups (equal: the lower one) are left
+ *   the k experts of largest v, in that order (equal: the lower id)
+ *   gate_j = scale p_j, or, with renorm, scale p_j / (sum of the selected p)
+ * A logit of -inf, of the lowest finite float or a NaN masks its expert: p = 0,
+ * and it is selected, with gate 0, only when fewer than k others are left
+ * (a token without any other gets k masked experts and zero gates).  +inf
+ * counts as the largest finite float.
+ * 1 <= E <= 256, 1 <= k <= 16 (MEMFINE_ERR_UNSUPPORTED otherwise), k <=
+ * top_groups E / groups, groups <= 16 dividing E.
+ */
+#define MEMFINE_SCORE_SOFTMAX 0
+#define MEMFINE_SCORE_SIGMOID 1
+typedef struct memfine_gating {
+  int32_t E, k;
+  int32_t score;       /* MEMFINE_SCORE_*                                  */
+  int32_t groups;      /* 1: no groups                                     */
+  int32_t top_groups;  /* 1 <= top_groups <= groups                        */
+  int32_t renorm;      /* 0 or 1                                           */
+  float scale;         /* finite                                           */
+} memfine_gating;
+
+/* d_logits float [T, E]; d_bias float [E] or null; d_idx int32 [T, k] and
+ * d_gates float [T, k] out. */
+int memfine_route_fwd(int64_t T, const memfine_gating* g, const float* d_logits,
+                      const float* d_bias, int32_t* d_idx, float* d_gates, void* stream);
+
+/* The gradient of the gates, with the selection held fixed: d_dlogits float
+ * [T, E] is overwritten, from the forward's d_logits and d_idx and d_dgates
+ * float [T, k].  Softmax gates without renorm reach every logit, the others
+ * those of the selected experts alone.  Slots whose id lies outside [0, E)
+ * pass no gradient; slots of one token with the same id add up. */
+int memfine_route_bwd(int64_t T, const memfine_gating* g, const float* d_logits,
+                      const int32_t* d_idx, const float* d_dgates, float* d_dlogits, void* stream);
+
+/* The router's product by itself, for routing from logits: d_logits = X Wr^T,
+ * float [T, E] (shapes, types and limits of memfine_router_fwd; k is not
+ * used), and its gradients dX = dlogits Wr, dWr = dlogits^T X (as
+ * memfine_router_bwd, dlogits being rounded to the shape's dtype for the
+ * products). */
+int memfine_router_logits(const memfine_shape* shape, const void* d_X, const void* d_Wr,
+                          float* d_logits, void* stream);
+int memfine_router_logits_bwd(const memfine_shape* shape, const void* d_X, const void* d_Wr,
+                              const float* d_dlogits, void* d_dX, float* d_dWr,
+                              int32_t accumulate_dX, int32_t accumulate_dWr,
+                              const memfine_allocator* alloc, void* stream);
+
+/* ------------------------------------------------------------------------
+ * MX4 matrices.  W [N, K] (N a multiple of 16, K of 32, N, K < 2^30) is held
+ * in the matrix cores' order in two buffers of memfine_mxw_code_bytes(N, K)
+ * and memfine_mxw_scale_bytes(N, K) bytes (< 0: invalid sizes); E matrices of
+ * one size follow each other in both.  memfine_mxw_pack lays out row-major codes
+ * uint8 [E, N, K / 2] and scales uint8 [E, N, K / 32] as a checkpoint holds
+ * them; memfine_mxw_quantize rounds values dtype [E, N, K];
+ * memfine_mxw_unpack gives the values back, dtype [E, N, K].
+ */
+int64_t memfine_mxw_code_bytes(int32_t N, int32_t K);
+int64_t memfine_mxw_scale_bytes(int32_t N, int32_t K);
+int memfine_mxw_pack(int32_t E, int32_t N, int32_t K, const uint8_t* d_row_codes,
+                     const uint8_t* d_row_scales, uint8_t* d_codes, uint8_t* d_scales,
+                     void* stream);
+int memfine_mxw_quantize(int32_t E, int32_t N, int32_t K, int32_t dtype, const void* d_W,
+                         uint8_t* d_codes, uint8_t* d_scales, void* stream);
+int memfine_mxw_unpack(int32_t E, int32_t N, int32_t K, const uint8_t* d_codes,
+                       const uint8_t* d_scales, int32_t dtype, void* d_W, void* stream);
+
+/*
+ * Y [T, N] = X [T, K] W^T with W in MX4 (d_codes, d_scales), T < 2^31.
+ *   d_X  bf16 [T, K] when d_XS is null, else e4m3 bytes [T, K] with the scales
+ *        d_XS [T, K / 32] (MX8, as memfine_norm_fwd gives them)
+ *   d_Y  y_dtype [T, N], MEMFINE_BF16 or MEMFINE_F32
+ * Sums in fp32.  On bf16 activations the products are those of the held
+ * values; on MX8 the matrix core forms sums of 128 products to about 2^-15 of
+ * the largest of them.
+ */
+int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const uint8_t* d_XS,
+                       const uint8_t* d_codes, const uint8_t* d_scales, int32_t y_dtype, void* d_Y,
+                       void* stream);
+
+/*
+ * The chunked forward, memfine_moe_fwd, with W1 and W2 in MX4 (E matrices
+ * [2F, h] and [h, F]); shape.dtype must be MEMFINE_BF16 (Y's type).
+ *   d_X  bf16 [T, h] when d_XS is null; the SwiGLU output is then rounded to
+ *        bf16 for the second product.  With d_XS: MX8, e4m3 [T, h] and scales
+ *        [T, h / 32]; the SwiGLU output is then rounded to MX8 as well.
+ * Everything else as memfine_moe_fwd.  memfine_moe_mxw_workspace_bytes: the
+ * working memory of its largest chunk (mx8 = 1: with d_XS).
+ */
+int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* d_X,
+                        const uint8_t* d_XS, const int32_t* d_idx, const float* d_gates,
+                        const uint8_t* d_W1_codes, const uint8_t* d_W1_scales,
+                        const uint8_t* d_W2_codes, const uint8_t* d_W2_scales, void* d_Y,
+                        const memfine_allocator* alloc, void* stream);
+int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chunks, int32_t mx8);
+
 /* Static, human-readable text for a status code. */
 const char* memfine_status_str(int status);
 
@@ -428,7 +582,15 @@ const char* memfine_status_str(int status);
 #define MEMFINE_K_ROUTER_BWD_DX 13 /* router: dz per token, dX contribution */
 #define MEMFINE_K_ROUTER_WGRAD 14 /* router: split-K partials of dz^T X     */
 #define MEMFINE_K_ROUTER_REDUCE 15 /* router: sum of the partials into dWr  */
-#define MEMFINE_K_NUM        16
+#define MEMFINE_K_NORM_FWD   16
+#define MEMFINE_K_NORM_BWD   17
+#define MEMFINE_K_ROUTE_FWD  18 /* routing from logits                      */
+#define MEMFINE_K_ROUTE_BWD  19
+#define MEMFINE_K_MX_LINEAR  20 /* MX4: the single linear map               */
+#define MEMFINE_K_MX_FC1     21 /* MX4: FC1 + SwiGLU                        */
+#define MEMFINE_K_MX_FC2     22
+#define MEMFINE_K_MX_COMBINE 23
+#define MEMFINE_K_NUM        24
 
 typedef struct memfine_kernel_stat {
   int64_t launches;

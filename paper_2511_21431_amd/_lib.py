@@ -24,7 +24,8 @@ PASS_FWD, PASS_BWD = 0, 1
 
 KERNELS = ["count", "dispatch", "fc1", "fc2", "combine", "fc1_recompute", "fc2_dgrad",
            "fc2_wgrad", "fc1_wgrad", "fc1_dgrad", "unpermute", "fc1_dgrad_wgrad",
-           "router_fwd", "router_bwd_dx", "router_wgrad", "router_reduce"]
+           "router_fwd", "router_bwd_dx", "router_wgrad", "router_reduce", "norm_fwd", "norm_bwd",
+           "route_fwd", "route_bwd", "mx_linear", "mx_fc1", "mx_fc2", "mx_combine"]
 
 
 class MemfineError(RuntimeError):
@@ -77,6 +78,16 @@ class Model(ctypes.Structure):
                 ("D_t", ctypes.c_int32), ("full_recompute", ctypes.c_int32)]
 
 
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+
+
+class Gating(ctypes.Structure):
+    """memfine_gating: how memfine_route_fwd selects experts and forms gates."""
+    _fields_ = [("E", ctypes.c_int32), ("k", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+                ("renorm", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 class KernelStat(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_int64), ("total_ms", ctypes.c_double),
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
@@ -88,6 +99,7 @@ I32P = ctypes.POINTER(ctypes.c_int32)
 I64P = ctypes.POINTER(ctypes.c_int64)
 SHP = ctypes.POINTER(Shape)
 ALP = ctypes.POINTER(Allocator)
+GTP = ctypes.POINTER(Gating)
 
 _SIGS = {
     "memfine_count": (ctypes.c_int, [SHP, P, P, I64P, P]),
@@ -115,6 +127,29 @@ _SIGS = {
     "memfine_router_fwd": (ctypes.c_int, [SHP, P, P, P, P, P, P]),
     "memfine_router_bwd": (ctypes.c_int, [SHP, P, P, P, P, P, P, P, ctypes.c_int32,
                                           ctypes.c_int32, ALP, P]),
+    "memfine_norm_fwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                        ctypes.c_float, P, P, P, P, P, P, P, P]),
+    "memfine_norm_bwd": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                        ctypes.c_float, P, P, P, P, P, P, ctypes.c_int32, ALP, P]),
+    "memfine_mx_values": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, P, P, ctypes.c_int32, P,
+                                         P]),
+    "memfine_route_fwd": (ctypes.c_int, [ctypes.c_int64, GTP, P, P, P, P, P]),
+    "memfine_route_bwd": (ctypes.c_int, [ctypes.c_int64, GTP, P, P, P, P, P]),
+    "memfine_router_logits": (ctypes.c_int, [SHP, P, P, P, P]),
+    "memfine_router_logits_bwd": (ctypes.c_int, [SHP, P, P, P, P, P, ctypes.c_int32,
+                                                 ctypes.c_int32, ALP, P]),
+    "memfine_mxw_code_bytes": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
+    "memfine_mxw_scale_bytes": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
+    "memfine_mxw_pack": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, P, P, P, P,
+                                        P]),
+    "memfine_mxw_quantize": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                            ctypes.c_int32, P, P, P, P]),
+    "memfine_mxw_unpack": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, P, P,
+                                          ctypes.c_int32, P, P]),
+    "memfine_linear_mxw": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, P, P, P,
+                                          P, ctypes.c_int32, P, P]),
+    "memfine_moe_fwd_mxw": (ctypes.c_int, [SHP, ctypes.c_int32, P, P, P, P, P, P, P, P, P, ALP, P]),
+    "memfine_moe_mxw_workspace_bytes": (ctypes.c_int64, [SHP, ctypes.c_int32, ctypes.c_int32]),
     "memfine_status_str": (ctypes.c_char_p, [ctypes.c_int]),
     "memfine_profile_begin": (ctypes.c_int, [ctypes.c_uint32]),
     "memfine_profile_end": (ctypes.c_int, [ctypes.POINTER(KernelStat)]),
@@ -463,6 +498,226 @@ def memfine_router_bwd(shape: Shape, X, Wr, idx, gates, dgates, dX, dWr, accumul
         _ptr(dWr, (E, h), torch.float32, "dWr"), int(bool(accumulate_dX)),
         int(bool(accumulate_dWr)), _alloc_arg(allocator), _stream(stream))
     _check(rc, "memfine_router_bwd")
+
+
+# ------------------------------------------------------- around the layer
+def _dtype_of(t, name) -> int:
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise ValueError(f"{name}: dtype {t.dtype} is neither bfloat16 nor float32")
+
+
+def _rows(t, name):
+    """(rows, columns) of a matrix argument."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected a matrix, got shape {tuple(t.shape)}")
+    return t.shape[0], t.shape[1]
+
+
+def _opt(t, shape_tuple, dtype, name):
+    return None if t is None else _ptr(t, shape_tuple, dtype, name)
+
+
+def memfine_norm_fwd(eps: float, X, w, R=None, S=None, Y=None, Q=None, QS=None,
+                     stream=None) -> None:
+    """S = X + R and its RMS norm Y, both [T, h] in X's dtype, and Y's MX8 form
+    in Q uint8 [T, h], QS uint8 [T, h/32]; outputs are the caller's, None: not
+    asked for."""
+    torch = _torch()
+    T, h = _rows(X, "X")
+    rc = lib().memfine_norm_fwd(
+        T, h, _dtype_of(X, "X"), float(eps), _ptr(X, (T, h), X.dtype, "X"),
+        _opt(R, (T, h), X.dtype, "R"), _ptr(w, (h,), X.dtype, "w"), _opt(S, (T, h), X.dtype, "S"),
+        _opt(Y, (T, h), X.dtype, "Y"), _opt(Q, (T, h), torch.uint8, "Q"),
+        _opt(QS, (T, h // 32), torch.uint8, "QS"), _stream(stream))
+    _check(rc, "memfine_norm_fwd")
+
+
+def memfine_norm_bwd(eps: float, X, w, dY, dX, dw, dS=None, accumulate_dw: bool = False,
+                     allocator=None, stream=None) -> None:
+    """Gradient of the norm: X is the norm's input (the forward's S), dX [T, h],
+    dw float [h]."""
+    torch = _torch()
+    T, h = _rows(X, "X")
+    rc = lib().memfine_norm_bwd(
+        T, h, _dtype_of(X, "X"), float(eps), _ptr(X, (T, h), X.dtype, "X"),
+        _ptr(w, (h,), X.dtype, "w"), _ptr(dY, (T, h), X.dtype, "dY"),
+        _opt(dS, (T, h), X.dtype, "dS"), _ptr(dX, (T, h), X.dtype, "dX"),
+        _ptr(dw, (h,), torch.float32, "dw"), int(bool(accumulate_dw)), _alloc_arg(allocator),
+        _stream(stream))
+    _check(rc, "memfine_norm_bwd")
+
+
+def memfine_mx_values(Q, QS, out, stream=None) -> None:
+    """The values of an MX8 tensor, into out [T, h], bfloat16 or float32."""
+    torch = _torch()
+    T, h = _rows(Q, "Q")
+    rc = lib().memfine_mx_values(T, h, _ptr(Q, (T, h), torch.uint8, "Q"),
+                                 _ptr(QS, (T, h // 32), torch.uint8, "QS"), _dtype_of(out, "out"),
+                                 _ptr(out, (T, h), out.dtype, "out"), _stream(stream))
+    _check(rc, "memfine_mx_values")
+
+
+def make_gating(E: int, k: int, score: str = "softmax", groups: int = 1, top_groups: int = 1,
+                renorm: bool = True, scale: float = 1.0) -> Gating:
+    """memfine_gating; score is "softmax" or "sigmoid"."""
+    scores = {"softmax": SCORE_SOFTMAX, "sigmoid": SCORE_SIGMOID}
+    if score not in scores:
+        raise ValueError(f"score: {score!r} is neither 'softmax' nor 'sigmoid'")
+    return Gating(int(E), int(k), scores[score], int(groups), int(top_groups), int(bool(renorm)),
+                  float(scale))
+
+
+def memfine_route_fwd(gating: Gating, logits, idx, gates, bias=None, stream=None) -> None:
+    """Routing from logits float [T, E] into idx int32 [T, k], gates float [T, k]."""
+    torch = _torch()
+    T, _ = _rows(logits, "logits")
+    E, k = gating.E, gating.k
+    rc = lib().memfine_route_fwd(
+        T, ctypes.byref(gating), _ptr(logits, (T, E), torch.float32, "logits"),
+        _opt(bias, (E,), torch.float32, "bias"), _ptr(idx, (T, k), torch.int32, "idx"),
+        _ptr(gates, (T, k), torch.float32, "gates"), _stream(stream))
+    _check(rc, "memfine_route_fwd")
+
+
+def memfine_route_bwd(gating: Gating, logits, idx, dgates, dlogits, stream=None) -> None:
+    """Gradient of the gates with respect to the logits, into dlogits float [T, E]."""
+    torch = _torch()
+    T, _ = _rows(logits, "logits")
+    E, k = gating.E, gating.k
+    rc = lib().memfine_route_bwd(
+        T, ctypes.byref(gating), _ptr(logits, (T, E), torch.float32, "logits"),
+        _ptr(idx, (T, k), torch.int32, "idx"), _ptr(dgates, (T, k), torch.float32, "dgates"),
+        _ptr(dlogits, (T, E), torch.float32, "dlogits"), _stream(stream))
+    _check(rc, "memfine_route_bwd")
+
+
+def memfine_router_logits(shape: Shape, X, Wr, logits, stream=None) -> None:
+    """logits float [T, E] = X Wr^T."""
+    torch = _torch()
+    dt = _dt(shape)
+    T, h, E = shape.T, shape.h, shape.E
+    rc = lib().memfine_router_logits(
+        ctypes.byref(shape), _ptr(X, (T, h), dt, "X"), _ptr(Wr, (E, h), dt, "Wr"),
+        _ptr(logits, (T, E), torch.float32, "logits"), _stream(stream))
+    _check(rc, "memfine_router_logits")
+
+
+def memfine_router_logits_bwd(shape: Shape, X, Wr, dlogits, dX, dWr, accumulate_dX=False,
+                              accumulate_dWr=False, allocator=None, stream=None) -> None:
+    torch = _torch()
+    dt = _dt(shape)
+    T, h, E = shape.T, shape.h, shape.E
+    rc = lib().memfine_router_logits_bwd(
+        ctypes.byref(shape), _ptr(X, (T, h), dt, "X"), _ptr(Wr, (E, h), dt, "Wr"),
+        _ptr(dlogits, (T, E), torch.float32, "dlogits"), _ptr(dX, (T, h), dt, "dX"),
+        _ptr(dWr, (E, h), torch.float32, "dWr"), int(bool(accumulate_dX)),
+        int(bool(accumulate_dWr)), _alloc_arg(allocator), _stream(stream))
+    _check(rc, "memfine_router_logits_bwd")
+
+
+def memfine_mxw_code_bytes(N: int, K: int) -> int:
+    v = lib().memfine_mxw_code_bytes(int(N), int(K))
+    if v < 0:
+        raise MemfineError(int(v), "memfine_mxw_code_bytes")
+    return int(v)
+
+
+def memfine_mxw_scale_bytes(N: int, K: int) -> int:
+    v = lib().memfine_mxw_scale_bytes(int(N), int(K))
+    if v < 0:
+        raise MemfineError(int(v), "memfine_mxw_scale_bytes")
+    return int(v)
+
+
+def _mxw_buffers(E, N, K, codes, scales, device):
+    torch = _torch()
+    cb, sb = memfine_mxw_code_bytes(N, K), memfine_mxw_scale_bytes(N, K)
+    if codes is None:
+        codes = torch.empty((E, cb), dtype=torch.uint8, device=device)
+    if scales is None:
+        scales = torch.empty((E, sb), dtype=torch.uint8, device=device)
+    return (codes, scales, _ptr(codes, (E, cb), torch.uint8, "codes"),
+            _ptr(scales, (E, sb), torch.uint8, "scales"))
+
+
+def memfine_mxw_pack(E: int, N: int, K: int, row_codes, row_scales, codes=None, scales=None,
+                     stream=None):
+    """Lays row-major MX4 matrices out, codes uint8 [E, N, K/2] and scales uint8
+    [E, N, K/32]; returns (codes, scales), allocated where None is given."""
+    torch = _torch()
+    codes, scales, pc, ps = _mxw_buffers(E, N, K, codes, scales, row_codes.device)
+    rc = lib().memfine_mxw_pack(
+        int(E), int(N), int(K), _ptr(row_codes, (E, N, K // 2), torch.uint8, "row_codes"),
+        _ptr(row_scales, (E, N, K // 32), torch.uint8, "row_scales"), pc, ps, _stream(stream))
+    _check(rc, "memfine_mxw_pack")
+    return codes, scales
+
+
+def memfine_mxw_quantize(W, codes=None, scales=None, stream=None):
+    """Rounds matrices [E, N, K] (bfloat16 or float32) to MX4, laid out; returns
+    (codes, scales), allocated where None is given."""
+    E, N, K = W.shape
+    codes, scales, pc, ps = _mxw_buffers(E, N, K, codes, scales, W.device)
+    rc = lib().memfine_mxw_quantize(int(E), int(N), int(K), _dtype_of(W, "W"),
+                                    _ptr(W, (E, N, K), W.dtype, "W"), pc, ps, _stream(stream))
+    _check(rc, "memfine_mxw_quantize")
+    return codes, scales
+
+
+def memfine_mxw_unpack(codes, scales, W, stream=None) -> None:
+    """The values of laid-out MX4 matrices, into W [E, N, K], bfloat16 or float32."""
+    E, N, K = W.shape
+    _, _, pc, ps = _mxw_buffers(E, N, K, codes, scales, W.device)
+    rc = lib().memfine_mxw_unpack(int(E), int(N), int(K), pc, ps, _dtype_of(W, "W"),
+                                  _ptr(W, (E, N, K), W.dtype, "W"), _stream(stream))
+    _check(rc, "memfine_mxw_unpack")
+
+
+def _act(X, XS, T, K):
+    """Pointers of activations [T, K]: bfloat16, or e4m3 bytes with scales (MX8)."""
+    torch = _torch()
+    dt = torch.bfloat16 if XS is None else torch.uint8
+    return _ptr(X, (T, K), dt, "X"), _opt(XS, (T, K // 32), torch.uint8, "XS")
+
+
+def memfine_linear_mxw(N: int, K: int, X, codes, scales, Y, XS=None, stream=None) -> None:
+    """Y [T, N] (bfloat16 or float32) = X [T, K] W^T, W one laid-out MX4 matrix
+    (codes, scales: [1, bytes]); X bfloat16, or e4m3 bytes with scales XS."""
+    T, _ = _rows(X, "X")
+    _, _, pc, ps = _mxw_buffers(1, N, K, codes, scales, X.device)
+    px, pxs = _act(X, XS, T, K)
+    rc = lib().memfine_linear_mxw(T, int(N), int(K), px, pxs, pc, ps, _dtype_of(Y, "Y"),
+                                  _ptr(Y, (T, N), Y.dtype, "Y"), _stream(stream))
+    _check(rc, "memfine_linear_mxw")
+
+
+def memfine_moe_fwd_mxw(shape: Shape, chunks: int, X, idx, gates, W1_codes, W1_scales, W2_codes,
+                        W2_scales, Y, XS=None, allocator=None, stream=None) -> None:
+    """memfine_moe_fwd with laid-out MX4 weights; X bfloat16 [T, h], or e4m3
+    bytes with scales XS uint8 [T, h/32]."""
+    torch = _torch()
+    T, h, F, E, k = shape.T, shape.h, shape.F, shape.E, shape.k
+    _, _, p1, q1 = _mxw_buffers(E, 2 * F, h, W1_codes, W1_scales, X.device)
+    _, _, p2, q2 = _mxw_buffers(E, h, F, W2_codes, W2_scales, X.device)
+    px, pxs = _act(X, XS, T, h)
+    rc = lib().memfine_moe_fwd_mxw(
+        ctypes.byref(shape), int(chunks), px, pxs, _ptr(idx, (T, k), torch.int32, "idx"),
+        _ptr(gates, (T, k), torch.float32, "gates"), p1, q1, p2, q2,
+        _ptr(Y, (T, h), torch.bfloat16, "Y"), _alloc_arg(allocator), _stream(stream))
+    _check(rc, "memfine_moe_fwd_mxw")
+
+
+def memfine_moe_mxw_workspace_bytes(shape: Shape, chunks: int, mx8: bool = False) -> int:
+    v = lib().memfine_moe_mxw_workspace_bytes(ctypes.byref(shape), int(chunks), int(bool(mx8)))
+    if v < 0:
+        raise MemfineError(int(v), "memfine_moe_mxw_workspace_bytes")
+    return int(v)
 
 
 def memfine_profile_begin(kernels: Sequence[str] = tuple(KERNELS)) -> None:

@@ -3,7 +3,9 @@
 // allocates, fills and releases every chunk's buffers in stream order
 // (paper Section 4.1, Eq. (6)/(7); Section 4.2, Eq. (8)/(9)).
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <unordered_map>
@@ -1186,6 +1188,115 @@ int check_router(const memfine_shape* shape) {
   if (shape->k > 16 || shape->k > shape->E || shape->E > 256) return MEMFINE_ERR_UNSUPPORTED;
   return MEMFINE_OK;
 }
+
+// Working memory of the router's gradients: the dense dz rows [T, EP], the
+// split-K tables and the partial dWr [splits, EP, h] (and, `padded`, Wr with
+// zero rows up to EP).
+struct RouterWs {
+  int splits;
+  int64_t o_offsets, o_order, o_tok, o_part, o_wr, total;
+  RouterSplit split(char* ws) const {
+    return {(int32_t*)(ws + o_offsets), (int32_t*)(ws + o_order), (int32_t*)(ws + o_tok), splits};
+  }
+};
+RouterWs router_ws(const memfine_shape& S, int EP, bool padded) {
+  const int64_t es = elem_bytes(S), T = S.T;
+  RouterWs w;
+  // split-K: as many row ranges as give at most 256 workgroups (one round of
+  // the CUs: at 32768 tokens, h 7168, 10 ranges = 280 tiles took 215 us, 9 =
+  // 252 tiles 145 us), each at least 256 rows
+  const int ntn = (S.h + 255) / 256;
+  const int64_t want = std::max(1, 256 / ntn), most = std::max<int64_t>(1, T / 256);
+  w.splits = (int)std::max<int64_t>(1, std::min(want, most));
+  w.o_offsets = align256(T * EP * es);
+  w.o_order = w.o_offsets + align256((w.splits + 1) * 4);
+  w.o_tok = w.o_order + align256(w.splits * 4);
+  w.o_part = w.o_tok + align256(T * 4);
+  w.o_wr = w.o_part + align256((int64_t)w.splits * EP * S.h * 4);
+  w.total = w.o_wr + (padded ? align256((int64_t)EP * S.h * es) : 0);
+  return w;
+}
+
+// dX (+)= D Wr with the dense dz rows D [T, EP], EP a multiple of 64.
+hipError_t router_dx(const memfine_shape& S, int EP, const void* D, const void* d_Wr, void* d_dX,
+                     int accumulate, hipStream_t s) {
+  const memfine_launch_options opt = launch_options();
+  GemmArgs g = {};
+  g.dtype = S.dtype;
+  g.n = (int)S.T;
+  g.E = g.groups = 1;
+  g.h = EP;    // reduction: the dense dz row
+  g.F = S.h;   // output columns: the hidden size
+  g.dY = D;
+  g.W2 = d_Wr;
+  g.ag = d_dX;
+  g.accumulate = accumulate;
+  g.tile_override = opt.tile;
+  g.raster = opt.raster;
+  g.cus = device_cus();
+  g.split_tail = opt.split_tail;
+  return launch_router_dx(g, s);
+}
+
+// dWr (+)= D^T X: the grouped weight-gradient GEMM over `splits` row ranges
+// of dz^T X (M = EP rows of the dense dz, N = h, K = the range), and the sum of
+// the ranges.
+hipError_t router_dwr(const memfine_shape& S, int EP, const RouterWs& w, char* ws, const void* d_X,
+                      float* d_dWr, int accumulate, hipStream_t s) {
+  const int64_t es = elem_bytes(S);
+  const double Td = (double)S.T, hd = (double)S.h;
+  const RouterSplit sp = w.split(ws);
+  float* part = (float*)(ws + w.o_part);
+  hipError_t err;
+  {
+    GemmArgs g = {};
+    g.dtype = S.dtype;
+    g.n = (int)S.T;
+    g.E = g.groups = w.splits;
+    g.h = S.h;
+    g.F = EP / 2;
+    g.offsets = sp.offsets;
+    g.order = sp.order;
+    g.tok_of_row = sp.tok;
+    g.X = d_X;
+    g.u = ws;
+    g.dW1 = part;
+    g.accumulate = 0;
+    g.T_h_bytes = S.T * (int64_t)S.h * es;
+    g.cus = device_cus();
+    KernelTimer kt(MEMFINE_K_ROUTER_WGRAD, s, 2.0 * Td * EP * hd,
+                   (double)es * (Td * hd + Td * EP) + 4.0 * w.splits * EP * hd);
+    err = launch_fc1_wgrad(g, s);
+  }
+  if (err == hipSuccess) {
+    KernelTimer kt(MEMFINE_K_ROUTER_REDUCE, s, 0.0,
+                   4.0 * (double)S.E * hd * (w.splits + (accumulate ? 2.0 : 1.0)));
+    err = launch_router_reduce(part, w.splits, EP, S.E, S.h, accumulate, d_dWr, s);
+  }
+  return err;
+}
+
+// logits = X Wr^T as a grouped GEMM (each tile of 64 to 256 tokens reads Wr
+// once), E a multiple of 32.
+hipError_t router_logits_gemm(const memfine_shape& S, const void* d_X, const void* d_Wr, float* lg,
+                              hipStream_t s) {
+  const memfine_launch_options opt = launch_options();
+  GemmArgs g = {};
+  g.dtype = S.dtype;
+  g.n = (int)S.T;
+  g.E = g.groups = 1;
+  g.h = S.E;   // output columns: the logits
+  g.F = S.h;   // reduction: the hidden size
+  g.a = const_cast<void*>(d_X);
+  g.W2 = d_Wr;
+  g.y = lg;
+  g.T_h_bytes = S.T * (int64_t)S.h * elem_bytes(S);
+  g.tile_override = opt.tile;
+  g.raster = opt.raster;
+  g.cus = device_cus();
+  g.split_tail = opt.split_tail;
+  return launch_router_logits(g, s);
+}
 }  // namespace
 
 int memfine_router_fwd(const memfine_shape* shape, const void* d_X, const void* d_Wr,
@@ -1209,25 +1320,7 @@ int memfine_router_fwd(const memfine_shape* shape, const void* d_X, const void* 
   const size_t lg_bytes = d_logits ? 0 : (size_t)(S.T * (int64_t)S.E * 4);
   float* lg = d_logits ? d_logits : (float*)ws_alloc(nullptr, lg_bytes, s);
   if (!lg) return MEMFINE_ERR_OOM;
-  hipError_t err;
-  {
-    const memfine_launch_options opt = launch_options();
-    GemmArgs g = {};
-    g.dtype = S.dtype;
-    g.n = (int)S.T;
-    g.E = g.groups = 1;
-    g.h = S.E;   // output columns: the logits
-    g.F = S.h;   // reduction: the hidden size
-    g.a = const_cast<void*>(d_X);
-    g.W2 = d_Wr;
-    g.y = lg;
-    g.T_h_bytes = S.T * (int64_t)S.h * elem_bytes(S);
-    g.tile_override = opt.tile;
-    g.raster = opt.raster;
-    g.cus = device_cus();
-    g.split_tail = opt.split_tail;
-    err = launch_router_logits(g, s);
-  }
+  hipError_t err = router_logits_gemm(S, d_X, d_Wr, lg, s);
   if (err == hipSuccess) err = launch_router_topk(lg, S.T, S.E, S.k, d_idx, d_gates, s);
   if (!d_logits) ws_release(nullptr, lg, lg_bytes, s);
   return hip_status(err);
@@ -1251,28 +1344,15 @@ int memfine_router_bwd(const memfine_shape* shape, const void* d_X, const void* 
   if (!d_X || !d_idx || !d_gates || !d_dgates || !d_dX) return MEMFINE_ERR_INVALID_ARG;
   const int64_t es = elem_bytes(S), T = S.T;
   const int EP = router_ep(S.E);
-  // split-K: as many row ranges as give at most 256 workgroups (one round of
-  // the CUs: at 32768 tokens, h 7168, 10 ranges = 280 tiles took 215 us, 9 =
-  // 252 tiles 145 us), each at least 256 rows
-  const int ntn = (S.h + 255) / 256;
-  const int64_t want = std::max(1, 256 / ntn), most = std::max<int64_t>(1, T / 256);
-  const int splits = (int)std::max<int64_t>(1, std::min(want, most));
   // dX (+)= dz Wr: per token in the dz kernel, or (E % 64 == 0, so that the
   // dense dz rows are whole K tiles) as a product from D, which reads Wr once
   // per block of 64 to 256 tokens instead of k rows of it per token
   const bool gemm_dx = S.E % 64 == 0;
-  const int64_t o_meta = align256(T * EP * es);
-  const int64_t o_order = o_meta + align256((splits + 1) * 4);
-  const int64_t o_tok = o_order + align256(splits * 4);
-  const int64_t o_part = o_tok + align256(T * 4);
-  const int64_t total = o_part + align256((int64_t)splits * EP * S.h * 4);
-  char* ws = (char*)ws_alloc(alloc, (size_t)total, s);
+  const RouterWs w = router_ws(S, EP, false);
+  char* ws = (char*)ws_alloc(alloc, (size_t)w.total, s);
   if (!ws) return MEMFINE_ERR_OOM;
   void* D = ws;
-  int32_t* offsets = (int32_t*)(ws + o_meta);
-  int32_t* order = (int32_t*)(ws + o_order);
-  int32_t* tok = (int32_t*)(ws + o_tok);
-  float* part = (float*)(ws + o_part);
+  const RouterSplit sp = w.split(ws);
   const double Td = (double)T, hd = (double)S.h;
   hipError_t err;
   {
@@ -1280,58 +1360,377 @@ int memfine_router_bwd(const memfine_shape* shape, const void* d_X, const void* 
                    (double)es * (Td * hd * (accumulate_dX ? 2.0 : 1.0) +
                                  Td * EP * (gemm_dx ? 2.0 : 1.0) + (double)S.E * hd) +
                        12.0 * Td * S.k);
-    const RouterSplit sp = {offsets, order, tok, splits};
     err = gemm_dx ? launch_router_dz(S.dtype, d_idx, d_gates, d_dgates, T, S.E, S.k, EP, D, sp, s)
                   : launch_router_bwd_dx(S.dtype, d_Wr, d_idx, d_gates, d_dgates, T, S.h, S.E, S.k,
                                          EP, accumulate_dX, d_dX, D, sp, s);
-    if (err == hipSuccess && gemm_dx) {
-      const memfine_launch_options opt = launch_options();
-      GemmArgs g = {};
-      g.dtype = S.dtype;
-      g.n = (int)T;
-      g.E = g.groups = 1;
-      g.h = EP;    // reduction: the dense dz row
-      g.F = S.h;   // output columns: the hidden size
-      g.dY = D;
-      g.W2 = d_Wr;
-      g.ag = d_dX;
-      g.accumulate = accumulate_dX;
-      g.tile_override = opt.tile;
-      g.raster = opt.raster;
-      g.cus = device_cus();
-      g.split_tail = opt.split_tail;
-      err = launch_router_dx(g, s);
-    }
+    if (err == hipSuccess && gemm_dx) err = router_dx(S, EP, D, d_Wr, d_dX, accumulate_dX, s);
   }
-  if (err == hipSuccess) {
-    // dWr partials: the grouped weight-gradient GEMM over `splits` row ranges
-    // of dz^T X (M = EP rows of the dense dz, N = h, K = the range)
-    GemmArgs g = {};
-    g.dtype = S.dtype;
-    g.n = (int)T;
-    g.E = g.groups = splits;
-    g.h = S.h;
-    g.F = EP / 2;
-    g.offsets = offsets;
-    g.order = order;
-    g.tok_of_row = tok;
-    g.X = d_X;
-    g.u = D;
-    g.dW1 = part;
-    g.accumulate = 0;
-    g.T_h_bytes = T * (int64_t)S.h * es;
-    g.cus = device_cus();
-    KernelTimer kt(MEMFINE_K_ROUTER_WGRAD, s, 2.0 * Td * EP * hd,
-                   (double)es * (Td * hd + Td * EP) + 4.0 * splits * EP * hd);
-    err = launch_fc1_wgrad(g, s);
-  }
-  if (err == hipSuccess) {
-    KernelTimer kt(MEMFINE_K_ROUTER_REDUCE, s, 0.0,
-                   4.0 * (double)S.E * hd * (splits + (accumulate_dWr ? 2.0 : 1.0)));
-    err = launch_router_reduce(part, splits, EP, S.E, S.h, accumulate_dWr, d_dWr, s);
-  }
-  ws_release(alloc, ws, (size_t)total, s);
+  if (err == hipSuccess) err = router_dwr(S, EP, w, ws, d_X, d_dWr, accumulate_dWr, s);
+  ws_release(alloc, ws, (size_t)w.total, s);
   return hip_status(err);
+}
+
+// ------------------------------------------------- around the layer
+namespace {
+bool aligned16(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if ((uintptr_t)p & 15) return false;
+  return true;
+}
+bool known_dtype(int32_t dtype) { return dtype == MEMFINE_BF16 || dtype == MEMFINE_F32; }
+
+int check_norm(int64_t T, int32_t h, int32_t dtype, float eps) {
+  if (T < 0 || h < 64 || h % 64 || !(eps >= 0.f) || !std::isfinite(eps))
+    return MEMFINE_ERR_INVALID_ARG;
+  if (!known_dtype(dtype) || h > kNormMaxH || T > INT32_MAX) return MEMFINE_ERR_UNSUPPORTED;
+  return MEMFINE_OK;
+}
+
+int check_gating(int64_t T, const memfine_gating* g) {
+  if (!g || T < 0 || g->E < 1 || g->k < 1 || g->k > g->E) return MEMFINE_ERR_INVALID_ARG;
+  if ((g->score != MEMFINE_SCORE_SOFTMAX && g->score != MEMFINE_SCORE_SIGMOID) || g->groups < 1 ||
+      g->E % g->groups || g->top_groups < 1 || g->top_groups > g->groups ||
+      (int64_t)g->top_groups * (g->E / g->groups) < g->k || (g->renorm != 0 && g->renorm != 1) ||
+      !std::isfinite(g->scale))
+    return MEMFINE_ERR_INVALID_ARG;
+  if (g->E > 256 || g->k > 16 || g->groups > 16 || T > INT32_MAX) return MEMFINE_ERR_UNSUPPORTED;
+  return MEMFINE_OK;
+}
+RouteArgs route_args(const memfine_gating& g) {
+  RouteArgs a = {};
+  a.E = g.E;
+  a.k = g.k;
+  a.score = g.score;
+  a.groups = g.groups;
+  a.top_groups = g.top_groups;
+  a.renorm = g.renorm;
+  a.scale = g.scale;
+  return a;
+}
+
+int check_mx4(int64_t E, int32_t N, int32_t K) {
+  if (E < 1 || N < 16 || N % 16 || K < 32 || K % 32) return MEMFINE_ERR_INVALID_ARG;
+  if (N >= (1 << 30) || K >= (1 << 30)) return MEMFINE_ERR_UNSUPPORTED;
+  return MEMFINE_OK;
+}
+
+// MX4 layer: one chunk's dispatch tables, its SwiGLU rows (bf16, or e4m3 and
+// their scales) and its fp32 output rows.
+struct MxLayout {
+  Layout tables;
+  int64_t o_a, o_as, o_y, total;
+};
+MxLayout mx_layout(const memfine_shape& s, int64_t n, bool mx8) {
+  MxLayout m;
+  layout(s, n, -1, true, false, m.tables);
+  m.o_a = m.tables.total;
+  m.o_as = m.o_a + align256(n * s.F * (mx8 ? 1 : 2));
+  m.o_y = m.o_as + align256(mx8 ? n * (s.F / 32) : 0);
+  m.total = m.o_y + align256(n * (int64_t)s.h * 4);
+  return m;
+}
+}  // namespace
+
+int memfine_norm_fwd(int64_t T, int32_t h, int32_t dtype, float eps, const void* d_X,
+                     const void* d_R, const void* d_w, void* d_S, void* d_Y, uint8_t* d_Q,
+                     uint8_t* d_QS, void* stream) {
+  int rc = check_norm(T, h, dtype, eps);
+  if (rc) return rc;
+  if ((!d_Q) != (!d_QS) || (d_S && !d_R)) return MEMFINE_ERR_INVALID_ARG;
+  if (T == 0) return MEMFINE_OK;
+  if (!d_X || !d_w || (!d_Y && !d_Q) || !aligned16({d_X, d_R, d_w, d_S, d_Y, d_Q, d_QS}))
+    return MEMFINE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  const double n = (double)T * h, es = dtype == MEMFINE_BF16 ? 2.0 : 4.0;
+  KernelTimer kt(MEMFINE_K_NORM_FWD, s, 6.0 * n,
+                 n * (es * (1.0 + !!d_R + !!d_S + !!d_Y) + (d_Q ? 1.03125 : 0.0)) + es * h);
+  return hip_status(launch_norm_fwd(dtype, d_X, d_R, d_w, eps, T, h, d_S, d_Y, d_Q, d_QS, s));
+}
+
+int memfine_norm_bwd(int64_t T, int32_t h, int32_t dtype, float eps, const void* d_X,
+                     const void* d_w, const void* d_dY, const void* d_dS, void* d_dX, float* d_dw,
+                     int32_t accumulate_dw, const memfine_allocator* alloc, void* stream) {
+  int rc = check_norm(T, h, dtype, eps);
+  if (rc) return rc;
+  if (!d_dw || (accumulate_dw != 0 && accumulate_dw != 1)) return MEMFINE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  if (T == 0)
+    return accumulate_dw ? MEMFINE_OK : hip_status(launch_fill_i32((int32_t*)d_dw, h, 0, s));
+  if (!d_X || !d_w || !d_dY || !d_dX || !aligned16({d_X, d_w, d_dY, d_dS, d_dX, d_dw}))
+    return MEMFINE_ERR_INVALID_ARG;
+  const int blocks = norm_bwd_blocks(dtype, T, h, device_cus());
+  const size_t bytes = (size_t)blocks * h * 4;
+  float* partial = (float*)ws_alloc(alloc, bytes, s);
+  if (!partial) return MEMFINE_ERR_OOM;
+  const double n = (double)T * h, es = dtype == MEMFINE_BF16 ? 2.0 : 4.0;
+  hipError_t err;
+  {
+    KernelTimer kt(MEMFINE_K_NORM_BWD, s, 10.0 * n,
+                   n * es * (3.0 + !!d_dS) + 8.0 * blocks * (double)h);
+    err = launch_norm_bwd(dtype, d_X, d_w, d_dY, d_dS, eps, T, h, d_dX, partial, blocks,
+                          accumulate_dw, d_dw, s);
+  }
+  ws_release(alloc, partial, bytes, s);
+  return hip_status(err);
+}
+
+int memfine_mx_values(int64_t T, int32_t h, const uint8_t* d_Q, const uint8_t* d_QS,
+                       int32_t dtype, void* d_out, void* stream) {
+  if (T < 0 || h < 32 || h % 32) return MEMFINE_ERR_INVALID_ARG;
+  if (!known_dtype(dtype) || T > INT32_MAX) return MEMFINE_ERR_UNSUPPORTED;
+  if (T == 0) return MEMFINE_OK;
+  if (!d_Q || !d_QS || !d_out || !aligned16({d_Q, d_QS, d_out})) return MEMFINE_ERR_INVALID_ARG;
+  return hip_status(launch_mx8_unpack(dtype, d_Q, d_QS, T * h, d_out, (hipStream_t)stream));
+}
+
+int memfine_route_fwd(int64_t T, const memfine_gating* g, const float* d_logits,
+                      const float* d_bias, int32_t* d_idx, float* d_gates, void* stream) {
+  int rc = check_gating(T, g);
+  if (rc) return rc;
+  if (T == 0) return MEMFINE_OK;
+  if (!d_logits || !d_idx || !d_gates || !aligned16({d_logits, d_bias, d_idx, d_gates}))
+    return MEMFINE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  KernelTimer kt(MEMFINE_K_ROUTE_FWD, s, 6.0 * T * g->E, 4.0 * T * g->E + 8.0 * T * g->k);
+  return hip_status(launch_route_fwd(d_logits, d_bias, T, route_args(*g), d_idx, d_gates, s));
+}
+
+int memfine_route_bwd(int64_t T, const memfine_gating* g, const float* d_logits,
+                      const int32_t* d_idx, const float* d_dgates, float* d_dlogits,
+                      void* stream) {
+  int rc = check_gating(T, g);
+  if (rc) return rc;
+  if (T == 0) return MEMFINE_OK;
+  if (!d_logits || !d_idx || !d_dgates || !d_dlogits ||
+      !aligned16({d_logits, d_idx, d_dgates, d_dlogits}))
+    return MEMFINE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  const bool dense = g->score == MEMFINE_SCORE_SOFTMAX && !g->renorm;
+  KernelTimer kt(MEMFINE_K_ROUTE_BWD, s, 6.0 * T * (dense ? g->E : g->k),
+                 4.0 * T * (g->E + (dense ? g->E : g->k)) + 8.0 * T * g->k);
+  return hip_status(launch_route_bwd(d_logits, d_idx, d_dgates, T, route_args(*g), d_dlogits, s));
+}
+
+int memfine_router_logits(const memfine_shape* shape, const void* d_X, const void* d_Wr,
+                          float* d_logits, void* stream) {
+  int rc = check_shape(shape);
+  if (rc) return rc;
+  if (shape->E > 256) return MEMFINE_ERR_UNSUPPORTED;
+  const memfine_shape& S = *shape;
+  if (S.T == 0) return MEMFINE_OK;
+  if (!d_X || !d_Wr || !d_logits || !aligned16({d_X, d_Wr, d_logits}))
+    return MEMFINE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  const double es = (double)elem_bytes(S), Td = (double)S.T;
+  KernelTimer kt(MEMFINE_K_ROUTER_FWD, s, 2.0 * Td * S.h * S.E,
+                 es * (Td * S.h + (double)S.E * S.h) + 4.0 * Td * S.E);
+  if (S.E > 64 && S.E % 32 == 0) return hip_status(router_logits_gemm(S, d_X, d_Wr, d_logits, s));
+  // the fused kernel, with a top-1 that goes to the workspace
+  const int64_t o_gates = align256(S.T * 4), bytes = o_gates + S.T * 4;
+  char* ws = (char*)ws_alloc(nullptr, (size_t)bytes, s);
+  if (!ws) return MEMFINE_ERR_OOM;
+  const hipError_t err = launch_router_fwd(S.dtype, d_X, d_Wr, S.T, S.h, S.E, 1, (int32_t*)ws,
+                                           (float*)(ws + o_gates), d_logits, device_cus(), s);
+  ws_release(nullptr, ws, (size_t)bytes, s);
+  return hip_status(err);
+}
+
+int memfine_router_logits_bwd(const memfine_shape* shape, const void* d_X, const void* d_Wr,
+                              const float* d_dlogits, void* d_dX, float* d_dWr,
+                              int32_t accumulate_dX, int32_t accumulate_dWr,
+                              const memfine_allocator* alloc, void* stream) {
+  int rc = check_shape(shape);
+  if (rc) return rc;
+  if (shape->E > 256) return MEMFINE_ERR_UNSUPPORTED;
+  if ((accumulate_dX != 0 && accumulate_dX != 1) || (accumulate_dWr != 0 && accumulate_dWr != 1))
+    return MEMFINE_ERR_INVALID_ARG;
+  const memfine_shape& S = *shape;
+  if (!d_Wr || !d_dWr) return MEMFINE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  if (S.T == 0) {
+    if (accumulate_dWr) return MEMFINE_OK;
+    return hip_status(launch_fill_i32((int32_t*)d_dWr, (int64_t)S.E * S.h, 0, s));
+  }
+  if (!d_X || !d_dlogits || !d_dX || !aligned16({d_X, d_Wr, d_dlogits, d_dX, d_dWr}))
+    return MEMFINE_ERR_INVALID_ARG;
+  // dlogits rows of whole K tiles, and Wr with as many rows
+  const int EP = (S.E + 63) / 64 * 64;
+  const bool padded = EP != S.E;
+  const RouterWs w = router_ws(S, EP, padded);
+  char* ws = (char*)ws_alloc(alloc, (size_t)w.total, s);
+  if (!ws) return MEMFINE_ERR_OOM;
+  const double es = (double)elem_bytes(S), Td = (double)S.T, hd = (double)S.h;
+  hipError_t err;
+  {
+    KernelTimer kt(MEMFINE_K_ROUTER_BWD_DX, s, 2.0 * Td * EP * hd,
+                   es * (Td * hd * (accumulate_dX ? 2.0 : 1.0) + 2.0 * Td * EP + S.E * hd) +
+                       4.0 * Td * S.E);
+    err = launch_logit_rows(S.dtype, d_dlogits, S.T, S.E, EP, ws, w.split(ws), s);
+    const void* wr = d_Wr;
+    if (err == hipSuccess && padded) {
+      const int64_t held = (int64_t)S.E * S.h * (int64_t)es, all = (int64_t)EP * S.h * (int64_t)es;
+      wr = ws + w.o_wr;
+      err = launch_copy_pad((int32_t*)(ws + w.o_wr), (const int32_t*)d_Wr, held / 4, all / 4, s);
+    }
+    if (err == hipSuccess) err = router_dx(S, EP, ws, wr, d_dX, accumulate_dX, s);
+  }
+  if (err == hipSuccess) err = router_dwr(S, EP, w, ws, d_X, d_dWr, accumulate_dWr, s);
+  ws_release(alloc, ws, (size_t)w.total, s);
+  return hip_status(err);
+}
+
+int64_t memfine_mxw_code_bytes(int32_t N, int32_t K) {
+  return check_mx4(1, N, K) ? MEMFINE_ERR_INVALID_ARG : mx4_code_bytes(N, K);
+}
+int64_t memfine_mxw_scale_bytes(int32_t N, int32_t K) {
+  return check_mx4(1, N, K) ? MEMFINE_ERR_INVALID_ARG : mx4_scale_bytes(N, K);
+}
+
+int memfine_mxw_pack(int32_t E, int32_t N, int32_t K, const uint8_t* d_row_codes,
+                     const uint8_t* d_row_scales, uint8_t* d_codes, uint8_t* d_scales,
+                     void* stream) {
+  int rc = check_mx4(E, N, K);
+  if (rc) return rc;
+  if (!d_row_codes || !d_row_scales || !d_codes || !d_scales ||
+      !aligned16({d_row_codes, d_codes, d_scales}))
+    return MEMFINE_ERR_INVALID_ARG;
+  return hip_status(launch_mx4_pack(E, N, K, d_row_codes, d_row_scales, d_codes, d_scales,
+                                    (hipStream_t)stream));
+}
+
+int memfine_mxw_quantize(int32_t E, int32_t N, int32_t K, int32_t dtype, const void* d_W,
+                         uint8_t* d_codes, uint8_t* d_scales, void* stream) {
+  int rc = check_mx4(E, N, K);
+  if (rc) return rc;
+  if (!known_dtype(dtype)) return MEMFINE_ERR_UNSUPPORTED;
+  if (!d_W || !d_codes || !d_scales || !aligned16({d_W, d_codes, d_scales}))
+    return MEMFINE_ERR_INVALID_ARG;
+  return hip_status(launch_mx4_quantize(dtype, E, N, K, d_W, d_codes, d_scales,
+                                        (hipStream_t)stream));
+}
+
+int memfine_mxw_unpack(int32_t E, int32_t N, int32_t K, const uint8_t* d_codes,
+                       const uint8_t* d_scales, int32_t dtype, void* d_W, void* stream) {
+  int rc = check_mx4(E, N, K);
+  if (rc) return rc;
+  if (!known_dtype(dtype)) return MEMFINE_ERR_UNSUPPORTED;
+  if (!d_W || !d_codes || !d_scales || !aligned16({d_W, d_codes, d_scales}))
+    return MEMFINE_ERR_INVALID_ARG;
+  return hip_status(launch_mx4_unpack(dtype, E, N, K, d_codes, d_scales, d_W,
+                                      (hipStream_t)stream));
+}
+
+int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const uint8_t* d_XS,
+                       const uint8_t* d_codes, const uint8_t* d_scales, int32_t y_dtype, void* d_Y,
+                       void* stream) {
+  int rc = check_mx4(1, N, K);
+  if (rc) return rc;
+  if (T < 0) return MEMFINE_ERR_INVALID_ARG;
+  if (!known_dtype(y_dtype) || T > INT32_MAX) return MEMFINE_ERR_UNSUPPORTED;
+  if (T == 0) return MEMFINE_OK;
+  if (!d_X || !d_codes || !d_scales || !d_Y || !aligned16({d_X, d_codes, d_scales, d_Y}))
+    return MEMFINE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  MxArgs g = {};
+  g.X = d_X;
+  g.XS = d_XS;
+  g.Wc = d_codes;
+  g.Ws = d_scales;
+  g.n = (int)T;
+  g.E = 1;
+  g.N = N;
+  g.K = K;
+  g.KT = (K + 127) / 128;
+  g.out = d_Y;
+  g.out_bf16 = y_dtype == MEMFINE_BF16;
+  const double nk = (double)N * K, xb = d_XS ? 1.03125 : 2.0;
+  KernelTimer kt(MEMFINE_K_MX_LINEAR, s, 2.0 * T * nk,
+                 0.53125 * nk + xb * T * K + (g.out_bf16 ? 2.0 : 4.0) * T * N);
+  return hip_status(launch_mx_linear(g, s));
+}
+
+int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chunks, int32_t mx8) {
+  if (check_shape(shape) || shape->dtype != MEMFINE_BF16 || chunks < 1 || (mx8 != 0 && mx8 != 1))
+    return MEMFINE_ERR_INVALID_ARG;
+  const int64_t n = max_chunk_tokens(shape->T, chunks) * shape->k;
+  return n == 0 ? 0 : mx_layout(*shape, n, mx8 != 0).total;
+}
+
+int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* d_X,
+                        const uint8_t* d_XS, const int32_t* d_idx, const float* d_gates,
+                        const uint8_t* d_W1_codes, const uint8_t* d_W1_scales,
+                        const uint8_t* d_W2_codes, const uint8_t* d_W2_scales, void* d_Y,
+                        const memfine_allocator* alloc, void* stream) {
+  int rc = check_shape(shape);
+  if (rc) return rc;
+  if (chunks < 1) return MEMFINE_ERR_INVALID_ARG;
+  if (shape->dtype != MEMFINE_BF16) return MEMFINE_ERR_UNSUPPORTED;
+  const memfine_shape& S = *shape;
+  if (S.T == 0) return MEMFINE_OK;
+  if (!d_X || !d_idx || !d_gates || !d_W1_codes || !d_W1_scales || !d_W2_codes || !d_W2_scales ||
+      !d_Y || !aligned16({d_X, d_W1_codes, d_W1_scales, d_W2_codes, d_W2_scales, d_Y}))
+    return MEMFINE_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  const int64_t C = std::min<int64_t>(chunks, S.T);
+  const bool mx8 = d_XS != nullptr;
+  const double hF = (double)S.h * S.F, xb = mx8 ? 1.03125 : 2.0;
+  for (int64_t i = 0; i < C; ++i) {
+    const int64_t t0 = i * S.T / C, t1 = (i + 1) * S.T / C;
+    const int64_t tokens = t1 - t0, n = tokens * S.k;
+    if (n == 0) continue;
+    const MxLayout L = mx_layout(S, n, mx8);
+    char* ws = (char*)ws_alloc(alloc, (size_t)L.total, s);
+    if (!ws) return MEMFINE_ERR_OOM;
+    const ChunkBuffers cb = carve(ws, L.tables);
+    MxArgs g = {};
+    g.X = d_X;
+    g.XS = d_XS;
+    g.tok_of_row = cb.m.tok_of_row;
+    g.Wc = d_W1_codes;
+    g.Ws = d_W1_scales;
+    g.n = (int)n;
+    g.E = S.E;
+    g.N = 2 * S.F;
+    g.K = S.h;
+    g.KT = (S.h + 127) / 128;
+    g.offsets = cb.m.offsets;
+    g.out = ws + L.o_a;
+    g.out_scale = mx8 ? (uint8_t*)(ws + L.o_as) : nullptr;
+    // weights of the experts that can have rows
+    const double nd = (double)n, wb = 0.53125 * hF * (double)std::min<int64_t>(S.E, n);
+    hipError_t err;
+    {
+      KernelTimer kt(MEMFINE_K_DISPATCH, s, 0.0, dispatch_work(n).bytes);
+      err = launch_dispatch(d_idx, d_gates, t0 * S.k, (int)n, S.E, S.k, cb.m, s);
+    }
+    if (err == hipSuccess) {
+      KernelTimer kt(MEMFINE_K_MX_FC1, s, 4.0 * nd * hF, 2.0 * wb + xb * (tokens * S.h + nd * S.F));
+      err = launch_mx_fc1(g, s);
+    }
+    g.X = ws + L.o_a;
+    g.XS = g.out_scale;
+    g.out_scale = nullptr;
+    g.tok_of_row = nullptr;
+    g.Wc = d_W2_codes;
+    g.Ws = d_W2_scales;
+    g.N = S.h;
+    g.K = S.F;
+    g.KT = (S.F + 127) / 128;
+    g.out = ws + L.o_y;
+    if (err == hipSuccess) {
+      KernelTimer kt(MEMFINE_K_MX_FC2, s, 2.0 * nd * hF, wb + xb * nd * S.F + 4.0 * nd * S.h);
+      err = launch_mx_fc2(g, s);
+    }
+    if (err == hipSuccess) {
+      KernelTimer kt(MEMFINE_K_MX_COMBINE, s, 2.0 * nd * S.h,
+                     4.0 * nd * S.h + 2.0 * tokens * S.h + 8.0 * nd);
+      err = launch_mx_combine((const float*)(ws + L.o_y), cb.m.row_of_slot, d_gates, t0, tokens,
+                              S.h, S.k, d_Y, s);
+    }
+    ws_release(alloc, ws, (size_t)L.total, s);
+    if (err != hipSuccess) return MEMFINE_ERR_HIP;
+  }
+  return MEMFINE_OK;
 }
 
 int memfine_profile_begin(uint32_t mask) {

@@ -45,6 +45,8 @@ struct ChunkMeta {
 };
 
 hipError_t launch_fill_i32(int32_t* p, int64_t n, int32_t v, hipStream_t s);
+// dst[0, held) = src, dst[held, n) = 0
+hipError_t launch_copy_pad(int32_t* dst, const int32_t* src, int64_t held, int64_t n, hipStream_t s);
 // Up to kCountOneSlots slots one workgroup counts, and writes the E + 1 counts
 // to `work` and to the pinned `host`: 2.0 us at 2048 slots against 2.6 + 4.2 for
 // clearing and counting, and no copy (the whole call 26 -> 20 us); at 16000
@@ -176,5 +178,66 @@ bool bwd_merges(const GemmArgs& g);
 hipError_t launch_bwd_merged(const GemmArgs& g, hipStream_t s);
 // FC1 dgrad and FC1 wgrad in one launch (independent problems).
 hipError_t launch_fc1_dgrad_wgrad(const GemmArgs& g, hipStream_t s);
+
+// Residual addition and RMS norm (h a multiple of 64, at most kNormMaxH; T <
+// 2^31): S = X + R and Y, and the MX8 form of Y (R, S, Y, Q with QS may be
+// null).  Backward: dX, and dw from `blocks` = norm_bwd_blocks rows of partial
+// sums [blocks, h].
+constexpr int kNormMaxH = 16384;
+hipError_t launch_norm_fwd(int dtype, const void* X, const void* R, const void* w, float eps,
+                           int64_t T, int h, void* S, void* Y, uint8_t* Q, uint8_t* QS,
+                           hipStream_t s);
+int norm_bwd_blocks(int dtype, int64_t T, int h, int cus);
+hipError_t launch_norm_bwd(int dtype, const void* X, const void* w, const void* dY, const void* dS,
+                           float eps, int64_t T, int h, void* dX, float* partial, int blocks,
+                           int accumulate, float* dw, hipStream_t s);
+// The values of n MX8 elements (n a multiple of 32).
+hipError_t launch_mx8_unpack(int dtype, const uint8_t* Q, const uint8_t* QS, int64_t n, void* out,
+                             hipStream_t s);
+
+// Routing from logits (E <= 256, k <= 16, groups <= 16 dividing E).
+struct RouteArgs {
+  int E, k, score;            // score: 0 softmax, 1 sigmoid
+  int groups, top_groups, renorm;
+  float scale;
+  int v;                      // experts per lane   (set by the launchers)
+  int lane_groups;            // groups are whole lanes
+};
+hipError_t launch_route_fwd(const float* logits, const float* bias, int64_t T, RouteArgs a,
+                            int32_t* idx, float* gates, hipStream_t s);
+hipError_t launch_route_bwd(const float* logits, const int32_t* idx, const float* dgates, int64_t T,
+                            RouteArgs a, float* dlogits, hipStream_t s);
+// dlogits as operand rows D [T, EP] of the router's gradient products.
+hipError_t launch_logit_rows(int dtype, const float* dlogits, int64_t T, int E, int EP, void* D,
+                             const RouterSplit& sp, hipStream_t s);
+
+// Products with MX4 matrices (layout: mx.hip).  Row-grouped as the grouped
+// GEMMs: rows [offsets[e], offsets[e + 1]) belong to matrix e; offsets null:
+// one matrix, n rows.
+struct MxArgs {
+  const void* X;              // activations: bf16 [., K], or e4m3 [., K] with XS
+  const uint8_t* XS;          // their scales [., K / 32], or null: bf16
+  const int32_t* tok_of_row;  // activation row of a grouped row, or null: the same
+  const uint8_t *Wc, *Ws;     // matrices [E] of [N, K]
+  int n, E, N, K, KT;         // KT = ceil(K / 128)
+  const int32_t* offsets;
+  void* out;                  // FC1: [n, N / 2] as X's format; FC2: fp32 [n, N]; linear: [n, N]
+  uint8_t* out_scale;         // FC1 on MX8: [n, N / 64]
+  int out_bf16;               // linear: bf16, else fp32
+  int col_blocks;             // (set by the launchers)
+};
+int64_t mx4_code_bytes(int64_t N, int64_t K);   // of one matrix
+int64_t mx4_scale_bytes(int64_t N, int64_t K);
+hipError_t launch_mx4_pack(int64_t E, int N, int K, const uint8_t* rc, const uint8_t* rs,
+                           uint8_t* codes, uint8_t* scales, hipStream_t s);
+hipError_t launch_mx4_quantize(int dtype, int64_t E, int N, int K, const void* W, uint8_t* codes,
+                               uint8_t* scales, hipStream_t s);
+hipError_t launch_mx4_unpack(int dtype, int64_t E, int N, int K, const uint8_t* codes,
+                             const uint8_t* scales, void* W, hipStream_t s);
+hipError_t launch_mx_linear(const MxArgs& g, hipStream_t s);
+hipError_t launch_mx_fc1(const MxArgs& g, hipStream_t s);
+hipError_t launch_mx_fc2(const MxArgs& g, hipStream_t s);
+hipError_t launch_mx_combine(const float* y, const int32_t* row_of_slot, const float* gates,
+                             int64_t t0, int64_t tokens, int h, int k, void* Y, hipStream_t s);
 
 }  // namespace memfine

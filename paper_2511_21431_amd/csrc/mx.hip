@@ -1,0 +1,470 @@
+// Products with MX4 matrices on gfx950: the expert layer's forward and a
+// single linear map, on bf16 or MX8 activations; and the matrices' layout.
+//
+// A matrix W [N, K] (K a multiple of 32, N of 16) is held as tiles of 16 rows
+// x 128 columns in the order in which a wave feeds them to the matrix cores:
+//   codes   [N / 16][KT][64 lanes][16 bytes], KT = ceil(K / 128): lane l holds
+//           row l % 16, columns 32 (l / 16) .. + 31 of the tile, two to a byte,
+//           the lower column in the low half
+//   scales  [N / 16][KS][64 lanes][4 bytes], KS = ceil(KT / 4): byte b of lane
+//           l is the scale of that row's block in tile 4 i + b
+// so that one 16-byte load per lane is a whole operand, contiguous over the
+// wave, with one scale.  Columns past K hold zeros with scale 1.
+//
+// The weights are operand A (16 rows of W), the activations operand B (16 rows
+// of X), so a lane's four accumulators are four neighbouring columns of one
+// output row.  On MX8 activations the product is one scaled MFMA of K = 128
+// (e2m1 x e4m3, both operands' block scales applied by the matrix core; its
+// products are exact and the sum of 128 is formed to about 2^-15 of its
+// largest term before it is added in fp32).  On bf16 activations the weights
+// are converted with their scale, exactly, by v_cvt_scalef32_pk_bf16_fp4 and
+// multiplied by four bf16 MFMAs of K = 32.
+#include "kernels.h"
+#include "mx.h"
+
+namespace memfine {
+namespace {
+
+typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
+
+constexpr int kTileBytes = 1024;   // codes of a 16 x 128 tile
+constexpr int kScaleBytes = 256;   // scales of four tiles
+
+// ------------------------------------------------------------ the operands
+// One tile's K of 16 activation rows, as the wave's operand B.  Lane l holds
+// row l % 16, lane group g = l / 16.  MX8: columns 16 g .. + 15 and 64 + 16 g
+// .. + 15 (the matrix core's order for 8-bit operands) and the scale of block g.
+// bf16: columns 32 g .. + 31, as the weights.
+template <bool MX8> struct Act;
+template <> struct Act<true> {
+  u32x4_t lo, hi;
+  uint32_t s;
+  __device__ __forceinline__ void load(const uint8_t* row, const uint8_t* srow, int k0, int K, int g) {
+    const int a = k0 + 16 * g, b = a + 64, c = k0 + 32 * g;
+    lo = hi = (u32x4_t){0, 0, 0, 0};
+    s = 127;
+    if (a < K) lo = *(const u32x4_t*)(row + a);
+    if (b < K) hi = *(const u32x4_t*)(row + b);
+    if (c < K) s = srow[c / kMxBlock];
+  }
+};
+template <> struct Act<false> {
+  u32x4_t v[4];
+  __device__ __forceinline__ void load(const uint8_t* row, const uint8_t*, int k0, int K, int g) {
+    const int c = k0 + 32 * g;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = (u32x4_t){0, 0, 0, 0};
+    if (c < K) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = *(const u32x4_t*)(row + 2 * (c + 8 * j));
+    }
+  }
+};
+
+// acc += tile (codes w, scale byte s per lane) x activations
+__device__ __forceinline__ void mx_mma(const u32x4_t& w, uint32_t s, const Act<true>& x, f32x4_t& acc) {
+  const i32x8_t a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+  const i32x8_t b = {(int)x.lo[0], (int)x.lo[1], (int)x.lo[2], (int)x.lo[3],
+                     (int)x.hi[0], (int)x.hi[1], (int)x.hi[2], (int)x.hi[3]};
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 0, 0, (int)s, 0, (int)x.s);
+}
+__device__ __forceinline__ void mx_mma(const u32x4_t& w, uint32_t s, const Act<false>& x, f32x4_t& acc) {
+  const float scale = __uint_as_float(s << 23);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bf16x2v_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 0);
+    const bf16x2v_t p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 1);
+    const bf16x2v_t p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 2);
+    const bf16x2v_t p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 3);
+    const bf16x8_t a = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, x.v[j]), acc, 0, 0, 0);
+  }
+}
+
+// --------------------------------------------------------------- row blocks
+// Rows [r0, r1) of expert e: the b-th block of RB rows of the grouped rows;
+// false past the last block.  Every wave finds it for itself: 64 experts'
+// block counts at a time, summed over the lanes.
+template <int RB>
+__device__ __forceinline__ bool locate(const MxArgs& g, int b, int& e, int& r0, int& r1) {
+  if (g.offsets == nullptr) {
+    e = 0;
+    r0 = b * RB;
+    r1 = min(g.n, r0 + RB);
+    return r0 < g.n;
+  }
+  const int lane = threadIdx.x & 63;
+  for (int e0 = 0; e0 < g.E; e0 += 64) {
+    const int ee = e0 + lane;
+    const int lo = ee < g.E ? g.offsets[ee] : 0, hi = ee < g.E ? g.offsets[ee + 1] : 0;
+    const int nb = (hi - lo + RB - 1) / RB;
+    int inc = nb;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(inc, o);
+      if (lane >= o) inc += y;
+    }
+    const uint64_t past = __ballot(inc > b);
+    if (past != 0) {
+      const int w = __builtin_ctzll(past);
+      e = e0 + w;
+      r0 = __builtin_amdgcn_readlane(lo, w) +
+           (b - (__builtin_amdgcn_readlane(inc, w) - __builtin_amdgcn_readlane(nb, w))) * RB;
+      r1 = min(__builtin_amdgcn_readlane(hi, w), r0 + RB);
+      return true;
+    }
+    b -= __builtin_amdgcn_readlane(inc, 63);
+  }
+  return false;
+}
+
+// -------------------------------------------------------------- few rows
+// A block of 16 rows x TILES tiles of W per workgroup; its W waves share the
+// reduction (wave w takes tiles w, w + W, ... along K) and add their partial
+// sums through LDS.
+//   kFc1     tiles: two of the gate half and the two of the up half of the same
+//            32 columns; SwiGLU, stored as a bf16 or MX8 row block
+//   kFc2     fp32 rows
+//   kLinear  bf16 or fp32 rows
+enum { kFc1, kFc2, kLinear };
+
+// a = silu(u) v of a lane's eight values (two tiles x four columns of row r),
+// stored at columns f and f + 16 on; on MX8 activations the 32 columns that
+// four lanes hold become one block.
+__device__ __forceinline__ void store_swiglu(const MxArgs& g, bool mx8, const f32x4_t (&gate)[2],
+                                             const f32x4_t (&up)[2], int64_t r, int f0, int lg,
+                                             bool live) {
+  float a[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float z = gate[i >> 2][i & 3];
+    a[i] = z * sigmoidf_(z) * up[i >> 2][i & 3];
+  }
+  const int F = g.N / 2;
+  if (mx8) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = umax(m, abs_bits(a[i]));
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+    m = umax(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+    const uint32_t s = mx8_scale(m);
+    const float inv = mx_inverse_scale(s);
+    if (live) {
+      uint8_t* out = (uint8_t*)g.out + r * F + f0 + 4 * lg;
+      *(uint32_t*)out = pack_e4m3x4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
+      *(uint32_t*)(out + 16) = pack_e4m3x4(a[4] * inv, a[5] * inv, a[6] * inv, a[7] * inv);
+      if (lg == 0) g.out_scale[r * (F / kMxBlock) + f0 / kMxBlock] = (uint8_t)s;
+    }
+  } else if (live) {
+    bf16_t* out = (bf16_t*)g.out + r * F + f0 + 4 * lg;
+    *(u32x2_t*)out = (u32x2_t){pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])};
+    *(u32x2_t*)(out + 16) = (u32x2_t){pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7])};
+  }
+}
+
+template <bool MX8, int MODE, int TILES, int W>
+__global__ __launch_bounds__(64 * W) void mx_rows_kernel(MxArgs g) {
+  __shared__ f32x4_t part[W][TILES][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = blockIdx.x % g.col_blocks, b = blockIdx.x / g.col_blocks;
+  int e, r0, r1;
+  if (!locate<16>(g, b, e, r0, r1)) return;  // uniform over the workgroup
+  const int lr = lane & 15, lg = lane >> 4;
+  const int r = min(r0 + lr, r1 - 1);  // rows past the block repeat its last, unstored
+  const int64_t src = g.tok_of_row ? g.tok_of_row[r] : r;
+  const uint8_t* xrow = (const uint8_t*)g.X + src * g.K * (MX8 ? 1 : 2);
+  const uint8_t* xs = MX8 ? g.XS + src * (g.K / kMxBlock) : nullptr;
+  const int NT = g.N / 16, KT = g.KT, KS = (KT + 3) / 4;
+  int tile[TILES];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    if (MODE == kFc1) tile[i] = (i & 1) + 2 * col + (i >> 1) * (NT / 2);
+    else tile[i] = min(col * TILES + i, NT - 1);
+  }
+  const uint8_t* wc = g.Wc + (int64_t)e * NT * KT * kTileBytes + lane * 16;
+  const uint8_t* ws = g.Ws + (int64_t)e * NT * KS * kScaleBytes + lane * 4;
+  f32x4_t acc[TILES];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) acc[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  for (int kt = w; kt < KT; kt += W) {
+    u32x4_t c[TILES];
+    uint32_t s[TILES];
+    Act<MX8> x;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      c[i] = *(const u32x4_t*)(wc + ((int64_t)tile[i] * KT + kt) * kTileBytes);
+      s[i] = ws[((int64_t)tile[i] * KS + kt / 4) * kScaleBytes + (kt & 3)];
+    }
+    x.load(xrow, xs, kt * 128, g.K, lg);
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) mx_mma(c[i], s[i], x, acc[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) part[w][i][lane] = acc[i];
+  __syncthreads();
+  const bool live = r0 + lr < r1;
+  const int64_t row = r0 + lr;
+  auto total = [&](int i) {
+    f32x4_t v = part[0][i][lane];
+#pragma unroll
+    for (int ww = 1; ww < W; ++ww) v += part[ww][i][lane];
+    return v;
+  };
+  if constexpr (MODE == kFc1) {
+    if (w > 0) return;
+    const f32x4_t gate[2] = {total(0), total(1)}, up[2] = {total(2), total(3)};
+    store_swiglu(g, MX8, gate, up, row, 32 * col, lg, live);
+  } else {
+    for (int i = w; i < TILES; i += W) {
+      const int n0 = (col * TILES + i) * 16;
+      if (n0 >= g.N || !live) continue;
+      const f32x4_t v = total(i);
+      if (MODE == kLinear && g.out_bf16)
+        *(u32x2_t*)((bf16_t*)g.out + row * g.N + n0 + 4 * lg) =
+            (u32x2_t){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      else
+        *(f32x4_t*)((float*)g.out + row * g.N + n0 + 4 * lg) = v;
+    }
+  }
+}
+
+// Y[t0 + i] = sum_j gate[t, j] y[row_of_slot[i k + j]], fp32 rows, bf16 out: a
+// thread takes four columns; a dropped slot (row < 0) adds nothing.
+__global__ __launch_bounds__(256) void mx_combine_kernel(const float* __restrict__ y,
+                                                         const int32_t* __restrict__ row_of_slot,
+                                                         const float* __restrict__ gates,
+                                                         int64_t t0, int64_t n, int h, int k,
+                                                         bf16_t* __restrict__ Y) {
+  const int64_t gid = blockIdx.x * 256ll + threadIdx.x;
+  if (gid >= n) return;
+  const int vpr = h / 4;
+  const int64_t i = gid / vpr, c = (gid - i * vpr) * 4;
+  float f[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int j0 = 0; j0 < k; j0 += 8) {
+    int r[8];
+    f32x4_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = j0 + j < k ? row_of_slot[i * k + j0 + j] : -1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j0 + j < k) v[j] = *(const f32x4_t*)(y + (int64_t)max(r[j], 0) * h + c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (r[j] < 0) continue;
+      const float gj = gates[(t0 + i) * k + j0 + j];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) f[q] = fmaf(gj, v[j][q], f[q]);
+    }
+  }
+  Vec4<bf16_t>::store(Y + (t0 + i) * h + c, f);
+}
+
+// -------------------------------------------------------------- the layout
+// From row-major codes [E, N, K / 2] and scales [E, N, K / 32]: a thread moves
+// one lane's 16 bytes of a tile, and in every fourth tile the lane's scales.
+__global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* __restrict__ rc,
+                                                       const uint8_t* __restrict__ rs, int64_t n,
+                                                       int N, int K, int KT,
+                                                       uint8_t* __restrict__ codes,
+                                                       uint8_t* __restrict__ scales) {
+  const int64_t id = blockIdx.x * 256ll + threadIdx.x;
+  if (id >= n) return;
+  const int lane = (int)(id & 63), NT = N / 16;
+  const int64_t tile = id >> 6;                 // over [E][NT][KT]
+  const int kt = (int)(tile % KT);
+  const int64_t rowt = tile / KT;               // over [E][NT]
+  const int64_t row = rowt * 16 + (lane & 15);  // over [E][N]
+  const int k = kt * 128 + 32 * (lane >> 4);
+  u32x4_t c = {0, 0, 0, 0};
+  if (k < K) c = *(const u32x4_t*)(rc + row * (K / 2) + k / 2);
+  *(u32x4_t*)(codes + id * 16) = c;
+  if ((kt & 3) == 0) {
+    uint32_t s = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int kb = k + 128 * b;
+      s |= (kb < K ? (uint32_t)rs[row * (K / kMxBlock) + kb / kMxBlock] : 127u) << (8 * b);
+    }
+    const int KS = (KT + 3) / 4;
+    *(uint32_t*)(scales + ((rowt * KS + kt / 4) * 64 + lane) * 4) = s;
+  }
+  (void)NT;
+}
+
+// From values W [E, N, K]: a thread rounds one lane's blocks of four tiles.
+template <typename T>
+__global__ __launch_bounds__(256) void mx4_quantize_kernel(const T* __restrict__ W, int64_t n, int N,
+                                                           int K, int KT,
+                                                           uint8_t* __restrict__ codes,
+                                                           uint8_t* __restrict__ scales) {
+  constexpr int E = Elem<T>::kVec;
+  const int64_t id = blockIdx.x * 256ll + threadIdx.x;
+  if (id >= n) return;
+  const int lane = (int)(id & 63), KS = (KT + 3) / 4;
+  const int64_t quad = id >> 6;                 // over [E][NT][KS]
+  const int ks = (int)(quad % KS);
+  const int64_t rowt = quad / KS;
+  const int64_t row = rowt * 16 + (lane & 15);
+  uint32_t sc = 0;
+  for (int b = 0; b < 4; ++b) {
+    const int kt = ks * 4 + b, k = kt * 128 + 32 * (lane >> 4);
+    uint32_t s = 127;
+    u32x4_t c = {0, 0, 0, 0};
+    if (k < K) {
+      float x[32];
+      uint32_t m = 0;
+#pragma unroll
+      for (int q = 0; q < 32; q += E) {
+        float f[E];
+        unpack16(*(const u32x4_t*)(W + row * K + k + q), f, (T*)nullptr);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          x[q + i] = f[i];
+          m = umax(m, abs_bits(f[i]));
+        }
+      }
+      s = mx4_scale(m);
+      const float inv = mx_inverse_scale(s);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t v = 0;
+        const float* y = x + 8 * j;
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[0] * inv, y[1] * inv, 1.f, 0);
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[2] * inv, y[3] * inv, 1.f, 1);
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[4] * inv, y[5] * inv, 1.f, 2);
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[6] * inv, y[7] * inv, 1.f, 3);
+        c[j] = v;
+      }
+    }
+    if (kt < KT) *(u32x4_t*)(codes + ((rowt * KT + kt) * 64 + lane) * 16) = c;
+    sc |= s << (8 * b);
+  }
+  *(uint32_t*)(scales + id * 4) = sc;
+}
+
+// The values of a held matrix, row-major: a thread writes one block of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void mx4_unpack_kernel(const uint8_t* __restrict__ codes,
+                                                         const uint8_t* __restrict__ scales,
+                                                         int64_t n, int N, int K, int KT,
+                                                         T* __restrict__ W) {
+  constexpr int E = Elem<T>::kVec;
+  const int64_t id = blockIdx.x * 256ll + threadIdx.x;
+  if (id >= n) return;
+  const int nb = K / kMxBlock, KS = (KT + 3) / 4;
+  const int64_t row = id / nb;
+  const int kb = (int)(id - row * nb), kt = kb / 4, lane = (int)(row & 15) + 16 * (kb & 3);
+  const int64_t rowt = row >> 4;  // N is a multiple of 16: over [E][NT]
+  const u32x4_t c = *(const u32x4_t*)(codes + ((rowt * KT + kt) * 64 + lane) * 16);
+  const float s = mx_scale_value(scales[((rowt * KS + kt / 4) * 64 + lane) * 4 + (kt & 3)]);
+  float x[32];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[j], 1.f, 0);
+    const f32x2_t p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[j], 1.f, 1);
+    const f32x2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[j], 1.f, 2);
+    const f32x2_t p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[j], 1.f, 3);
+    const float f[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[8 * j + i] = f[i] * s;
+  }
+  T* out = W + row * K + kb * kMxBlock;
+#pragma unroll
+  for (int q = 0; q < 32; q += E) {
+    float f[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) f[i] = x[q + i];
+    *(u32x4_t*)(out + q) = pack16(f, (T*)nullptr);
+  }
+}
+
+hipError_t grid_of(int64_t threads, unsigned* blocks) {
+  const int64_t b = (threads + 255) / 256;
+  if (b > INT32_MAX) return hipErrorInvalidValue;
+  *blocks = (unsigned)b;
+  return hipSuccess;
+}
+
+// Blocks of RB rows that n rows of E experts (one group: offsets null) can form.
+int64_t row_blocks(const MxArgs& g, int RB) {
+  if (!g.offsets) return (g.n + RB - 1) / RB;
+  return (int64_t)g.n / RB + (g.E < g.n ? g.E : g.n);
+}
+
+template <bool MX8, int MODE, int TILES, int W>
+hipError_t run_rows(MxArgs g, hipStream_t s) {
+  g.col_blocks = MODE == kFc1 ? g.N / 64 : (g.N / 16 + TILES - 1) / TILES;
+  const int64_t blocks = row_blocks(g, 16) * g.col_blocks;
+  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  mx_rows_kernel<MX8, MODE, TILES, W><<<(unsigned)blocks, 64 * W, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t mx4_code_bytes(int64_t N, int64_t K) { return N / 16 * ((K + 127) / 128) * kTileBytes; }
+int64_t mx4_scale_bytes(int64_t N, int64_t K) { return N / 16 * ((K + 511) / 512) * kScaleBytes; }
+
+hipError_t launch_mx4_pack(int64_t E, int N, int K, const uint8_t* rc, const uint8_t* rs,
+                           uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  const int KT = (K + 127) / 128;
+  const int64_t n = E * (N / 16) * KT * 64;
+  unsigned blocks;
+  if (n == 0) return hipSuccess;
+  if (hipError_t err = grid_of(n, &blocks)) return err;
+  mx4_pack_kernel<<<blocks, 256, 0, s>>>(rc, rs, n, N, K, KT, codes, scales);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_quantize(int dtype, int64_t E, int N, int K, const void* W, uint8_t* codes,
+                               uint8_t* scales, hipStream_t s) {
+  const int KT = (K + 127) / 128;
+  const int64_t n = E * (N / 16) * ((KT + 3) / 4) * 64;
+  unsigned blocks;
+  if (n == 0) return hipSuccess;
+  if (hipError_t err = grid_of(n, &blocks)) return err;
+  if (dtype == 0)
+    mx4_quantize_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)W, n, N, K, KT, codes, scales);
+  else
+    mx4_quantize_kernel<float><<<blocks, 256, 0, s>>>((const float*)W, n, N, K, KT, codes, scales);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_unpack(int dtype, int64_t E, int N, int K, const uint8_t* codes,
+                             const uint8_t* scales, void* W, hipStream_t s) {
+  const int KT = (K + 127) / 128;
+  const int64_t n = E * N * (K / kMxBlock);
+  unsigned blocks;
+  if (n == 0) return hipSuccess;
+  if (hipError_t err = grid_of(n, &blocks)) return err;
+  if (dtype == 0)
+    mx4_unpack_kernel<bf16_t><<<blocks, 256, 0, s>>>(codes, scales, n, N, K, KT, (bf16_t*)W);
+  else
+    mx4_unpack_kernel<float><<<blocks, 256, 0, s>>>(codes, scales, n, N, K, KT, (float*)W);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_linear(const MxArgs& g, hipStream_t s) {
+  if (g.n == 0) return hipSuccess;
+  return g.XS ? run_rows<true, kLinear, 4, 4>(g, s) : run_rows<false, kLinear, 4, 4>(g, s);
+}
+hipError_t launch_mx_fc1(const MxArgs& g, hipStream_t s) {
+  if (g.n == 0) return hipSuccess;
+  return g.XS ? run_rows<true, kFc1, 4, 4>(g, s) : run_rows<false, kFc1, 4, 4>(g, s);
+}
+hipError_t launch_mx_fc2(const MxArgs& g, hipStream_t s) {
+  if (g.n == 0) return hipSuccess;
+  return g.XS ? run_rows<true, kFc2, 4, 4>(g, s) : run_rows<false, kFc2, 4, 4>(g, s);
+}
+
+hipError_t launch_mx_combine(const float* y, const int32_t* row_of_slot, const float* gates,
+                             int64_t t0, int64_t tokens, int h, int k, void* Y, hipStream_t s) {
+  const int64_t n = tokens * (h / 4);
+  unsigned blocks;
+  if (n == 0) return hipSuccess;
+  if (hipError_t err = grid_of(n, &blocks)) return err;
+  mx_combine_kernel<<<blocks, 256, 0, s>>>(y, row_of_slot, gates, t0, n, h, k, (bf16_t*)Y);
+  return hipGetLastError();
+}
+
+}  // namespace memfine

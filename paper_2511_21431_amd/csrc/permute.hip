@@ -23,6 +23,14 @@ __global__ void fill_i32_kernel(int32_t* __restrict__ p, int64_t n, int32_t v) {
     p[i] = v;
 }
 
+// dst[i] = src[i] for i < held, 0 up to n.
+__global__ void copy_pad_kernel(int32_t* __restrict__ dst, const int32_t* __restrict__ src,
+                                int64_t held, int64_t n) {
+  for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < n;
+       i += (int64_t)gridDim.x * blockDim.x)
+    dst[i] = i < held ? src[i] : 0;
+}
+
 // work[e] += #slots with id e; work[E] += #ids outside [0, E).
 __global__ __launch_bounds__(256) void count_kernel(const int32_t* __restrict__ idx, int64_t nslots,
                                                     int E, int32_t* __restrict__ work) {
@@ -332,6 +340,14 @@ hipError_t launch_fill_i32(int32_t* p, int64_t n, int32_t v, hipStream_t s) {
   if (n <= 0) return hipSuccess;
   const int blocks = (int)std::min<int64_t>((n + 255) / 256, 1024);
   fill_i32_kernel<<<blocks, 256, 0, s>>>(p, n, v);
+  return hipGetLastError();
+}
+
+hipError_t launch_copy_pad(int32_t* dst, const int32_t* src, int64_t held, int64_t n,
+                           hipStream_t s) {
+  if (n <= 0) return hipSuccess;
+  const int blocks = (int)std::min<int64_t>((n + 255) / 256, 1024);
+  copy_pad_kernel<<<blocks, 256, 0, s>>>(dst, src, held, n);
   return hipGetLastError();
 }
 
