@@ -1415,10 +1415,16 @@ int check_mx4(int64_t E, int32_t N, int32_t K) {
 }
 
 // MX4 layer: one chunk's dispatch tables, its SwiGLU rows (bf16, or e4m3 and
-// their scales) and its fp32 output rows.
+// their scales) and its output rows.  These are fp32 where they are few or
+// where the SwiGLU rows were already rounded to bf16 (Y would then have a third
+// error of that size); many rows on MX8 activations are bf16, as in the bf16
+// layer: they are written and read once, half the bytes (65536 rows of 7168:
+// 2.96 -> 2.66 ms for the call).
+constexpr int64_t kMxWideRows = 4096;
 struct MxLayout {
   Layout tables;
   int64_t o_a, o_as, o_y, total;
+  bool y_bf16;
 };
 MxLayout mx_layout(const memfine_shape& s, int64_t n, bool mx8) {
   MxLayout m;
@@ -1426,7 +1432,8 @@ MxLayout mx_layout(const memfine_shape& s, int64_t n, bool mx8) {
   m.o_a = m.tables.total;
   m.o_as = m.o_a + align256(n * s.F * (mx8 ? 1 : 2));
   m.o_y = m.o_as + align256(mx8 ? n * (s.F / 32) : 0);
-  m.total = m.o_y + align256(n * (int64_t)s.h * 4);
+  m.y_bf16 = mx8 && n > kMxWideRows;
+  m.total = m.o_y + align256(n * (int64_t)s.h * (m.y_bf16 ? 2 : 4));
   return m;
 }
 }  // namespace
@@ -1646,7 +1653,7 @@ int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const u
   const double nk = (double)N * K, xb = d_XS ? 1.03125 : 2.0;
   KernelTimer kt(MEMFINE_K_MX_LINEAR, s, 2.0 * T * nk,
                  0.53125 * nk + xb * T * K + (g.out_bf16 ? 2.0 : 4.0) * T * N);
-  return hip_status(launch_mx_linear(g, s));
+  return hip_status(launch_mx_rows(g, s));
 }
 
 int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chunks, int32_t mx8) {
@@ -1698,6 +1705,7 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
     g.out_scale = mx8 ? (uint8_t*)(ws + L.o_as) : nullptr;
     // weights of the experts that can have rows
     const double nd = (double)n, wb = 0.53125 * hF * (double)std::min<int64_t>(S.E, n);
+    const double yb = L.y_bf16 ? 2.0 : 4.0;
     hipError_t err;
     {
       KernelTimer kt(MEMFINE_K_DISPATCH, s, 0.0, dispatch_work(n).bytes);
@@ -1717,15 +1725,18 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
     g.K = S.F;
     g.KT = (S.F + 127) / 128;
     g.out = ws + L.o_y;
+    g.out_bf16 = L.y_bf16;
     if (err == hipSuccess) {
-      KernelTimer kt(MEMFINE_K_MX_FC2, s, 2.0 * nd * hF, wb + xb * nd * S.F + 4.0 * nd * S.h);
-      err = launch_mx_fc2(g, s);
+      KernelTimer kt(MEMFINE_K_MX_FC2, s, 2.0 * nd * hF, wb + xb * nd * S.F + yb * nd * S.h);
+      err = launch_mx_rows(g, s);
     }
     if (err == hipSuccess) {
       KernelTimer kt(MEMFINE_K_MX_COMBINE, s, 2.0 * nd * S.h,
-                     4.0 * nd * S.h + 2.0 * tokens * S.h + 8.0 * nd);
-      err = launch_mx_combine((const float*)(ws + L.o_y), cb.m.row_of_slot, d_gates, t0, tokens,
-                              S.h, S.k, d_Y, s);
+                     yb * nd * S.h + 2.0 * tokens * S.h + 8.0 * nd);
+      err = L.y_bf16 ? launch_combine(MEMFINE_BF16, ws + L.o_y, cb.m.row_of_slot, d_gates, t0,
+                                      (int)tokens, S.h, S.k, d_Y, s)
+                     : launch_mx_combine((const float*)(ws + L.o_y), cb.m.row_of_slot, d_gates, t0,
+                                         tokens, S.h, S.k, d_Y, s);
     }
     ws_release(alloc, ws, (size_t)L.total, s);
     if (err != hipSuccess) return MEMFINE_ERR_HIP;

@@ -221,9 +221,9 @@ struct MxArgs {
   const uint8_t *Wc, *Ws;     // matrices [E] of [N, K]
   int n, E, N, K, KT;         // KT = ceil(K / 128)
   const int32_t* offsets;
-  void* out;                  // FC1: [n, N / 2] as X's format; FC2: fp32 [n, N]; linear: [n, N]
+  void* out;                  // FC1: [n, N / 2] as X's format; else [n, N]
   uint8_t* out_scale;         // FC1 on MX8: [n, N / 64]
-  int out_bf16;               // linear: bf16, else fp32
+  int out_bf16;               // [n, N]: bf16, else fp32
   int col_blocks;             // (set by the launchers)
 };
 int64_t mx4_code_bytes(int64_t N, int64_t K);   // of one matrix
@@ -234,9 +234,8 @@ hipError_t launch_mx4_quantize(int dtype, int64_t E, int N, int K, const void* W
                                uint8_t* scales, hipStream_t s);
 hipError_t launch_mx4_unpack(int dtype, int64_t E, int N, int K, const uint8_t* codes,
                              const uint8_t* scales, void* W, hipStream_t s);
-hipError_t launch_mx_linear(const MxArgs& g, hipStream_t s);
 hipError_t launch_mx_fc1(const MxArgs& g, hipStream_t s);
-hipError_t launch_mx_fc2(const MxArgs& g, hipStream_t s);
+hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s);  // FC2, linear
 hipError_t launch_mx_combine(const float* y, const int32_t* row_of_slot, const float* gates,
                              int64_t t0, int64_t tokens, int h, int k, void* Y, hipStream_t s);
 

@@ -19,6 +19,8 @@
 // largest term before it is added in fp32).  On bf16 activations the weights
 // are converted with their scale, exactly, by v_cvt_scalef32_pk_bf16_fp4 and
 // multiplied by four bf16 MFMAs of K = 32.
+#include <type_traits>
+
 #include "kernels.h"
 #include "mx.h"
 
@@ -61,15 +63,18 @@ template <> struct Act<false> {
   }
 };
 
-// acc += tile (codes w, scale byte s per lane) x activations
+// acc += tile x activations; the tile's codes are w, its scale byte SW of s;
+// the activations' scale byte SX of x.s
+template <int SW = 0, int SX = 0>
 __device__ __forceinline__ void mx_mma(const u32x4_t& w, uint32_t s, const Act<true>& x, f32x4_t& acc) {
   const i32x8_t a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
   const i32x8_t b = {(int)x.lo[0], (int)x.lo[1], (int)x.lo[2], (int)x.lo[3],
                      (int)x.hi[0], (int)x.hi[1], (int)x.hi[2], (int)x.hi[3]};
-  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 0, 0, (int)s, 0, (int)x.s);
+  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 0, SW, (int)s, SX, (int)x.s);
 }
+template <int SW = 0, int SX = 0>
 __device__ __forceinline__ void mx_mma(const u32x4_t& w, uint32_t s, const Act<false>& x, f32x4_t& acc) {
-  const float scale = __uint_as_float(s << 23);
+  const float scale = __uint_as_float((s >> (8 * SW) & 255u) << 23);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const bf16x2v_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 0);
@@ -124,9 +129,8 @@ __device__ __forceinline__ bool locate(const MxArgs& g, int b, int& e, int& r0, 
 // sums through LDS.
 //   kFc1     tiles: two of the gate half and the two of the up half of the same
 //            32 columns; SwiGLU, stored as a bf16 or MX8 row block
-//   kFc2     fp32 rows
-//   kLinear  bf16 or fp32 rows
-enum { kFc1, kFc2, kLinear };
+//   kRows    bf16 or fp32 rows (FC2, linear)
+enum { kFc1, kRows };
 
 // a = silu(u) v of a lane's eight values (two tiles x four columns of row r),
 // stored at columns f and f + 16 on; on MX8 activations the 32 columns that
@@ -160,6 +164,15 @@ __device__ __forceinline__ void store_swiglu(const MxArgs& g, bool mx8, const f3
     *(u32x2_t*)out = (u32x2_t){pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])};
     *(u32x2_t*)(out + 16) = (u32x2_t){pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7])};
   }
+}
+
+// four columns n .. n + 3 of an output row
+__device__ __forceinline__ void store_row(const MxArgs& g, const f32x4_t& v, int64_t row, int n) {
+  if (g.out_bf16)
+    *(u32x2_t*)((bf16_t*)g.out + row * g.N + n) =
+        (u32x2_t){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  else
+    *(f32x4_t*)((float*)g.out + row * g.N + n) = v;
 }
 
 template <bool MX8, int MODE, int TILES, int W>
@@ -218,14 +231,256 @@ __global__ __launch_bounds__(64 * W) void mx_rows_kernel(MxArgs g) {
     for (int i = w; i < TILES; i += W) {
       const int n0 = (col * TILES + i) * 16;
       if (n0 >= g.N || !live) continue;
-      const f32x4_t v = total(i);
-      if (MODE == kLinear && g.out_bf16)
-        *(u32x2_t*)((bf16_t*)g.out + row * g.N + n0 + 4 * lg) =
-            (u32x2_t){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-      else
-        *(f32x4_t*)((float*)g.out + row * g.N + n0 + 4 * lg) = v;
+      store_row(g, total(i), row, n0 + 4 * lg);
     }
   }
+}
+
+// ------------------------------------------------------------- many rows
+// A block of BM rows x 256 columns of W (FC1: 128 of the gate half and the
+// same 128 of the up half) per workgroup of four waves, 64 columns each.  The
+// activations, shared by the waves, go from memory straight into an LDS ring
+// of S stages of 128 columns of K; the weights, of which each wave reads its
+// own, straight into registers one stage ahead.
+//
+// LDS rows are kRow = 128 (e4m3) or 256 (bf16) bytes; the 16-byte unit c of row r
+// lies in slot c ^ (r % 8), so that the 16 rows a read takes at once fall on
+// different banks.
+constexpr uint32_t kPast = 0x80000000u;  // an offset past any buffer: reads zero
+
+typedef __attribute__((address_space(3))) void lds_t;
+
+template <int N> __device__ __forceinline__ void wait_loads() {  // at most N loads in flight
+  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+__device__ __forceinline__ void wait_lds() {  // this wave's LDS operations have returned
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int32_t)bytes,
+                                           0x00020000);
+}
+
+// f(Const<0>()), ..., f(Const<N - 1>())
+template <int I> using Const = std::integral_constant<int, I>;
+template <int N, int I = 0, class F> __device__ __forceinline__ void unroll_for(const F& f) {
+  if constexpr (I < N) {
+    f(Const<I>());
+    unroll_for<N, I + 1>(f);
+  }
+}
+
+// Activation rows of a workgroup's block, copied to LDS: the rows' values by
+// 16-byte direct copies, on MX8 the rows' scale bytes (four a row and stage)
+// through registers.  Columns past K read as zero.
+template <bool MX8, int BM> struct ActTile {
+  static constexpr int kRow = MX8 ? 128 : 256, kUnits = kRow / 16;
+  static constexpr int kBytes = BM * kRow;
+  static constexpr int kCopies = kBytes / 4096;             // 1024-byte copies per wave
+  static constexpr int kScales = MX8 ? (BM + 63) / 64 : 0;  // scale bytes per thread
+  static constexpr int kStage = kBytes + (MX8 ? 256 * kScales : 0);
+  __amdgpu_buffer_rsrc_t rx, rs;
+  uint32_t off[kCopies], soff[kScales ? kScales : 1];
+  int col;
+
+  __device__ __forceinline__ void init(const MxArgs& g, int r0, int r1, int w, int lane) {
+    constexpr int es = MX8 ? 1 : 2;
+    // gathered rows are addressed from X (below 2^31 bytes, checked by the
+    // caller), grouped rows from the block's first
+    const bool gather = g.tok_of_row != nullptr;
+    const int64_t base = gather ? 0 : r0;
+    rx = rsrc_of((const uint8_t*)g.X + base * g.K * es, 0x7fffffff);
+    // (the swizzle and with it the column of a lane's unit repeat every 8 rows)
+    const int unit0 = (w * 64 + lane) % kUnits ^ ((w * 64 + lane) / kUnits & 7);
+    col = unit0 * 16 / es;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int r = min(r0 + ((i * 4 + w) * 64 + lane) / kUnits, r1 - 1);  // rows past the block:
+      off[i] = (uint32_t)(gather ? g.tok_of_row[r] : r - r0) * (uint32_t)(g.K * es) + unit0 * 16;
+    }
+    if constexpr (MX8) {
+      rs = rsrc_of(g.XS + base * (g.K / kMxBlock), 0x7fffffff);
+#pragma unroll
+      for (int i = 0; i < kScales; ++i) {
+        const int r = min(r0 + (int)threadIdx.x / 4 + 64 * i, r1 - 1);     // repeat its last
+        soff[i] = (uint32_t)(gather ? g.tok_of_row[r] : r - r0) * (uint32_t)(g.K / kMxBlock) +
+                  (threadIdx.x & 3);
+      }
+    }
+  }
+  __device__ __forceinline__ void copy(int kt, int K, char* lds, int w) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_t*)(lds + (i * 4 + w) * 1024), 16,
+                                               kt * 128 + col < K ? off[i] : kPast, kt * kRow, 0, 0);
+  }
+  __device__ __forceinline__ void load_scales(int kt, int K, uint8_t (&v)[2]) {
+#pragma unroll
+    for (int i = 0; i < kScales; ++i)
+      v[i] = __builtin_amdgcn_raw_buffer_load_b8(
+          rs, kt * 128 + 32 * (int)(threadIdx.x & 3) < K ? soff[i] : kPast, kt * 4, 0);
+  }
+  // The scale of row r, block b at byte b BM + (r % 16) (BM / 16) + r / 16: a
+  // lane's, for all its rows, are neighbours.
+  __device__ __forceinline__ void store_scales(char* lds, const uint8_t (&v)[2]) {
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) {
+      const int r = (int)threadIdx.x / 4 + 64 * i, b = threadIdx.x & 3;
+      // (of 32 rows: the other half of the threads writes bytes that nobody reads)
+      const int at = BM == 32 && r >= 32 ? threadIdx.x : b * BM + (r & 15) * (BM / 16) + (r >> 4);
+      lds[kBytes + at] = (char)v[i];
+    }
+  }
+  __device__ __forceinline__ static void read_scales(const char* lds, int lr, int lg,
+                                                     uint32_t (&s)[(BM + 63) / 64]) {
+    const char* p = lds + kBytes + lg * BM + lr * (BM / 16);
+    if constexpr (BM == 32) s[0] = *(const uint16_t*)p;
+    else
+#pragma unroll
+      for (int i = 0; i < BM / 64; ++i) s[i] = *(const uint32_t*)(p + 4 * i);
+  }
+  // operand B of rows 16 i .. + 15 (row: the lane's row of i = 0; its scale apart)
+  __device__ __forceinline__ static void read(const char* row, int i, int lr, int lg, Act<MX8>& x) {
+    const int sw = lr & 7;
+    if constexpr (MX8) {
+      x.lo = *(const u32x4_t*)(row + ((lg ^ sw) << 4) + 16 * i * kRow);
+      x.hi = *(const u32x4_t*)(row + (((4 + lg) ^ sw) << 4) + 16 * i * kRow);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x.v[j] = *(const u32x4_t*)(row + (((4 * lg + j) ^ sw) << 4) + 16 * i * kRow);
+    }
+  }
+};
+
+template <bool MX8, int MODE, int BM, int S>
+__device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
+  typedef ActTile<MX8, BM> A;
+  constexpr int MI = BM / 16;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  // 64 consecutive tiles, 8 row blocks x 8 column blocks, to one XCD
+  // (workgroup ids go to the 8 XCDs by turns): they share operands in its L2
+  const int id = blockIdx.x, tile_id = (id / 512) * 512 + (id % 8) * 64 + id / 8 % 64;
+  const int band = tile_id / (8 * g.col_blocks), in = tile_id % (8 * g.col_blocks);
+  const int cb = in / 8;
+  int e, r0, r1;
+  if (!locate<BM>(g, band * 8 + in % 8, e, r0, r1)) return;
+  const int NT = g.N / 16, KT = g.KT, KS = (KT + 3) / 4;
+  __amdgpu_buffer_rsrc_t rc[4], rs[4];  // the wave's four tile rows: codes, scales
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    int tile;
+    if (MODE == kFc1) tile = min((cb * 4 + w) * 2 + (i & 1), NT / 2 - 1) + (i >> 1) * (NT / 2);
+    else tile = min((cb * 4 + w) * 4 + i, NT - 1);
+    const int64_t t = (int64_t)e * NT + tile;
+    rc[i] = rsrc_of(g.Wc + t * KT * kTileBytes, (uint32_t)KT * kTileBytes);
+    rs[i] = rsrc_of(g.Ws + t * KS * kScaleBytes, (uint32_t)KS * kScaleBytes);
+  }
+  A a;
+  a.init(g, r0, r1, w, lane);
+  auto load_w = [&](int kt, u32x4_t (&c)[4]) {  // past K: zeros
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c[i] = __builtin_amdgcn_raw_buffer_load_b128(rc[i], lane * 16, kt * kTileBytes, 0);
+  };
+  auto load_ws = [&](int kt, uint32_t (&s)[4]) {  // of tiles kt .. kt + 3, kt % 4 == 0
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      s[i] = __builtin_amdgcn_raw_buffer_load_b32(rs[i], lane * 4, (kt >> 2) * kScaleBytes, 0);
+  };
+  f32x4_t acc[MI][4];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+
+  // stages 0 .. S - 3 whole; of stage S - 2 the copies are in flight and the
+  // scales in registers
+  u32x4_t c0[4], c1[4];
+  uint32_t ws[4], wsn[4];
+  uint8_t xs[2] = {};
+  char *cur = smem, *next = smem + (S - 2) * A::kStage;  // stage of step kt, of step kt + S - 2
+  constexpr int kEnd = S * A::kStage;
+#pragma unroll
+  for (int kt = 0; kt < S - 2; ++kt) {
+    a.copy(kt, g.K, smem + kt * A::kStage, w);
+    a.load_scales(kt, g.K, xs);
+    a.store_scales(smem + kt * A::kStage, xs);
+  }
+  load_ws(0, ws);
+  load_w(0, c0);
+  a.load_scales(S - 2, g.K, xs);
+  a.copy(S - 2, g.K, next, w);
+
+  // step kt = 4 i + U on the weights c, with those of the next step loaded into cn
+  auto step = [&](auto U, int kt, u32x4_t (&c)[4], u32x4_t (&cn)[4]) {
+    __builtin_amdgcn_sched_barrier(0);  // the previous step's products stay before the barrier
+    // All but the copies issued last (of stage kt + S - 2) has arrived.
+    a.store_scales(next, xs);
+    wait_loads<A::kCopies>();
+    wait_lds();
+    // publishes every wave's copies of stage kt, and all waves are done with
+    // the stage of step kt - 1, which the next copies overwrite
+    __builtin_amdgcn_s_barrier();
+    next = next + A::kStage == smem + kEnd ? smem : next + A::kStage;
+    if (U == 0) load_ws(kt + 4, wsn);
+    load_w(kt + 1, cn);
+    a.load_scales(kt + S - 1, g.K, xs);
+    a.copy(kt + S - 1, g.K, next, w);
+    __builtin_amdgcn_sched_barrier(0);  // the loads stay here, a step before their use
+    const char* row = cur + lr * A::kRow;
+    uint32_t xw[(BM + 63) / 64] = {};
+    if constexpr (MX8) A::read_scales(cur, lr, lg, xw);
+    unroll_for<MI>([&](auto i) {
+      Act<MX8> x;
+      A::read(row, i, lr, lg, x);
+      if constexpr (MX8) x.s = xw[i / 4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mx_mma<U, i % 4>(c[j], ws[j], x, acc[i][j]);
+    });
+    if (U == 3) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ws[j] = wsn[j];
+    }
+    cur = cur + A::kStage == smem + kEnd ? smem : cur + A::kStage;
+  };
+  int kt = 0;
+  for (; kt + 3 < KT; kt += 4) {
+    step(Const<0>(), kt, c0, c1);
+    step(Const<1>(), kt + 1, c1, c0);
+    step(Const<2>(), kt + 2, c0, c1);
+    step(Const<3>(), kt + 3, c1, c0);
+  }
+  if (kt < KT) step(Const<0>(), kt, c0, c1);
+  if (kt + 1 < KT) step(Const<1>(), kt + 1, c1, c0);
+  if (kt + 2 < KT) step(Const<2>(), kt + 2, c0, c1);
+  wait_loads<0>();  // the copies past K have landed before the workgroup's LDS is given up
+
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int64_t row = r0 + 16 * i + lr;
+    const bool live = row < r1;
+    if constexpr (MODE == kFc1) {
+      const int f0 = (cb * 4 + w) * 32;
+      const f32x4_t gate[2] = {acc[i][0], acc[i][1]}, up[2] = {acc[i][2], acc[i][3]};
+      store_swiglu(g, MX8, gate, up, row, f0, lg, live && f0 < g.N / 2);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int n0 = ((cb * 4 + w) * 4 + j) * 16;
+        if (n0 < g.N && live) store_row(g, acc[i][j], row, n0 + 4 * lg);
+      }
+    }
+  }
+}
+
+template <bool MX8, int MODE, int BM, int S, int WAVES>
+__global__ __launch_bounds__(256, WAVES) void mx_tile_kernel(MxArgs g) {
+  __shared__ __attribute__((aligned(1024))) char smem[S * ActTile<MX8, BM>::kStage];
+  mx_tile<MX8, MODE, BM, S>(g, smem);
 }
 
 // Y[t0 + i] = sum_j gate[t, j] y[row_of_slot[i k + j]], fp32 rows, bf16 out: a
@@ -400,6 +655,28 @@ hipError_t run_rows(MxArgs g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <bool MX8, int MODE, int BM, int S, int WAVES>
+hipError_t run_tiles(MxArgs g, hipStream_t s) {
+  g.col_blocks = (MODE == kFc1 ? g.N / 2 + 127 : g.N + 255) / (MODE == kFc1 ? 128 : 256);
+  const int64_t bands = (row_blocks(g, BM) + 7) / 8;
+  // whole rounds of 64 tiles on each of 8 XCDs
+  const int64_t blocks = (bands * 8 * g.col_blocks + 511) / 512 * 512;
+  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  mx_tile_kernel<MX8, MODE, BM, S, WAVES><<<(unsigned)blocks, 256, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+// Rows of an average matrix decide the block.
+template <bool MX8, int MODE> hipError_t run(const MxArgs& g, hipStream_t s) {
+  if (g.n == 0) return hipSuccess;
+  const int groups = g.offsets ? g.E : 1;
+  const int rows = (g.n + groups - 1) / groups;
+  if (rows <= 16) return run_rows<MX8, MODE, 4, 4>(g, s);
+  if (rows <= 64) return run_tiles<MX8, MODE, 32, 3, 2>(g, s);
+  if (rows <= 128 || !MX8) return run_tiles<MX8, MODE, 64, 3, 2>(g, s);
+  return run_tiles<MX8, MODE, MX8 ? 128 : 64, 3, 2>(g, s);
+}
+
 }  // namespace
 
 int64_t mx4_code_bytes(int64_t N, int64_t K) { return N / 16 * ((K + 127) / 128) * kTileBytes; }
@@ -444,17 +721,11 @@ hipError_t launch_mx4_unpack(int dtype, int64_t E, int N, int K, const uint8_t* 
   return hipGetLastError();
 }
 
-hipError_t launch_mx_linear(const MxArgs& g, hipStream_t s) {
-  if (g.n == 0) return hipSuccess;
-  return g.XS ? run_rows<true, kLinear, 4, 4>(g, s) : run_rows<false, kLinear, 4, 4>(g, s);
-}
 hipError_t launch_mx_fc1(const MxArgs& g, hipStream_t s) {
-  if (g.n == 0) return hipSuccess;
-  return g.XS ? run_rows<true, kFc1, 4, 4>(g, s) : run_rows<false, kFc1, 4, 4>(g, s);
+  return g.XS ? run<true, kFc1>(g, s) : run<false, kFc1>(g, s);
 }
-hipError_t launch_mx_fc2(const MxArgs& g, hipStream_t s) {
-  if (g.n == 0) return hipSuccess;
-  return g.XS ? run_rows<true, kFc2, 4, 4>(g, s) : run_rows<false, kFc2, 4, 4>(g, s);
+hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s) {
+  return g.XS ? run<true, kRows>(g, s) : run<false, kRows>(g, s);
 }
 
 hipError_t launch_mx_combine(const float* y, const int32_t* row_of_slot, const float* gates,
