@@ -1410,7 +1410,8 @@ RouteArgs route_args(const memfine_gating& g) {
 
 int check_mx4(int64_t E, int32_t N, int32_t K) {
   if (E < 1 || N < 16 || N % 16 || K < 32 || K % 32) return MEMFINE_ERR_INVALID_ARG;
-  if (N >= (1 << 30) || K >= (1 << 30)) return MEMFINE_ERR_UNSUPPORTED;
+  // (the kernels address 256 activation rows with 31-bit offsets)
+  if (N >= (1 << 30) || K > (1 << 20)) return MEMFINE_ERR_UNSUPPORTED;
   return MEMFINE_OK;
 }
 
@@ -1650,6 +1651,7 @@ int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const u
   g.KT = (K + 127) / 128;
   g.out = d_Y;
   g.out_bf16 = y_dtype == MEMFINE_BF16;
+  g.cus = device_cus();
   const double nk = (double)N * K, xb = d_XS ? 1.03125 : 2.0;
   KernelTimer kt(MEMFINE_K_MX_LINEAR, s, 2.0 * T * nk,
                  0.53125 * nk + xb * T * K + (g.out_bf16 ? 2.0 : 4.0) * T * N);
@@ -1689,54 +1691,75 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
     char* ws = (char*)ws_alloc(alloc, (size_t)L.total, s);
     if (!ws) return MEMFINE_ERR_OOM;
     const ChunkBuffers cb = carve(ws, L.tables);
-    MxArgs g = {};
-    g.X = d_X;
-    g.XS = d_XS;
-    g.tok_of_row = cb.m.tok_of_row;
-    g.Wc = d_W1_codes;
-    g.Ws = d_W1_scales;
-    g.n = (int)n;
-    g.E = S.E;
-    g.N = 2 * S.F;
-    g.K = S.h;
-    g.KT = (S.h + 127) / 128;
-    g.offsets = cb.m.offsets;
-    g.out = ws + L.o_a;
-    g.out_scale = mx8 ? (uint8_t*)(ws + L.o_as) : nullptr;
+    MxArgs g1 = {};  // FC1
+    g1.X = d_X;
+    g1.XS = d_XS;
+    g1.tok_of_row = cb.m.tok_of_row;
+    g1.Wc = d_W1_codes;
+    g1.Ws = d_W1_scales;
+    g1.n = (int)n;
+    g1.E = S.E;
+    g1.N = 2 * S.F;
+    g1.K = S.h;
+    g1.KT = (S.h + 127) / 128;
+    g1.cus = device_cus();
+    g1.offsets = cb.m.offsets;
+    g1.out = ws + L.o_a;
+    g1.out_scale = mx8 ? (uint8_t*)(ws + L.o_as) : nullptr;
+    MxArgs g2 = g1;  // FC2
+    g2.X = g1.out;
+    g2.XS = g1.out_scale;
+    g2.out_scale = nullptr;
+    g2.tok_of_row = nullptr;
+    g2.Wc = d_W2_codes;
+    g2.Ws = d_W2_scales;
+    g2.N = S.h;
+    g2.K = S.F;
+    g2.KT = (S.F + 127) / 128;
+    g2.out = ws + L.o_y;
+    g2.out_bf16 = L.y_bf16;
     // weights of the experts that can have rows
     const double nd = (double)n, wb = 0.53125 * hF * (double)std::min<int64_t>(S.E, n);
     const double yb = L.y_bf16 ? 2.0 : 4.0;
-    hipError_t err;
-    {
-      KernelTimer kt(MEMFINE_K_DISPATCH, s, 0.0, dispatch_work(n).bytes);
-      err = launch_dispatch(d_idx, d_gates, t0 * S.k, (int)n, S.E, S.k, cb.m, s);
-    }
-    if (err == hipSuccess) {
-      KernelTimer kt(MEMFINE_K_MX_FC1, s, 4.0 * nd * hF, 2.0 * wb + xb * (tokens * S.h + nd * S.F));
-      err = launch_mx_fc1(g, s);
-    }
-    g.X = ws + L.o_a;
-    g.XS = g.out_scale;
-    g.out_scale = nullptr;
-    g.tok_of_row = nullptr;
-    g.Wc = d_W2_codes;
-    g.Ws = d_W2_scales;
-    g.N = S.h;
-    g.K = S.F;
-    g.KT = (S.F + 127) / 128;
-    g.out = ws + L.o_y;
-    g.out_bf16 = L.y_bf16;
-    if (err == hipSuccess) {
-      KernelTimer kt(MEMFINE_K_MX_FC2, s, 2.0 * nd * hF, wb + xb * nd * S.F + yb * nd * S.h);
-      err = launch_mx_rows(g, s);
-    }
-    if (err == hipSuccess) {
-      KernelTimer kt(MEMFINE_K_MX_COMBINE, s, 2.0 * nd * S.h,
-                     yb * nd * S.h + 2.0 * tokens * S.h + 8.0 * nd);
-      err = L.y_bf16 ? launch_combine(MEMFINE_BF16, ws + L.o_y, cb.m.row_of_slot, d_gates, t0,
-                                      (int)tokens, S.h, S.k, d_Y, s)
-                     : launch_mx_combine((const float*)(ws + L.o_y), cb.m.row_of_slot, d_gates, t0,
-                                         tokens, S.h, S.k, d_Y, s);
+    hipError_t err = hipSuccess;
+    if (tokens == 1 && mx_one_token(g1, g2)) {
+      // one token's slots name distinct experts: nothing to group or combine
+      g1.ids = g2.ids = d_idx + t0 * S.k;
+      g2.gates = d_gates + t0 * S.k;
+      g1.X = (const char*)d_X + t0 * S.h * (mx8 ? 1 : 2);
+      g1.XS = mx8 ? d_XS + t0 * (S.h / 32) : nullptr;
+      g2.out = (char*)d_Y + t0 * S.h * 2;
+      g2.out_bf16 = 1;
+      {
+        KernelTimer kt(MEMFINE_K_MX_FC1, s, 4.0 * nd * hF, 2.0 * wb + xb * (S.h + nd * S.F));
+        err = launch_mx_one_fc1(g1, s);
+      }
+      if (err == hipSuccess) {
+        KernelTimer kt(MEMFINE_K_MX_FC2, s, 2.0 * nd * hF, wb + xb * nd * S.F + 2.0 * S.h);
+        err = launch_mx_one_fc2(g2, s);
+      }
+    } else {
+      {
+        KernelTimer kt(MEMFINE_K_DISPATCH, s, 0.0, dispatch_work(n).bytes);
+        err = launch_dispatch(d_idx, d_gates, t0 * S.k, (int)n, S.E, S.k, cb.m, s);
+      }
+      if (err == hipSuccess) {
+        KernelTimer kt(MEMFINE_K_MX_FC1, s, 4.0 * nd * hF,
+                       2.0 * wb + xb * (tokens * S.h + nd * S.F));
+        err = launch_mx_fc1(g1, s);
+      }
+      if (err == hipSuccess) {
+        KernelTimer kt(MEMFINE_K_MX_FC2, s, 2.0 * nd * hF, wb + xb * nd * S.F + yb * nd * S.h);
+        err = launch_mx_rows(g2, s);
+      }
+      if (err == hipSuccess) {
+        KernelTimer kt(MEMFINE_K_MX_COMBINE, s, 2.0 * nd * S.h,
+                       yb * nd * S.h + 2.0 * tokens * S.h + 8.0 * nd);
+        err = L.y_bf16 ? launch_combine(MEMFINE_BF16, ws + L.o_y, cb.m.row_of_slot, d_gates, t0,
+                                        (int)tokens, S.h, S.k, d_Y, s)
+                       : launch_mx_combine((const float*)(ws + L.o_y), cb.m.row_of_slot, d_gates,
+                                           t0, tokens, S.h, S.k, d_Y, s);
+      }
     }
     ws_release(alloc, ws, (size_t)L.total, s);
     if (err != hipSuccess) return MEMFINE_ERR_HIP;

@@ -224,6 +224,9 @@ struct MxArgs {
   void* out;                  // FC1: [n, N / 2] as X's format; else [n, N]
   uint8_t* out_scale;         // FC1 on MX8: [n, N / 64]
   int out_bf16;               // [n, N]: bf16, else fp32
+  int cus;                    // compute units of the device
+  const int32_t* ids;         // one token: its slots' experts [n], or null
+  const float* gates;         // one token: its slots' gates [n]
   int col_blocks;             // (set by the launchers)
 };
 int64_t mx4_code_bytes(int64_t N, int64_t K);   // of one matrix
@@ -236,6 +239,12 @@ hipError_t launch_mx4_unpack(int dtype, int64_t E, int N, int K, const uint8_t* 
                              const uint8_t* scales, void* W, hipStream_t s);
 hipError_t launch_mx_fc1(const MxArgs& g, hipStream_t s);
 hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s);  // FC2, linear
+// One token's n slots without dispatch and combine: FC1 of every slot's
+// expert on the token's row into slot rows, and Y = sum of gate FC2 over them.
+// mx_one_token: whether both fit (else the calls above).
+bool mx_one_token(const MxArgs& fc1, const MxArgs& fc2);
+hipError_t launch_mx_one_fc1(const MxArgs& g, hipStream_t s);
+hipError_t launch_mx_one_fc2(const MxArgs& g, hipStream_t s);
 hipError_t launch_mx_combine(const float* y, const int32_t* row_of_slot, const float* gates,
                              int64_t t0, int64_t tokens, int h, int k, void* Y, hipStream_t s);
 

@@ -19,6 +19,7 @@
 // largest term before it is added in fp32).  On bf16 activations the weights
 // are converted with their scale, exactly, by v_cvt_scalef32_pk_bf16_fp4 and
 // multiplied by four bf16 MFMAs of K = 32.
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -32,6 +33,22 @@ typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
 constexpr int kTileBytes = 1024;   // codes of a 16 x 128 tile
 constexpr int kScaleBytes = 256;   // scales of four tiles
 
+// f(Const<0>()), ..., f(Const<N - 1>())
+template <int I> using Const = std::integral_constant<int, I>;
+template <int N, int I = 0, class F> __device__ __forceinline__ void unroll_for(const F& f) {
+  if constexpr (I < N) {
+    f(Const<I>());
+    unroll_for<N, I + 1>(f);
+  }
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int32_t)bytes,
+                                           0x00020000);
+}
+
+constexpr uint32_t kPast = 0x80000000u;  // an offset past any buffer: reads zero
+
 // ------------------------------------------------------------ the operands
 // One tile's K of 16 activation rows, as the wave's operand B.  Lane l holds
 // row l % 16, lane group g = l / 16.  MX8: columns 16 g .. + 15 and 64 + 16 g
@@ -41,26 +58,9 @@ template <bool MX8> struct Act;
 template <> struct Act<true> {
   u32x4_t lo, hi;
   uint32_t s;
-  __device__ __forceinline__ void load(const uint8_t* row, const uint8_t* srow, int k0, int K, int g) {
-    const int a = k0 + 16 * g, b = a + 64, c = k0 + 32 * g;
-    lo = hi = (u32x4_t){0, 0, 0, 0};
-    s = 127;
-    if (a < K) lo = *(const u32x4_t*)(row + a);
-    if (b < K) hi = *(const u32x4_t*)(row + b);
-    if (c < K) s = srow[c / kMxBlock];
-  }
 };
 template <> struct Act<false> {
   u32x4_t v[4];
-  __device__ __forceinline__ void load(const uint8_t* row, const uint8_t*, int k0, int K, int g) {
-    const int c = k0 + 32 * g;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = (u32x4_t){0, 0, 0, 0};
-    if (c < K) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = *(const u32x4_t*)(row + 2 * (c + 8 * j));
-    }
-  }
 };
 
 // acc += tile x activations; the tile's codes are w, its scale byte SW of s;
@@ -124,9 +124,9 @@ __device__ __forceinline__ bool locate(const MxArgs& g, int b, int& e, int& r0, 
 }
 
 // -------------------------------------------------------------- few rows
-// A block of 16 rows x TILES tiles of W per workgroup; its W waves share the
-// reduction (wave w takes tiles w, w + W, ... along K) and add their partial
-// sums through LDS.
+// MB blocks of 16 rows x TILES tiles of W per workgroup; its W waves share the
+// reduction (wave w takes groups w, w + W, ... of four tiles along K) and add
+// their partial sums through LDS.
 //   kFc1     tiles: two of the gate half and the two of the up half of the same
 //            32 columns; SwiGLU, stored as a bf16 or MX8 row block
 //   kRows    bf16 or fp32 rows (FC2, linear)
@@ -175,65 +175,328 @@ __device__ __forceinline__ void store_row(const MxArgs& g, const f32x4_t& v, int
     *(f32x4_t*)((float*)g.out + row * g.N + n) = v;
 }
 
-template <bool MX8, int MODE, int TILES, int W>
-__global__ __launch_bounds__(64 * W) void mx_rows_kernel(MxArgs g) {
-  __shared__ f32x4_t part[W][TILES][64];
+// Rows of activations as operand B, loaded by a wave for itself: lane l
+// takes row l % 16 of a block of 16.  Rows are addressed from `base`, an
+// offset past 2^31 bytes away at most; columns past K read as zero.
+template <bool MX8> struct ActRows {
+  __amdgpu_buffer_rsrc_t rx, rs;
+  uint32_t off, soff;
+  __device__ __forceinline__ void init(const MxArgs& g, int64_t base, int64_t row, int lg) {
+    constexpr int es = MX8 ? 1 : 2;
+    rx = rsrc_of((const uint8_t*)g.X + base * g.K * es, 0x7fffffff);
+    off = (uint32_t)(row - base) * (uint32_t)(g.K * es) + (MX8 ? 16 : 64) * lg;
+    if constexpr (MX8) {
+      rs = rsrc_of(g.XS + base * (g.K / kMxBlock), 0x7fffffff);
+      soff = (uint32_t)(row - base) * (uint32_t)(g.K / kMxBlock) + lg;
+    }
+  }
+  __device__ __forceinline__ void load(int kt, int K, int lg, Act<MX8>& x) const {
+    const int left = K - kt * 128;  // columns from this tile on
+    if constexpr (MX8) {
+      x.lo = __builtin_amdgcn_raw_buffer_load_b128(rx, 16 * lg < left ? off : kPast, kt * 128, 0);
+      x.hi = __builtin_amdgcn_raw_buffer_load_b128(rx, 64 + 16 * lg < left ? off : kPast,
+                                                   kt * 128 + 64, 0);
+      x.s = __builtin_amdgcn_raw_buffer_load_b8(rs, 32 * lg < left ? soff : kPast, kt * 4, 0);
+    } else {
+      const uint32_t o = 32 * lg < left ? off : kPast;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x.v[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, o, kt * 256 + 16 * j, 0);
+    }
+  }
+};
+
+// One wave's part of a product of MB blocks of 16 rows with TILES tiles of 16
+// rows of W: the K tiles of groups (four tiles, one scale word) first, first +
+// stride, ... below `groups`.  Loads run U tiles ahead of the products, and
+// twice that deep over the two halves of the ring.
+template <bool MX8, int TILES, int MB, int U> struct RowsLoop {
+  struct Unit {
+    u32x4_t c[U][TILES];
+    Act<MX8> x[U][MB];
+  };
+  __amdgpu_buffer_rsrc_t rc[TILES], rs[TILES];
+  ActRows<MX8> act[MB];
+  int K, KT, lane;
+
+  __device__ __forceinline__ void set_tile(const MxArgs& g, int i, int e, int tile) {
+    const int NT = g.N / 16, KS = (g.KT + 3) / 4;
+    const int64_t t = (int64_t)e * NT + tile;
+    rc[i] = rsrc_of(g.Wc + t * g.KT * kTileBytes, (uint32_t)g.KT * kTileBytes);
+    rs[i] = rsrc_of(g.Ws + t * KS * kScaleBytes, (uint32_t)KS * kScaleBytes);
+  }
+  __device__ __forceinline__ void load(int kt, Unit& u) const {
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const bool in = kt + q < KT;
+      const uint32_t off = in ? lane * 16 : kPast, at = in ? (kt + q) * kTileBytes : 0;
+#pragma unroll
+      for (int i = 0; i < TILES; ++i)
+        u.c[q][i] = __builtin_amdgcn_raw_buffer_load_b128(rc[i], off, at, 0);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) act[m].load(kt + q, K, lane >> 4, u.x[q][m]);
+    }
+  }
+  __device__ __forceinline__ void load_scales(int grp, uint32_t (&s)[TILES]) const {
+    const bool in = grp * 4 < KT;
+    const uint32_t off = in ? lane * 4 : kPast, at = in ? grp * kScaleBytes : 0;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+      s[i] = __builtin_amdgcn_raw_buffer_load_b32(rs[i], off, at, 0);
+  }
+  template <int Q0>
+  __device__ __forceinline__ void mma(const Unit& u, const uint32_t (&s)[TILES],
+                                      f32x4_t (&acc)[MB][TILES]) const {
+    unroll_for<U>([&](auto q) {
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+          mx_mma<Q0 + decltype(q)::value, 0>(u.c[q][i], s[i], u.x[q][m], acc[m][i]);
+    });
+  }
+  __device__ __forceinline__ void run(int first, int stride, int groups,
+                                      f32x4_t (&acc)[MB][TILES]) const {
+    if (first >= groups) return;
+    Unit a, b;
+    uint32_t s[TILES], sn[TILES];
+    load_scales(first, s);
+    load(first * 4, a);
+    load(first * 4 + U, b);
+    for (int grp = first; grp < groups; grp += stride) {
+      const int next = grp + stride < groups ? (grp + stride) * 4 : 1 << 20;  // past K: no traffic
+      load_scales(next >> 2, sn);
+      unroll_for<2 / U>([&](auto h) {  // U tiles from a, U from b
+        constexpr int q = decltype(h)::value * 2 * U;
+        const int at = q + 2 * U < 4 ? grp * 4 + q + 2 * U : next + q + 2 * U - 4;
+        mma<q>(a, s, acc);
+        load(at, a);
+        __builtin_amdgcn_sched_barrier(0);
+        mma<q + U>(b, s, acc);
+        load(at + U, b);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) s[i] = sn[i];
+    }
+  }
+};
+
+template <bool MX8, int MODE, int TILES, int MB, int W>
+__device__ __forceinline__ void mx_rows(const MxArgs& g, f32x4_t (*part)[MB][TILES][64]) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = blockIdx.x % g.col_blocks, b = blockIdx.x / g.col_blocks;
   int e, r0, r1;
-  if (!locate<16>(g, b, e, r0, r1)) return;  // uniform over the workgroup
+  if (!locate<16 * MB>(g, b, e, r0, r1)) return;  // uniform over the workgroup
   const int lr = lane & 15, lg = lane >> 4;
-  const int r = min(r0 + lr, r1 - 1);  // rows past the block repeat its last, unstored
-  const int64_t src = g.tok_of_row ? g.tok_of_row[r] : r;
-  const uint8_t* xrow = (const uint8_t*)g.X + src * g.K * (MX8 ? 1 : 2);
-  const uint8_t* xs = MX8 ? g.XS + src * (g.K / kMxBlock) : nullptr;
-  const int NT = g.N / 16, KT = g.KT, KS = (KT + 3) / 4;
-  int tile[TILES];
+  const int NT = g.N / 16;
+  RowsLoop<MX8, TILES, MB, 1> loop;
+  loop.K = g.K;
+  loop.KT = g.KT;
+  loop.lane = lane;
 #pragma unroll
-  for (int i = 0; i < TILES; ++i) {
-    if (MODE == kFc1) tile[i] = (i & 1) + 2 * col + (i >> 1) * (NT / 2);
-    else tile[i] = min(col * TILES + i, NT - 1);
+  for (int m = 0; m < MB; ++m) {
+    const int r = min(r0 + 16 * m + lr, r1 - 1);  // rows past the block repeat its last, unstored
+    if (g.tok_of_row) loop.act[m].init(g, 0, g.tok_of_row[r], lg);
+    else loop.act[m].init(g, r0, r, lg);
   }
-  const uint8_t* wc = g.Wc + (int64_t)e * NT * KT * kTileBytes + lane * 16;
-  const uint8_t* ws = g.Ws + (int64_t)e * NT * KS * kScaleBytes + lane * 4;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+    loop.set_tile(g, i, e, MODE == kFc1 ? (i & 1) + 2 * col + (i >> 1) * (NT / 2)
+                                        : min(col * TILES + i, NT - 1));
+  f32x4_t acc[MB][TILES];
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) acc[m][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  loop.run(w, W, (g.KT + 3) / 4, acc);
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) part[w][m][i][lane] = acc[m][i];
+  __syncthreads();
+  auto total = [&](int m, int i) {
+    f32x4_t v = part[0][m][i][lane];
+#pragma unroll
+    for (int ww = 1; ww < W; ++ww) v += part[ww][m][i][lane];
+    return v;
+  };
+  if constexpr (MODE == kFc1) {
+    if (w >= MB) return;
+    const int64_t row = r0 + 16 * w + lr;
+    const f32x4_t gate[2] = {total(w, 0), total(w, 1)}, up[2] = {total(w, 2), total(w, 3)};
+    store_swiglu(g, MX8, gate, up, row, 32 * col, lg, row < r1);
+  } else {
+    for (int q = w; q < TILES * MB; q += W) {
+      const int i = q % TILES, m = q / TILES;
+      const int n0 = (col * TILES + i) * 16;
+      const int64_t row = r0 + 16 * m + lr;
+      if (n0 < g.N && row < r1) store_row(g, total(m, i), row, n0 + 4 * lg);
+    }
+  }
+}
+
+template <bool MX8, int MODE, int TILES, int MB, int W>
+__global__ __launch_bounds__(64 * W) void mx_rows_kernel(MxArgs g) {
+  __shared__ f32x4_t part[W][MB][TILES][64];
+  mx_rows<MX8, MODE, TILES, MB, W>(g, part);
+}
+
+// ---------------------------------------------------------------- one row
+// Products of single rows: the J slots of one token with their experts'
+// matrices, or one row with one matrix.  Slots name distinct experts, so there
+// is nothing to group: no dispatch and no rows to combine.
+//   kFc1   a workgroup takes one slot and 32 columns: a = SwiGLU of the row
+//   kRows  a workgroup takes TILES tiles of columns and all J slots (ids null:
+//          one matrix, gate 1): Y = sum_j gate_j W[id_j] a_j in slot order
+//          over each wave's part, the waves' parts in wave order
+// The rows lie in LDS, and the waves share the units (two K tiles of a slot),
+// every wave's next unit in flight while it multiplies one.
+__host__ __device__ constexpr int one_row_bytes(bool mx8, int KT) {
+  return mx8 ? (KT * 132 + 15) / 16 * 16 : KT * 256;  // values and scales
+}
+
+template <bool MX8, int MODE, int TILES, int W>
+__device__ __forceinline__ void mx_one(const MxArgs& g, char* smem) {
+  constexpr int es = MX8 ? 1 : 2;
+  struct Unit {
+    u32x4_t c[2][TILES];
+    uint32_t s[TILES];
+  };
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  const int KT = g.KT, KS = (KT + 3) / 4, NT = g.N / 16, per = (KT + 1) / 2;
+  const int col = blockIdx.x % g.col_blocks, slot0 = MODE == kFc1 ? blockIdx.x / g.col_blocks : 0;
+  const int J = MODE == kFc1 ? 1 : g.n, units = J * per;
+  const int row_bytes = one_row_bytes(MX8, KT);
+  auto expert = [&](int j) {
+    const int e = g.ids ? __builtin_amdgcn_readfirstlane(g.ids[slot0 + j]) : 0;
+    return (unsigned)e < (unsigned)g.E ? e : -1;  // a dropped slot reads and adds nothing
+  };
+  auto load = [&](int u, Unit& x) {
+    const int j = u / per, kt = (u - j * per) * 2;
+    const int e = u < units ? expert(j) : -1;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const int tile = MODE == kFc1 ? (i & 1) + 2 * col + (i >> 1) * (NT / 2)
+                                    : min(col * TILES + i, NT - 1);
+      const int64_t t = (int64_t)max(e, 0) * NT + tile;
+      const auto rc = rsrc_of(g.Wc + t * KT * kTileBytes, (uint32_t)KT * kTileBytes);
+      const auto rs = rsrc_of(g.Ws + t * KS * kScaleBytes, (uint32_t)KS * kScaleBytes);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const bool in = e >= 0 && kt + q < KT;
+        x.c[q][i] = __builtin_amdgcn_raw_buffer_load_b128(rc, in ? lane * 16 : kPast,
+                                                          in ? (kt + q) * kTileBytes : 0, 0);
+      }
+      x.s[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, e >= 0 ? lane * 4 : kPast,
+                                                    e >= 0 ? (kt >> 2) * kScaleBytes : 0, 0);
+    }
+  };
+  // The rows (FC1: the token's one row, whatever the slot), zero past K; loads
+  // return in order, so these are issued before the first weights.
+  const int chunks = KT * 8 * es, scales = KT * 4;  // of 16 bytes and of one, a row
+  constexpr int kHeld = 4;
+  u32x4_t held[kHeld];
+  const uint8_t* X = (const uint8_t*)g.X;
+  auto chunk = [&](int i, int& at) {
+    const int j = i / chunks, c = i - j * chunks;
+    at = j * row_bytes + c * 16;
+    return i < J * chunks && c * 16 < g.K * es ? *(const u32x4_t*)(X + (int64_t)j * g.K * es + c * 16)
+                                               : (u32x4_t){0, 0, 0, 0};
+  };
+  int at[kHeld];
+#pragma unroll
+  for (int q = 0; q < kHeld; ++q) held[q] = chunk(threadIdx.x + q * 64 * W, at[q]);
+  __builtin_amdgcn_sched_barrier(0);
+  Unit a, b;
+  load(w, a);
+  load(w + W, b);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int q = 0; q < kHeld; ++q)
+    if ((int)threadIdx.x + q * 64 * W < J * chunks) *(u32x4_t*)(smem + at[q]) = held[q];
+  for (int i = threadIdx.x + kHeld * 64 * W; i < J * chunks; i += 64 * W) {
+    const u32x4_t v = chunk(i, at[0]);
+    *(u32x4_t*)(smem + at[0]) = v;
+  }
+  if constexpr (MX8)
+    for (int i = threadIdx.x; i < J * scales; i += 64 * W) {
+      const int j = i / scales, c = i - j * scales, n = g.K / kMxBlock;
+      smem[j * row_bytes + KT * 128 + c] = c < n ? (char)g.XS[(int64_t)j * n + c] : (char)127;
+    }
+  __syncthreads();
   f32x4_t acc[TILES];
 #pragma unroll
   for (int i = 0; i < TILES; ++i) acc[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-  for (int kt = w; kt < KT; kt += W) {
-    u32x4_t c[TILES];
+  auto mma = [&](int u, const Unit& x) {
+    const int j = u / per, kt = (u - j * per) * 2;
+    if (u >= units || expert(j) < 0) return;  // uniform
+    const char* row = smem + j * row_bytes;
+    f32x4_t p[TILES];
     uint32_t s[TILES];
-    Act<MX8> x;
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
-      c[i] = *(const u32x4_t*)(wc + ((int64_t)tile[i] * KT + kt) * kTileBytes);
-      s[i] = ws[((int64_t)tile[i] * KS + kt / 4) * kScaleBytes + (kt & 3)];
+      p[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      s[i] = x.s[i] >> (8 * (kt & 2));
     }
-    x.load(xrow, xs, kt * 128, g.K, lg);
+    unroll_for<2>([&](auto q) {
+      if (kt + q >= KT) return;
+      Act<MX8> v;
+      if constexpr (MX8) {
+        v.lo = *(const u32x4_t*)(row + (kt + q) * 128 + 16 * lg);
+        v.hi = *(const u32x4_t*)(row + (kt + q) * 128 + 64 + 16 * lg);
+        v.s = *(const uint8_t*)(row + KT * 128 + (kt + q) * 4 + lg);
+      } else {
 #pragma unroll
-    for (int i = 0; i < TILES; ++i) mx_mma(c[i], s[i], x, acc[i]);
+        for (int i = 0; i < 4; ++i)
+          v.v[i] = *(const u32x4_t*)(row + (kt + q) * 256 + 64 * lg + 16 * i);
+      }
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) mx_mma<decltype(q)::value, 0>(x.c[q][i], s[i], v, p[i]);
+    });
+    const float gate = MODE == kRows && g.ids ? g.gates[j] : 1.f;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) acc[i] += gate * p[i];
+  };
+  for (int u = w; u < units; u += 2 * W) {
+    mma(u, a);
+    load(u + 2 * W, a);
+    mma(u + W, b);
+    load(u + 3 * W, b);
   }
+  __syncthreads();  // all have read the rows, whose LDS takes the sums
+  f32x4_t* part = (f32x4_t*)smem;  // [W][TILES][64]
 #pragma unroll
-  for (int i = 0; i < TILES; ++i) part[w][i][lane] = acc[i];
+  for (int i = 0; i < TILES; ++i) part[(w * TILES + i) * 64 + lane] = acc[i];
   __syncthreads();
-  const bool live = r0 + lr < r1;
-  const int64_t row = r0 + lr;
   auto total = [&](int i) {
-    f32x4_t v = part[0][i][lane];
+    f32x4_t v = part[i * 64 + lane];
 #pragma unroll
-    for (int ww = 1; ww < W; ++ww) v += part[ww][i][lane];
+    for (int ww = 1; ww < W; ++ww) v += part[(ww * TILES + i) * 64 + lane];
     return v;
   };
   if constexpr (MODE == kFc1) {
     if (w > 0) return;
     const f32x4_t gate[2] = {total(0), total(1)}, up[2] = {total(2), total(3)};
-    store_swiglu(g, MX8, gate, up, row, 32 * col, lg, live);
-  } else {
-    for (int i = w; i < TILES; i += W) {
-      const int n0 = (col * TILES + i) * 16;
-      if (n0 >= g.N || !live) continue;
-      store_row(g, total(i), row, n0 + 4 * lg);
-    }
+    store_swiglu(g, MX8, gate, up, slot0, 32 * col, lg, lr == 0);
+  } else if (w < TILES) {
+    const int n0 = (col * TILES + w) * 16;
+    if (n0 < g.N && lr == 0) store_row(g, total(w), 0, n0 + 4 * lg);
   }
+}
+
+// LDS: the rows, then the waves' sums in their place; at most kOneLds, what
+// every launch may ask for.
+constexpr int64_t kOneLds = 64 << 10;
+int64_t one_lds(const MxArgs& g, bool mx8, int rows, int tiles, int waves) {
+  return std::max<int64_t>((int64_t)rows * one_row_bytes(mx8, g.KT), (int64_t)waves * tiles * 1024);
+}
+
+template <bool MX8, int MODE, int TILES, int W>
+__global__ __launch_bounds__(64 * W) void mx_one_kernel(MxArgs g) {
+  extern __shared__ __attribute__((aligned(16))) char one_smem[];
+  mx_one<MX8, MODE, TILES, W>(g, one_smem);
 }
 
 // ------------------------------------------------------------- many rows
@@ -246,8 +509,6 @@ __global__ __launch_bounds__(64 * W) void mx_rows_kernel(MxArgs g) {
 // LDS rows are kRow = 128 (e4m3) or 256 (bf16) bytes; the 16-byte unit c of row r
 // lies in slot c ^ (r % 8), so that the 16 rows a read takes at once fall on
 // different banks.
-constexpr uint32_t kPast = 0x80000000u;  // an offset past any buffer: reads zero
-
 typedef __attribute__((address_space(3))) void lds_t;
 
 template <int N> __device__ __forceinline__ void wait_loads() {  // at most N loads in flight
@@ -256,20 +517,6 @@ template <int N> __device__ __forceinline__ void wait_loads() {  // at most N lo
 }
 __device__ __forceinline__ void wait_lds() {  // this wave's LDS operations have returned
   __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
-}
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* base, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int32_t)bytes,
-                                           0x00020000);
-}
-
-// f(Const<0>()), ..., f(Const<N - 1>())
-template <int I> using Const = std::integral_constant<int, I>;
-template <int N, int I = 0, class F> __device__ __forceinline__ void unroll_for(const F& f) {
-  if constexpr (I < N) {
-    f(Const<I>());
-    unroll_for<N, I + 1>(f);
-  }
 }
 
 // Activation rows of a workgroup's block, copied to LDS: the rows' values by
@@ -646,13 +893,27 @@ int64_t row_blocks(const MxArgs& g, int RB) {
   return (int64_t)g.n / RB + (g.E < g.n ? g.E : g.n);
 }
 
-template <bool MX8, int MODE, int TILES, int W>
+template <bool MX8, int MODE, int TILES, int MB, int W>
 hipError_t run_rows(MxArgs g, hipStream_t s) {
   g.col_blocks = MODE == kFc1 ? g.N / 64 : (g.N / 16 + TILES - 1) / TILES;
-  const int64_t blocks = row_blocks(g, 16) * g.col_blocks;
+  const int64_t blocks = row_blocks(g, 16 * MB) * g.col_blocks;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  mx_rows_kernel<MX8, MODE, TILES, W><<<(unsigned)blocks, 64 * W, 0, s>>>(g);
+  mx_rows_kernel<MX8, MODE, TILES, MB, W><<<(unsigned)blocks, 64 * W, 0, s>>>(g);
   return hipGetLastError();
+}
+
+// Few rows: as many columns a workgroup as still give the CUs two each.
+template <bool MX8, int MODE, int MB> hipError_t run_few(const MxArgs& g, hipStream_t s) {
+  const int64_t busy = g.offsets ? std::min<int64_t>(g.E, g.n) : (g.n + 16 * MB - 1) / (16 * MB);
+  if constexpr (MODE == kFc1) {
+    if (busy * (g.N / 64) >= 2 * g.cus) return run_rows<MX8, MODE, 4, MB, 4>(g, s);
+    return run_rows<MX8, MODE, 4, MB, 8>(g, s);
+  } else {
+    const int64_t tiles = busy * (g.N / 16);
+    if (tiles >= 8 * g.cus) return run_rows<MX8, MODE, 4, MB, 4>(g, s);
+    if (tiles >= 4 * g.cus) return run_rows<MX8, MODE, 2, MB, 4>(g, s);
+    return run_rows<MX8, MODE, 1, MB, 8>(g, s);
+  }
 }
 
 template <bool MX8, int MODE, int BM, int S, int WAVES>
@@ -666,12 +927,26 @@ hipError_t run_tiles(MxArgs g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <bool MX8, int MODE, int TILES, int W>
+hipError_t run_one(MxArgs g, hipStream_t s) {
+  g.col_blocks = MODE == kFc1 ? g.N / 64 : (g.N / 16 + TILES - 1) / TILES;
+  const int64_t blocks = (int64_t)g.col_blocks * (MODE == kFc1 ? g.n : 1);
+  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  const size_t lds = (size_t)one_lds(g, MX8, MODE == kFc1 ? 1 : g.n, TILES, W);
+  mx_one_kernel<MX8, MODE, TILES, W><<<(unsigned)blocks, 64 * W, lds, s>>>(g);
+  return hipGetLastError();
+}
+
 // Rows of an average matrix decide the block.
 template <bool MX8, int MODE> hipError_t run(const MxArgs& g, hipStream_t s) {
   if (g.n == 0) return hipSuccess;
+  if constexpr (MODE == kRows)
+    if (!g.offsets && g.n == 1 && one_lds(g, MX8, 1, 1, 8) <= kOneLds)
+      return run_one<MX8, MODE, 1, 8>(g, s);
   const int groups = g.offsets ? g.E : 1;
   const int rows = (g.n + groups - 1) / groups;
-  if (rows <= 16) return run_rows<MX8, MODE, 4, 4>(g, s);
+  if (rows <= 8) return run_few<MX8, MODE, 1>(g, s);
+  if (rows <= 32) return run_few<MX8, MODE, 2>(g, s);
   if (rows <= 64) return run_tiles<MX8, MODE, 32, 3, 2>(g, s);
   if (rows <= 128 || !MX8) return run_tiles<MX8, MODE, 64, 3, 2>(g, s);
   return run_tiles<MX8, MODE, MX8 ? 128 : 64, 3, 2>(g, s);
@@ -726,6 +1001,17 @@ hipError_t launch_mx_fc1(const MxArgs& g, hipStream_t s) {
 }
 hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s) {
   return g.XS ? run<true, kRows>(g, s) : run<false, kRows>(g, s);
+}
+
+bool mx_one_token(const MxArgs& fc1, const MxArgs& fc2) {
+  return one_lds(fc1, fc1.XS, 1, 4, 8) <= kOneLds &&
+         one_lds(fc2, fc2.XS, fc2.n, 1, 8) <= kOneLds;
+}
+hipError_t launch_mx_one_fc1(const MxArgs& g, hipStream_t s) {
+  return g.XS ? run_one<true, kFc1, 4, 8>(g, s) : run_one<false, kFc1, 4, 8>(g, s);
+}
+hipError_t launch_mx_one_fc2(const MxArgs& g, hipStream_t s) {
+  return g.XS ? run_one<true, kRows, 1, 8>(g, s) : run_one<false, kRows, 1, 8>(g, s);
 }
 
 hipError_t launch_mx_combine(const float* y, const int32_t* row_of_slot, const float* gates,
