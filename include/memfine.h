@@ -508,7 +508,7 @@ int memfine_router_logits_bwd(const memfine_shape* shape, const void* d_X, const
                               const memfine_allocator* alloc, void* stream);
 
 /* ------------------------------------------------------------------------
- * MX4 matrices.  W [N, K] (N a multiple of 16, K of 32; N < 2^30, K <= 2^20) is held
+ * MX4 matrices.  W [N, K] (N a multiple of 16, K of 32; N <= 2^22, K <= 2^20) is held
  * in the matrix cores' order in two buffers of memfine_mxw_code_bytes(N, K)
  * and memfine_mxw_scale_bytes(N, K) bytes (< 0: invalid sizes); E matrices of
  * one size follow each other in both.  memfine_mxw_pack lays out row-major codes

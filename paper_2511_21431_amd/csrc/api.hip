@@ -1410,8 +1410,8 @@ RouteArgs route_args(const memfine_gating& g) {
 
 int check_mx4(int64_t E, int32_t N, int32_t K) {
   if (E < 1 || N < 16 || N % 16 || K < 32 || K % 32) return MEMFINE_ERR_INVALID_ARG;
-  // (the kernels address 256 activation rows with 31-bit offsets)
-  if (N >= (1 << 30) || K > (1 << 20)) return MEMFINE_ERR_UNSUPPORTED;
+  // (the kernels address 128 rows of activations and of results with 31-bit offsets)
+  if (N > (1 << 22) || K > (1 << 20)) return MEMFINE_ERR_UNSUPPORTED;
   return MEMFINE_OK;
 }
 
@@ -1426,15 +1426,33 @@ struct MxLayout {
   Layout tables;
   int64_t o_a, o_as, o_y, total;
   bool y_bf16;
+  int splits;  // FC2's partial results
 };
+// FC2 of n grouped rows, as far as its kernel's choice goes.
+MxArgs mx_fc2_args(const memfine_shape& s, int64_t n, const int32_t* offsets) {
+  MxArgs g = {};
+  g.n = (int)n;
+  g.E = s.E;
+  g.N = s.h;
+  g.K = s.F;
+  g.KT = (s.F + 127) / 128;
+  g.cus = device_cus();
+  g.offsets = offsets;
+  return g;
+}
 MxLayout mx_layout(const memfine_shape& s, int64_t n, bool mx8) {
+  static const int32_t grouped = 0;
   MxLayout m;
   layout(s, n, -1, true, false, m.tables);
+  m.y_bf16 = mx8 && n > kMxWideRows;
+  MxArgs g = mx_fc2_args(s, n, &grouped);
+  g.XS = mx8 ? (const uint8_t*)&grouped : nullptr;
+  m.splits = mx_splits(g);
+  if (m.splits > 1) m.y_bf16 = false;
   m.o_a = m.tables.total;
   m.o_as = m.o_a + align256(n * s.F * (mx8 ? 1 : 2));
   m.o_y = m.o_as + align256(mx8 ? n * (s.F / 32) : 0);
-  m.y_bf16 = mx8 && n > kMxWideRows;
-  m.total = m.o_y + align256(n * (int64_t)s.h * (m.y_bf16 ? 2 : 4));
+  m.total = m.o_y + align256(n * (int64_t)s.h * (m.y_bf16 ? 2 : 4) * m.splits);
   return m;
 }
 }  // namespace
@@ -1655,7 +1673,16 @@ int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const u
   const double nk = (double)N * K, xb = d_XS ? 1.03125 : 2.0;
   KernelTimer kt(MEMFINE_K_MX_LINEAR, s, 2.0 * T * nk,
                  0.53125 * nk + xb * T * K + (g.out_bf16 ? 2.0 : 4.0) * T * N);
-  return hip_status(launch_mx_rows(g, s));
+  const int splits = mx_splits(g);
+  if (splits == 1) return hip_status(launch_mx_rows(g, s));
+  const size_t bytes = (size_t)splits * T * N * 4;
+  g.out = ws_alloc(nullptr, bytes, s);
+  if (!g.out) return MEMFINE_ERR_OOM;
+  hipError_t err = launch_mx_rows(g, s);
+  if (err == hipSuccess)
+    err = launch_mx_sum((const float*)g.out, splits, T * N, g.out_bf16, d_Y, s);
+  ws_release(nullptr, g.out, bytes, s);
+  return hip_status(err);
 }
 
 int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chunks, int32_t mx8) {
@@ -1706,21 +1733,16 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
     g1.offsets = cb.m.offsets;
     g1.out = ws + L.o_a;
     g1.out_scale = mx8 ? (uint8_t*)(ws + L.o_as) : nullptr;
-    MxArgs g2 = g1;  // FC2
+    MxArgs g2 = mx_fc2_args(S, n, cb.m.offsets);
     g2.X = g1.out;
     g2.XS = g1.out_scale;
-    g2.out_scale = nullptr;
-    g2.tok_of_row = nullptr;
     g2.Wc = d_W2_codes;
     g2.Ws = d_W2_scales;
-    g2.N = S.h;
-    g2.K = S.F;
-    g2.KT = (S.F + 127) / 128;
     g2.out = ws + L.o_y;
     g2.out_bf16 = L.y_bf16;
     // weights of the experts that can have rows
     const double nd = (double)n, wb = 0.53125 * hF * (double)std::min<int64_t>(S.E, n);
-    const double yb = L.y_bf16 ? 2.0 : 4.0;
+    const double yb = L.y_bf16 ? 2.0 : 4.0 * L.splits;
     hipError_t err = hipSuccess;
     if (tokens == 1 && mx_one_token(g1, g2)) {
       // one token's slots name distinct experts: nothing to group or combine
@@ -1757,8 +1779,8 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
                        yb * nd * S.h + 2.0 * tokens * S.h + 8.0 * nd);
         err = L.y_bf16 ? launch_combine(MEMFINE_BF16, ws + L.o_y, cb.m.row_of_slot, d_gates, t0,
                                         (int)tokens, S.h, S.k, d_Y, s)
-                       : launch_mx_combine((const float*)(ws + L.o_y), cb.m.row_of_slot, d_gates,
-                                           t0, tokens, S.h, S.k, d_Y, s);
+                       : launch_mx_combine((const float*)(ws + L.o_y), L.splits, n * S.h,
+                                           cb.m.row_of_slot, d_gates, t0, tokens, S.h, S.k, d_Y, s);
       }
     }
     ws_release(alloc, ws, (size_t)L.total, s);

@@ -227,7 +227,7 @@ struct MxArgs {
   int cus;                    // compute units of the device
   const int32_t* ids;         // one token: its slots' experts [n], or null
   const float* gates;         // one token: its slots' gates [n]
-  int col_blocks;             // (set by the launchers)
+  int col_blocks, row_blocks, col_shares, splits, run;  // (set by the launchers)
 };
 int64_t mx4_code_bytes(int64_t N, int64_t K);   // of one matrix
 int64_t mx4_scale_bytes(int64_t N, int64_t K);
@@ -238,14 +238,20 @@ hipError_t launch_mx4_quantize(int dtype, int64_t E, int N, int K, const void* W
 hipError_t launch_mx4_unpack(int dtype, int64_t E, int N, int K, const uint8_t* codes,
                              const uint8_t* scales, void* W, hipStream_t s);
 hipError_t launch_mx_fc1(const MxArgs& g, hipStream_t s);
-hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s);  // FC2, linear
+// FC2, linear.  Where mx_splits(g) > 1 the reduction is split: `out` then takes
+// that many partial fp32 results [splits][n][N] (launch_mx_sum adds them up).
+int mx_splits(const MxArgs& g);
+hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s);
+hipError_t launch_mx_sum(const float* part, int splits, int64_t n, int out_bf16, void* out,
+                         hipStream_t s);
 // One token's n slots without dispatch and combine: FC1 of every slot's
 // expert on the token's row into slot rows, and Y = sum of gate FC2 over them.
 // mx_one_token: whether both fit (else the calls above).
 bool mx_one_token(const MxArgs& fc1, const MxArgs& fc2);
 hipError_t launch_mx_one_fc1(const MxArgs& g, hipStream_t s);
 hipError_t launch_mx_one_fc2(const MxArgs& g, hipStream_t s);
-hipError_t launch_mx_combine(const float* y, const int32_t* row_of_slot, const float* gates,
-                             int64_t t0, int64_t tokens, int h, int k, void* Y, hipStream_t s);
+hipError_t launch_mx_combine(const float* y, int splits, int64_t stride, const int32_t* row_of_slot,
+                             const float* gates, int64_t t0, int64_t tokens, int h, int k, void* Y,
+                             hipStream_t s);
 
 }  // namespace memfine

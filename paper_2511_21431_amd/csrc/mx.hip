@@ -48,6 +48,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* base, uint
 }
 
 constexpr uint32_t kPast = 0x80000000u;  // an offset past any buffer: reads zero
+// Cache policy of weights that a call reads once: non-temporal, which keeps
+// them from displacing the activations (1 and 64 tokens through 32 experts, h
+// 7168, F 2048: 42.4 -> 39.2 and 178 -> 171 us).
+constexpr int kOnce = 2;
+
+template <int N> __device__ __forceinline__ void wait_loads() {  // at most N loads in flight
+  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+__device__ __forceinline__ void wait_lds() {  // this wave's LDS operations have returned
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+}
 
 // ------------------------------------------------------------ the operands
 // One tile's K of 16 activation rows, as the wave's operand B.  Lane l holds
@@ -123,14 +135,8 @@ __device__ __forceinline__ bool locate(const MxArgs& g, int b, int& e, int& r0, 
   return false;
 }
 
-// -------------------------------------------------------------- few rows
-// MB blocks of 16 rows x TILES tiles of W per workgroup; its W waves share the
-// reduction (wave w takes groups w, w + W, ... of four tiles along K) and add
-// their partial sums through LDS.
-//   kFc1     tiles: two of the gate half and the two of the up half of the same
-//            32 columns; SwiGLU, stored as a bf16 or MX8 row block
-//   kRows    bf16 or fp32 rows (FC2, linear)
-enum { kFc1, kRows };
+// ------------------------------------------------------------ the results
+enum { kFc1, kRows };  // SwiGLU rows in X's format; bf16 or fp32 rows (FC2, linear)
 
 // a = silu(u) v of a lane's eight values (two tiles x four columns of row r),
 // stored at columns f and f + 16 on; on MX8 activations the 32 columns that
@@ -175,6 +181,7 @@ __device__ __forceinline__ void store_row(const MxArgs& g, const f32x4_t& v, int
     *(f32x4_t*)((float*)g.out + row * g.N + n) = v;
 }
 
+// -------------------------------------------------------------- few rows
 // Rows of activations as operand B, loaded by a wave for itself: lane l
 // takes row l % 16 of a block of 16.  Rows are addressed from `base`, an
 // offset past 2^31 bytes away at most; columns past K read as zero.
@@ -206,140 +213,193 @@ template <bool MX8> struct ActRows {
   }
 };
 
-// One wave's part of a product of MB blocks of 16 rows with TILES tiles of 16
-// rows of W: the K tiles of groups (four tiles, one scale word) first, first +
-// stride, ... below `groups`.  Loads run U tiles ahead of the products, and
-// twice that deep over the two halves of the ring.
-template <bool MX8, int TILES, int MB, int U> struct RowsLoop {
-  struct Unit {
-    u32x4_t c[U][TILES];
-    Act<MX8> x[U][MB];
-  };
-  __amdgpu_buffer_rsrc_t rc[TILES], rs[TILES];
-  ActRows<MX8> act[MB];
-  int K, KT, lane;
-
-  __device__ __forceinline__ void set_tile(const MxArgs& g, int i, int e, int tile) {
-    const int NT = g.N / 16, KS = (g.KT + 3) / 4;
-    const int64_t t = (int64_t)e * NT + tile;
-    rc[i] = rsrc_of(g.Wc + t * g.KT * kTileBytes, (uint32_t)g.KT * kTileBytes);
+// FC1 of a block of 16 rows x 32 columns (two tiles of the gate half, two of
+// the up half) per workgroup.  Its W waves share the reduction: wave w takes
+// groups w, w + W, ... of four K tiles (one scale word), a K tile's loads in
+// flight while the one before it is multiplied, and the waves' sums meet in
+// LDS.  Bound by the read of the weights: 256 slots over 32 experts (h 7168, F
+// 2048, 499 MB) 85 us on MX8, 92 on bf16.
+template <bool MX8, int W>
+__device__ __forceinline__ void mx_fc1_rows(const MxArgs& g, f32x4_t (*part)[4][64]) {
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // four row blocks of one column block follow each other on one XCD (workgroup
+  // ids go to the 8 XCDs by turns): those of one matrix share it in its L2
+  const int seq = blockIdx.x / 8, cols8 = (g.col_blocks + 7) / 8;
+  const int col = seq / 4 % cols8 * 8 + blockIdx.x % 8, b = seq / (4 * cols8) * 4 + seq % 4;
+  int e, r0, r1;
+  if (col >= g.col_blocks || !locate<16>(g, b, e, r0, r1)) return;  // uniform over the workgroup
+  const int lr = lane & 15, lg = lane >> 4;
+  const int NT = g.N / 16, KT = g.KT, KS = (KT + 3) / 4;
+  ActRows<MX8> act;
+  const int r = min(r0 + lr, r1 - 1);  // rows past the block repeat its last, unstored
+  act.init(g, g.tok_of_row ? 0 : r0, g.tok_of_row ? g.tok_of_row[r] : r, lg);
+  __amdgpu_buffer_rsrc_t rc[4], rs[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t t = (int64_t)e * NT + (i & 1) + 2 * col + (i >> 1) * (NT / 2);
+    rc[i] = rsrc_of(g.Wc + t * KT * kTileBytes, (uint32_t)KT * kTileBytes);
     rs[i] = rsrc_of(g.Ws + t * KS * kScaleBytes, (uint32_t)KS * kScaleBytes);
   }
-  __device__ __forceinline__ void load(int kt, Unit& u) const {
+  struct Unit {
+    u32x4_t c[4];
+    Act<MX8> x;
+  };
+  auto load = [&](int kt, Unit& u) {
+    const bool in = kt < KT;
 #pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const bool in = kt + q < KT;
-      const uint32_t off = in ? lane * 16 : kPast, at = in ? (kt + q) * kTileBytes : 0;
+    for (int i = 0; i < 4; ++i)
+      u.c[i] = __builtin_amdgcn_raw_buffer_load_b128(rc[i], in ? lane * 16 : kPast,
+                                                     in ? kt * kTileBytes : 0, kOnce);
+    act.load(kt, g.K, lg, u.x);
+  };
+  auto load_scales = [&](int grp, uint32_t (&s)[4]) {
+    const bool in = grp < KS;
 #pragma unroll
-      for (int i = 0; i < TILES; ++i)
-        u.c[q][i] = __builtin_amdgcn_raw_buffer_load_b128(rc[i], off, at, 0);
+    for (int i = 0; i < 4; ++i)
+      s[i] = __builtin_amdgcn_raw_buffer_load_b32(rs[i], in ? lane * 4 : kPast,
+                                                  in ? grp * kScaleBytes : 0, 0);
+  };
+  f32x4_t acc[4];
 #pragma unroll
-      for (int m = 0; m < MB; ++m) act[m].load(kt + q, K, lane >> 4, u.x[q][m]);
-    }
-  }
-  __device__ __forceinline__ void load_scales(int grp, uint32_t (&s)[TILES]) const {
-    const bool in = grp * 4 < KT;
-    const uint32_t off = in ? lane * 4 : kPast, at = in ? grp * kScaleBytes : 0;
+  for (int i = 0; i < 4; ++i) acc[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  Unit u[2];
+  uint32_t s[4], sn[4];
+  load_scales(w, s);
+  load(w * 4, u[0]);
+  load(w * 4 + 1, u[1]);
+  for (int grp = w; grp < KS; grp += W) {
+    load_scales(grp + W, sn);
+    unroll_for<4>([&](auto q) {
 #pragma unroll
-    for (int i = 0; i < TILES; ++i)
-      s[i] = __builtin_amdgcn_raw_buffer_load_b32(rs[i], off, at, 0);
-  }
-  template <int Q0>
-  __device__ __forceinline__ void mma(const Unit& u, const uint32_t (&s)[TILES],
-                                      f32x4_t (&acc)[MB][TILES]) const {
-    unroll_for<U>([&](auto q) {
-#pragma unroll
-      for (int m = 0; m < MB; ++m)
-#pragma unroll
-        for (int i = 0; i < TILES; ++i)
-          mx_mma<Q0 + decltype(q)::value, 0>(u.c[q][i], s[i], u.x[q][m], acc[m][i]);
+      for (int i = 0; i < 4; ++i) mx_mma<decltype(q)::value, 0>(u[q % 2].c[i], s[i], u[q % 2].x, acc[i]);
+      load(q < 2 ? grp * 4 + q + 2 : (grp + W) * 4 + q - 2, u[q % 2]);
+      __builtin_amdgcn_sched_barrier(0);
     });
-  }
-  __device__ __forceinline__ void run(int first, int stride, int groups,
-                                      f32x4_t (&acc)[MB][TILES]) const {
-    if (first >= groups) return;
-    Unit a, b;
-    uint32_t s[TILES], sn[TILES];
-    load_scales(first, s);
-    load(first * 4, a);
-    load(first * 4 + U, b);
-    for (int grp = first; grp < groups; grp += stride) {
-      const int next = grp + stride < groups ? (grp + stride) * 4 : 1 << 20;  // past K: no traffic
-      load_scales(next >> 2, sn);
-      unroll_for<2 / U>([&](auto h) {  // U tiles from a, U from b
-        constexpr int q = decltype(h)::value * 2 * U;
-        const int at = q + 2 * U < 4 ? grp * 4 + q + 2 * U : next + q + 2 * U - 4;
-        mma<q>(a, s, acc);
-        load(at, a);
-        __builtin_amdgcn_sched_barrier(0);
-        mma<q + U>(b, s, acc);
-        load(at + U, b);
-        __builtin_amdgcn_sched_barrier(0);
-      });
 #pragma unroll
-      for (int i = 0; i < TILES; ++i) s[i] = sn[i];
-    }
+    for (int i = 0; i < 4; ++i) s[i] = sn[i];
   }
-};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) part[w][i][lane] = acc[i];
+  __syncthreads();
+  if (w > 0) return;
+  f32x4_t v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = part[0][i][lane];
+#pragma unroll
+    for (int ww = 1; ww < W; ++ww) v[i] += part[ww][i][lane];
+  }
+  const f32x4_t gate[2] = {v[0], v[1]}, up[2] = {v[2], v[3]};
+  store_swiglu(g, MX8, gate, up, r0 + lr, 32 * col, lg, r0 + lr < r1);
+}
 
-template <bool MX8, int MODE, int TILES, int MB, int W>
-__device__ __forceinline__ void mx_rows(const MxArgs& g, f32x4_t (*part)[MB][TILES][64]) {
+template <bool MX8, int W> __global__ __launch_bounds__(64 * W, 2) void mx_fc1_rows_kernel(MxArgs g) {
+  __shared__ f32x4_t part[W][4][64];
+  mx_fc1_rows<MX8, W>(g, part);
+}
+
+// MB blocks of 16 rows per workgroup, each wave with its group of four K tiles
+// of the activations in registers; the workgroup walks over the column blocks
+// [c0, c1) of its share, so that the weights stream without a pause: a K tile
+// is loaded for the next column block as soon as it has been multiplied.  The
+// waves' sums meet in LDS, in two buffers by turns, so that one barrier a
+// column block is enough.  Past eight groups the reduction is split over
+// g.splits workgroups, which write fp32 partial rows [splits][n][N].  Bound by
+// the read of the weights (48 rows, 28672 x 4096: 62 MB in 20 us, of which
+// about 6 go by before the first and after the last of them arrive).
+template <bool MX8, int TILES, int MB, int W>
+__device__ __forceinline__ void mx_cols(const MxArgs& g, f32x4_t (*part)[W][MB][TILES][64]) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = blockIdx.x % g.col_blocks, b = blockIdx.x / g.col_blocks;
-  int e, r0, r1;
-  if (!locate<16 * MB>(g, b, e, r0, r1)) return;  // uniform over the workgroup
   const int lr = lane & 15, lg = lane >> 4;
-  const int NT = g.N / 16;
-  RowsLoop<MX8, TILES, MB, 1> loop;
-  loop.K = g.K;
-  loop.KT = g.KT;
-  loop.lane = lane;
+  const int b = blockIdx.x % g.row_blocks, rest = blockIdx.x / g.row_blocks;
+  const int share = rest % g.col_shares, z = rest / g.col_shares;
+  const int c0 = share * g.col_blocks / g.col_shares, c1 = (share + 1) * g.col_blocks / g.col_shares;
+  int e, r0, r1;
+  if (!locate<16 * MB>(g, b, e, r0, r1)) return;
+  const int NT = g.N / 16, KT = g.KT, KS = (KT + 3) / 4;
+  const int per = (KS + g.splits - 1) / g.splits, grp = z * per + w;  // this wave's group
+  const int left = w < per ? KT - 4 * grp : 0;                          // its K tiles
+  float* partial = (float*)g.out + (int64_t)z * g.n * g.N;
+  const int64_t t0 = (int64_t)e * NT;
+  // the matrix's codes and scales of one tile row, by the row's number
+  auto load = [&](int col, int q, u32x4_t (&c)[TILES]) {
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const int64_t t = t0 + min(col * TILES + i, NT - 1);
+      const bool in = q < left && col < c1;
+      c[i] = __builtin_amdgcn_raw_buffer_load_b128(
+          rsrc_of(g.Wc + t * KT * kTileBytes, (uint32_t)KT * kTileBytes), in ? lane * 16 : kPast,
+          in ? (4 * grp + q) * kTileBytes : 0, kOnce);
+    }
+  };
+  auto load_scales = [&](int col, uint32_t (&s)[TILES]) {
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const int64_t t = t0 + min(col * TILES + i, NT - 1);
+      const bool in = left > 0 && col < c1;
+      s[i] = __builtin_amdgcn_raw_buffer_load_b32(
+          rsrc_of(g.Ws + t * KS * kScaleBytes, (uint32_t)KS * kScaleBytes), in ? lane * 4 : kPast,
+          in ? grp * kScaleBytes : 0, 0);
+    }
+  };
+  Act<MX8> x[4][MB];
 #pragma unroll
   for (int m = 0; m < MB; ++m) {
     const int r = min(r0 + 16 * m + lr, r1 - 1);  // rows past the block repeat its last, unstored
-    if (g.tok_of_row) loop.act[m].init(g, 0, g.tok_of_row[r], lg);
-    else loop.act[m].init(g, r0, r, lg);
+    ActRows<MX8> act;
+    act.init(g, g.tok_of_row ? 0 : r0, g.tok_of_row ? g.tok_of_row[r] : r, lg);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) act.load(left > 0 ? 4 * grp + q : KT, g.K, lg, x[q][m]);
   }
+  u32x4_t c[4][TILES];
+  uint32_t s[TILES], sn[TILES];
+  load_scales(c0, s);
 #pragma unroll
-  for (int i = 0; i < TILES; ++i)
-    loop.set_tile(g, i, e, MODE == kFc1 ? (i & 1) + 2 * col + (i >> 1) * (NT / 2)
-                                        : min(col * TILES + i, NT - 1));
-  f32x4_t acc[MB][TILES];
+  for (int q = 0; q < 4; ++q) load(c0, q, c[q]);
+  for (int col = c0; col < c1; ++col) {
+    f32x4_t acc[MB][TILES];
 #pragma unroll
-  for (int m = 0; m < MB; ++m)
+    for (int m = 0; m < MB; ++m)
 #pragma unroll
-    for (int i = 0; i < TILES; ++i) acc[m][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-  loop.run(w, W, (g.KT + 3) / 4, acc);
+      for (int i = 0; i < TILES; ++i) acc[m][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    load_scales(col + 1, sn);
+    unroll_for<4>([&](auto q) {
 #pragma unroll
-  for (int m = 0; m < MB; ++m)
+      for (int m = 0; m < MB; ++m)
 #pragma unroll
-    for (int i = 0; i < TILES; ++i) part[w][m][i][lane] = acc[m][i];
-  __syncthreads();
-  auto total = [&](int m, int i) {
-    f32x4_t v = part[0][m][i][lane];
+        for (int i = 0; i < TILES; ++i) mx_mma<decltype(q)::value, 0>(c[q][i], s[i], x[q][m], acc[m][i]);
+      load(col + 1, q, c[q]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    auto& buf = part[(col - c0) & 1];
 #pragma unroll
-    for (int ww = 1; ww < W; ++ww) v += part[ww][m][i][lane];
-    return v;
-  };
-  if constexpr (MODE == kFc1) {
-    if (w >= MB) return;
-    const int64_t row = r0 + 16 * w + lr;
-    const f32x4_t gate[2] = {total(w, 0), total(w, 1)}, up[2] = {total(w, 2), total(w, 3)};
-    store_swiglu(g, MX8, gate, up, row, 32 * col, lg, row < r1);
-  } else {
-    for (int q = w; q < TILES * MB; q += W) {
-      const int i = q % TILES, m = q / TILES;
-      const int n0 = (col * TILES + i) * 16;
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) buf[w][m][i][lane] = acc[m][i];
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int q0 = 0; q0 < TILES * MB; q0 += W) {
+      const int q = q0 + w;
+      if (q >= TILES * MB) break;
+      const int i = q % TILES, m = q / TILES, n0 = (col * TILES + i) * 16;
       const int64_t row = r0 + 16 * m + lr;
-      if (n0 < g.N && row < r1) store_row(g, total(m, i), row, n0 + 4 * lg);
+      f32x4_t v = buf[0][m][i][lane];
+#pragma unroll
+      for (int ww = 1; ww < W; ++ww) v += buf[ww][m][i][lane];
+      if (n0 >= g.N || row >= r1) continue;
+      if (g.splits > 1) *(f32x4_t*)(partial + row * g.N + n0 + 4 * lg) = v;
+      else store_row(g, v, row, n0 + 4 * lg);
     }
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) s[i] = sn[i];
   }
 }
 
-template <bool MX8, int MODE, int TILES, int MB, int W>
-__global__ __launch_bounds__(64 * W) void mx_rows_kernel(MxArgs g) {
-  __shared__ f32x4_t part[W][MB][TILES][64];
-  mx_rows<MX8, MODE, TILES, MB, W>(g, part);
+template <bool MX8, int TILES, int MB, int W>
+__global__ __launch_bounds__(64 * W, 2) void mx_cols_kernel(MxArgs g) {
+  __shared__ f32x4_t part[2][W][MB][TILES][64];
+  mx_cols<MX8, TILES, MB, W>(g, part);
 }
 
 // ---------------------------------------------------------------- one row
@@ -387,7 +447,7 @@ __device__ __forceinline__ void mx_one(const MxArgs& g, char* smem) {
       for (int q = 0; q < 2; ++q) {
         const bool in = e >= 0 && kt + q < KT;
         x.c[q][i] = __builtin_amdgcn_raw_buffer_load_b128(rc, in ? lane * 16 : kPast,
-                                                          in ? (kt + q) * kTileBytes : 0, 0);
+                                                          in ? (kt + q) * kTileBytes : 0, kOnce);
       }
       x.s[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, e >= 0 ? lane * 4 : kPast,
                                                     e >= 0 ? (kt >> 2) * kScaleBytes : 0, 0);
@@ -511,23 +571,17 @@ __global__ __launch_bounds__(64 * W) void mx_one_kernel(MxArgs g) {
 // different banks.
 typedef __attribute__((address_space(3))) void lds_t;
 
-template <int N> __device__ __forceinline__ void wait_loads() {  // at most N loads in flight
-  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
-  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
-}
-__device__ __forceinline__ void wait_lds() {  // this wave's LDS operations have returned
-  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
-}
 
-// Activation rows of a workgroup's block, copied to LDS: the rows' values by
-// 16-byte direct copies, on MX8 the rows' scale bytes (four a row and stage)
-// through registers.  Columns past K read as zero.
+// Activation rows of a workgroup's block, copied to LDS: the rows' values 16
+// bytes a lane, on MX8 the rows' scale bytes (four a row and stage) one a lane,
+// which the copy widens to a dword.  Columns past K read as zero.
 template <bool MX8, int BM> struct ActTile {
   static constexpr int kRow = MX8 ? 128 : 256, kUnits = kRow / 16;
   static constexpr int kBytes = BM * kRow;
   static constexpr int kCopies = kBytes / 4096;             // 1024-byte copies per wave
-  static constexpr int kScales = MX8 ? (BM + 63) / 64 : 0;  // scale bytes per thread
-  static constexpr int kStage = kBytes + (MX8 ? 256 * kScales : 0);
+  static constexpr int kScales = MX8 ? (BM + 63) / 64 : 0;  // 256-byte copies of scales per wave
+  static constexpr int kIssue = kCopies + kScales;
+  static constexpr int kStage = kBytes + 1024 * kScales;
   __amdgpu_buffer_rsrc_t rx, rs;
   uint32_t off[kCopies], soff[kScales ? kScales : 1];
   int col;
@@ -562,36 +616,19 @@ template <bool MX8, int BM> struct ActTile {
     for (int i = 0; i < kCopies; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_t*)(lds + (i * 4 + w) * 1024), 16,
                                                kt * 128 + col < K ? off[i] : kPast, kt * kRow, 0, 0);
-  }
-  __device__ __forceinline__ void load_scales(int kt, int K, uint8_t (&v)[2]) {
+    // (32 rows: the other half of the lanes copies what nobody reads)
 #pragma unroll
     for (int i = 0; i < kScales; ++i)
-      v[i] = __builtin_amdgcn_raw_buffer_load_b8(
-          rs, kt * 128 + 32 * (int)(threadIdx.x & 3) < K ? soff[i] : kPast, kt * 4, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rs, (lds_t*)(lds + kBytes + (i * 4 + w) * 256), 1,
+          kt * 128 + 32 * (int)(threadIdx.x & 3) < K ? soff[i] : kPast, kt * 4, 0, 0);
   }
-  // The scale of row r, block b at byte b BM + (r % 16) (BM / 16) + r / 16: a
-  // lane's, for all its rows, are neighbours.
-  __device__ __forceinline__ void store_scales(char* lds, const uint8_t (&v)[2]) {
-#pragma unroll
-    for (int i = 0; i < kScales; ++i) {
-      const int r = (int)threadIdx.x / 4 + 64 * i, b = threadIdx.x & 3;
-      // (of 32 rows: the other half of the threads writes bytes that nobody reads)
-      const int at = BM == 32 && r >= 32 ? threadIdx.x : b * BM + (r & 15) * (BM / 16) + (r >> 4);
-      lds[kBytes + at] = (char)v[i];
-    }
-  }
-  __device__ __forceinline__ static void read_scales(const char* lds, int lr, int lg,
-                                                     uint32_t (&s)[(BM + 63) / 64]) {
-    const char* p = lds + kBytes + lg * BM + lr * (BM / 16);
-    if constexpr (BM == 32) s[0] = *(const uint16_t*)p;
-    else
-#pragma unroll
-      for (int i = 0; i < BM / 64; ++i) s[i] = *(const uint32_t*)(p + 4 * i);
-  }
-  // operand B of rows 16 i .. + 15 (row: the lane's row of i = 0; its scale apart)
-  __device__ __forceinline__ static void read(const char* row, int i, int lr, int lg, Act<MX8>& x) {
+  // operand B of rows 16 i .. + 15
+  __device__ __forceinline__ static void read(const char* lds, int i, int lr, int lg, Act<MX8>& x) {
     const int sw = lr & 7;
+    const char* row = lds + lr * kRow;
     if constexpr (MX8) {
+      x.s = *(const uint32_t*)(lds + kBytes + (lr * 4 + lg) * 4 + i * 256);
       x.lo = *(const u32x4_t*)(row + ((lg ^ sw) << 4) + 16 * i * kRow);
       x.hi = *(const u32x4_t*)(row + (((4 + lg) ^ sw) << 4) + 16 * i * kRow);
     } else {
@@ -608,9 +645,10 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
   constexpr int MI = BM / 16;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lg = lane >> 4;
-  // 64 consecutive tiles, 8 row blocks x 8 column blocks, to one XCD
-  // (workgroup ids go to the 8 XCDs by turns): they share operands in its L2
-  const int id = blockIdx.x, tile_id = (id / 512) * 512 + (id % 8) * 64 + id / 8 % 64;
+  // runs of `run` consecutive tiles (8 row blocks x run / 8 column blocks) to
+  // one XCD (workgroup ids go to the 8 XCDs by turns): they share operands in its L2
+  const int id = blockIdx.x, turn = id / (8 * g.run);
+  const int tile_id = (turn * 8 + id % 8) * g.run + id / 8 % g.run;
   const int band = tile_id / (8 * g.col_blocks), in = tile_id % (8 * g.col_blocks);
   const int cb = in / 8;
   int e, r0, r1;
@@ -631,7 +669,8 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
   auto load_w = [&](int kt, u32x4_t (&c)[4]) {  // past K: zeros
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      c[i] = __builtin_amdgcn_raw_buffer_load_b128(rc[i], lane * 16, kt * kTileBytes, 0);
+      c[i] = __builtin_amdgcn_raw_buffer_load_b128(
+          rc[i], kt < KT ? lane * 16 : kPast, kt < KT ? kt * kTileBytes : 0, 0);
   };
   auto load_ws = [&](int kt, uint32_t (&s)[4]) {  // of tiles kt .. kt + 3, kt % 4 == 0
 #pragma unroll
@@ -644,95 +683,99 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 
-  // stages 0 .. S - 3 whole; of stage S - 2 the copies are in flight and the
-  // scales in registers
-  u32x4_t c0[4], c1[4];
+  u32x4_t c[2][4];  // the weights of this step and the next
   uint32_t ws[4], wsn[4];
-  uint8_t xs[2] = {};
-  char *cur = smem, *next = smem + (S - 2) * A::kStage;  // stage of step kt, of step kt + S - 2
+  char *cur = smem, *next = smem + (S - 1) * A::kStage;  // stage of step kt, of step kt + S - 1
   constexpr int kEnd = S * A::kStage;
-#pragma unroll
-  for (int kt = 0; kt < S - 2; ++kt) {
-    a.copy(kt, g.K, smem + kt * A::kStage, w);
-    a.load_scales(kt, g.K, xs);
-    a.store_scales(smem + kt * A::kStage, xs);
-  }
   load_ws(0, ws);
-  load_w(0, c0);
-  a.load_scales(S - 2, g.K, xs);
-  a.copy(S - 2, g.K, next, w);
+  load_w(0, c[0]);
+#pragma unroll
+  for (int kt = 0; kt + 1 < S; ++kt) a.copy(kt, g.K, smem + kt * A::kStage, w);
 
-  // step kt = 4 i + U on the weights c, with those of the next step loaded into cn
-  auto step = [&](auto U, int kt, u32x4_t (&c)[4], u32x4_t (&cn)[4]) {
+  // step kt = 4 i + U on the weights c[U % 2]
+  auto step = [&](auto U, int kt) {
     __builtin_amdgcn_sched_barrier(0);  // the previous step's products stay before the barrier
-    // All but the copies issued last (of stage kt + S - 2) has arrived.
-    a.store_scales(next, xs);
-    wait_loads<A::kCopies>();
+    // The stage and the weights of step kt have arrived; the copies of the
+    // S - 2 stages after it, issued after the weights, may be in flight.
+    wait_loads<(S - 2) * A::kIssue>();
     wait_lds();
     // publishes every wave's copies of stage kt, and all waves are done with
     // the stage of step kt - 1, which the next copies overwrite
     __builtin_amdgcn_s_barrier();
-    next = next + A::kStage == smem + kEnd ? smem : next + A::kStage;
     if (U == 0) load_ws(kt + 4, wsn);
-    load_w(kt + 1, cn);
-    a.load_scales(kt + S - 1, g.K, xs);
+    load_w(kt + 1, c[(U + 1) % 2]);
     a.copy(kt + S - 1, g.K, next, w);
     __builtin_amdgcn_sched_barrier(0);  // the loads stay here, a step before their use
-    const char* row = cur + lr * A::kRow;
-    uint32_t xw[(BM + 63) / 64] = {};
-    if constexpr (MX8) A::read_scales(cur, lr, lg, xw);
+    // a row block's operand is read while the one before it is multiplied (left
+    // to the scheduler, the reads of all of them moved up and 128 rows spilled)
+    Act<MX8> x[2];
+    A::read(cur, 0, lr, lg, x[0]);
     unroll_for<MI>([&](auto i) {
-      Act<MX8> x;
-      A::read(row, i, lr, lg, x);
-      if constexpr (MX8) x.s = xw[i / 4];
+      if constexpr (i + 1 < MI) A::read(cur, i + 1, lr, lg, x[(i + 1) % 2]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) mx_mma<U, i % 4>(c[j], ws[j], x, acc[i][j]);
+      for (int j = 0; j < 4; ++j) mx_mma<U, 0>(c[U % 2][j], ws[j], x[i % 2], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
     });
     if (U == 3) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) ws[j] = wsn[j];
     }
     cur = cur + A::kStage == smem + kEnd ? smem : cur + A::kStage;
+    next = next + A::kStage == smem + kEnd ? smem : next + A::kStage;
   };
   int kt = 0;
   for (; kt + 3 < KT; kt += 4) {
-    step(Const<0>(), kt, c0, c1);
-    step(Const<1>(), kt + 1, c1, c0);
-    step(Const<2>(), kt + 2, c0, c1);
-    step(Const<3>(), kt + 3, c1, c0);
+    step(Const<0>(), kt);
+    step(Const<1>(), kt + 1);
+    step(Const<2>(), kt + 2);
+    step(Const<3>(), kt + 3);
   }
-  if (kt < KT) step(Const<0>(), kt, c0, c1);
-  if (kt + 1 < KT) step(Const<1>(), kt + 1, c1, c0);
-  if (kt + 2 < KT) step(Const<2>(), kt + 2, c0, c1);
+  if (kt < KT) step(Const<0>(), kt);
+  if (kt + 1 < KT) step(Const<1>(), kt + 1);
+  if (kt + 2 < KT) step(Const<2>(), kt + 2);
   wait_loads<0>();  // the copies past K have landed before the workgroup's LDS is given up
 
+  if constexpr (MODE == kFc1) {
+    const int f0 = (cb * 4 + w) * 32;
 #pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    const int64_t row = r0 + 16 * i + lr;
-    const bool live = row < r1;
-    if constexpr (MODE == kFc1) {
-      const int f0 = (cb * 4 + w) * 32;
+    for (int i = 0; i < MI; ++i) {
+      const int64_t row = r0 + 16 * i + lr;
       const f32x4_t gate[2] = {acc[i][0], acc[i][1]}, up[2] = {acc[i][2], acc[i][3]};
-      store_swiglu(g, MX8, gate, up, row, f0, lg, live && f0 < g.N / 2);
-    } else {
+      store_swiglu(g, MX8, gate, up, row, f0, lg, row < r1 && f0 < g.N / 2);
+    }
+  } else {
+    // through a buffer over the block's rows: an offset past it stores nothing
+    const int es = g.out_bf16 ? 2 : 4, n0 = (cb * 4 + w) * 64;
+    const auto ro = rsrc_of((char*)g.out + (int64_t)r0 * g.N * es, 0x7fffffff);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int r = 16 * i + lr;
+      const uint32_t off = (uint32_t)r * (uint32_t)(g.N * es) + (n0 + 4 * lg) * es;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int n0 = ((cb * 4 + w) * 4 + j) * 16;
-        if (n0 < g.N && live) store_row(g, acc[i][j], row, n0 + 4 * lg);
+        const f32x4_t v = acc[i][j];
+        const uint32_t o = r0 + r < r1 && n0 + 16 * j < g.N ? off + 16 * j * es : kPast;
+        if (g.out_bf16)
+          __builtin_amdgcn_raw_buffer_store_b64(
+              (u32x2_t){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}, ro, o, 0, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), ro, o, 0, 0);
       }
     }
   }
 }
 
-template <bool MX8, int MODE, int BM, int S, int WAVES>
-__global__ __launch_bounds__(256, WAVES) void mx_tile_kernel(MxArgs g) {
+template <bool MX8, int MODE, int BM, int S>
+__global__ __launch_bounds__(256, 2) void mx_tile_kernel(MxArgs g) {
   __shared__ __attribute__((aligned(1024))) char smem[S * ActTile<MX8, BM>::kStage];
   mx_tile<MX8, MODE, BM, S>(g, smem);
 }
 
-// Y[t0 + i] = sum_j gate[t, j] y[row_of_slot[i k + j]], fp32 rows, bf16 out: a
-// thread takes four columns; a dropped slot (row < 0) adds nothing.
-__global__ __launch_bounds__(256) void mx_combine_kernel(const float* __restrict__ y,
+// Y[t0 + i] = sum_j gate[t, j] y[row_of_slot[i k + j]], y the sum of `splits`
+// fp32 rows `stride` floats apart, bf16 out: a thread takes four columns; a
+// dropped slot (row < 0) adds nothing.
+__global__ __launch_bounds__(256) void mx_combine_kernel(const float* __restrict__ y, int splits,
+                                                         int64_t stride,
                                                          const int32_t* __restrict__ row_of_slot,
                                                          const float* __restrict__ gates,
                                                          int64_t t0, int64_t n, int h, int k,
@@ -750,6 +793,11 @@ __global__ __launch_bounds__(256) void mx_combine_kernel(const float* __restrict
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (j0 + j < k) v[j] = *(const f32x4_t*)(y + (int64_t)max(r[j], 0) * h + c);
+    for (int s = 1; s < splits; ++s) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j0 + j < k) v[j] += *(const f32x4_t*)(y + s * stride + (int64_t)max(r[j], 0) * h + c);
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (r[j] < 0) continue;
@@ -759,6 +807,18 @@ __global__ __launch_bounds__(256) void mx_combine_kernel(const float* __restrict
     }
   }
   Vec4<bf16_t>::store(Y + (t0 + i) * h + c, f);
+}
+
+// out[i] = the sum of `splits` partial arrays of n floats (n a multiple of 16).
+template <typename T>
+__global__ __launch_bounds__(256) void mx_sum_kernel(const float* __restrict__ part, int splits,
+                                                     int64_t n, T* __restrict__ out) {
+  const int64_t i = (blockIdx.x * 256ll + threadIdx.x) * 4;
+  if (i >= n) return;
+  f32x4_t v = *(const f32x4_t*)(part + i);
+  for (int s = 1; s < splits; ++s) v += *(const f32x4_t*)(part + s * n + i);
+  const float f[4] = {v[0], v[1], v[2], v[3]};
+  Vec4<T>::store(out + i, f);
 }
 
 // -------------------------------------------------------------- the layout
@@ -893,37 +953,51 @@ int64_t row_blocks(const MxArgs& g, int RB) {
   return (int64_t)g.n / RB + (g.E < g.n ? g.E : g.n);
 }
 
-template <bool MX8, int MODE, int TILES, int MB, int W>
-hipError_t run_rows(MxArgs g, hipStream_t s) {
-  g.col_blocks = MODE == kFc1 ? g.N / 64 : (g.N / 16 + TILES - 1) / TILES;
-  const int64_t blocks = row_blocks(g, 16 * MB) * g.col_blocks;
+// Matrices with rows, about.
+int64_t busy(const MxArgs& g, int RB) {
+  return g.offsets ? std::min<int64_t>(g.E, g.n) : (g.n + RB - 1) / RB;
+}
+
+template <bool MX8, int W> hipError_t run_fc1_rows(MxArgs g, hipStream_t s) {
+  g.col_blocks = g.N / 64;
+  const int64_t blocks = (int64_t)((g.col_blocks + 7) / 8 * 8) * ((row_blocks(g, 16) + 3) / 4 * 4);
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  mx_rows_kernel<MX8, MODE, TILES, MB, W><<<(unsigned)blocks, 64 * W, 0, s>>>(g);
+  mx_fc1_rows_kernel<MX8, W><<<(unsigned)blocks, 64 * W, 0, s>>>(g);
   return hipGetLastError();
 }
 
-// Few rows: as many columns a workgroup as still give the CUs two each.
-template <bool MX8, int MODE, int MB> hipError_t run_few(const MxArgs& g, hipStream_t s) {
-  const int64_t busy = g.offsets ? std::min<int64_t>(g.E, g.n) : (g.n + 16 * MB - 1) / (16 * MB);
-  if constexpr (MODE == kFc1) {
-    if (busy * (g.N / 64) >= 2 * g.cus) return run_rows<MX8, MODE, 4, MB, 4>(g, s);
-    return run_rows<MX8, MODE, 4, MB, 8>(g, s);
-  } else {
-    const int64_t tiles = busy * (g.N / 16);
-    if (tiles >= 8 * g.cus) return run_rows<MX8, MODE, 4, MB, 4>(g, s);
-    if (tiles >= 4 * g.cus) return run_rows<MX8, MODE, 2, MB, 4>(g, s);
-    return run_rows<MX8, MODE, 1, MB, 8>(g, s);
-  }
+int groups_of(const MxArgs& g) { return (g.KT + 3) / 4; }
+int splits_of(const MxArgs& g) { return (groups_of(g) + 7) / 8; }
+
+// Two workgroups a CU of W = 4 waves, one of 8.
+template <bool MX8, int MB, int W> hipError_t run_cols(MxArgs g, hipStream_t s) {
+  constexpr int TILES = 2;
+  g.splits = splits_of(g);
+  g.col_blocks = (g.N / 16 + TILES - 1) / TILES;
+  const int64_t rb = row_blocks(g, 16 * MB);
+  const int64_t want = (8 / W) * g.cus / (busy(g, 16 * MB) * g.splits);
+  g.col_shares = (int)std::max<int64_t>(1, std::min<int64_t>(g.col_blocks, want));
+  const int64_t blocks = rb * g.col_shares * g.splits;
+  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  g.row_blocks = (int)rb;
+  mx_cols_kernel<MX8, TILES, MB, W><<<(unsigned)blocks, 64 * W, 0, s>>>(g);
+  return hipGetLastError();
+}
+template <bool MX8, int MB> hipError_t run_cols(const MxArgs& g, hipStream_t s) {
+  return groups_of(g) <= 4 ? run_cols<MX8, MB, 4>(g, s) : run_cols<MX8, MB, 8>(g, s);
 }
 
-template <bool MX8, int MODE, int BM, int S, int WAVES>
+template <bool MX8, int MODE, int BM, int S>
 hipError_t run_tiles(MxArgs g, hipStream_t s) {
   g.col_blocks = (MODE == kFc1 ? g.N / 2 + 127 : g.N + 255) / (MODE == kFc1 ? 128 : 256);
   const int64_t bands = (row_blocks(g, BM) + 7) / 8;
-  // whole rounds of 64 tiles on each of 8 XCDs
-  const int64_t blocks = (bands * 8 * g.col_blocks + 511) / 512 * 512;
+  // at least one run for every XCD among the tiles that there are surely
+  // (a grouped call's trailing row blocks can be empty)
+  const int64_t sure = std::max<int64_t>(busy(g, BM), g.n / BM) * g.col_blocks;
+  g.run = sure >= 512 ? 64 : sure >= 256 ? 32 : sure >= 128 ? 16 : 8;
+  const int64_t blocks = (bands * 8 * g.col_blocks + 8 * g.run - 1) / (8 * g.run) * (8 * g.run);
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  mx_tile_kernel<MX8, MODE, BM, S, WAVES><<<(unsigned)blocks, 256, 0, s>>>(g);
+  mx_tile_kernel<MX8, MODE, BM, S><<<(unsigned)blocks, 256, 0, s>>>(g);
   return hipGetLastError();
 }
 
@@ -937,19 +1011,62 @@ hipError_t run_one(MxArgs g, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Rows of an average matrix decide the block.
-template <bool MX8, int MODE> hipError_t run(const MxArgs& g, hipStream_t s) {
-  if (g.n == 0) return hipSuccess;
-  if constexpr (MODE == kRows)
-    if (!g.offsets && g.n == 1 && one_lds(g, MX8, 1, 1, 8) <= kOneLds)
-      return run_one<MX8, MODE, 1, 8>(g, s);
+enum Kind { kOneRow, kFewRows, kTiles32, kTiles64, kTiles128 };
+
+// The kernel of a call, by the rows of an average matrix, the K tiles and the
+// tiles of 256 columns (FC1: 128 of each half) that there are for the CUs.
+// Measured both ways (us, kernel alone; E experts, rows each):
+//   FC1, few rows against 32-row tiles: h 7168 F 2048 E 32, 8 rows 86 / 92, 16
+//     rows 126 / 97 (64-row tiles); h 2048 F 1408 E 16, 2 rows 14.1 / 15.2, 8
+//     rows 18.3 / 16.2; h 4096 F 512 E 8 (32 tiles), 8 rows 12 / 20, 32 rows
+//     17 / 19, 128 rows 31 / 21.
+//   FC2 and linear: K 4096 N 28672, 64 rows 25 / 39, 128 rows 35 / 39 (bf16 50 /
+//     48); K 7168 N 4096, 128 rows 23 / 30, 256 rows 31 / 29; K 2048 N 7168, 64
+//     rows 11 / 12, 128 rows 18 / 12; K 704 E 64, 6 rows 21 / 15.
+//   64-row against 32-row tiles, MX8: h 7168 F 2048 E 32, 16 rows 95 / 116, 128
+//     rows 194 / 224; h 4096 F 512 E 8, 128 rows (64 tiles of 64) 23 / 20; h 2048
+//     F 704 E 64, 12 rows 28 / 26, 384 rows 85 / 112.
+//   bf16: E 32, 64 rows 200 / 186, 256 rows 441 / 464.
+//   128-row against 64-row tiles, MX8: E 32, 2048 rows 1459 / 1544 (FC2 959 / 974),
+//     256 rows 285 / 275; h 2048 F 704 E 64, 384 rows 93 / 85.
+Kind kind_of(const MxArgs& g, int mode) {
+  const bool mx8 = g.XS != nullptr;
+  if (mode == kRows && !g.offsets && g.n == 1 && one_lds(g, mx8, 1, 1, 8) <= kOneLds) return kOneRow;
   const int groups = g.offsets ? g.E : 1;
   const int rows = (g.n + groups - 1) / groups;
-  if (rows <= 8) return run_few<MX8, MODE, 1>(g, s);
-  if (rows <= 32) return run_few<MX8, MODE, 2>(g, s);
-  if (rows <= 64) return run_tiles<MX8, MODE, 32, 3, 2>(g, s);
-  if (rows <= 128 || !MX8) return run_tiles<MX8, MODE, 64, 3, 2>(g, s);
-  return run_tiles<MX8, MODE, MX8 ? 128 : 64, 3, 2>(g, s);
+  const int64_t cols = mode == kFc1 ? (g.N / 2 + 127) / 128 : (g.N + 255) / 256;
+  auto tiles = [&](int BM) { return std::max<int64_t>(busy(g, BM), g.n / BM) * cols; };
+  bool few;
+  if (mode == kFc1) few = rows <= (g.KT >= 32 ? 8 : 4) || tiles(32) < g.cus / 4;
+  else if (g.KT >= 32) few = rows <= 64 || tiles(32) < g.cus / 2;
+  else few = (rows <= 8 && g.KT >= 16) || tiles(32) < g.cus / 4;
+  if (few) return kFewRows;
+  if (!mx8) return rows >= 256 && tiles(64) >= 2 * g.cus ? kTiles64 : kTiles32;
+  if (rows >= 512 && tiles(128) >= 8 * g.cus) return kTiles128;
+  return tiles(64) >= (rows >= 64 ? g.cus / 2 : 2 * g.cus) ? kTiles64 : kTiles32;
+}
+
+template <bool MX8, int MODE> hipError_t run(const MxArgs& g, hipStream_t s) {
+  if (g.n == 0) return hipSuccess;
+  switch (kind_of(g, MODE)) {
+    case kOneRow:
+      if constexpr (MODE == kRows) return run_one<MX8, MODE, 1, 8>(g, s);
+      return hipErrorInvalidValue;
+    case kFewRows:
+      if constexpr (MODE == kFc1) {
+        if (busy(g, 16) * (g.N / 64) >= 2 * g.cus) return run_fc1_rows<MX8, 4>(g, s);
+        return run_fc1_rows<MX8, 8>(g, s);
+      } else {
+        // 64 rows of MX8 activations fit in registers, 32 of bf16
+        if (MX8 && (g.offsets ? g.n > 8 * g.E : g.n > 32)) return run_cols<MX8, MX8 ? 4 : 2>(g, s);
+        return run_cols<MX8, 2>(g, s);
+      }
+    case kTiles32: return run_tiles<MX8, MODE, 32, 3>(g, s);
+    case kTiles64: return run_tiles<MX8, MODE, 64, 3>(g, s);
+    default:
+      if constexpr (MX8) return run_tiles<MX8, MODE, 128, 3>(g, s);
+      return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace
@@ -1003,6 +1120,17 @@ hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s) {
   return g.XS ? run<true, kRows>(g, s) : run<false, kRows>(g, s);
 }
 
+int mx_splits(const MxArgs& g) { return kind_of(g, kRows) == kFewRows ? splits_of(g) : 1; }
+hipError_t launch_mx_sum(const float* part, int splits, int64_t n, int out_bf16, void* out,
+                         hipStream_t s) {
+  unsigned blocks;
+  if (n == 0) return hipSuccess;
+  if (hipError_t err = grid_of(n / 4, &blocks)) return err;
+  if (out_bf16) mx_sum_kernel<bf16_t><<<blocks, 256, 0, s>>>(part, splits, n, (bf16_t*)out);
+  else mx_sum_kernel<float><<<blocks, 256, 0, s>>>(part, splits, n, (float*)out);
+  return hipGetLastError();
+}
+
 bool mx_one_token(const MxArgs& fc1, const MxArgs& fc2) {
   return one_lds(fc1, fc1.XS, 1, 4, 8) <= kOneLds &&
          one_lds(fc2, fc2.XS, fc2.n, 1, 8) <= kOneLds;
@@ -1014,13 +1142,15 @@ hipError_t launch_mx_one_fc2(const MxArgs& g, hipStream_t s) {
   return g.XS ? run_one<true, kRows, 1, 8>(g, s) : run_one<false, kRows, 1, 8>(g, s);
 }
 
-hipError_t launch_mx_combine(const float* y, const int32_t* row_of_slot, const float* gates,
-                             int64_t t0, int64_t tokens, int h, int k, void* Y, hipStream_t s) {
+hipError_t launch_mx_combine(const float* y, int splits, int64_t stride, const int32_t* row_of_slot,
+                             const float* gates, int64_t t0, int64_t tokens, int h, int k, void* Y,
+                             hipStream_t s) {
   const int64_t n = tokens * (h / 4);
   unsigned blocks;
   if (n == 0) return hipSuccess;
   if (hipError_t err = grid_of(n, &blocks)) return err;
-  mx_combine_kernel<<<blocks, 256, 0, s>>>(y, row_of_slot, gates, t0, n, h, k, (bf16_t*)Y);
+  mx_combine_kernel<<<blocks, 256, 0, s>>>(y, splits, stride, row_of_slot, gates, t0, n, h, k,
+                                           (bf16_t*)Y);
   return hipGetLastError();
 }
 
