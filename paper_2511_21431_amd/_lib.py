@@ -9,6 +9,7 @@ no fallback: if the library is not built, loading it raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional, Sequence
 
@@ -79,6 +80,7 @@ class Model(ctypes.Structure):
 
 
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+SCORES = {"softmax": SCORE_SOFTMAX, "sigmoid": SCORE_SIGMOID}
 
 
 class Gating(ctypes.Structure):
@@ -196,9 +198,15 @@ def make_shape(T: int, h: int, F: int, E: int, k: int, dtype: int) -> Shape:
 
 
 # ----------------------------------------------------------- tensor checks
+_TORCH = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
 
 
 def _dt(shape: Shape):
@@ -206,27 +214,33 @@ def _dt(shape: Shape):
     return torch.bfloat16 if shape.dtype == BF16 else torch.float32
 
 
-def _ptr(t, shape_tuple, dtype, name):
+def _ptr(t, shape_tuple, dtype, name) -> int:
+    """Address of a contiguous device tensor of that shape and dtype.  (One
+    condition for the tensor that passes: a call of a few microseconds on the
+    GPU has half a dozen of these.)"""
+    if t is not None and t.shape == shape_tuple and t.dtype == dtype and t.is_contiguous():
+        if t.is_cuda:
+            return t.data_ptr()
+        if t.numel() == 0:
+            return 0
+        raise ValueError(f"{name} must be a device tensor")
     if t is None:
         raise ValueError(f"{name} is required")
     if tuple(t.shape) != tuple(shape_tuple):
         raise ValueError(f"{name}: shape {tuple(t.shape)} != expected {tuple(shape_tuple)}")
     if t.dtype != dtype:
         raise ValueError(f"{name}: dtype {t.dtype} != expected {dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if not t.is_cuda and t.numel() > 0:
-        raise ValueError(f"{name} must be a device tensor")
-    return ctypes.c_void_p(t.data_ptr() if t.numel() > 0 else 0)
+    raise ValueError(f"{name} must be contiguous")
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream):
+    """Handle of the stream (None: torch's current stream on the current device)."""
     if stream is None:
         torch = _torch()
-        stream = torch.cuda.current_stream()
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if hasattr(stream, "cuda_stream"):
-        return ctypes.c_void_p(stream.cuda_stream)
-    return ctypes.c_void_p(int(stream))
+        return stream.cuda_stream
+    return int(stream)
 
 
 class TorchAllocator:
@@ -566,11 +580,9 @@ def memfine_mx_values(Q, QS, out, stream=None) -> None:
 def make_gating(E: int, k: int, score: str = "softmax", groups: int = 1, top_groups: int = 1,
                 renorm: bool = True, scale: float = 1.0) -> Gating:
     """memfine_gating; score is "softmax" or "sigmoid"."""
-    scores = {"softmax": SCORE_SOFTMAX, "sigmoid": SCORE_SIGMOID}
-    if score not in scores:
+    if score not in SCORES:
         raise ValueError(f"score: {score!r} is neither 'softmax' nor 'sigmoid'")
-    return Gating(int(E), int(k), scores[score], int(groups), int(top_groups), int(bool(renorm)),
-                  float(scale))
+    return Gating(E, k, SCORES[score], groups, top_groups, bool(renorm), scale)
 
 
 def memfine_route_fwd(gating: Gating, logits, idx, gates, bias=None, stream=None) -> None:
@@ -635,9 +647,14 @@ def memfine_mxw_scale_bytes(N: int, K: int) -> int:
     return int(v)
 
 
+@functools.lru_cache(maxsize=256)
+def _mxw_bytes(N: int, K: int):
+    return memfine_mxw_code_bytes(N, K), memfine_mxw_scale_bytes(N, K)
+
+
 def _mxw_buffers(E, N, K, codes, scales, device):
     torch = _torch()
-    cb, sb = memfine_mxw_code_bytes(N, K), memfine_mxw_scale_bytes(N, K)
+    cb, sb = _mxw_bytes(N, K)
     if codes is None:
         codes = torch.empty((E, cb), dtype=torch.uint8, device=device)
     if scales is None:
