@@ -201,7 +201,8 @@ struct RouteArgs {
   int groups, top_groups, renorm;
   float scale;
   int v;                      // experts per lane   (set by the launchers)
-  int lane_groups;            // groups are whole lanes
+  int lane_groups;            // groups are 1 << group_shift whole lanes
+  int group_shift;
 };
 hipError_t launch_route_fwd(const float* logits, const float* bias, int64_t T, RouteArgs a,
                             int32_t* idx, float* gates, hipStream_t s);

@@ -15,6 +15,13 @@
 // Sixteen lanes hold a token (lane l: experts l v .. l v + v - 1, v = E / 16
 // rounded up), so every reduction over the experts is four DPP steps inside a
 // row of 16 lanes and a wave works on four tokens at once.
+//
+// The forward is bound by vector instructions (131072 tokens of 256 logits: 134
+// MB, 28 us at the copy rate).  Each lane sorts its values once (a network of
+// minima and maxima, no ids); a round of the selection then takes the largest
+// head of the 16 lists and pops it; the ids come last, all k at once: lane j
+// looks its value up among the owning lane's values.  Searching the id and
+// clearing it in every round took 71 us instead.
 #include <cfloat>
 
 #include "common.h"
@@ -25,16 +32,11 @@ namespace {
 
 constexpr int kTokens = 16;  // tokens per workgroup of 256 threads
 
-// e^x for x <= 0, to about one unit in the last place: the product's rounding
-// error is carried into the result (v_exp_f32 of the rounded product alone is
-// off by |x| units).
+// e^x for x <= 0.  The rounding of x log2(e) is a relative error of |x| 2^-24:
+// nothing beside the sums' where e^x counts in them, and below 1e-6 down to
+// e^-16 of the largest.
 __device__ __forceinline__ float exp_neg(float x) {
-  constexpr float kLog2e = 1.44269502f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.693147182f;
-  x = fmaxf(x, -150.f);  // e^-150 is 0, and the product below stays finite
-  const float t = x * kLog2e;
-  const float lo = fmaf(x, kLog2eLow, fmaf(x, kLog2e, -t));
-  const float e = __builtin_amdgcn_exp2f(t);
-  return fmaf(e, lo * kLn2, e);
+  return __builtin_amdgcn_exp2f(fmaxf(x, -150.f) * 1.44269502f);
 }
 // sigmoid(z) and 1 - sigmoid(z), both without cancellation; |z| finite.
 __device__ __forceinline__ float sigmoid_pair(float z, float* complement) {
@@ -79,50 +81,84 @@ template <int kCtrl> __device__ __forceinline__ void merge_two(float& a, float& 
   b = fmaxf(fminf(a, oa), fmaxf(b, ob));
   a = fmaxf(a, oa);
 }
-// Rank of this lane's (score, id) among the row's 16 lanes: how many other
-// lanes have a larger score, or the same with a lower id.
-template <int N> __device__ __forceinline__ void count_better(float s, int id, int& n) {
-  const float os = dpp_f<kRor + N>(s);
-  const int oid = dpp_i<kRor + N>(id);
-  n += (os > s || (os == s && oid < id)) ? 1 : 0;
-  if constexpr (N < 15) count_better<N + 1>(s, id, n);
+// The lowest lane of this lane's row of 16 where `yes` holds (it holds in one).
+__device__ __forceinline__ int first_lane(bool yes, int lane) {
+  return __builtin_ctz((uint32_t)(__ballot(yes) >> (lane & 48)) & 0xffffu);
+}
+// v sorted from the largest on (a merge-exchange network).
+template <int V> __device__ __forceinline__ void sort_down(uint32_t (&v)[V]) {
+#pragma unroll
+  for (int p = 1; p < V; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j <= V - 1 - k; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < V && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            const uint32_t a = v[i + j], b = v[i + j + k];
+            v[i + j] = max(a, b);
+            v[i + j + k] = min(a, b);
+          }
+}
+// How many of the lanes l - 1, ..., l - 15 of the row have this lane's (x, n),
+// n >= 0; lanes that do not exist have n = -1.
+template <int N> __device__ __forceinline__ void count_same(uint32_t x, int n, int& c) {
+  const uint32_t ox = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x110 + N, 0xf, 0xf, false);
+  const int on = __builtin_amdgcn_update_dpp(-1, n, 0x110 + N, 0xf, 0xf, false);
+  c += (ox == x && on == n) ? 1 : 0;
+  if constexpr (N < 15) count_same<N + 1>(x, n, c);
 }
 
-// Order-preserving key of a value (0: not a candidate, 1: masked or NaN).
+// Values of the selection: what is masked ranks below every number, what is no
+// candidate (past E, outside the chosen groups) below that; and their keys,
+// integers of the same order (0: no candidate).
+constexpr float kMasked = -FLT_MAX, kNone = -INFINITY;
 __device__ __forceinline__ uint32_t value_key(float v) {
-  const uint32_t u = __float_as_uint(v + 0.f);
-  return v != v ? 1u : (u >> 31) ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(v + 0.f);  // (-0 as +0)
+  return v == kNone ? 0u : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 __device__ __forceinline__ bool unmasked(float z) { return z > -FLT_MAX; }  // false for a NaN
 
-// A lane's v experts of a row of E floats: 16-, 8- or 4-byte loads, `fill`
-// past the row.
+// A lane's v experts (from e0 = l v on) of a row of E floats that starts `row`
+// floats into a buffer: 16-, 8- or 4-byte loads, `fill` past the row.
 template <int V>
-__device__ __forceinline__ void load_share(const float* __restrict__ row, int E, int v, int l,
+__device__ __forceinline__ void load_share(__amdgpu_buffer_rsrc_t buf, int row, int E, int v, int l,
                                            float fill, float (&z)[V]) {
+  constexpr uint32_t kPast = 0x80000000u;  // past the buffer: reads zero
   const int e0 = l * v;
+  const uint32_t off = (uint32_t)(row + e0) * 4;
+  auto in = [&](int q) { return q < v && e0 + q < E; };
   if (v % 4 == 0 && E % 4 == 0) {
 #pragma unroll
     for (int q = 0; q < V; q += 4) {
-      f32x4_t x = {fill, fill, fill, fill};
-      if (q < v && e0 + q < E) x = *(const f32x4_t*)(row + e0 + q);
+      const f32x4_t x = __builtin_bit_cast(
+          f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(buf, in(q) ? off + 4 * q : kPast, 0, 0));
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (q + i < V) z[q + i] = x[i];
+      for (int i = 0; i < 4; ++i) z[q + i] = x[i];
     }
   } else if (v % 2 == 0 && E % 2 == 0) {
 #pragma unroll
     for (int q = 0; q < V; q += 2) {
-      f32x2_t x = {fill, fill};
-      if (q < v && e0 + q < E) x = *(const f32x2_t*)(row + e0 + q);
+      const f32x2_t x = __builtin_bit_cast(
+          f32x2_t, __builtin_amdgcn_raw_buffer_load_b64(buf, in(q) ? off + 4 * q : kPast, 0, 0));
       z[q] = x[0];
-      if (q + 1 < V) z[q + 1] = x[1];
+      z[q + 1] = x[1];
     }
   } else {
 #pragma unroll
-    for (int q = 0; q < V; ++q) z[q] = q < v && e0 + q < E ? row[e0 + q] : fill;
+    for (int q = 0; q < V; ++q)
+      z[q] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buf, in(q) ? off + 4 * q : kPast, 0, 0));
   }
+  if (16 * V != E) {
+#pragma unroll
+    for (int q = 0; q < V; ++q) z[q] = in(q) ? z[q] : fill;
+  }
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t floats(const float* p, int64_t n) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), (short)0, (int32_t)(n * 4),
+                                           0x00020000);
 }
 
 // The row's softmax statistics: maximum (a finite number) and 1 / sum of e^(z - max); 0 for a
@@ -141,41 +177,58 @@ __device__ __forceinline__ void softmax_stats(const float (&z)[V], float& m, flo
   if (!(m > -INFINITY)) m = 0.f;
 }
 
-template <int V>
+// H: the heads of a lane's list that the k rounds can reach (k <= 8: at most 8).
+template <int V, int H>
 __global__ __launch_bounds__(256) void route_fwd_kernel(const float* __restrict__ logits,
                                                         const float* __restrict__ bias, int64_t T,
                                                         RouteArgs a, int32_t* __restrict__ idx,
                                                         float* __restrict__ gates) {
-  __shared__ int32_t won[kTokens][16];
+  // every lane's values; 16-byte aligned rows, spread over the banks
+  constexpr int kRow = V + 4;
+  __shared__ __attribute__((aligned(16))) uint32_t held[kTokens][16][kRow];
   const int l = threadIdx.x & 15, tok = threadIdx.x >> 4, lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * kTokens + tok;
   const float* row = logits + min(t, T - 1) * a.E;  // tokens past T repeat the last, unstored
   const int v = a.v, E = a.E;
   float z[V], b[V];
-  load_share<V>(row, E, v, l, -INFINITY, z);
-  if (bias) load_share<V>(bias, E, v, l, 0.f, b);
+  const int64_t t0 = (int64_t)blockIdx.x * kTokens;
+  const int rows = (int)min((int64_t)kTokens, T - t0);
+  load_share<V>(floats(logits + t0 * E, rows * E), min(tok, rows - 1) * E, E, v, l, -INFINITY, z);
+  if (bias) load_share<V>(floats(bias, E), 0, E, v, l, 0.f, b);
 #pragma unroll
   for (int q = 0; q < V; ++q) z[q] = z[q] > FLT_MAX ? FLT_MAX : z[q];
   float m = 0.f, inv = 0.f;
   if (a.score == 0) softmax_stats<V>(z, m, inv);
-  // values of the selection, -inf where masked, and their keys
-  uint32_t key[V];
+  float p[V];
+  if (a.score == 0) {
+#pragma unroll
+    for (int q = 0; q < V; ++q) p[q] = exp_neg(z[q] - m) * inv;
+  } else {
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      float c;
+      p[q] = sigmoid_pair(z[q], &c);
+    }
+  }
+  if (bias) {
+#pragma unroll
+    for (int q = 0; q < V; ++q) p[q] += b[q];
+  }
 #pragma unroll
   for (int q = 0; q < V; ++q) {
-    float p, c;
-    if (a.score == 0) p = exp_neg(z[q] - m) * inv;
-    else p = sigmoid_pair(z[q], &c);
-    const bool ok = unmasked(z[q]);
-    const float val = bias ? p + b[q] : p;
-    z[q] = ok && val == val ? val : -INFINITY;
-    key[q] = q < v && l * v + q < E ? (ok ? value_key(val) : 1u) : 0u;
+    const bool ok = unmasked(z[q]) & (p[q] > kMasked);  // (a NaN of the bias masks too)
+    const bool in = (l * v + q < E) & (q < v);
+    const float val = ok ? p[q] : kMasked;
+    z[q] = in ? val : kNone;
   }
   if (a.groups > 1) {
-    float ga = -INFINITY, gb = -INFINITY;
     const int gs = E / a.groups;  // experts per group
-    bool mine[V];
-    if (a.lane_groups) {  // a group is the experts of 16 / groups neighbouring lanes
-      const int L = 16 / a.groups;
+    uint32_t chosen = 0;          // by group
+    float s = kNone;              // lane g, or every lane of group g: the group's score
+    int id = l;                   // its group
+    if (a.lane_groups) {          // a group is the experts of 16 / groups neighbouring lanes
+      const int L = 1 << a.group_shift;
+      float ga = -INFINITY, gb = -INFINITY;
 #pragma unroll
       for (int q = 0; q < V; ++q) {
         gb = fmaxf(gb, fminf(ga, z[q]));
@@ -184,17 +237,11 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const float* __restrict_
       if (L > 1) merge_two<kXor1>(ga, gb);
       if (L > 2) merge_two<kXor2>(ga, gb);
       if (L > 4) merge_two<kHalfMirror>(ga, gb);
-      float s = gs > 1 ? ga + gb : ga;
-      s = s == s ? s : -INFINITY;
-      int better = 0;
-      count_better<1>(s, l / L, better);
-      const bool chosen = better < a.top_groups * L;
-#pragma unroll
-      for (int q = 0; q < V; ++q) mine[q] = chosen;
-    } else {  // any division: one group after the other, lane g keeps group g's score
-      float s = -INFINITY;
+      s = gs > 1 ? ga + gb : ga;
+      id = l >> a.group_shift;
+    } else {  // any division: one group after the other
       for (int g = 0; g < a.groups; ++g) {
-        ga = gb = -INFINITY;
+        float ga = -INFINITY, gb = -INFINITY;
 #pragma unroll
         for (int q = 0; q < V; ++q) {
           const int e = l * v + q;
@@ -207,53 +254,89 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const float* __restrict_
         merge_two<kXor2>(ga, gb);
         merge_two<kHalfMirror>(ga, gb);
         merge_two<kMirror>(ga, gb);
-        float sg = gs > 1 ? ga + gb : ga;
-        sg = sg == sg ? sg : -INFINITY;
-        if (l == g) s = sg;
+        if (l == g) s = gs > 1 ? ga + gb : ga;
       }
-      int better = 0;
-      count_better<1>(s, l, better);
-      const uint64_t all = __ballot(better < a.top_groups && l < a.groups);
-      const uint32_t chosen = (uint32_t)(all >> (lane & 48)) & 0xffffu;
-#pragma unroll
-      for (int q = 0; q < V; ++q) mine[q] = (chosen >> ((l * v + q) / gs & 15)) & 1u;
     }
+    // a score with a masked expert in it is the lowest (equal ones: the lower group)
+    if (id < a.groups) s = s > kMasked * 0.5f ? s : kMasked;
+    for (int j = 0; j < a.top_groups; ++j) {
+      const float best = row_max(s);
+      const int g = first_lane(s == best, lane) >> a.group_shift;  // that lane's group
+      chosen |= 1u << g;
+      if (id == g) s = kNone;
+    }
+    if (a.lane_groups) {
+      const bool in = (chosen >> id) & 1u;
 #pragma unroll
-    for (int q = 0; q < V; ++q) key[q] = mine[q] ? key[q] : 0u;
+      for (int q = 0; q < V; ++q) {
+        const float was = z[q];
+        z[q] = in ? was : kNone;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const float was = z[q];
+        z[q] = (chosen >> ((l * v + q) / gs & 15)) & 1u ? was : kNone;
+      }
+    }
   }
-  // k rounds: the row's largest key, the lowest lane that holds it, its first
-  // expert with it (ids rise with the lane, then with q)
+  uint32_t key[V];
+#pragma unroll
+  for (int q = 0; q < V; ++q) key[q] = value_key(z[q]);
+#pragma unroll
+  for (int q = 0; q < V; q += 4)
+    *(u32x4_t*)&held[tok][l][q] = (u32x4_t){key[q], key[q + 1], key[q + 2], key[q + 3]};
+  sort_down<V>(key);
+  // k rounds: the largest head of the row, of the lowest lane that has it (ids
+  // rise with the lane, so equal values come in the order of their ids)
+  uint32_t mine = 0;
+  int owner = 0;
   for (int j = 0; j < a.k; ++j) {
-    uint32_t top = key[0];
+    const uint32_t best = row_umax(key[0]);
+    const int o = first_lane(key[0] == best, lane);
+    const bool pop = l == o;
 #pragma unroll
-    for (int q = 1; q < V; ++q) top = max(top, key[q]);
-    const uint32_t best = row_umax(top);
-    const uint32_t holders = (uint32_t)(__ballot(top == best) >> (lane & 48)) & 0xffffu;
-    int first = V;
-#pragma unroll
-    for (int q = V - 1; q >= 0; --q) first = key[q] == best ? q : first;
-    if (l != __builtin_ctz(holders)) first = V;
-#pragma unroll
-    for (int q = 0; q < V; ++q) key[q] = first == q ? 0u : key[q];
-    if (first < V) won[tok][j] = l * v + first;
+    for (int i = 0; i + 1 < H; ++i) {
+      const uint32_t next = key[i + 1], now = key[i];
+      key[i] = pop ? next : now;
+    }
+    key[H - 1] = pop ? 0u : key[H - 1];
+    if (l == j) {
+      mine = best;
+      owner = o;
+    }
   }
   __syncthreads();
+  // slot l's expert: the owner's c-th with that value, c earlier slots having taken it
   const bool slot = l < a.k;
-  const int e = slot ? won[tok][l] : 0;
-  float p = 0.f;
+  // (values fall with the lane, so equal ones are neighbours)
+  int c = 0;
+  const uint32_t before = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mine, 0x111, 0xf, 0xf, false);
+  if (__any(slot && before == mine)) count_same<1>(mine, owner, c);
+  uint32_t has = 0;
+#pragma unroll
+  for (int q = 0; q < V; q += 4) {
+    const u32x4_t x = *(const u32x4_t*)&held[tok][owner][q];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) has |= x[i] == mine ? 1u << (q + i) : 0u;
+  }
+  for (; __any(slot && c > 0); --c)
+    if (c > 0) has &= has - 1;
+  const int e = slot ? owner * v + __builtin_ctz(has | 0x80000000u) : 0;
+  float g = 0.f;
   if (slot) {
-    const float zz = fminf(row[e], FLT_MAX);
-    float c;
-    if (unmasked(row[e])) p = a.score == 0 ? exp_neg(zz - m) * inv : sigmoid_pair(zz, &c);
+    const float zr = row[e], zz = fminf(zr, FLT_MAX);
+    float comp;
+    if (unmasked(zr)) g = a.score == 0 ? exp_neg(zz - m) * inv : sigmoid_pair(zz, &comp);
   }
   float f = a.scale;
   if (a.renorm) {
-    const float sum = row_sum(p);
+    const float sum = row_sum(g);
     f = sum > 0.f ? a.scale / sum : 0.f;
   }
   if (slot && t < T) {
     idx[t * a.k + l] = e;
-    gates[t * a.k + l] = p * f;
+    gates[t * a.k + l] = g * f;
   }
 }
 
@@ -285,7 +368,8 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(const float* __restrict_
   float p = 0.f, dz = 0.f;
   if (dense) {
     float s[V], m, inv;
-    load_share<V>(row, E, a.v, l, -INFINITY, s);
+    const int held = (int)min((int64_t)kTokens, T - t0);
+    load_share<V>(floats(logits + t0 * E, held * E), min(tok, held - 1) * E, E, a.v, l, -INFINITY, s);
 #pragma unroll
     for (int q = 0; q < V; ++q) s[q] = s[q] > FLT_MAX ? FLT_MAX : s[q];
     softmax_stats<V>(s, m, inv);
@@ -367,10 +451,14 @@ hipError_t launch_route_fwd(const float* logits, const float* bias, int64_t T, R
   if (a.E > 256 || a.k > 16 || a.groups > 16 || blocks > INT32_MAX) return hipErrorInvalidValue;
   a.v = (a.E + 15) / 16;
   a.lane_groups = a.E % 16 == 0 && 16 % a.groups == 0;
+  a.group_shift = a.lane_groups ? __builtin_ctz(16 / a.groups) : 0;
   const unsigned g = (unsigned)blocks;
-  if (a.v <= 4) route_fwd_kernel<4><<<g, 256, 0, s>>>(logits, bias, T, a, idx, gates);
-  else if (a.v <= 8) route_fwd_kernel<8><<<g, 256, 0, s>>>(logits, bias, T, a, idx, gates);
-  else route_fwd_kernel<16><<<g, 256, 0, s>>>(logits, bias, T, a, idx, gates);
+#define MEMFINE_ROUTE(V_, H_) route_fwd_kernel<V_, H_><<<g, 256, 0, s>>>(logits, bias, T, a, idx, gates)
+  if (a.v <= 4) MEMFINE_ROUTE(4, 4);
+  else if (a.v <= 8) MEMFINE_ROUTE(8, 8);
+  else if (a.k <= 8) MEMFINE_ROUTE(16, 8);
+  else MEMFINE_ROUTE(16, 16);
+#undef MEMFINE_ROUTE
   return hipGetLastError();
 }
 
