@@ -99,29 +99,27 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(
 // Backward: workgroup b takes rows b, b + grid, ...; each lane keeps the sums
 // of dw of its own columns in registers over its rows and writes them as row b
 // of `part` [grid, h].
-template <typename T, int V>
-__global__ __launch_bounds__(1024) void norm_bwd_kernel(
+template <typename T, int V, int kThreads>
+__global__ __launch_bounds__(kThreads) void norm_bwd_kernel(
     const T* __restrict__ X, const T* __restrict__ w, const T* __restrict__ dY,
     const T* __restrict__ dS, float eps, int64_t T_, int h, T* __restrict__ dX,
     float* __restrict__ partial) {
   constexpr int E = Elem<T>::kVec;
   __shared__ float part[2][2][16];
   const int nv = h / E, W = blockDim.x >> 6, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  float wt[V][E], acc[V][E];
+  u32x4_t rw[V];
+  float acc[V][E];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int c = i * blockDim.x + threadIdx.x;
-    unpack16(((const u32x4_t*)w)[c < nv ? c : 0], wt[i], (T*)nullptr);
+    rw[i] = ((const u32x4_t*)w)[c < nv ? c : 0];
 #pragma unroll
-    for (int q = 0; q < E; ++q) {
-      acc[i][q] = 0.f;
-      if (c >= nv) wt[i][q] = 0.f;
-    }
+    for (int q = 0; q < E; ++q) acc[i][q] = 0.f;
   }
   int parity = 0;
-  for (int64_t t = blockIdx.x; t < T_; t += gridDim.x, parity ^= 1) {
+  u32x4_t rx[V], rd[V], rs[V];
+  auto load = [&](int64_t t) {
     const int64_t row = t * h;
-    u32x4_t rx[V], rd[V], rs[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int c = i * blockDim.x + threadIdx.x;
@@ -130,6 +128,10 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(
       rd[i] = ((const u32x4_t*)(dY + row))[at];
       if (dS) rs[i] = ((const u32x4_t*)(dS + row))[at];
     }
+  };
+  load(blockIdx.x);  // (no more workgroups than rows)
+  for (int64_t t = blockIdx.x; t < T_; t += gridDim.x, parity ^= 1) {
+    const int64_t row = t * h;
     float x[V][E], d[V][E], sq = 0.f, pr = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -137,13 +139,19 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(
       unpack16(rx[i], x[i], (T*)nullptr);
       unpack16(rd[i], d[i], (T*)nullptr);
       if (c < nv) {
+        float wt[E];
+        unpack16(rw[i], wt, (T*)nullptr);
 #pragma unroll
         for (int q = 0; q < E; ++q) {
           sq = fmaf(x[i][q], x[i][q], sq);
-          pr = fmaf(d[i][q] * wt[i][q], x[i][q], pr);
+          pr = fmaf(d[i][q] * wt[q], x[i][q], pr);
         }
       }
     }
+    u32x4_t now[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) now[i] = rs[i];
+    if (t + gridDim.x < T_) load(t + gridDim.x);  // the next row, in flight over this one's sums
     sq = wave_sum(sq);
     pr = wave_sum(pr);
     if (W > 1) {
@@ -165,12 +173,13 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int c = i * blockDim.x + threadIdx.x;
-      float o[E];
-      if (dS) unpack16(rs[i], o, (T*)nullptr);
+      float o[E], wt[E];
+      if (dS) unpack16(now[i], o, (T*)nullptr);
+      unpack16(rw[i], wt, (T*)nullptr);
 #pragma unroll
       for (int q = 0; q < E; ++q) {
         acc[i][q] = fmaf(d[i][q], x[i][q] * r, acc[i][q]);
-        const float g = r * (d[i][q] * wt[i][q] - x[i][q] * k);
+        const float g = r * (d[i][q] * wt[q] - x[i][q] * k);
         o[q] = dS ? o[q] + g : g;
       }
       if (c < nv) ((u32x4_t*)(dX + row))[c] = pack16(o, (T*)nullptr);
@@ -188,21 +197,25 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(
   }
 }
 
-// dw (+)= the sum of the partial rows: a workgroup owns 64 columns, its four
-// waves a quarter of the rows each (every fourth), summed in a fixed order.
-__global__ __launch_bounds__(256) void norm_dw_kernel(const float* __restrict__ partial, int rows,
-                                                      int h, int accumulate,
-                                                      float* __restrict__ dw) {
-  __shared__ float part[4][64];
+// dw (+)= the sum of the partial rows: a workgroup owns 64 columns, its sixteen
+// waves every sixteenth row each, summed in a fixed order (four waves: a chain
+// of loads four times as long, 12 us of the 117 of 16385 rows of 4096, now 5).
+constexpr int kDwWaves = 16;
+__global__ __launch_bounds__(64 * kDwWaves) void norm_dw_kernel(const float* __restrict__ partial,
+                                                                int rows, int h, int accumulate,
+                                                                float* __restrict__ dw) {
+  __shared__ float part[kDwWaves][64];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int c = blockIdx.x * 64 + lane;  // h is a multiple of 64
   float s = 0.f;
 #pragma unroll 8
-  for (int i = wv; i < rows; i += 4) s += partial[(int64_t)i * h + c];
+  for (int i = wv; i < rows; i += kDwWaves) s += partial[(int64_t)i * h + c];
   part[wv][lane] = s;
   __syncthreads();
   if (wv == 0) {
-    s = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kDwWaves; ++i) s += part[i][lane];
     dw[c] = accumulate ? dw[c] + s : s;
   }
 }
@@ -254,8 +267,7 @@ hipError_t launch_norm_fwd(int dtype, const void* X, const void* R, const void* 
                                                  h, (T_*)S, (T_*)Y, Q, QS)
   if (dtype == 0) {
     if (rs.V == 1) MEMFINE_NORM(bf16_t, 1);
-    else if (rs.V == 2) MEMFINE_NORM(bf16_t, 2);
-    else MEMFINE_NORM(bf16_t, 4);
+    else MEMFINE_NORM(bf16_t, 2);  // (16384 elements are 16 waves of two vectors)
   } else {
     if (rs.V == 1) MEMFINE_NORM(float, 1);
     else if (rs.V == 2) MEMFINE_NORM(float, 2);
@@ -265,10 +277,13 @@ hipError_t launch_norm_fwd(int dtype, const void* X, const void* R, const void* 
   return hipGetLastError();
 }
 
-// Rows of dw partials: enough workgroups to keep 16 waves on every CU.
+// Rows of dw partials: one round of workgroups, of as many waves a CU as its
+// registers hold (bf16, two vectors a lane: 12, else 16; 16 of them, in two
+// rounds, 115 us at 16385 rows of 4096, 12 106).
 int norm_bwd_blocks(int dtype, int64_t T, int h, int cus) {
   const RowShape rs = row_shape(h / (dtype == 0 ? 8 : 4));
-  const int64_t want = (int64_t)cus * (16 / rs.waves > 0 ? 16 / rs.waves : 1);
+  const int waves = dtype == 0 && rs.V > 1 ? 12 : 16;
+  const int64_t want = (int64_t)cus * (waves / rs.waves > 0 ? waves / rs.waves : 1);
   return (int)(T < want ? T : want);
 }
 
@@ -279,20 +294,21 @@ hipError_t launch_norm_bwd(int dtype, const void* X, const void* w, const void* 
   const RowShape rs = row_shape(h / (dtype == 0 ? 8 : 4));
   const dim3 grid(blocks), block(64 * rs.waves);
   if (rs.waves > 16) return hipErrorInvalidValue;
-#define MEMFINE_NORM(T_, V_)                                                                     \
-  norm_bwd_kernel<T_, V_><<<grid, block, 0, s>>>((const T_*)X, (const T_*)w, (const T_*)dY,      \
-                                                 (const T_*)dS, eps, T, h, (T_*)dX, partial)
+#define MEMFINE_NORM(T_, V_, N_)                                                                  \
+  norm_bwd_kernel<T_, V_, N_><<<grid, block, 0, s>>>((const T_*)X, (const T_*)w, (const T_*)dY,   \
+                                                     (const T_*)dS, eps, T, h, (T_*)dX, partial)
   if (dtype == 0) {
-    if (rs.V == 1) MEMFINE_NORM(bf16_t, 1);
-    else if (rs.V == 2) MEMFINE_NORM(bf16_t, 2);
-    else MEMFINE_NORM(bf16_t, 4);
+    if (rs.V == 1) MEMFINE_NORM(bf16_t, 1, 512);
+    else if (rs.waves <= 8) MEMFINE_NORM(bf16_t, 2, 512);
+    else MEMFINE_NORM(bf16_t, 2, 1024);  // (16384 elements are 16 waves of two vectors)
   } else {
-    if (rs.V == 1) MEMFINE_NORM(float, 1);
-    else if (rs.V == 2) MEMFINE_NORM(float, 2);
-    else MEMFINE_NORM(float, 4);
+    if (rs.V == 1) MEMFINE_NORM(float, 1, 512);
+    else if (rs.V == 2 && rs.waves <= 8) MEMFINE_NORM(float, 2, 512);
+    else if (rs.V == 2) MEMFINE_NORM(float, 2, 1024);
+    else MEMFINE_NORM(float, 4, 1024);
   }
 #undef MEMFINE_NORM
-  norm_dw_kernel<<<h / 64, 256, 0, s>>>(partial, blocks, h, accumulate, dw);
+  norm_dw_kernel<<<h / 64, 64 * kDwWaves, 0, s>>>(partial, blocks, h, accumulate, dw);
   return hipGetLastError();
 }
 
