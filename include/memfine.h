@@ -467,7 +467,10 @@ int memfine_mx_values(int64_t T, int32_t h, const uint8_t* d_Q, const uint8_t* d
  * A logit of -inf, of the lowest finite float or a NaN masks its expert: p = 0,
  * and it is selected, with gate 0, only when fewer than k others are left
  * (a token without any other gets k masked experts and zero gates).  +inf
- * counts as the largest finite float.
+ * counts as the largest finite float.  A bias of -inf or NaN makes its expert
+ * the last choice alike, with its own gate.  p and v are floats: in the
+ * selection a p below 2^-126 counts as 0 (equal values: the lower id), while
+ * renormalised gates keep the ratios of such p.
  * 1 <= E <= 256, 1 <= k <= 16 (MEMFINE_ERR_UNSUPPORTED otherwise), k <=
  * top_groups E / groups, groups <= 16 dividing E.
  */
@@ -531,9 +534,13 @@ int memfine_mxw_unpack(int32_t E, int32_t N, int32_t K, const uint8_t* d_codes,
  *   d_X  bf16 [T, K] when d_XS is null, else e4m3 bytes [T, K] with the scales
  *        d_XS [T, K / 32] (MX8, as memfine_norm_fwd gives them)
  *   d_Y  y_dtype [T, N], MEMFINE_BF16 or MEMFINE_F32
- * Sums in fp32.  On bf16 activations the products are those of the held
- * values; on MX8 the matrix core forms sums of 128 products to about 2^-15 of
- * the largest of them.
+ * Sums in fp32, in an order that depends on T, N and K alone.  On bf16
+ * activations the products are those of the held values; on MX8 the matrix core
+ * cuts each product off, towards zero, at 2^-13 of the power of two at or below
+ * the largest of eight neighbouring ones.  A
+ * reduction of K > 4096 over few rows (T <= 64, or below 128 blocks of 32 rows
+ * x 256 columns) is split and takes ceil(K / 4096) T N floats of the library's
+ * per-stream working memory, as the layer's calls with a null allocator do.
  */
 int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const uint8_t* d_XS,
                        const uint8_t* d_codes, const uint8_t* d_scales, int32_t y_dtype, void* d_Y,
@@ -544,9 +551,11 @@ int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const u
  * [2F, h] and [h, F]); shape.dtype must be MEMFINE_BF16 (Y's type).
  *   d_X  bf16 [T, h] when d_XS is null; the SwiGLU output is then rounded to
  *        bf16 for the second product.  With d_XS: MX8, e4m3 [T, h] and scales
- *        [T, h / 32]; the SwiGLU output is then rounded to MX8 as well.
+ *        [T, h / 32]; the SwiGLU output is then rounded to MX8 as well, and the
+ *        second product's rows, before the gates, to bf16 in chunks of more
+ *        than 4096 rows (else they stay fp32).
  * Everything else as memfine_moe_fwd.  memfine_moe_mxw_workspace_bytes: the
- * working memory of its largest chunk (mx8 = 1: with d_XS).
+ * working memory of the chunk that needs the most (mx8 = 1: with d_XS).
  */
 int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* d_X,
                         const uint8_t* d_XS, const int32_t* d_idx, const float* d_gates,

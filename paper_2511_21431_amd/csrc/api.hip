@@ -1688,8 +1688,11 @@ int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const u
 int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chunks, int32_t mx8) {
   if (check_shape(shape) || shape->dtype != MEMFINE_BF16 || chunks < 1 || (mx8 != 0 && mx8 != 1))
     return MEMFINE_ERR_INVALID_ARG;
+  if (shape->T == 0) return 0;
+  // chunks of two sizes, of which the smaller may need more (FC2's partial rows)
   const int64_t n = max_chunk_tokens(shape->T, chunks) * shape->k;
-  return n == 0 ? 0 : mx_layout(*shape, n, mx8 != 0).total;
+  const int64_t m = shape->T / std::min<int64_t>(chunks, shape->T) * shape->k;
+  return std::max(mx_layout(*shape, n, mx8 != 0).total, mx_layout(*shape, m, mx8 != 0).total);
 }
 
 int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* d_X,

@@ -177,6 +177,18 @@ __device__ __forceinline__ void softmax_stats(const float (&z)[V], float& m, flo
   if (!(m > -INFINITY)) m = 0.f;
 }
 
+// A slot's score over a factor that the row's slots share, so that the largest
+// is 1/2 or more and scores far below the smallest float keep their ratios:
+// softmax e^(z - max), sigmoid e^(min(z, 0) - min(max, 0)) / (1 + e^-|z|); the
+// maximum is over the selected logits.  ok: the slot counts; 0 otherwise.
+__device__ __forceinline__ float relative_score(int score, float zr, bool ok) {
+  const float z = fminf(zr, FLT_MAX);
+  const float top = row_max(ok ? z : -INFINITY);
+  if (!ok) return 0.f;
+  if (score == 0) return exp_neg(z - top);
+  return exp_neg(fminf(z, 0.f) - fminf(top, 0.f)) * __builtin_amdgcn_rcpf(1.f + exp_neg(-fabsf(z)));
+}
+
 // H: the heads of a lane's list that the k rounds can reach (k <= 8: at most 8).
 template <int V, int H>
 __global__ __launch_bounds__(256) void route_fwd_kernel(const float* __restrict__ logits,
@@ -323,16 +335,17 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const float* __restrict_
   for (; __any(slot && c > 0); --c)
     if (c > 0) has &= has - 1;
   const int e = slot ? owner * v + __builtin_ctz(has | 0x80000000u) : 0;
-  float g = 0.f;
-  if (slot) {
-    const float zr = row[e], zz = fminf(zr, FLT_MAX);
-    float comp;
-    if (unmasked(zr)) g = a.score == 0 ? exp_neg(zz - m) * inv : sigmoid_pair(zz, &comp);
-  }
-  float f = a.scale;
+  const float zr = slot ? row[e] : -INFINITY;
+  const bool ok = unmasked(zr);
+  float g = 0.f, f = a.scale;
   if (a.renorm) {
-    const float sum = row_sum(g);
+    g = relative_score(a.score, zr, ok);
+    const float sum = row_sum(g);  // 1/2 and more, or no slot counts
     f = sum > 0.f ? a.scale / sum : 0.f;
+  } else if (ok) {
+    float comp;
+    g = a.score == 0 ? exp_neg(fminf(zr, FLT_MAX) - m) * inv
+                     : sigmoid_pair(fminf(zr, FLT_MAX), &comp);
   }
   if (slot && t < T) {
     idx[t * a.k + l] = e;
@@ -361,9 +374,9 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(const float* __restrict_
   // slot l; an id outside [0, E) passes no gradient
   int id = l < a.k ? idx[tr * a.k + l] : -1;
   id = id >= 0 && id < E ? id : -1;
-  const float dg = id >= 0 ? dgates[tr * a.k + l] * a.scale : 0.f;
   const float zr = id >= 0 ? row[id] : -INFINITY;
-  const bool ok = unmasked(zr);
+  const bool ok = unmasked(zr);  // a masked expert's gate is 0 whatever the logits: no gradient
+  const float dg = ok ? dgates[tr * a.k + l] * a.scale : 0.f;
   const float z = ok ? fminf(zr, FLT_MAX) : 0.f;
   float p = 0.f, dz = 0.f;
   if (dense) {
@@ -381,17 +394,15 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(const float* __restrict_
       if (q < a.v && l * a.v + q < E)
         rows[tok * E + l * a.v + q] = unmasked(s[q]) ? -c * (exp_neg(s[q] - m) * inv) : 0.f;
   } else {
-    float comp = 1.f;
-    if (a.score == 0) {
-      const float m = row_max(ok ? z : -INFINITY);
-      p = ok ? exp_neg(z - m) : 0.f;
-    } else {
+    float comp = 1.f;  // sigmoid: 1 - p
+    if (a.score != 0) {
       p = sigmoid_pair(z, &comp);
       if (!ok) p = 0.f;
     }
     if (a.renorm) {
-      const float sum = row_sum(p);
-      const float g = sum > 0.f ? p / sum : 0.f;
+      const float r = relative_score(a.score, zr, ok);
+      const float sum = row_sum(r);
+      const float g = sum > 0.f ? r / sum : 0.f;
       dz = g * comp * (dg - row_sum(g * dg));
     } else {
       dz = dg * p * comp;
