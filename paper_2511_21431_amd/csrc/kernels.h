@@ -228,7 +228,7 @@ struct MxArgs {
   int cus;                    // compute units of the device
   const int32_t* ids;         // one token: its slots' experts [n], or null
   const float* gates;         // one token: its slots' gates [n]
-  int col_blocks, row_blocks, col_shares, splits, run;  // (set by the launchers)
+  int col_blocks, row_blocks, col_shares, splits;  // (set by the launchers)
 };
 int64_t mx4_code_bytes(int64_t N, int64_t K);   // of one matrix
 int64_t mx4_scale_bytes(int64_t N, int64_t K);
