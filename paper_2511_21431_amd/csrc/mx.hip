@@ -84,16 +84,20 @@ __device__ __forceinline__ void mx_mma(const u32x4_t& w, uint32_t s, const Act<t
                      (int)x.hi[0], (int)x.hi[1], (int)x.hi[2], (int)x.hi[3]};
   acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 0, SW, (int)s, SX, (int)x.s);
 }
+// Eight MX4 values with their scale, exactly.
+__device__ __forceinline__ bf16x8_t bf16_of(uint32_t w, float scale) {
+  const bf16x2v_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  const bf16x2v_t p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2v_t p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  const bf16x2v_t p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  return (bf16x8_t){p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+}
 template <int SW = 0, int SX = 0>
 __device__ __forceinline__ void mx_mma(const u32x4_t& w, uint32_t s, const Act<false>& x, f32x4_t& acc) {
   const float scale = __uint_as_float((s >> (8 * SW) & 255u) << 23);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const bf16x2v_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 0);
-    const bf16x2v_t p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 1);
-    const bf16x2v_t p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 2);
-    const bf16x2v_t p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], scale, 3);
-    const bf16x8_t a = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+    const bf16x8_t a = bf16_of(w[j], scale);
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, x.v[j]), acc, 0, 0, 0);
   }
 }
@@ -656,19 +660,15 @@ template <bool MX8, int BM> struct ActTile {
           rs, (lds_t*)(lds + kBytes + (i * 4 + w) * 256), 1,
           kt * 128 + 32 * (int)(threadIdx.x & 3) < K ? soff[i] : kPast, kt * 4, 0, 0);
   }
-  // operand B of rows 16 i .. + 15
+  // 16-byte unit u of row lr of the rows 16 i .. + 15
+  __device__ __forceinline__ static u32x4_t unit(const char* lds, int i, int lr, int u) {
+    return *(const u32x4_t*)(lds + lr * kRow + ((u ^ (lr & 7)) << 4) + 16 * i * kRow);
+  }
+  // operand B of those rows
   __device__ __forceinline__ static void read(const char* lds, int i, int lr, int lg, Act<MX8>& x) {
-    const int sw = lr & 7;
-    const char* row = lds + lr * kRow;
-    if constexpr (MX8) {
-      x.s = *(const uint32_t*)(lds + kBytes + (lr * 4 + lg) * 4 + i * 256);
-      x.lo = *(const u32x4_t*)(row + ((lg ^ sw) << 4) + 16 * i * kRow);
-      x.hi = *(const u32x4_t*)(row + (((4 + lg) ^ sw) << 4) + 16 * i * kRow);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        x.v[j] = *(const u32x4_t*)(row + (((4 * lg + j) ^ sw) << 4) + 16 * i * kRow);
-    }
+    x.s = *(const uint32_t*)(lds + kBytes + (lr * 4 + lg) * 4 + i * 256);
+    x.lo = unit(lds, i, lr, lg);
+    x.hi = unit(lds, i, lr, 4 + lg);
   }
 };
 
@@ -736,14 +736,41 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
     __builtin_amdgcn_sched_barrier(0);  // the loads stay here, a step before their use
     // a row block's operand is read while the one before it is multiplied (left
     // to the scheduler, the reads of all of them moved up and 128 rows spilled)
-    Act<MX8> x[2];
-    A::read(cur, 0, lr, lg, x[0]);
-    unroll_for<MI>([&](auto i) {
-      if constexpr (i + 1 < MI) A::read(cur, i + 1, lr, lg, x[(i + 1) % 2]);
+    if constexpr (MX8) {
+      Act<MX8> x[2];
+      A::read(cur, 0, lr, lg, x[0]);
+      unroll_for<MI>([&](auto i) {
+        if constexpr (i + 1 < MI) A::read(cur, i + 1, lr, lg, x[(i + 1) % 2]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) mx_mma<U, 0>(c[U % 2][j], ws[j], x[i % 2], acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);
-    });
+        for (int j = 0; j < 4; ++j) mx_mma<U, 0>(c[U % 2][j], ws[j], x[i % 2], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    } else {
+      // quarter by quarter of the lanes' columns, so that 16 registers hold the
+      // converted weights
+      float scale[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) scale[j] = __uint_as_float((ws[j] >> (8 * U) & 255u) << 23);
+      u32x4_t x[2][MI];
+      auto read = [&](int q, u32x4_t (&v)[MI]) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) v[i] = A::unit(cur, i, lr, 4 * lg + q);
+      };
+      read(0, x[0]);
+      unroll_for<4>([&](auto q) {
+        if constexpr (q + 1 < 4) read(q + 1, x[(q + 1) % 2]);
+        bf16x8_t a[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = bf16_of(c[U % 2][j][(int)q], scale[j]);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                a[j], __builtin_bit_cast(bf16x8_t, x[q % 2][i]), acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    }
     if (U == 3) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) ws[j] = wsn[j];
