@@ -711,27 +711,35 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 
-  u32x4_t c[2][4];  // the weights of this step and the next
+  // The weights of this step and the D after it.  32 rows of MX8 leave the least
+  // time between a step's loads and their use: two steps ahead 25 us against 30 (256 rows,
+  // 4096 x 8192); for the others a step more costs a workgroup a CU and gains nothing.
+  constexpr int D = MX8 && BM == 32 ? 2 : 1;
+  static_assert(D < S, "weights come before the copies of their own step");
+  u32x4_t c[2 * D][4];
   uint32_t ws[4], wsn[4];
   char *cur = smem, *next = smem + (S - 1) * A::kStage;  // stage of step kt, of step kt + S - 1
   constexpr int kEnd = S * A::kStage;
   load_ws(0, ws);
-  load_w(0, c[0]);
 #pragma unroll
-  for (int kt = 0; kt + 1 < S; ++kt) a.copy(kt, g.K, smem + kt * A::kStage, w);
+  for (int kt = 0; kt + 1 < S; ++kt) {
+    if (kt < D) load_w(kt, c[kt]);
+    a.copy(kt, g.K, smem + kt * A::kStage, w);
+  }
 
-  // step kt = 4 i + U on the weights c[U % 2]
+  // step kt = 4 i + U on the weights c[U % (2 D)]
   auto step = [&](auto U, int kt) {
     __builtin_amdgcn_sched_barrier(0);  // the previous step's products stay before the barrier
     // The stage and the weights of step kt have arrived; the copies of the
-    // S - 2 stages after it, issued after the weights, may be in flight.
-    wait_loads<(S - 2) * A::kIssue>();
+    // S - 2 stages after it, issued after those weights, and with D = 2 the
+    // weights issued between them, may be in flight.
+    wait_loads<(S - 2) * A::kIssue + (D - 1) * 4>();
     wait_lds();
     // publishes every wave's copies of stage kt, and all waves are done with
     // the stage of step kt - 1, which the next copies overwrite
     __builtin_amdgcn_s_barrier();
     if (U == 0) load_ws(kt + 4, wsn);
-    load_w(kt + 1, c[(U + 1) % 2]);
+    load_w(kt + D, c[(U + D) % (2 * D)]);
     a.copy(kt + S - 1, g.K, next, w);
     __builtin_amdgcn_sched_barrier(0);  // the loads stay here, a step before their use
     // a row block's operand is read while the one before it is multiplied (left
@@ -742,7 +750,7 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
       unroll_for<MI>([&](auto i) {
         if constexpr (i + 1 < MI) A::read(cur, i + 1, lr, lg, x[(i + 1) % 2]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mx_mma<U, 0>(c[U % 2][j], ws[j], x[i % 2], acc[i][j]);
+        for (int j = 0; j < 4; ++j) mx_mma<U, 0>(c[U % (2 * D)][j], ws[j], x[i % 2], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
       });
     } else {
@@ -761,7 +769,7 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
         if constexpr (q + 1 < 4) read(q + 1, x[(q + 1) % 2]);
         bf16x8_t a[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = bf16_of(c[U % 2][j][(int)q], scale[j]);
+        for (int j = 0; j < 4; ++j) a[j] = bf16_of(c[U % (2 * D)][j][(int)q], scale[j]);
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
