@@ -1077,7 +1077,10 @@ enum Kind { kOneRow, kFewRows, kTiles32, kTiles64, kTiles128 };
 //   FC1, few rows against 32-row tiles: h 7168 F 2048 E 32, 8 rows 86 / 92, 16
 //     rows 126 / 97 (64-row tiles); h 2048 F 1408 E 16, 2 rows 14.1 / 15.2, 8
 //     rows 18.3 / 16.2; h 4096 F 512 E 8 (32 tiles), 8 rows 12 / 20, 32 rows
-//     17 / 19, 128 rows 31 / 21.
+//     17 / 19, 128 rows 31 / 21; with tiles for half the CUs or fewer, h 7168 F 2048
+//     E 8, 10 rows 27 / 36 (bf16 29 / 49), 15 rows 35 / 37 (38 / 49), 22 rows 43 /
+//     38 (49 / 49); h 2048 F 2048 E 8, 5 rows 12 / 15, 15 rows 15 / 16, 22 rows 17 /
+//     16; h 4096 F 512 E 32, 10 rows 24 / 23 (27 / 29).
 //   FC2 and linear: K 4096 N 28672, 64 rows 25 / 39, 128 rows 35 / 39 (bf16 50 /
 //     48); K 7168 N 4096, 128 rows 23 / 30, 256 rows 31 / 29; K 2048 N 7168, 64
 //     rows 11 / 12, 128 rows 18 / 12; K 704 E 64, 6 rows 21 / 15.
@@ -1095,7 +1098,8 @@ Kind kind_of(const MxArgs& g, int mode) {
   const int64_t cols = mode == kFc1 ? (g.N / 2 + 127) / 128 : (g.N + 255) / 256;
   auto tiles = [&](int BM) { return std::max<int64_t>(busy(g, BM), g.n / BM) * cols; };
   bool few;
-  if (mode == kFc1) few = rows <= (g.KT >= 32 ? 8 : 4) || tiles(32) < g.cus / 4;
+  if (mode == kFc1) few = rows <= (g.KT >= 32 ? 8 : 4) || tiles(32) < g.cus / 4 ||
+                          (rows <= 16 && tiles(32) <= g.cus / 2);
   else if (g.KT >= 32) few = rows <= 64 || tiles(32) < g.cus / 2;
   else few = (rows <= 8 && g.KT >= 16) || tiles(32) < g.cus / 4;
   if (few) return kFewRows;
