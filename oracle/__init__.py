@@ -15,9 +15,11 @@ Contents
 ``memory_model`` the paper's memory cost model (Section 3: Eq. (1), Table 2,
                  Eq. (2), Eq. (3)) and the MACT chunk choice (Section 4.2:
                  Eq. (8), Eq. (9), bins), in exact rational arithmetic.
+``around``       the residual RMS norm, routing from logits, the MX block formats
+                 and the layer on MX4 weights (definitions of include/memfine.h).
 
 Pins (what each function is checked against, other than itself) are listed
 in the module docstrings.  Functions with no independent pin say
 "parity unpinned" there.
 """
-from . import memory_model, moe  # noqa: F401
+from . import around, memory_model, moe  # noqa: F401

@@ -1748,7 +1748,7 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
     const double yb = L.y_bf16 ? 2.0 : 4.0 * L.splits;
     hipError_t err = hipSuccess;
     if (tokens == 1 && mx_one_token(g1, g2)) {
-      // one token's slots name distinct experts: nothing to group or combine
+      // one token: no rows to group or combine
       g1.ids = g2.ids = d_idx + t0 * S.k;
       g2.gates = d_gates + t0 * S.k;
       g1.X = (const char*)d_X + t0 * S.h * (mx8 ? 1 : 2);

@@ -21,7 +21,8 @@
 // minima and maxima, no ids); a round of the selection then takes the largest
 // head of the 16 lists and pops it; the ids come last, all k at once: lane j
 // looks its value up among the owning lane's values.  Searching the id and
-// clearing it in every round took 71 us instead.
+// clearing it in every round took 71 us instead of 51.  The backward is bound by
+// memory (100003 tokens of 160: 128 MB in 33 us).
 #include <cfloat>
 
 #include "common.h"
