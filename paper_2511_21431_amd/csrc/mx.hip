@@ -733,6 +733,7 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
   for (int kt = 0; kt + 1 < S; ++kt) {
     if (kt < D) load_w(kt, c[kt]);
     a.copy(kt, g.K, smem + kt * A::kStage, w);
+    __builtin_amdgcn_sched_barrier(0);  // in this order, which the first step's wait counts on
   }
 
   // step kt = 4 i + U on the weights c[U % (2 D)]
