@@ -175,6 +175,16 @@ __device__ __forceinline__ bool locate_tile(const MxArgs& g, int& cb, int& e, in
 // ------------------------------------------------------------ the results
 enum { kFc1, kRows };  // SwiGLU rows in X's format; bf16 or fp32 rows (FC2, linear)
 
+// Lane group g (16 lanes) holds columns 4 g .. 4 g + 3 of two tiles, in x and y; after
+// this, columns 8 (g / 2) .. + 7 of tile g % 2, the first four of them in x.  Stores
+// then write twice as many bytes a lane, whole 64-byte lines of bf16 rows (500 rows, 1024
+// x 14336: 17.2 to 15.1 us; 65536 rows over 32 experts, 7168 x 2048: 2.60 to 2.50 ms).
+__device__ __forceinline__ void join_columns(uint32_t& x, uint32_t& y) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+  x = r[0];
+  y = r[1];
+}
+
 // a = silu(u) v of a lane's eight values (two tiles x four columns of row r),
 // stored at columns f and f + 16 on; on MX8 activations the 32 columns that
 // four lanes hold become one block.
@@ -196,16 +206,21 @@ __device__ __forceinline__ void store_swiglu(const MxArgs& g, bool mx8, const f3
     m = umax(m, (uint32_t)__shfl_xor((int)m, 32, 64));
     const uint32_t s = mx8_scale(m);
     const float inv = mx_inverse_scale(s);
+    uint32_t x = pack_e4m3x4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
+    uint32_t y = pack_e4m3x4(a[4] * inv, a[5] * inv, a[6] * inv, a[7] * inv);
+    join_columns(x, y);
     if (live) {
-      uint8_t* out = (uint8_t*)g.out + r * F + f0 + 4 * lg;
-      *(uint32_t*)out = pack_e4m3x4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
-      *(uint32_t*)(out + 16) = pack_e4m3x4(a[4] * inv, a[5] * inv, a[6] * inv, a[7] * inv);
+      *(u32x2_t*)((uint8_t*)g.out + r * F + f0 + 16 * (lg & 1) + 8 * (lg >> 1)) = (u32x2_t){x, y};
       if (lg == 0) g.out_scale[r * (F / kMxBlock) + f0 / kMxBlock] = (uint8_t)s;
     }
-  } else if (live) {
-    bf16_t* out = (bf16_t*)g.out + r * F + f0 + 4 * lg;
-    *(u32x2_t*)out = (u32x2_t){pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])};
-    *(u32x2_t*)(out + 16) = (u32x2_t){pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7])};
+  } else {
+    uint32_t x0 = pack_bf16x2(a[0], a[1]), x1 = pack_bf16x2(a[2], a[3]);
+    uint32_t y0 = pack_bf16x2(a[4], a[5]), y1 = pack_bf16x2(a[6], a[7]);
+    join_columns(x0, y0);
+    join_columns(x1, y1);
+    if (live)
+      *(u32x4_t*)((bf16_t*)g.out + r * F + f0 + 16 * (lg & 1) + 8 * (lg >> 1)) =
+          (u32x4_t){x0, x1, y0, y1};
   }
 }
 
@@ -822,16 +837,27 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int r = 16 * i + lr;
-      const uint32_t off = (uint32_t)r * (uint32_t)(g.N * es) + (n0 + 4 * lg) * es;
+      const uint32_t off = (uint32_t)r * (uint32_t)(g.N * es);
+      const bool live = r0 + r < r1;
+      if (g.out_bf16) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x4_t v = acc[i][j];
-        const uint32_t o = r0 + r < r1 && n0 + 16 * j < g.N ? off + 16 * j * es : kPast;
-        if (g.out_bf16)
-          __builtin_amdgcn_raw_buffer_store_b64(
-              (u32x2_t){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}, ro, o, 0, 0);
-        else
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), ro, o, 0, 0);
+        for (int j = 0; j < 4; j += 2) {
+          const f32x4_t v = acc[i][j], u = acc[i][j + 1];
+          uint32_t x0 = pack_bf16x2(v[0], v[1]), x1 = pack_bf16x2(v[2], v[3]);
+          uint32_t y0 = pack_bf16x2(u[0], u[1]), y1 = pack_bf16x2(u[2], u[3]);
+          join_columns(x0, y0);
+          join_columns(x1, y1);
+          const int n = n0 + 16 * (j + (lg & 1)) + 8 * (lg >> 1);
+          __builtin_amdgcn_raw_buffer_store_b128((u32x4_t){x0, x1, y0, y1}, ro,
+                                                 live && n < g.N ? off + n * 2 : kPast, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int n = n0 + 16 * j + 4 * lg;
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, acc[i][j]), ro,
+                                                 live && n < g.N ? off + n * 4 : kPast, 0, 0);
+        }
       }
     }
   }
