@@ -621,7 +621,7 @@ __global__ __launch_bounds__(64 * W) void mx_one_kernel(MxArgs g) {
 // own, straight into registers one or two stages ahead.
 //
 // 128 rows on MX8 are bound by the matrix cores (65536 rows, 7168 x 4096: 1.48
-// ms, 2.6 PFLOP/s; K of 2048, 7168 columns: 0.96 ms, 2.0 PFLOP/s, as about 10 us
+// ms, 2.6 PFLOP/s; K of 2048, 7168 columns: 0.87 ms, 2.2 PFLOP/s, as about 7 us
 // a round of tiles go by before the first step and after the last), 64 rows on bf16 by the
 // same for short K (4108 rows, 2048 x 2816: 56 us) and reach 1.5 PFLOP/s for long
 // (8192 rows, 8192 x 8192).
