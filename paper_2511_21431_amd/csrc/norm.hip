@@ -77,7 +77,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(
     float g[E];
     unpack16(wt[i], g, (T*)nullptr);
 #pragma unroll
-    for (int q = 0; q < E; ++q) g[q] *= x[i][q] * r;
+    for (int q = 0; q < E; ++q) g[q] = g[q] * x[i][q] * r;  // (bf16: w x is exact)
     if (Y && c < nv) ((u32x4_t*)(Y + row))[c] = pack16(g, (T*)nullptr);
     if (Q) {
       // 32 / E consecutive lanes hold a block (h is a multiple of 64, so a
