@@ -84,6 +84,10 @@ __device__ __forceinline__ void mx_mma(const u32x4_t& w, uint32_t s, const Act<t
                      (int)x.hi[0], (int)x.hi[1], (int)x.hi[2], (int)x.hi[3]};
   acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 0, SW, (int)s, SX, (int)x.s);
 }
+// The conversion's scale operand of a scale byte.  It reads the float's exponent
+// field alone, as the matrix core reads a scale byte: 0 is 2^-127 (the bits of +0), 255
+// (the bits of infinity) makes all values NaN, those of zero codes among them.
+__device__ __forceinline__ float cvt_scale(uint32_t s) { return __uint_as_float(s << 23); }
 // Eight MX4 values with their scale, exactly.
 __device__ __forceinline__ bf16x8_t bf16_of(uint32_t w, float scale) {
   const bf16x2v_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
@@ -94,7 +98,7 @@ __device__ __forceinline__ bf16x8_t bf16_of(uint32_t w, float scale) {
 }
 template <int SW = 0, int SX = 0>
 __device__ __forceinline__ void mx_mma(const u32x4_t& w, uint32_t s, const Act<false>& x, f32x4_t& acc) {
-  const float scale = __uint_as_float((s >> (8 * SW) & 255u) << 23);
+  const float scale = cvt_scale(s >> (8 * SW) & 255u);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const bf16x8_t a = bf16_of(w[j], scale);
@@ -782,7 +786,7 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
       // converted weights
       float scale[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) scale[j] = __uint_as_float((ws[j] >> (8 * U) & 255u) << 23);
+      for (int j = 0; j < 4; ++j) scale[j] = cvt_scale(ws[j] >> (8 * U) & 255u);
       u32x4_t x[2][MI];
       auto read = [&](int q, u32x4_t (&v)[MI]) {
 #pragma unroll
