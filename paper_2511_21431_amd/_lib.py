@@ -517,6 +517,8 @@ def memfine_router_bwd(shape: Shape, X, Wr, idx, gates, dgates, dX, dWr, accumul
 # ------------------------------------------------------- around the layer
 def _dtype_of(t, name) -> int:
     torch = _torch()
+    if t is None:
+        raise ValueError(f"{name} is required")
     if t.dtype == torch.bfloat16:
         return BF16
     if t.dtype == torch.float32:
@@ -652,15 +654,23 @@ def _mxw_bytes(N: int, K: int):
     return memfine_mxw_code_bytes(N, K), memfine_mxw_scale_bytes(N, K)
 
 
-def _mxw_buffers(E, N, K, codes, scales, device):
+def _mxw_weights(E, N, K, codes, scales, names=("codes", "scales")):
+    """Pointers of E laid-out MX4 matrices."""
+    torch = _torch()
+    cb, sb = _mxw_bytes(N, K)
+    return (_ptr(codes, (E, cb), torch.uint8, names[0]),
+            _ptr(scales, (E, sb), torch.uint8, names[1]))
+
+
+def _mxw_outputs(E, N, K, codes, scales, device):
+    """(codes, scales, their pointers), allocated where None is given."""
     torch = _torch()
     cb, sb = _mxw_bytes(N, K)
     if codes is None:
         codes = torch.empty((E, cb), dtype=torch.uint8, device=device)
     if scales is None:
         scales = torch.empty((E, sb), dtype=torch.uint8, device=device)
-    return (codes, scales, _ptr(codes, (E, cb), torch.uint8, "codes"),
-            _ptr(scales, (E, sb), torch.uint8, "scales"))
+    return (codes, scales) + _mxw_weights(E, N, K, codes, scales)
 
 
 def memfine_mxw_pack(E: int, N: int, K: int, row_codes, row_scales, codes=None, scales=None,
@@ -668,7 +678,7 @@ def memfine_mxw_pack(E: int, N: int, K: int, row_codes, row_scales, codes=None, 
     """Lays row-major MX4 matrices out, codes uint8 [E, N, K/2] and scales uint8
     [E, N, K/32]; returns (codes, scales), allocated where None is given."""
     torch = _torch()
-    codes, scales, pc, ps = _mxw_buffers(E, N, K, codes, scales, row_codes.device)
+    codes, scales, pc, ps = _mxw_outputs(E, N, K, codes, scales, row_codes.device)
     rc = lib().memfine_mxw_pack(
         int(E), int(N), int(K), _ptr(row_codes, (E, N, K // 2), torch.uint8, "row_codes"),
         _ptr(row_scales, (E, N, K // 32), torch.uint8, "row_scales"), pc, ps, _stream(stream))
@@ -680,7 +690,7 @@ def memfine_mxw_quantize(W, codes=None, scales=None, stream=None):
     """Rounds matrices [E, N, K] (bfloat16 or float32) to MX4, laid out; returns
     (codes, scales), allocated where None is given."""
     E, N, K = W.shape
-    codes, scales, pc, ps = _mxw_buffers(E, N, K, codes, scales, W.device)
+    codes, scales, pc, ps = _mxw_outputs(E, N, K, codes, scales, W.device)
     rc = lib().memfine_mxw_quantize(int(E), int(N), int(K), _dtype_of(W, "W"),
                                     _ptr(W, (E, N, K), W.dtype, "W"), pc, ps, _stream(stream))
     _check(rc, "memfine_mxw_quantize")
@@ -690,7 +700,7 @@ def memfine_mxw_quantize(W, codes=None, scales=None, stream=None):
 def memfine_mxw_unpack(codes, scales, W, stream=None) -> None:
     """The values of laid-out MX4 matrices, into W [E, N, K], bfloat16 or float32."""
     E, N, K = W.shape
-    _, _, pc, ps = _mxw_buffers(E, N, K, codes, scales, W.device)
+    pc, ps = _mxw_weights(E, N, K, codes, scales)
     rc = lib().memfine_mxw_unpack(int(E), int(N), int(K), pc, ps, _dtype_of(W, "W"),
                                   _ptr(W, (E, N, K), W.dtype, "W"), _stream(stream))
     _check(rc, "memfine_mxw_unpack")
@@ -707,7 +717,7 @@ def memfine_linear_mxw(N: int, K: int, X, codes, scales, Y, XS=None, stream=None
     """Y [T, N] (bfloat16 or float32) = X [T, K] W^T, W one laid-out MX4 matrix
     (codes, scales: [1, bytes]); X bfloat16, or e4m3 bytes with scales XS."""
     T, _ = _rows(X, "X")
-    _, _, pc, ps = _mxw_buffers(1, N, K, codes, scales, X.device)
+    pc, ps = _mxw_weights(1, N, K, codes, scales)
     px, pxs = _act(X, XS, T, K)
     rc = lib().memfine_linear_mxw(T, int(N), int(K), px, pxs, pc, ps, _dtype_of(Y, "Y"),
                                   _ptr(Y, (T, N), Y.dtype, "Y"), _stream(stream))
@@ -720,8 +730,8 @@ def memfine_moe_fwd_mxw(shape: Shape, chunks: int, X, idx, gates, W1_codes, W1_s
     bytes with scales XS uint8 [T, h/32]."""
     torch = _torch()
     T, h, F, E, k = shape.T, shape.h, shape.F, shape.E, shape.k
-    _, _, p1, q1 = _mxw_buffers(E, 2 * F, h, W1_codes, W1_scales, X.device)
-    _, _, p2, q2 = _mxw_buffers(E, h, F, W2_codes, W2_scales, X.device)
+    p1, q1 = _mxw_weights(E, 2 * F, h, W1_codes, W1_scales, ("W1_codes", "W1_scales"))
+    p2, q2 = _mxw_weights(E, h, F, W2_codes, W2_scales, ("W2_codes", "W2_scales"))
     px, pxs = _act(X, XS, T, h)
     rc = lib().memfine_moe_fwd_mxw(
         ctypes.byref(shape), int(chunks), px, pxs, _ptr(idx, (T, k), torch.int32, "idx"),

@@ -1,0 +1,64 @@
+"""The binding's checks of the calls around the layer, without a GPU: tensors
+that stand for device memory, whose addresses are never followed, show what a
+call would have been given."""
+import pytest
+import torch
+
+import paper_2511_21431_amd as mf
+
+bf, u8 = torch.bfloat16, torch.uint8
+
+
+class Device:
+    """A contiguous device tensor, as far as the binding looks."""
+    is_cuda, device = True, "cpu"
+
+    def __init__(self, *shape, dtype=u8):
+        self.shape, self.dtype = torch.Size(shape), dtype
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 4096
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+
+def weights(E, N, K):
+    return (Device(E, mf.memfine_mxw_code_bytes(N, K)), Device(E, mf.memfine_mxw_scale_bytes(N, K)))
+
+
+@pytest.mark.parametrize("missing", (0, 1))
+def test_weights_are_required(missing):
+    """Weights are read, never made: None is refused, whatever else is right."""
+    T, N, K, E, F, k = 3, 64, 64, 4, 64, 2
+    X, Y = Device(T, K, dtype=bf), Device(T, N, dtype=bf)
+    w = list(weights(1, N, K))
+    w[missing] = None
+    name = ("codes", "scales")[missing]
+    with pytest.raises(ValueError, match=f"^{name} is required"):
+        mf.memfine_linear_mxw(N, K, X, *w, Y, stream=0)
+    with pytest.raises(ValueError, match=f"^{name} is required"):
+        mf.memfine_mxw_unpack(*w, Device(1, N, K, dtype=bf), stream=0)
+    for at in (0, 2):
+        w = [*weights(E, 2 * F, K), *weights(E, K, F)]
+        w[at + missing] = None
+        name = ("W1_codes", "W1_scales", "W2_codes", "W2_scales")[at + missing]
+        with pytest.raises(ValueError, match=f"^{name} is required"):
+            mf.memfine_moe_fwd_mxw(mf.make_shape(T, K, F, E, k, mf.BF16), 1, X,
+                                   Device(T, k, dtype=torch.int32),
+                                   Device(T, k, dtype=torch.float32), *w, Device(T, K, dtype=bf),
+                                   stream=0)
+
+
+def test_outputs_are_required():
+    w = weights(1, 64, 64)
+    with pytest.raises(ValueError, match="^Y is required"):
+        mf.memfine_linear_mxw(64, 64, Device(3, 64, dtype=bf), *w, None, stream=0)
+    with pytest.raises(ValueError, match="^out is required"):
+        mf.memfine_mx_values(Device(3, 64), Device(3, 2), None, stream=0)
