@@ -243,6 +243,16 @@ def _stream(stream):
     return int(stream)
 
 
+def _torch_stream(handle, device):
+    """The torch stream object for a stream handle."""
+    torch = _torch()
+    ptr = int(handle or 0)
+    for cand in (torch.cuda.current_stream(device), torch.cuda.default_stream(device)):
+        if cand.cuda_stream == ptr:
+            return cand
+    return torch.cuda.ExternalStream(ptr, device=device)
+
+
 class TorchAllocator:
     """Serves the layer's per-chunk buffers from torch's caching allocator,
     so that torch.cuda.max_memory_allocated sees the layer's true peak.
@@ -266,13 +276,7 @@ class TorchAllocator:
         self.struct = Allocator(self._alloc, self._release, None)
 
     def _stream(self, stream):
-        """The torch stream object for the library's stream handle."""
-        torch = _torch()
-        ptr = int(stream or 0)
-        for cand in (torch.cuda.current_stream(self.device), torch.cuda.default_stream(self.device)):
-            if cand.cuda_stream == ptr:
-                return cand
-        return torch.cuda.ExternalStream(ptr, device=self.device)
+        return _torch_stream(stream, self.device)
 
     def _do_alloc(self, nbytes, stream, ctx):
         torch = _torch()
@@ -662,14 +666,23 @@ def _mxw_weights(E, N, K, codes, scales, names=("codes", "scales")):
             _ptr(scales, (E, sb), torch.uint8, names[1]))
 
 
-def _mxw_outputs(E, N, K, codes, scales, device):
-    """(codes, scales, their pointers), allocated where None is given."""
+def _mxw_outputs(E, N, K, codes, scales, device, stream):
+    """(codes, scales, their pointers), allocated where None is given: in the order
+    of the call's stream, which writes them (memory of the current stream's order
+    could still be in use there), and kept for the current stream's uses."""
     torch = _torch()
     cb, sb = _mxw_bytes(N, K)
-    if codes is None:
-        codes = torch.empty((E, cb), dtype=torch.uint8, device=device)
-    if scales is None:
-        scales = torch.empty((E, sb), dtype=torch.uint8, device=device)
+
+    def made(t, nbytes):
+        if t is not None:
+            return t
+        if stream is None or device.type != "cuda":
+            return torch.empty((E, nbytes), dtype=torch.uint8, device=device)
+        with torch.cuda.stream(_torch_stream(_stream(stream), device)):
+            t = torch.empty((E, nbytes), dtype=torch.uint8, device=device)
+        t.record_stream(torch.cuda.current_stream(device))
+        return t
+    codes, scales = made(codes, cb), made(scales, sb)
     return (codes, scales) + _mxw_weights(E, N, K, codes, scales)
 
 
@@ -678,7 +691,8 @@ def memfine_mxw_pack(E: int, N: int, K: int, row_codes, row_scales, codes=None, 
     """Lays row-major MX4 matrices out, codes uint8 [E, N, K/2] and scales uint8
     [E, N, K/32]; returns (codes, scales), allocated where None is given."""
     torch = _torch()
-    codes, scales, pc, ps = _mxw_outputs(E, N, K, codes, scales, row_codes.device)
+    codes, scales, pc, ps = _mxw_outputs(E, N, K, codes, scales, row_codes.device,
+                                         stream)
     rc = lib().memfine_mxw_pack(
         int(E), int(N), int(K), _ptr(row_codes, (E, N, K // 2), torch.uint8, "row_codes"),
         _ptr(row_scales, (E, N, K // 32), torch.uint8, "row_scales"), pc, ps, _stream(stream))
@@ -690,7 +704,7 @@ def memfine_mxw_quantize(W, codes=None, scales=None, stream=None):
     """Rounds matrices [E, N, K] (bfloat16 or float32) to MX4, laid out; returns
     (codes, scales), allocated where None is given."""
     E, N, K = W.shape
-    codes, scales, pc, ps = _mxw_outputs(E, N, K, codes, scales, W.device)
+    codes, scales, pc, ps = _mxw_outputs(E, N, K, codes, scales, W.device, stream)
     rc = lib().memfine_mxw_quantize(int(E), int(N), int(K), _dtype_of(W, "W"),
                                     _ptr(W, (E, N, K), W.dtype, "W"), pc, ps, _stream(stream))
     _check(rc, "memfine_mxw_quantize")
