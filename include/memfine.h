@@ -500,9 +500,9 @@ int memfine_route_bwd(int64_t T, const memfine_gating* g, const float* d_logits,
 
 /* The router's product by itself, for routing from logits: d_logits = X Wr^T,
  * float [T, E] (shapes, types and limits of memfine_router_fwd; k is not
- * used), and its gradients dX = dlogits Wr, dWr = dlogits^T X (as
- * memfine_router_bwd, dlogits being rounded to the shape's dtype for the
- * products). */
+ * used; no working memory), and its gradients dX = dlogits Wr, dWr = dlogits^T
+ * X (as memfine_router_bwd, working memory from `alloc` as there; dlogits are
+ * rounded to the shape's dtype for the products). */
 int memfine_router_logits(const memfine_shape* shape, const void* d_X, const void* d_Wr,
                           float* d_logits, void* stream);
 int memfine_router_logits_bwd(const memfine_shape* shape, const void* d_X, const void* d_Wr,

@@ -1551,14 +1551,9 @@ int memfine_router_logits(const memfine_shape* shape, const void* d_X, const voi
   KernelTimer kt(MEMFINE_K_ROUTER_FWD, s, 2.0 * Td * S.h * S.E,
                  es * (Td * S.h + (double)S.E * S.h) + 4.0 * Td * S.E);
   if (S.E > 64 && S.E % 32 == 0) return hip_status(router_logits_gemm(S, d_X, d_Wr, d_logits, s));
-  // the fused kernel, with a top-1 that goes to the workspace
-  const int64_t o_gates = align256(S.T * 4), bytes = o_gates + S.T * 4;
-  char* ws = (char*)ws_alloc(nullptr, (size_t)bytes, s);
-  if (!ws) return MEMFINE_ERR_OOM;
-  const hipError_t err = launch_router_fwd(S.dtype, d_X, d_Wr, S.T, S.h, S.E, 1, (int32_t*)ws,
-                                           (float*)(ws + o_gates), d_logits, device_cus(), s);
-  ws_release(nullptr, ws, (size_t)bytes, s);
-  return hip_status(err);
+  // the fused kernel, which then selects nothing (k = 0): no working memory
+  return hip_status(launch_router_fwd(S.dtype, d_X, d_Wr, S.T, S.h, S.E, 0, nullptr, nullptr,
+                                      d_logits, device_cus(), s));
 }
 
 int memfine_router_logits_bwd(const memfine_shape* shape, const void* d_X, const void* d_Wr,
