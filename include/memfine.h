@@ -19,7 +19,10 @@
  *   into each chunk's buffers and reused by the next chunk in stream order
  *   (grown from a per-device stream-ordered pool when a call needs more,
  *   kept until memfine_workspace_trim or the end of the process: see
- *   memfine_workspace_held); one pinned host buffer of 1025 ints per device
+ *   memfine_workspace_held), and, for such calls made while their stream is
+ *   being captured into a graph, blocks that belong to that capture alone and
+ *   stay until the process ends (a caller that captures often passes an
+ *   allocator whose memory lives as long as its graphs); one pinned host buffer of 1025 ints per device
  *   for memfine_count; and, only when the side-stream launch option is on,
  *   two side streams and three events per device (kept until the process
  *   ends).
@@ -244,7 +247,9 @@ int64_t memfine_workspace_bytes(const memfine_shape* shape, int32_t chunks, int3
  * keep_bytes; afterwards the held bytes are at most keep_bytes.  A caller
  * that raises the chunk count to free memory trims to
  * memfine_workspace_bytes(new chunks, MEMFINE_PASS_BWD).  Not to be called
- * while a layer call runs on the same stream from another thread.
+ * while a layer call runs on the same stream from another thread, and refused
+ * (MEMFINE_ERR_INVALID_ARG) while the stream is being captured.  The blocks of
+ * captured calls are neither counted nor released.
  */
 int memfine_workspace_held(void* stream, int64_t* bytes_out);
 int memfine_workspace_trim(void* stream, int64_t keep_bytes);

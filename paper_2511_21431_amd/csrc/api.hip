@@ -176,7 +176,7 @@ hipMemPool_t device_pool() {
 // drained.  The block is re-allocated (from the pool, in stream order) when
 // a larger workspace is asked for and kept until the process ends.  A
 // request while the stream's block is taken gets a pool allocation of its
-// own.
+// own, and a call that is being captured blocks of its capture (below).
 struct WsBlock {
   void* p = nullptr;
   size_t bytes = 0;
@@ -196,11 +196,64 @@ void* pool_alloc(size_t bytes, hipStream_t s) {
   return p;
 }
 
+// Blocks of captured calls.  A graph keeps the addresses that its calls were
+// given, and its replays are ordered by the caller alone: on any stream, beside
+// later calls on the capture's own.  So a capture gets blocks of its own (one
+// for calls that follow each other on a stream), which nothing else uses and
+// nobody frees: the library does not learn of the graph's end.  They are
+// ordinary allocations, made while the thread's capture mode lets them be; a
+// pool allocation would become a node of the graph.
+struct GraphBlock {
+  int dev;
+  hipStream_t s;
+  unsigned long long capture;
+  size_t bytes;
+  bool busy;
+};
+std::unordered_map<void*, GraphBlock> g_graph_ws;  // under g_ws_mu
+
+// Whether s is being captured, and the capture's id (unique in the process).
+bool capturing(hipStream_t s, unsigned long long* id) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamGetCaptureInfo(s, &st, id) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return st == hipStreamCaptureStatusActive;
+}
+
+void* graph_alloc(int dev, size_t bytes, hipStream_t s, unsigned long long id) {
+  std::lock_guard<std::mutex> lk(g_ws_mu);
+  for (auto& e : g_graph_ws) {
+    GraphBlock& b = e.second;
+    if (b.capture == id && b.s == s && b.dev == dev && !b.busy && b.bytes >= bytes) {
+      b.busy = true;
+      return e.first;
+    }
+  }
+  hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+  if (hipThreadExchangeStreamCaptureMode(&mode) != hipSuccess) {
+    (void)hipGetLastError();
+    return nullptr;
+  }
+  void* p = nullptr;
+  const hipError_t err = hipMalloc(&p, bytes);
+  (void)hipThreadExchangeStreamCaptureMode(&mode);
+  if (err != hipSuccess) {
+    (void)hipGetLastError();
+    return nullptr;
+  }
+  g_graph_ws[p] = {dev, s, id, bytes, true};
+  return p;
+}
+
 void* ws_alloc(const memfine_allocator* a, size_t bytes, hipStream_t s) {
   if (bytes == 0) bytes = 256;
   if (a && a->alloc) return a->alloc(bytes, (void*)s, a->ctx);
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return nullptr;
+  unsigned long long id = 0;
+  if (capturing(s, &id)) return graph_alloc(dev, bytes, s, id);
   {
     std::lock_guard<std::mutex> lk(g_ws_mu);
     WsBlock& b = g_ws[{dev, s}];
@@ -232,6 +285,11 @@ void ws_release(const memfine_allocator* a, void* p, size_t bytes, hipStream_t s
     auto it = g_ws.find({dev, s});
     if (it != g_ws.end() && it->second.p == p) {
       it->second.busy = false;
+      return;
+    }
+    auto graph = g_graph_ws.find(p);
+    if (graph != g_graph_ws.end()) {
+      graph->second.busy = false;
       return;
     }
   }
@@ -590,6 +648,8 @@ int memfine_workspace_trim(void* stream, int64_t keep_bytes) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MEMFINE_ERR_HIP;
   hipStream_t s = (hipStream_t)stream;
+  unsigned long long id = 0;
+  if (capturing(s, &id)) return MEMFINE_ERR_INVALID_ARG;  // would free inside the graph
   std::lock_guard<std::mutex> lk(g_ws_mu);
   auto it = g_ws.find({dev, s});
   if (it == g_ws.end()) return MEMFINE_OK;

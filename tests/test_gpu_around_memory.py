@@ -56,3 +56,78 @@ def test_router_logits_take_no_memory(mf, E, dtype):
         assert mf.memfine_workspace_held() == 0
     side.synchronize()
     assert t.equal(z, want)
+
+
+def test_captured_calls_keep_their_memory(mf):
+    """Calls without an allocator that were captured into a graph: replays give the
+    eager results whatever the capture's stream does in between (larger calls,
+    which replace its block, trimming) and beside work on other streams."""
+    t = torch()
+    rng = np.random.default_rng(11)
+    bf = t.bfloat16
+    T, N, K, h, F, E, k = 16, 528, 8224, 256, 320, 6, 2   # K over 4096: split and summed
+    lin = packed(mf, 1, N, K, *rows(rng, 1, N, K)[:2])
+    w1 = packed(mf, E, 2 * F, h, *rows(rng, E, 2 * F, h, 119, 122)[:2])
+    w2 = packed(mf, E, h, F, *rows(rng, E, h, F, 119, 122)[:2])
+    big = packed(mf, 1, 1040, 12320, *rows(rng, 1, 1040, 12320)[:2])
+    shape = mf.make_shape(T, h, F, E, k, mf.BF16)
+    w, Wr = t.randn(h, device="cuda").to(bf), t.randn(E, h, device="cuda").to(bf)
+    wide = t.randn(64, 12320, device="cuda").to(bf)
+    idx = dev(rng.integers(0, E, (T, k)).astype(np.int32))
+    g = t.rand(T, k, device="cuda")
+    X, R, dl = t.empty(T, K, dtype=bf, device="cuda"), t.empty(T, h, dtype=bf, device="cuda"), t.empty(T, E, device="cuda")
+
+    def results():
+        return [t.zeros(T, N, device="cuda"), t.zeros(T, h, dtype=bf, device="cuda"),
+                t.zeros(T, h, dtype=bf, device="cuda"), t.zeros(h, device="cuda"),
+                t.zeros(T, h, dtype=bf, device="cuda"), t.zeros(E, h, device="cuda")]
+
+    def calls(o):
+        mf.memfine_linear_mxw(N, K, X, *lin, o[0])
+        mf.memfine_moe_fwd_mxw(shape, 2, R, idx, g, *w1, *w2, o[1])
+        mf.memfine_norm_bwd(1e-6, R, w, R, o[2], o[3])
+        mf.memfine_router_logits_bwd(shape, R, Wr, dl, o[4], o[5])
+
+    def other(n):
+        out = t.empty(64, 1040, device="cuda")
+        for _ in range(n):
+            mf.memfine_linear_mxw(1040, 12320, wide, *big, out)
+        return out
+
+    side, third = t.cuda.Stream(), t.cuda.Stream()
+    want_other = other(1)
+    graphs, outs = [], []
+    for _ in range(2):
+        t.cuda.synchronize()
+        with t.cuda.stream(side):
+            mf.memfine_workspace_trim(0)
+        log("capture")
+        graph, o = t.cuda.CUDAGraph(), results()
+        with t.cuda.graph(graph, stream=side):
+            calls(o)
+        with t.cuda.stream(side):
+            assert mf.memfine_workspace_held() == 0
+        graphs.append(graph)
+        outs.append(o)
+    for i in range(6):
+        X.copy_(t.randn(X.shape, device="cuda"))
+        R.copy_(t.randn(R.shape, device="cuda"))
+        dl.copy_(t.randn(dl.shape, device="cuda"))
+        want = results()
+        calls(want)
+        t.cuda.synchronize()
+        log("replay", i)
+        with t.cuda.stream(side):
+            if i == 4:
+                mf.memfine_workspace_trim(0)
+            got_other = other(20)
+        with t.cuda.stream(third):
+            graphs[i % 2].replay()          # beside work on the stream that it was captured on
+        with t.cuda.stream(side):
+            graphs[1 - i % 2].replay()
+        t.cuda.synchronize()
+        assert t.equal(got_other, want_other), i
+        for o in outs:
+            assert all(t.equal(a, b) for a, b in zip(o, want)), i
+            for x in o:
+                x.zero_()
