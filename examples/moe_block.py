@@ -50,7 +50,7 @@ class ServedBlock:
         """attended [tokens, K]: the heads' outputs; stream [tokens, h]: the
         residual stream, to which the projection is added in place.  Returns the
         experts' output, which the next block adds."""
-        mf.memfine_linear_mxw(self.h, self.K, attended, *self.Wo, self.o)
+        mf.memfine_linear_mxw(self.h, self.K, attended, *self.Wo, self.o, allocator=allocator)
         mf.memfine_norm_fwd(EPS, self.o, self.w, R=stream, S=stream, Y=self.y, Q=self.q, QS=self.qs)
         mf.memfine_router_logits(self.shape, self.y, self.Wr, self.logits)
         mf.memfine_route_fwd(self.gating, self.logits, self.idx, self.gates, bias=self.bias)

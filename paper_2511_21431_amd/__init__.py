@@ -9,7 +9,7 @@ from ._lib import (BF16, CHUNK_EXPERTS, CHUNK_TOKENS, ERR_SCRATCH, F32, NOALLOC_
                    memfine_activation_memory, memfine_count, memfine_dispatch,
                    memfine_get_launch_options, memfine_mact_select, memfine_mact_thresholds,
                    memfine_moe_bwd, memfine_moe_fwd, memfine_moe_fwd_noalloc, memfine_plan, memfine_pool_high_water,
-                   memfine_linear_mxw, memfine_moe_fwd_mxw, memfine_moe_mxw_workspace_bytes,
+                   memfine_linear_mxw, memfine_linear_mxw_workspace_bytes, memfine_moe_fwd_mxw, memfine_moe_mxw_workspace_bytes,
                    memfine_mx_values, memfine_mxw_code_bytes, memfine_mxw_pack,
                    memfine_mxw_quantize, memfine_mxw_scale_bytes, memfine_mxw_unpack,
                    memfine_norm_bwd, memfine_norm_fwd,

@@ -150,6 +150,10 @@ _SIGS = {
                                           ctypes.c_int32, P, P]),
     "memfine_linear_mxw": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, P, P, P,
                                           P, ctypes.c_int32, P, P]),
+    "memfine_linear_mxw_alloc": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, P,
+                                                P, P, P, ctypes.c_int32, P, ALP, P]),
+    "memfine_linear_mxw_workspace_bytes": (ctypes.c_int64, [ctypes.c_int64, ctypes.c_int32,
+                                                            ctypes.c_int32, ctypes.c_int32]),
     "memfine_moe_fwd_mxw": (ctypes.c_int, [SHP, ctypes.c_int32, P, P, P, P, P, P, P, P, P, ALP, P]),
     "memfine_moe_mxw_workspace_bytes": (ctypes.c_int64, [SHP, ctypes.c_int32, ctypes.c_int32]),
     "memfine_status_str": (ctypes.c_char_p, [ctypes.c_int]),
@@ -727,15 +731,25 @@ def _act(X, XS, T, K):
     return _ptr(X, (T, K), dt, "X"), _opt(XS, (T, K // 32), torch.uint8, "XS")
 
 
-def memfine_linear_mxw(N: int, K: int, X, codes, scales, Y, XS=None, stream=None) -> None:
+def memfine_linear_mxw(N: int, K: int, X, codes, scales, Y, XS=None, stream=None,
+                       allocator=None) -> None:
     """Y [T, N] (bfloat16 or float32) = X [T, K] W^T, W one laid-out MX4 matrix
-    (codes, scales: [1, bytes]); X bfloat16, or e4m3 bytes with scales XS."""
+    (codes, scales: [1, bytes]); X bfloat16, or e4m3 bytes with scales XS.  The
+    allocator serves the partial results of a split reduction."""
     T, _ = _rows(X, "X")
     pc, ps = _mxw_weights(1, N, K, codes, scales)
     px, pxs = _act(X, XS, T, K)
-    rc = lib().memfine_linear_mxw(T, int(N), int(K), px, pxs, pc, ps, _dtype_of(Y, "Y"),
-                                  _ptr(Y, (T, N), Y.dtype, "Y"), _stream(stream))
+    rc = lib().memfine_linear_mxw_alloc(T, int(N), int(K), px, pxs, pc, ps, _dtype_of(Y, "Y"),
+                                        _ptr(Y, (T, N), Y.dtype, "Y"), _alloc_arg(allocator),
+                                        _stream(stream))
     _check(rc, "memfine_linear_mxw")
+
+
+def memfine_linear_mxw_workspace_bytes(T: int, N: int, K: int, mx8: bool = False) -> int:
+    v = lib().memfine_linear_mxw_workspace_bytes(int(T), int(N), int(K), int(bool(mx8)))
+    if v < 0:
+        raise MemfineError(int(v), "memfine_linear_mxw_workspace_bytes")
+    return int(v)
 
 
 def memfine_moe_fwd_mxw(shape: Shape, chunks: int, X, idx, gates, W1_codes, W1_scales, W2_codes,

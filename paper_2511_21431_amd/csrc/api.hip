@@ -1515,6 +1515,25 @@ MxLayout mx_layout(const memfine_shape& s, int64_t n, bool mx8) {
   m.total = m.o_y + align256(n * (int64_t)s.h * (m.y_bf16 ? 2 : 4) * m.splits);
   return m;
 }
+
+// The linear map's product, as far as its kernel's choice goes, and its working
+// memory: the partial results of a split reduction.
+MxArgs linear_args(int64_t T, int32_t N, int32_t K, bool mx8) {
+  static const uint8_t scaled = 0;
+  MxArgs g = {};
+  g.n = (int)T;
+  g.E = 1;
+  g.N = N;
+  g.K = K;
+  g.KT = (K + 127) / 128;
+  g.cus = device_cus();
+  g.XS = mx8 ? &scaled : nullptr;
+  return g;
+}
+int64_t linear_workspace(const MxArgs& g) {
+  const int splits = g.n == 0 ? 1 : mx_splits(g);
+  return splits == 1 ? 0 : (int64_t)splits * g.n * g.N * 4;
+}
 }  // namespace
 
 int memfine_norm_fwd(int64_t T, int32_t h, int32_t dtype, float eps, const void* d_X,
@@ -1701,9 +1720,22 @@ int memfine_mxw_unpack(int32_t E, int32_t N, int32_t K, const uint8_t* d_codes,
                                       (hipStream_t)stream));
 }
 
+int64_t memfine_linear_mxw_workspace_bytes(int64_t T, int32_t N, int32_t K, int32_t mx8) {
+  if (check_mx4(1, N, K) || T < 0 || T > INT32_MAX || (mx8 != 0 && mx8 != 1))
+    return MEMFINE_ERR_INVALID_ARG;
+  return linear_workspace(linear_args(T, N, K, mx8 != 0));
+}
+
 int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const uint8_t* d_XS,
                        const uint8_t* d_codes, const uint8_t* d_scales, int32_t y_dtype, void* d_Y,
                        void* stream) {
+  return memfine_linear_mxw_alloc(T, N, K, d_X, d_XS, d_codes, d_scales, y_dtype, d_Y, nullptr,
+                                  stream);
+}
+
+int memfine_linear_mxw_alloc(int64_t T, int32_t N, int32_t K, const void* d_X, const uint8_t* d_XS,
+                             const uint8_t* d_codes, const uint8_t* d_scales, int32_t y_dtype,
+                             void* d_Y, const memfine_allocator* alloc, void* stream) {
   int rc = check_mx4(1, N, K);
   if (rc) return rc;
   if (T < 0) return MEMFINE_ERR_INVALID_ARG;
@@ -1712,31 +1744,24 @@ int memfine_linear_mxw(int64_t T, int32_t N, int32_t K, const void* d_X, const u
   if (!d_X || !d_codes || !d_scales || !d_Y || !aligned16({d_X, d_codes, d_scales, d_Y}))
     return MEMFINE_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
-  MxArgs g = {};
+  MxArgs g = linear_args(T, N, K, d_XS != nullptr);
+  const int64_t bytes = linear_workspace(g);
   g.X = d_X;
   g.XS = d_XS;
   g.Wc = d_codes;
   g.Ws = d_scales;
-  g.n = (int)T;
-  g.E = 1;
-  g.N = N;
-  g.K = K;
-  g.KT = (K + 127) / 128;
   g.out = d_Y;
   g.out_bf16 = y_dtype == MEMFINE_BF16;
-  g.cus = device_cus();
   const double nk = (double)N * K, xb = d_XS ? 1.03125 : 2.0;
   KernelTimer kt(MEMFINE_K_MX_LINEAR, s, 2.0 * T * nk,
                  0.53125 * nk + xb * T * K + (g.out_bf16 ? 2.0 : 4.0) * T * N);
-  const int splits = mx_splits(g);
-  if (splits == 1) return hip_status(launch_mx_rows(g, s));
-  const size_t bytes = (size_t)splits * T * N * 4;
-  g.out = ws_alloc(nullptr, bytes, s);
+  if (bytes == 0) return hip_status(launch_mx_rows(g, s));
+  g.out = ws_alloc(alloc, (size_t)bytes, s);
   if (!g.out) return MEMFINE_ERR_OOM;
   hipError_t err = launch_mx_rows(g, s);
   if (err == hipSuccess)
-    err = launch_mx_sum((const float*)g.out, splits, T * N, g.out_bf16, d_Y, s);
-  ws_release(nullptr, g.out, bytes, s);
+    err = launch_mx_sum((const float*)g.out, mx_splits(g), T * N, g.out_bf16, d_Y, s);
+  ws_release(alloc, g.out, (size_t)bytes, s);
   return hip_status(err);
 }
 

@@ -62,3 +62,15 @@ def test_outputs_are_required():
         mf.memfine_linear_mxw(64, 64, Device(3, 64, dtype=bf), *w, None, stream=0)
     with pytest.raises(ValueError, match="^out is required"):
         mf.memfine_mx_values(Device(3, 64), Device(3, 2), None, stream=0)
+
+
+def test_linear_working_memory():
+    """Partial results of a split reduction, none where it is not split."""
+    f = mf.memfine_linear_mxw_workspace_bytes
+    assert f(0, 64, 8192) == f(1, 64, 8192) == f(16, 64, 4096) == f(16, 64, 4096, True) == 0
+    assert f(16, 64, 4128) == f(16, 64, 8192, True) == 2 * 16 * 64 * 4
+    assert f(64, 528, 12320) == 4 * 64 * 528 * 4
+    assert f(5000, 8192, 8192) == 0
+    for bad in ((-1, 64, 64), (1, 8, 64), (1, 64, 48), (2**31, 64, 64)):
+        with pytest.raises(mf.MemfineError):
+            f(*bad)

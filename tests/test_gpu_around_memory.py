@@ -131,3 +131,33 @@ def test_captured_calls_keep_their_memory(mf):
             assert all(t.equal(a, b) for a, b in zip(o, want)), i
             for x in o:
                 x.zero_()
+
+
+@pytest.mark.parametrize("mx8", (False, True))
+def test_linear_on_the_callers_memory(mf, mx8):
+    """A split reduction takes the documented bytes from the caller's allocator
+    and gives them back; a failing allocator is an error that leaves nothing."""
+    from test_gpu_mxw import activations
+    t = torch()
+    rng = np.random.default_rng(12)
+    for T, N, K in ((16, 528, 8224), (64, 96, 4128), (16, 96, 4096), (1, 96, 8192)):
+        W = packed(mf, 1, N, K, *rows(rng, 1, N, K)[:2])
+        X, XS, _ = activations(rng, T, K, mx8)
+        want, got = (t.full((T, N), float("nan"), device="cuda") for _ in range(2))
+        mf.memfine_linear_mxw(N, K, X, *W, want, XS=XS)
+        a, need = mf.TorchAllocator(), mf.memfine_linear_mxw_workspace_bytes(T, N, K, mx8)
+        side = t.cuda.Stream()
+        t.cuda.synchronize()
+        with t.cuda.stream(side):
+            mf.memfine_workspace_trim(0)
+            mf.memfine_linear_mxw(N, K, X, *W, got, XS=XS, allocator=a)
+            assert mf.memfine_workspace_held() == 0
+        side.synchronize()
+        assert t.equal(got, want)
+        assert (a.high_water, a.calls, a.live_bytes) == (need, int(need > 0), 0)
+        a = mf.TorchAllocator()
+        a.fail_at = 1
+        if need:
+            with pytest.raises(mf.MemfineError) as e:
+                mf.memfine_linear_mxw(N, K, X, *W, got, XS=XS, allocator=a)
+            assert e.value.code == -4 and a.live_bytes == 0
