@@ -33,15 +33,27 @@ namespace {
 
 constexpr int kTokens = 16;  // tokens per workgroup of 256 threads
 
-// e^x for x <= 0.  The rounding of x log2(e) is a relative error of |x| 2^-24:
-// nothing beside the sums' where e^x counts in them, and below 1e-6 down to
-// e^-16 of the largest.
+// e^x for x <= 0, to choose experts by and for the softmax's sum.  The rounding
+// of x log2(e) is a relative error of |x| 2^-24: nothing beside the sum's own
+// where e^x counts in it.
 __device__ __forceinline__ float exp_neg(float x) {
   return __builtin_amdgcn_exp2f(fmaxf(x, -150.f) * 1.44269502f);
 }
-// sigmoid(z) and 1 - sigmoid(z), both without cancellation; |z| finite.
-__device__ __forceinline__ float sigmoid_pair(float z, float* complement) {
-  const float e = exp_neg(-fabsf(z));
+// The same for what is handed out, gates and gradients, where an expert far below
+// the best counts by itself: what the rounded product x log2(e) lacks, in the
+// product and in the constant, multiplies the result as 1 + it (to 2^-22 in all,
+// where the product alone is off by 4e-6 at e^-80).
+__device__ __forceinline__ float exp_neg_exact(float x) {
+  constexpr float kLog2e = 1.44269502f;
+  constexpr float kRest = (float)(1.4426950408889634074 - (double)kLog2e);
+  x = fmaxf(x, -150.f);
+  const float h = x * kLog2e;
+  const float rest = fmaf(x, kRest, fmaf(x, kLog2e, -h));
+  const float e = __builtin_amdgcn_exp2f(h);
+  return fmaf(e, rest * 0.693147181f, e);
+}
+// sigmoid(z) and 1 - sigmoid(z), both without cancellation; e = e^-|z|, |z| finite.
+__device__ __forceinline__ float sigmoid_pair(float z, float e, float* complement) {
   const float r = __builtin_amdgcn_rcpf(1.f + e);
   *complement = z >= 0.f ? e * r : r;
   return z >= 0.f ? r : e * r;
@@ -186,8 +198,9 @@ __device__ __forceinline__ float relative_score(int score, float zr, bool ok) {
   const float z = fminf(zr, FLT_MAX);
   const float top = row_max(ok ? z : -INFINITY);
   if (!ok) return 0.f;
-  if (score == 0) return exp_neg(z - top);
-  return exp_neg(fminf(z, 0.f) - fminf(top, 0.f)) * __builtin_amdgcn_rcpf(1.f + exp_neg(-fabsf(z)));
+  if (score == 0) return exp_neg_exact(z - top);
+  return exp_neg_exact(fminf(z, 0.f) - fminf(top, 0.f)) *
+         __builtin_amdgcn_rcpf(1.f + exp_neg(-fabsf(z)));
 }
 
 // H: the heads of a lane's list that the k rounds can reach (k <= 8: at most 8).
@@ -220,7 +233,7 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const float* __restrict_
 #pragma unroll
     for (int q = 0; q < V; ++q) {
       float c;
-      p[q] = sigmoid_pair(z[q], &c);
+      p[q] = sigmoid_pair(z[q], exp_neg(-fabsf(z[q])), &c);
     }
   }
   if (bias) {
@@ -344,9 +357,9 @@ __global__ __launch_bounds__(256) void route_fwd_kernel(const float* __restrict_
     const float sum = row_sum(g);  // 1/2 and more, or no slot counts
     f = sum > 0.f ? a.scale / sum : 0.f;
   } else if (ok) {
+    const float zs = fminf(zr, FLT_MAX), e = exp_neg_exact(a.score == 0 ? zs - m : -fabsf(zs));
     float comp;
-    g = a.score == 0 ? exp_neg(fminf(zr, FLT_MAX) - m) * inv
-                     : sigmoid_pair(fminf(zr, FLT_MAX), &comp);
+    g = a.score == 0 ? e * inv : sigmoid_pair(zs, e, &comp);
   }
   if (slot && t < T) {
     idx[t * a.k + l] = e;
@@ -387,17 +400,17 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(const float* __restrict_
 #pragma unroll
     for (int q = 0; q < V; ++q) s[q] = s[q] > FLT_MAX ? FLT_MAX : s[q];
     softmax_stats<V>(s, m, inv);
-    p = ok ? exp_neg(z - m) * inv : 0.f;
+    p = ok ? exp_neg_exact(z - m) * inv : 0.f;
     dz = p * dg;
     const float c = row_sum(dz);
 #pragma unroll
     for (int q = 0; q < V; ++q)
       if (q < a.v && l * a.v + q < E)
-        rows[tok * E + l * a.v + q] = unmasked(s[q]) ? -c * (exp_neg(s[q] - m) * inv) : 0.f;
+        rows[tok * E + l * a.v + q] = unmasked(s[q]) ? -c * (exp_neg_exact(s[q] - m) * inv) : 0.f;
   } else {
     float comp = 1.f;  // sigmoid: 1 - p
     if (a.score != 0) {
-      p = sigmoid_pair(z, &comp);
+      p = sigmoid_pair(z, exp_neg_exact(-fabsf(z)), &comp);
       if (!ok) p = 0.f;
     }
     if (a.renorm) {
