@@ -27,6 +27,16 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
 }
 
+// Index of a thread of a grid of 256-thread workgroups that goes on in y.
+__device__ __forceinline__ int64_t thread_id() {
+  return (blockIdx.y * (int64_t)gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+}
+// That grid (device code: thread_id) for so many threads, of 256 a workgroup.
+inline dim3 grid_of(int64_t threads) {
+  const int64_t blocks = (threads + 255) / 256, x = blocks < (1 << 23) ? blocks : 1 << 23;
+  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+
 // Element access for the two storage types of the layer.
 template <typename T> struct Elem;
 template <> struct Elem<bf16_t> {

@@ -44,6 +44,10 @@ struct ChunkMeta {
   int32_t* clear;        // [2]       set to 0 beside the dispatch, or null
 };
 
+// A launch holds fewer than 2^32 work-items in a dimension of its grid: what more
+// rows than that need goes in several launches, or on in the grid's y.
+constexpr int64_t kMostItems = int64_t(1) << 31;
+
 hipError_t launch_fill_i32(int32_t* p, int64_t n, int32_t v, hipStream_t s);
 // dst[0, held) = src, dst[held, n) = 0
 hipError_t launch_copy_pad(int32_t* dst, const int32_t* src, int64_t held, int64_t n, hipStream_t s);

@@ -882,7 +882,7 @@ __global__ __launch_bounds__(256) void mx_combine_kernel(const float* __restrict
                                                          const float* __restrict__ gates,
                                                          int64_t t0, int64_t n, int h, int k,
                                                          bf16_t* __restrict__ Y) {
-  const int64_t gid = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t gid = thread_id();
   if (gid >= n) return;
   const int vpr = h / 4;
   const int64_t i = gid / vpr, c = (gid - i * vpr) * 4;
@@ -915,7 +915,7 @@ __global__ __launch_bounds__(256) void mx_combine_kernel(const float* __restrict
 template <typename T>
 __global__ __launch_bounds__(256) void mx_sum_kernel(const float* __restrict__ part, int splits,
                                                      int64_t n, T* __restrict__ out) {
-  const int64_t i = (blockIdx.x * 256ll + threadIdx.x) * 4;
+  const int64_t i = thread_id() * 4;
   if (i >= n) return;
   f32x4_t v = *(const f32x4_t*)(part + i);
   for (int s = 1; s < splits; ++s) v += *(const f32x4_t*)(part + s * n + i);
@@ -931,7 +931,7 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* __restrict
                                                        int N, int K, int KT,
                                                        uint8_t* __restrict__ codes,
                                                        uint8_t* __restrict__ scales) {
-  const int64_t id = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t id = thread_id();
   if (id >= n) return;
   const int lane = (int)(id & 63), NT = N / 16;
   const int64_t tile = id >> 6;                 // over [E][NT][KT]
@@ -962,7 +962,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T* __restrict__
                                                            uint8_t* __restrict__ codes,
                                                            uint8_t* __restrict__ scales) {
   constexpr int E = Elem<T>::kVec;
-  const int64_t id = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t id = thread_id();
   if (id >= n) return;
   const int lane = (int)(id & 63), KS = (KT + 3) / 4;
   const int64_t quad = id >> 6;                 // over [E][NT][KS]
@@ -1013,7 +1013,7 @@ __global__ __launch_bounds__(256) void mx4_unpack_kernel(const uint8_t* __restri
                                                          int64_t n, int N, int K, int KT,
                                                          T* __restrict__ W) {
   constexpr int E = Elem<T>::kVec;
-  const int64_t id = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t id = thread_id();
   if (id >= n) return;
   const int nb = K / kMxBlock, KS = (KT + 3) / 4;
   const int64_t row = id / nb;
@@ -1042,28 +1042,21 @@ __global__ __launch_bounds__(256) void mx4_unpack_kernel(const uint8_t* __restri
   }
 }
 
-hipError_t grid_of(int64_t threads, unsigned* blocks) {
-  const int64_t b = (threads + 255) / 256;
-  if (b > INT32_MAX) return hipErrorInvalidValue;
-  *blocks = (unsigned)b;
-  return hipSuccess;
-}
-
 // Blocks of RB rows that n rows of E experts (one group: offsets null) can form.
 int64_t row_blocks(const MxArgs& g, int RB) {
-  if (!g.offsets) return (g.n + RB - 1) / RB;
+  if (!g.offsets) return ((int64_t)g.n + RB - 1) / RB;
   return (int64_t)g.n / RB + (g.E < g.n ? g.E : g.n);
 }
 
 // Matrices with rows, about.
 int64_t busy(const MxArgs& g, int RB) {
-  return g.offsets ? std::min<int64_t>(g.E, g.n) : (g.n + RB - 1) / RB;
+  return g.offsets ? std::min<int64_t>(g.E, g.n) : ((int64_t)g.n + RB - 1) / RB;
 }
 
 template <bool MX8, int W> hipError_t run_fc1_rows(MxArgs g, hipStream_t s) {
   g.col_blocks = g.N / 64;
   const int64_t blocks = (int64_t)((g.col_blocks + 7) / 8 * 8) * ((row_blocks(g, 16) + 3) / 4 * 4);
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (blocks > kMostItems / (64 * W)) return hipErrorInvalidValue;
   mx_fc1_rows_kernel<MX8, W><<<(unsigned)blocks, 64 * W, 0, s>>>(g);
   return hipGetLastError();
 }
@@ -1080,7 +1073,7 @@ template <bool MX8, int MB, int W> hipError_t run_cols(MxArgs g, hipStream_t s) 
   const int64_t want = (8 / W) * g.cus / (busy(g, 16 * MB) * g.splits);
   g.col_shares = (int)std::max<int64_t>(1, std::min<int64_t>(g.col_blocks, want));
   const int64_t blocks = rb * g.col_shares * g.splits;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (blocks > kMostItems / (64 * W)) return hipErrorInvalidValue;
   g.row_blocks = (int)rb;
   mx_cols_kernel<MX8, TILES, MB, W><<<(unsigned)blocks, 64 * W, 0, s>>>(g);
   return hipGetLastError();
@@ -1093,7 +1086,7 @@ template <bool MX8, int MODE, int BM, int S>
 hipError_t run_tiles(MxArgs g, hipStream_t s) {
   g.col_blocks = (MODE == kFc1 ? g.N / 2 + 127 : g.N + 255) / (MODE == kFc1 ? 128 : 256);
   const int64_t blocks = (row_blocks(g, BM) * g.col_blocks + 7) / 8 * 8;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (blocks > kMostItems / 256) return hipErrorInvalidValue;
   mx_tile_kernel<MX8, MODE, BM, S><<<(unsigned)blocks, 256, 0, s>>>(g);
   return hipGetLastError();
 }
@@ -1102,7 +1095,7 @@ template <bool MX8, int MODE, int TILES, int W>
 hipError_t run_one(MxArgs g, hipStream_t s) {
   g.col_blocks = MODE == kFc1 ? g.N / 64 : (g.N / 16 + TILES - 1) / TILES;
   const int64_t blocks = (int64_t)g.col_blocks * (MODE == kFc1 ? g.n : 1);
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (blocks > kMostItems / (64 * W)) return hipErrorInvalidValue;
   const size_t lds = (size_t)one_lds(g, MX8, MODE == kFc1 ? 1 : g.n, TILES, W);
   mx_one_kernel<MX8, MODE, TILES, W><<<(unsigned)blocks, 64 * W, lds, s>>>(g);
   return hipGetLastError();
@@ -1133,7 +1126,7 @@ Kind kind_of(const MxArgs& g, int mode) {
   const bool mx8 = g.XS != nullptr;
   if (mode == kRows && !g.offsets && g.n == 1 && one_lds(g, mx8, 1, 1, 8) <= kOneLds) return kOneRow;
   const int groups = g.offsets ? g.E : 1;
-  const int rows = (g.n + groups - 1) / groups;
+  const int rows = (int)(((int64_t)g.n + groups - 1) / groups);
   const int64_t cols = mode == kFc1 ? (g.N / 2 + 127) / 128 : (g.N + 255) / 256;
   auto tiles = [&](int BM) { return std::max<int64_t>(busy(g, BM), g.n / BM) * cols; };
   bool few;
@@ -1179,10 +1172,8 @@ hipError_t launch_mx4_pack(int64_t E, int N, int K, const uint8_t* rc, const uin
                            uint8_t* codes, uint8_t* scales, hipStream_t s) {
   const int KT = (K + 127) / 128;
   const int64_t n = E * (N / 16) * KT * 64;
-  unsigned blocks;
   if (n == 0) return hipSuccess;
-  if (hipError_t err = grid_of(n, &blocks)) return err;
-  mx4_pack_kernel<<<blocks, 256, 0, s>>>(rc, rs, n, N, K, KT, codes, scales);
+  mx4_pack_kernel<<<grid_of(n), 256, 0, s>>>(rc, rs, n, N, K, KT, codes, scales);
   return hipGetLastError();
 }
 
@@ -1190,13 +1181,12 @@ hipError_t launch_mx4_quantize(int dtype, int64_t E, int N, int K, const void* W
                                uint8_t* scales, hipStream_t s) {
   const int KT = (K + 127) / 128;
   const int64_t n = E * (N / 16) * ((KT + 3) / 4) * 64;
-  unsigned blocks;
   if (n == 0) return hipSuccess;
-  if (hipError_t err = grid_of(n, &blocks)) return err;
+  const dim3 grid = grid_of(n);
   if (dtype == 0)
-    mx4_quantize_kernel<bf16_t><<<blocks, 256, 0, s>>>((const bf16_t*)W, n, N, K, KT, codes, scales);
+    mx4_quantize_kernel<bf16_t><<<grid, 256, 0, s>>>((const bf16_t*)W, n, N, K, KT, codes, scales);
   else
-    mx4_quantize_kernel<float><<<blocks, 256, 0, s>>>((const float*)W, n, N, K, KT, codes, scales);
+    mx4_quantize_kernel<float><<<grid, 256, 0, s>>>((const float*)W, n, N, K, KT, codes, scales);
   return hipGetLastError();
 }
 
@@ -1204,13 +1194,12 @@ hipError_t launch_mx4_unpack(int dtype, int64_t E, int N, int K, const uint8_t* 
                              const uint8_t* scales, void* W, hipStream_t s) {
   const int KT = (K + 127) / 128;
   const int64_t n = E * N * (K / kMxBlock);
-  unsigned blocks;
   if (n == 0) return hipSuccess;
-  if (hipError_t err = grid_of(n, &blocks)) return err;
+  const dim3 grid = grid_of(n);
   if (dtype == 0)
-    mx4_unpack_kernel<bf16_t><<<blocks, 256, 0, s>>>(codes, scales, n, N, K, KT, (bf16_t*)W);
+    mx4_unpack_kernel<bf16_t><<<grid, 256, 0, s>>>(codes, scales, n, N, K, KT, (bf16_t*)W);
   else
-    mx4_unpack_kernel<float><<<blocks, 256, 0, s>>>(codes, scales, n, N, K, KT, (float*)W);
+    mx4_unpack_kernel<float><<<grid, 256, 0, s>>>(codes, scales, n, N, K, KT, (float*)W);
   return hipGetLastError();
 }
 
@@ -1218,17 +1207,31 @@ hipError_t launch_mx_fc1(const MxArgs& g, hipStream_t s) {
   return g.XS ? run<true, kFc1>(g, s) : run<false, kFc1>(g, s);
 }
 hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s) {
-  return g.XS ? run<true, kRows>(g, s) : run<false, kRows>(g, s);
+  // One matrix and more rows than a launch of the smallest tiles holds (and than
+  // leave room for a tile below 2^31): equal parts, each far beyond those of few rows.
+  const int64_t col_blocks = (g.N + 255) / 256;
+  const int64_t most = std::min<int64_t>(kMostItems / 256 / col_blocks * 32, 1 << 28);
+  if (g.offsets || g.n <= most) return g.XS ? run<true, kRows>(g, s) : run<false, kRows>(g, s);
+  const int64_t parts = (g.n + most - 1) / most, xb = g.XS ? 1 : 2, yb = g.out_bf16 ? 2 : 4;
+  for (int64_t i = 0; i < parts; ++i) {
+    const int64_t r0 = i * g.n / parts, r1 = (i + 1) * g.n / parts;
+    MxArgs p = g;
+    p.n = (int)(r1 - r0);
+    p.X = (const char*)g.X + r0 * g.K * xb;
+    if (g.XS) p.XS = g.XS + r0 * (g.K / kMxBlock);
+    p.out = (char*)g.out + r0 * g.N * yb;
+    if (hipError_t err = g.XS ? run<true, kRows>(p, s) : run<false, kRows>(p, s)) return err;
+  }
+  return hipSuccess;
 }
 
 int mx_splits(const MxArgs& g) { return kind_of(g, kRows) == kFewRows ? splits_of(g) : 1; }
 hipError_t launch_mx_sum(const float* part, int splits, int64_t n, int out_bf16, void* out,
                          hipStream_t s) {
-  unsigned blocks;
   if (n == 0) return hipSuccess;
-  if (hipError_t err = grid_of(n / 4, &blocks)) return err;
-  if (out_bf16) mx_sum_kernel<bf16_t><<<blocks, 256, 0, s>>>(part, splits, n, (bf16_t*)out);
-  else mx_sum_kernel<float><<<blocks, 256, 0, s>>>(part, splits, n, (float*)out);
+  const dim3 grid = grid_of(n / 4);
+  if (out_bf16) mx_sum_kernel<bf16_t><<<grid, 256, 0, s>>>(part, splits, n, (bf16_t*)out);
+  else mx_sum_kernel<float><<<grid, 256, 0, s>>>(part, splits, n, (float*)out);
   return hipGetLastError();
 }
 
@@ -1247,11 +1250,9 @@ hipError_t launch_mx_combine(const float* y, int splits, int64_t stride, const i
                              const float* gates, int64_t t0, int64_t tokens, int h, int k, void* Y,
                              hipStream_t s) {
   const int64_t n = tokens * (h / 4);
-  unsigned blocks;
   if (n == 0) return hipSuccess;
-  if (hipError_t err = grid_of(n, &blocks)) return err;
-  mx_combine_kernel<<<blocks, 256, 0, s>>>(y, splits, stride, row_of_slot, gates, t0, n, h, k,
-                                           (bf16_t*)Y);
+  mx_combine_kernel<<<grid_of(n), 256, 0, s>>>(y, splits, stride, row_of_slot, gates, t0, n, h, k,
+                                               (bf16_t*)Y);
   return hipGetLastError();
 }
 

@@ -10,6 +10,8 @@
 // waves owns a row at a time; lane-consecutive 16-byte vectors; sums in fp32.
 // bf16: 32768 rows of 7168 with R, S, Y and MX8 367 us (2.12 GB, 5.8 TB/s), its
 // values read back 143 us; 16385 rows of 4096 backward 102 us (537 MB, 5.2 TB/s).
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 #include "mx.h"
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(256) void mx8_unpack_kernel(const uint8_t* __restri
                                                          const uint8_t* __restrict__ QS, int64_t n,
                                                          T* __restrict__ out) {
   constexpr int E = Elem<T>::kVec;
-  const int64_t v = blockIdx.x * 256ll + threadIdx.x;
+  const int64_t v = thread_id();
   if (v >= n / E) return;
   const float s = mx_scale_value(QS[v * E / kMxBlock]);
   float f[E];
@@ -255,6 +257,19 @@ RowShape row_shape(int nv) {
   return {V, (nv + 64 * V - 1) / (64 * V)};
 }
 
+template <typename T, int V>
+void run_norm_fwd(const void* X, const void* R, const void* w, float eps, int64_t rows, int h,
+                  int waves, void* S, void* Y, uint8_t* Q, uint8_t* QS, hipStream_t s) {
+  const int64_t most = kMostItems / (64 * waves);
+  auto at = [](auto* p, int64_t i) { return p ? p + i : nullptr; };
+  for (int64_t t = 0; t < rows; t += most) {
+    const int64_t i = t * h;
+    norm_fwd_kernel<T, V><<<(unsigned)std::min(most, rows - t), 64 * waves, 0, s>>>(
+        (const T*)X + i, at((const T*)R, i), (const T*)w, eps, h, at((T*)S, i), at((T*)Y, i),
+        at(Q, i), at(QS, i / kMxBlock));
+  }
+}
+
 }  // namespace
 
 hipError_t launch_norm_fwd(int dtype, const void* X, const void* R, const void* w, float eps,
@@ -262,11 +277,8 @@ hipError_t launch_norm_fwd(int dtype, const void* X, const void* R, const void* 
                            hipStream_t s) {
   if (T == 0) return hipSuccess;
   const RowShape rs = row_shape(h / (dtype == 0 ? 8 : 4));
-  const dim3 grid((unsigned)T), block(64 * rs.waves);
-  if (rs.waves > 16 || T > INT32_MAX) return hipErrorInvalidValue;
-#define MEMFINE_NORM(T_, V_)                                                                   \
-  norm_fwd_kernel<T_, V_><<<grid, block, 0, s>>>((const T_*)X, (const T_*)R, (const T_*)w, eps, \
-                                                 h, (T_*)S, (T_*)Y, Q, QS)
+  if (rs.waves > 16) return hipErrorInvalidValue;
+#define MEMFINE_NORM(T_, V_) run_norm_fwd<T_, V_>(X, R, w, eps, T, h, rs.waves, S, Y, Q, QS, s)
   if (dtype == 0) {
     if (rs.V == 1) MEMFINE_NORM(bf16_t, 1);
     else MEMFINE_NORM(bf16_t, 2);  // (16384 elements are 16 waves of two vectors)
@@ -317,12 +329,9 @@ hipError_t launch_norm_bwd(int dtype, const void* X, const void* w, const void* 
 hipError_t launch_mx8_unpack(int dtype, const uint8_t* Q, const uint8_t* QS, int64_t n, void* out,
                              hipStream_t s) {
   if (n == 0) return hipSuccess;
-  const int64_t blocks = (n / (dtype == 0 ? 8 : 4) + 255) / 256;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  if (dtype == 0)
-    mx8_unpack_kernel<bf16_t><<<(unsigned)blocks, 256, 0, s>>>(Q, QS, n, (bf16_t*)out);
-  else
-    mx8_unpack_kernel<float><<<(unsigned)blocks, 256, 0, s>>>(Q, QS, n, (float*)out);
+  const dim3 grid = grid_of(n / (dtype == 0 ? 8 : 4));
+  if (dtype == 0) mx8_unpack_kernel<bf16_t><<<grid, 256, 0, s>>>(Q, QS, n, (bf16_t*)out);
+  else mx8_unpack_kernel<float><<<grid, 256, 0, s>>>(Q, QS, n, (float*)out);
   return hipGetLastError();
 }
 

@@ -23,6 +23,7 @@
 // looks its value up among the owning lane's values.  Searching the id and
 // clearing it in every round took 71 us instead of 51.  The backward is bound by
 // memory (100003 tokens of 160: 128 MB in 33 us).
+#include <algorithm>
 #include <cfloat>
 
 #include "common.h"
@@ -467,37 +468,50 @@ __global__ __launch_bounds__(256) void logit_rows_kernel(const float* __restrict
   Vec4<T>::store(D + el, f);
 }
 
+// Tokens of a launch, 16 lanes each.
+constexpr int64_t kMostTokens = kMostItems / 16;
+
 }  // namespace
 
 hipError_t launch_route_fwd(const float* logits, const float* bias, int64_t T, RouteArgs a,
                             int32_t* idx, float* gates, hipStream_t s) {
   if (T == 0) return hipSuccess;
-  const int64_t blocks = (T + kTokens - 1) / kTokens;
-  if (a.E > 256 || a.k > 16 || a.groups > 16 || blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (a.E > 256 || a.k > 16 || a.groups > 16) return hipErrorInvalidValue;
   a.v = (a.E + 15) / 16;
   a.lane_groups = a.E % 16 == 0 && 16 % a.groups == 0;
   a.group_shift = a.lane_groups ? __builtin_ctz(16 / a.groups) : 0;
-  const unsigned g = (unsigned)blocks;
-#define MEMFINE_ROUTE(V_, H_) route_fwd_kernel<V_, H_><<<g, 256, 0, s>>>(logits, bias, T, a, idx, gates)
-  if (a.v <= 4) MEMFINE_ROUTE(4, 4);
-  else if (a.v <= 8) MEMFINE_ROUTE(8, 8);
-  else if (a.k <= 8) MEMFINE_ROUTE(16, 8);
-  else MEMFINE_ROUTE(16, 16);
+  for (int64_t t0 = 0; t0 < T; t0 += kMostTokens) {
+    const int64_t n = std::min(kMostTokens, T - t0);
+    const unsigned g = (unsigned)((n + kTokens - 1) / kTokens);
+    const float* z = logits + t0 * a.E;
+    int32_t* id = idx + t0 * a.k;
+    float* out = gates + t0 * a.k;
+#define MEMFINE_ROUTE(V_, H_) route_fwd_kernel<V_, H_><<<g, 256, 0, s>>>(z, bias, n, a, id, out)
+    if (a.v <= 4) MEMFINE_ROUTE(4, 4);
+    else if (a.v <= 8) MEMFINE_ROUTE(8, 8);
+    else if (a.k <= 8) MEMFINE_ROUTE(16, 8);
+    else MEMFINE_ROUTE(16, 16);
 #undef MEMFINE_ROUTE
+  }
   return hipGetLastError();
 }
 
 hipError_t launch_route_bwd(const float* logits, const int32_t* idx, const float* dgates, int64_t T,
                             RouteArgs a, float* dlogits, hipStream_t s) {
   if (T == 0) return hipSuccess;
-  const int64_t blocks = (T + kTokens - 1) / kTokens;
-  if (a.E > 256 || a.k > 16 || blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (a.E > 256 || a.k > 16) return hipErrorInvalidValue;
   a.v = (a.E + 15) / 16;
-  const unsigned g = (unsigned)blocks;
   const size_t lds = (size_t)kTokens * a.E * 4;
-  if (a.v <= 4) route_bwd_kernel<4><<<g, 256, lds, s>>>(logits, idx, dgates, T, a, dlogits);
-  else if (a.v <= 8) route_bwd_kernel<8><<<g, 256, lds, s>>>(logits, idx, dgates, T, a, dlogits);
-  else route_bwd_kernel<16><<<g, 256, lds, s>>>(logits, idx, dgates, T, a, dlogits);
+  for (int64_t t0 = 0; t0 < T; t0 += kMostTokens) {
+    const int64_t n = std::min(kMostTokens, T - t0);
+    const unsigned g = (unsigned)((n + kTokens - 1) / kTokens);
+    const float *z = logits + t0 * a.E, *d = dgates + t0 * a.k;
+    const int32_t* id = idx + t0 * a.k;
+    float* out = dlogits + t0 * a.E;
+    if (a.v <= 4) route_bwd_kernel<4><<<g, 256, lds, s>>>(z, id, d, n, a, out);
+    else if (a.v <= 8) route_bwd_kernel<8><<<g, 256, lds, s>>>(z, id, d, n, a, out);
+    else route_bwd_kernel<16><<<g, 256, lds, s>>>(z, id, d, n, a, out);
+  }
   return hipGetLastError();
 }
 
