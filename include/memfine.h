@@ -566,7 +566,8 @@ int64_t memfine_linear_mxw_workspace_bytes(int64_t T, int32_t N, int32_t K, int3
  *        [T, h / 32]; the SwiGLU output is then rounded to MX8 as well, and the
  *        second product's rows, before the gates, to bf16 in chunks of more
  *        than 4096 rows (else they stay fp32).
- * Everything else as memfine_moe_fwd.  memfine_moe_mxw_workspace_bytes: the
+ * Everything else as memfine_moe_fwd, but at most 2^31 - 257 slots a chunk
+ * (MEMFINE_ERR_UNSUPPORTED beyond).  memfine_moe_mxw_workspace_bytes: the
  * working memory of the chunk that needs the most (mx8 = 1: with d_XS).
  */
 int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* d_X,

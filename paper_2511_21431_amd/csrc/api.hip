@@ -1482,6 +1482,8 @@ int check_mx4(int64_t E, int32_t N, int32_t K) {
 // layer: they are written and read once, half the bytes (65536 rows of 7168:
 // 2.96 -> 2.66 ms for the call).
 constexpr int64_t kMxWideRows = 4096;
+// Rows of a chunk: the kernels count to the end of a row block of up to 128 in ints.
+constexpr int64_t kMxMostRows = INT32_MAX - 256;
 struct MxLayout {
   Layout tables;
   int64_t o_a, o_as, o_y, total;
@@ -1771,6 +1773,7 @@ int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chun
   if (shape->T == 0) return 0;
   // chunks of two sizes, of which the smaller may need more (FC2's partial rows)
   const int64_t n = max_chunk_tokens(shape->T, chunks) * shape->k;
+  if (n > kMxMostRows) return MEMFINE_ERR_UNSUPPORTED;
   const int64_t m = shape->T / std::min<int64_t>(chunks, shape->T) * shape->k;
   return std::max(mx_layout(*shape, n, mx8 != 0).total, mx_layout(*shape, m, mx8 != 0).total);
 }
@@ -1790,6 +1793,7 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
       !d_Y || !aligned16({d_X, d_W1_codes, d_W1_scales, d_W2_codes, d_W2_scales, d_Y}))
     return MEMFINE_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
+  if (max_chunk_tokens(S.T, chunks) * S.k > kMxMostRows) return MEMFINE_ERR_UNSUPPORTED;
   const int64_t C = std::min<int64_t>(chunks, S.T);
   const bool mx8 = d_XS != nullptr;
   const double hF = (double)S.h * S.F, xb = mx8 ? 1.03125 : 2.0;

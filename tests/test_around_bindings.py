@@ -74,3 +74,17 @@ def test_linear_working_memory():
     for bad in ((-1, 64, 64), (1, 8, 64), (1, 64, 48), (2**31, 64, 64)):
         with pytest.raises(mf.MemfineError):
             f(*bad)
+
+
+def test_experts_rows_of_a_chunk():
+    """2^31 - 256 slots in one chunk: row blocks would end past an int."""
+    import ctypes
+    T, k, P = 2**23 - 1, 256, ctypes.c_void_p(4096)
+    shape = mf.make_shape(T, 64, 64, 1024, k, mf.BF16)
+    f, b = mf.lib().memfine_moe_fwd_mxw, mf.lib().memfine_moe_mxw_workspace_bytes
+    args = [P, None, P, P, P, P, P, P, P]
+    for xs in (None, P):
+        args[1] = xs
+        assert f(ctypes.byref(shape), 1, *args, None, None) == -2
+        assert b(ctypes.byref(shape), 1, int(xs is not None)) == -2
+        assert b(ctypes.byref(shape), 2, int(xs is not None)) > 0
