@@ -27,11 +27,11 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // One row per workgroup; V vectors per lane, vector i of lane l of wave w at
-// column ((i W + w) 64 + l) VEC, W = blockDim.x / 64.
+// column ((i W + w) 64 + l) VEC, W = blockDim.x / 64.  S may be X or R.
 template <typename T, int V>
 __global__ __launch_bounds__(1024) void norm_fwd_kernel(
-    const T* __restrict__ X, const T* __restrict__ R, const T* __restrict__ w, float eps, int h,
-    T* __restrict__ S, T* __restrict__ Y, uint8_t* __restrict__ Q, uint8_t* __restrict__ QS) {
+    const T* X, const T* R, const T* __restrict__ w, float eps, int h, T* S, T* __restrict__ Y,
+    uint8_t* __restrict__ Q, uint8_t* __restrict__ QS) {
   constexpr int E = Elem<T>::kVec;
   __shared__ float part[16];
   const int nv = h / E, W = blockDim.x >> 6, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
@@ -102,12 +102,12 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(
 
 // Backward: workgroup b takes rows b, b + grid, ...; each lane keeps the sums
 // of dw of its own columns in registers over its rows and writes them as row b
-// of `part` [grid, h].
+// of `part` [grid, h].  dX may be dY or dS: a row is loaded before it is stored, and
+// the row loaded ahead belongs to this workgroup alone.
 template <typename T, int V, int kThreads>
 __global__ __launch_bounds__(kThreads) void norm_bwd_kernel(
-    const T* __restrict__ X, const T* __restrict__ w, const T* __restrict__ dY,
-    const T* __restrict__ dS, float eps, int64_t T_, int h, T* __restrict__ dX,
-    float* __restrict__ partial) {
+    const T* __restrict__ X, const T* __restrict__ w, const T* dY, const T* dS, float eps,
+    int64_t T_, int h, T* dX, float* __restrict__ partial) {
   constexpr int E = Elem<T>::kVec;
   __shared__ float part[2][2][16];
   const int nv = h / E, W = blockDim.x >> 6, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
