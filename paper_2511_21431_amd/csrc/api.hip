@@ -212,8 +212,10 @@ struct GraphBlock {
 };
 std::unordered_map<void*, GraphBlock> g_graph_ws;  // under g_ws_mu
 
-// Whether s is being captured, and the capture's id (unique in the process).
+// Whether s is being captured, and the capture's id (unique in the process).  The
+// null stream cannot be: its calls are spared the query (0.15 us).
 bool capturing(hipStream_t s, unsigned long long* id) {
+  if (s == nullptr) return false;
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
   if (hipStreamGetCaptureInfo(s, &st, id) != hipSuccess) {
     (void)hipGetLastError();
