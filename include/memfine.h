@@ -563,9 +563,10 @@ int64_t memfine_linear_mxw_workspace_bytes(int64_t T, int32_t N, int32_t K, int3
  * [2F, h] and [h, F]); shape.dtype must be MEMFINE_BF16 (Y's type).
  *   d_X  bf16 [T, h] when d_XS is null; the SwiGLU output is then rounded to
  *        bf16 for the second product.  With d_XS: MX8, e4m3 [T, h] and scales
- *        [T, h / 32]; the SwiGLU output is then rounded to MX8 as well, and the
- *        second product's rows, before the gates, to bf16 in chunks of more
- *        than 4096 rows (else they stay fp32).
+ *        [T, h / 32]; the SwiGLU output is then rounded to MX8 as well.
+ * The second product's rows stay fp32 up to Y, but on MX8 activations may, in
+ * chunks of more than 4096 rows, be rounded to fp16 times a power of two for each
+ * 64 columns: by 2^-12 of a value, or 2^-41 of the largest of its 64 columns.
  * Everything else as memfine_moe_fwd, but at most 2^31 - 257 slots a chunk
  * (MEMFINE_ERR_UNSUPPORTED beyond).  memfine_moe_mxw_workspace_bytes: the
  * working memory of the chunk that needs the most (mx8 = 1: with d_XS).

@@ -1478,18 +1478,17 @@ int check_mx4(int64_t E, int32_t N, int32_t K) {
 }
 
 // MX4 layer: one chunk's dispatch tables, its SwiGLU rows (bf16, or e4m3 and
-// their scales) and its output rows.  These are fp32 where they are few or
-// where the SwiGLU rows were already rounded to bf16 (Y would then have a third
-// error of that size); many rows on MX8 activations are bf16, as in the bf16
-// layer: they are written and read once, half the bytes (65536 rows of 7168:
-// 2.96 -> 2.66 ms for the call).
+// their scales) and its output rows.  These are fp32, but fp16 with an exponent
+// per 64 columns where there are many on MX8 activations, which are written and
+// read once (65536 rows of 7168: half of 1.9 GB); few stay in the caches, and on
+// bf16 activations the products take longer than their rows.
 constexpr int64_t kMxWideRows = 4096;
 // Rows of a chunk: the kernels count to the end of a row block of up to 128 in ints.
 constexpr int64_t kMxMostRows = INT32_MAX - 256;
 struct MxLayout {
   Layout tables;
-  int64_t o_a, o_as, o_y, total;
-  bool y_bf16;
+  int64_t o_a, o_as, o_y, o_ye, total;
+  bool y_half;
   int splits;  // FC2's partial results
 };
 // FC2 of n grouped rows, as far as its kernel's choice goes.
@@ -1508,15 +1507,15 @@ MxLayout mx_layout(const memfine_shape& s, int64_t n, bool mx8) {
   static const int32_t grouped = 0;
   MxLayout m;
   layout(s, n, -1, true, false, m.tables);
-  m.y_bf16 = mx8 && n > kMxWideRows;
   MxArgs g = mx_fc2_args(s, n, &grouped);
   g.XS = mx8 ? (const uint8_t*)&grouped : nullptr;
   m.splits = mx_splits(g);
-  if (m.splits > 1) m.y_bf16 = false;
+  m.y_half = mx8 && n > kMxWideRows && mx_tiled(g);
   m.o_a = m.tables.total;
   m.o_as = m.o_a + align256(n * s.F * (mx8 ? 1 : 2));
   m.o_y = m.o_as + align256(mx8 ? n * (s.F / 32) : 0);
-  m.total = m.o_y + align256(n * (int64_t)s.h * (m.y_bf16 ? 2 : 4) * m.splits);
+  m.o_ye = m.o_y + align256(n * (int64_t)s.h * (m.y_half ? 2 : 4) * m.splits);
+  m.total = m.o_ye + align256(m.y_half ? n * (s.h / 64) : 0);
   return m;
 }
 
@@ -1828,10 +1827,10 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
     g2.Wc = d_W2_codes;
     g2.Ws = d_W2_scales;
     g2.out = ws + L.o_y;
-    g2.out_bf16 = L.y_bf16;
+    g2.out_scale = L.y_half ? (uint8_t*)(ws + L.o_ye) : nullptr;
     // weights of the experts that can have rows
     const double nd = (double)n, wb = 0.53125 * hF * (double)std::min<int64_t>(S.E, n);
-    const double yb = L.y_bf16 ? 2.0 : 4.0 * L.splits;
+    const double yb = L.y_half ? 2.0 : 4.0 * L.splits;
     hipError_t err = hipSuccess;
     if (tokens == 1 && mx_one_token(g1, g2)) {
       // one token: no rows to group or combine
@@ -1866,8 +1865,8 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
       if (err == hipSuccess) {
         KernelTimer kt(MEMFINE_K_MX_COMBINE, s, 2.0 * nd * S.h,
                        yb * nd * S.h + 2.0 * tokens * S.h + 8.0 * nd);
-        err = L.y_bf16 ? launch_combine(MEMFINE_BF16, ws + L.o_y, cb.m.row_of_slot, d_gates, t0,
-                                        (int)tokens, S.h, S.k, d_Y, s)
+        err = L.y_half ? launch_mx_combine_half(ws + L.o_y, g2.out_scale, cb.m.row_of_slot, d_gates,
+                                                t0, tokens, S.h, S.k, d_Y, s)
                        : launch_mx_combine((const float*)(ws + L.o_y), L.splits, n * S.h,
                                            cb.m.row_of_slot, d_gates, t0, tokens, S.h, S.k, d_Y, s);
       }

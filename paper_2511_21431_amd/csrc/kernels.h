@@ -227,8 +227,9 @@ struct MxArgs {
   int n, E, N, K, KT;         // KT = ceil(K / 128)
   const int32_t* offsets;
   void* out;                  // FC1: [n, N / 2] as X's format; else [n, N]
-  uint8_t* out_scale;         // FC1 on MX8: [n, N / 64]
-  int out_bf16;               // [n, N]: bf16, else fp32
+  uint8_t* out_scale;         // FC1 on MX8: the scales [n, N / 64].  FC2 in tiles (mx_tiled):
+                              // the exponents [n, N / 64] of fp16 rows, or null
+  int out_bf16;               // [n, N]: bf16, else fp32 (or fp16, out_scale)
   int cus;                    // compute units of the device
   const int32_t* ids;         // one token: its slots' experts [n], or null
   const float* gates;         // one token: its slots' gates [n]
@@ -249,6 +250,8 @@ int mx_splits(const MxArgs& g);
 hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s);
 hipError_t launch_mx_sum(const float* part, int splits, int64_t n, int out_bf16, void* out,
                          hipStream_t s);
+// Whether launch_mx_rows multiplies by tiles, which also write fp16 rows.
+bool mx_tiled(const MxArgs& g);
 // One token's n slots without dispatch and combine: FC1 of every slot's
 // expert on the token's row into slot rows, and Y = sum of gate FC2 over them.
 // mx_one_token: whether both fit (else the calls above).
@@ -258,5 +261,9 @@ hipError_t launch_mx_one_fc2(const MxArgs& g, hipStream_t s);
 hipError_t launch_mx_combine(const float* y, int splits, int64_t stride, const int32_t* row_of_slot,
                              const float* gates, int64_t t0, int64_t tokens, int h, int k, void* Y,
                              hipStream_t s);
+
+hipError_t launch_mx_combine_half(const void* y, const uint8_t* ye, const int32_t* row_of_slot,
+                                  const float* gates, int64_t t0, int64_t tokens, int h, int k,
+                                  void* Y, hipStream_t s);
 
 }  // namespace memfine

@@ -177,7 +177,7 @@ __device__ __forceinline__ bool locate_tile(const MxArgs& g, int& cb, int& e, in
 }
 
 // ------------------------------------------------------------ the results
-enum { kFc1, kRows };  // SwiGLU rows in X's format; bf16 or fp32 rows (FC2, linear)
+enum { kFc1, kRows };  // SwiGLU rows in X's format; bf16, fp16 or fp32 rows (FC2, linear)
 
 // Lane group g (16 lanes) holds columns 4 g .. 4 g + 3 of two tiles, in x and y; after
 // this, columns 8 (g / 2) .. + 7 of tile g % 2, the first four of them in x.  Stores
@@ -235,6 +235,22 @@ __device__ __forceinline__ void store_row(const MxArgs& g, const f32x4_t& v, int
         (u32x2_t){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
   else
     *(f32x4_t*)((float*)g.out + row * g.N + n) = v;
+}
+
+// FC2's rows in two bytes a value: fp16 times a power of two for each 64 columns of
+// a row, held as the biased exponent e of their largest finite magnitude (15 at the
+// least): the stored values are those times 2^(141 - e), at most 2^15.  Rounding
+// takes up to 2^-12 of a value (2^-41 of the largest of its 64 where that is more),
+// bf16 2^-9, of which k in a sum show beside Y's own rounding: 8192 tokens, k 8, are
+// 2.4e-3 of the 2-norm off with bf16 rows, 1.7e-3 with these and with fp32 ones of
+// twice the bytes.
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+constexpr uint32_t kHalfLeast = 15;
+__device__ __forceinline__ float half_factor(uint32_t e) { return __uint_as_float((268u - e) << 23); }
+__device__ __forceinline__ float half_value(uint32_t e) { return __uint_as_float((e - 14u) << 23); }
+__device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
 }
 
 // -------------------------------------------------------------- few rows
@@ -836,24 +852,51 @@ __device__ __forceinline__ void mx_tile(const MxArgs& g, char* smem) {
     }
   } else {
     // through a buffer over the block's rows: an offset past it stores nothing
-    const int es = g.out_bf16 ? 2 : 4, n0 = (cb * 4 + w) * 64;
+    const int es = g.out_bf16 || g.out_scale ? 2 : 4, n0 = (cb * 4 + w) * 64;
     const auto ro = rsrc_of((char*)g.out + (int64_t)r0 * g.N * es, kPast);
+    const auto re = rsrc_of(g.out_scale + (int64_t)r0 * (g.N / 64), kPast);
+    // two tiles' columns of a row, 16 bytes a lane
+    auto store = [&](uint32_t off, bool live, int j, uint32_t x0, uint32_t x1, uint32_t y0,
+                     uint32_t y1) {
+      join_columns(x0, y0);
+      join_columns(x1, y1);
+      const int n = n0 + 16 * (j + (lg & 1)) + 8 * (lg >> 1);
+      __builtin_amdgcn_raw_buffer_store_b128((u32x4_t){x0, x1, y0, y1}, ro,
+                                             live && n < g.N ? off + n * 2 : kPast, 0, 0);
+    };
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int r = 16 * i + lr;
       const uint32_t off = (uint32_t)r * (uint32_t)(g.N * es);
       const bool live = r0 + r < r1;
-      if (g.out_bf16) {
+      if (g.out_scale) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t a = abs_bits(acc[i][j][q]);
+            m = umax(m, a < 0x7f800000u ? a : 0u);  // infinities and NaN stay what they are
+          }
+        m = umax(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+        m = umax(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+        const uint32_t e = umax(m >> 23, kHalfLeast);
+        const float f = half_factor(e);
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const f32x4_t v = acc[i][j] * f, u = acc[i][j + 1] * f;
+          store(off, live, j, pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3]), pack_f16x2(u[0], u[1]),
+                pack_f16x2(u[2], u[3]));
+        }
+        __builtin_amdgcn_raw_buffer_store_b8(
+            (uint8_t)e, re,
+            live && lg == 0 && n0 < g.N ? (uint32_t)r * (uint32_t)(g.N / 64) + n0 / 64 : kPast, 0, 0);
+      } else if (g.out_bf16) {
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
           const f32x4_t v = acc[i][j], u = acc[i][j + 1];
-          uint32_t x0 = pack_bf16x2(v[0], v[1]), x1 = pack_bf16x2(v[2], v[3]);
-          uint32_t y0 = pack_bf16x2(u[0], u[1]), y1 = pack_bf16x2(u[2], u[3]);
-          join_columns(x0, y0);
-          join_columns(x1, y1);
-          const int n = n0 + 16 * (j + (lg & 1)) + 8 * (lg >> 1);
-          __builtin_amdgcn_raw_buffer_store_b128((u32x4_t){x0, x1, y0, y1}, ro,
-                                                 live && n < g.N ? off + n * 2 : kPast, 0, 0);
+          store(off, live, j, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3]));
         }
       } else {
 #pragma unroll
@@ -909,6 +952,45 @@ __global__ __launch_bounds__(256) void mx_combine_kernel(const float* __restrict
     }
   }
   Vec4<bf16_t>::store(Y + (t0 + i) * h + c, f);
+}
+
+// The same from fp16 rows with their exponents [n, h / 64]: a thread takes eight
+// columns; the rows are read for the last time.
+__global__ __launch_bounds__(256) void mx_combine_half_kernel(
+    const uint16_t* __restrict__ y, const uint8_t* __restrict__ ye,
+    const int32_t* __restrict__ row_of_slot, const float* __restrict__ gates, int64_t t0, int64_t n,
+    int h, int k, bf16_t* __restrict__ Y) {
+  const int64_t gid = thread_id();
+  if (gid >= n) return;
+  const int vpr = h / 8;
+  const int64_t i = gid / vpr;
+  const int c = (int)(gid - i * vpr);
+  float f[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) f[q] = 0.f;
+  for (int j0 = 0; j0 < k; j0 += 8) {
+    int r[8];
+    u32x4_t v[8];
+    float e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = j0 + j < k ? row_of_slot[i * k + j0 + j] : -1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j0 + j < k) {
+        const int64_t row = max(r[j], 0);
+        v[j] = __builtin_nontemporal_load((const u32x4_t*)(y + row * h) + c);
+        e[j] = half_value(ye[row * (h / 64) + c / 8]);
+      }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (r[j] < 0) continue;
+      const float gj = gates[(t0 + i) * k + j0 + j];
+      const f16x8_t x = __builtin_bit_cast(f16x8_t, v[j]);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) f[q] = fmaf(gj, (float)x[q] * e[j], f[q]);
+    }
+  }
+  *(u32x4_t*)(Y + (t0 + i) * h + c * 8) = pack16(f, (bf16_t*)nullptr);
 }
 
 // out[i] = the sum of `splits` partial arrays of n floats (n a multiple of 16).
@@ -1225,6 +1307,7 @@ hipError_t launch_mx_rows(const MxArgs& g, hipStream_t s) {
   return hipSuccess;
 }
 
+bool mx_tiled(const MxArgs& g) { return kind_of(g, kRows) > kFewRows; }
 int mx_splits(const MxArgs& g) { return kind_of(g, kRows) == kFewRows ? splits_of(g) : 1; }
 hipError_t launch_mx_sum(const float* part, int splits, int64_t n, int out_bf16, void* out,
                          hipStream_t s) {
@@ -1253,6 +1336,16 @@ hipError_t launch_mx_combine(const float* y, int splits, int64_t stride, const i
   if (n == 0) return hipSuccess;
   mx_combine_kernel<<<grid_of(n), 256, 0, s>>>(y, splits, stride, row_of_slot, gates, t0, n, h, k,
                                                (bf16_t*)Y);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_combine_half(const void* y, const uint8_t* ye, const int32_t* row_of_slot,
+                                  const float* gates, int64_t t0, int64_t tokens, int h, int k,
+                                  void* Y, hipStream_t s) {
+  const int64_t n = tokens * (h / 8);
+  if (n == 0) return hipSuccess;
+  mx_combine_half_kernel<<<grid_of(n), 256, 0, s>>>((const uint16_t*)y, ye, row_of_slot, gates, t0, n,
+                                                    h, k, (bf16_t*)Y);
   return hipGetLastError();
 }
 
