@@ -971,9 +971,13 @@ __global__ __launch_bounds__(256) void mx_combine_half_kernel(
   for (int j0 = 0; j0 < k; j0 += 8) {
     int r[8];
     u32x4_t v[8];
-    float e[8];
+    float g[8], e[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r[j] = j0 + j < k ? row_of_slot[i * k + j0 + j] : -1;
+    for (int j = 0; j < 8; ++j) {
+      const bool in = j0 + j < k;
+      r[j] = in ? row_of_slot[i * k + j0 + j] : -1;
+      g[j] = in ? gates[(t0 + i) * k + j0 + j] : 0.f;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (j0 + j < k) {
@@ -984,10 +988,9 @@ __global__ __launch_bounds__(256) void mx_combine_half_kernel(
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (r[j] < 0) continue;
-      const float gj = gates[(t0 + i) * k + j0 + j];
       const f16x8_t x = __builtin_bit_cast(f16x8_t, v[j]);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) f[q] = fmaf(gj, (float)x[q] * e[j], f[q]);
+      for (int q = 0; q < 8; ++q) f[q] = fmaf(g[j], (float)x[q] * e[j], f[q]);
     }
   }
   *(u32x4_t*)(Y + (t0 + i) * h + c * 8) = pack16(f, (bf16_t*)nullptr);
