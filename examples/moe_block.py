@@ -49,7 +49,11 @@ class ServedBlock:
     def step(self, attended, stream, allocator=None):
         """attended [tokens, K]: the heads' outputs; stream [tokens, h]: the
         residual stream, to which the projection is added in place.  Returns the
-        experts' output, which the next block adds."""
+        experts' output, which the next block adds.  allocator: working memory of
+        the caller's, for steps captured into a graph (without one each capture
+        keeps memory of the library's until the process ends); it serves one
+        request at a time, memfine_moe_mxw_workspace_bytes or
+        memfine_linear_mxw_workspace_bytes, whichever is more."""
         mf.memfine_linear_mxw(self.h, self.K, attended, *self.Wo, self.o, allocator=allocator)
         mf.memfine_norm_fwd(EPS, self.o, self.w, R=stream, S=stream, Y=self.y, Q=self.q, QS=self.qs)
         mf.memfine_router_logits(self.shape, self.y, self.Wr, self.logits)

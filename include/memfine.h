@@ -410,20 +410,27 @@ int memfine_router_bwd(const memfine_shape* shape, const void* d_X, const void* 
  * Around the layer: the norm in front of it, routing from logits, and the
  * layer's forward with 4-bit weights.  Pointers must be 16-byte aligned
  * (MEMFINE_ERR_INVALID_ARG otherwise, as for a null pointer that is not
- * optional); T = 0 does nothing but what is said below.
+ * optional), but for the activations' scales d_XS and the row-major scales
+ * d_row_scales, which may lie anywhere, and the experts' d_idx and d_gates,
+ * aligned as their elements; T = 0 does nothing but what is said below.
  *
  * The MX formats hold blocks of 32 consecutive values of a row and one scale
  * byte s per block, 2^(s - 127): MX8 has e4m3 values (one byte each), MX4 has
  * e2m1 values (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; two to a byte,
  * the first in the low half).  The scale is the smallest power of two, at
  * least 2^-127, that keeps the block's largest magnitude within 448 (MX8) or 6
- * (MX4) times it; values are rounded to nearest, ties to even.  A block that
- * holds a NaN or an infinity gets s = 255, and all its values are NaN.
+ * (MX4) times it; values are rounded to nearest, ties to even.  (Not the
+ * conversion of the OCP specification, which takes the power of two below the
+ * largest magnitude, over 256 or 4, and lets what is then past the largest value
+ * saturate; matrices that were rounded so are packed as they are.)  A block that
+ * holds a NaN or an infinity gets s = 255, and all its values are NaN, in every
+ * product too.
  */
 
 /*
  * Residual addition and root-mean-square norm of T rows of h elements (h a
- * multiple of 64, at most 16384, else MEMFINE_ERR_UNSUPPORTED; T < 2^31):
+ * multiple of 64, else MEMFINE_ERR_INVALID_ARG; h <= 16384 and T < 2^31, else
+ * MEMFINE_ERR_UNSUPPORTED):
  *   S = X + R            rounded to dtype; without R (null) S is X
  *   Y = S / sqrt(mean(S^2) + eps) * w
  *   d_X, d_R  dtype [T, h];   d_w  dtype [h];   eps >= 0

@@ -641,7 +641,7 @@ __global__ __launch_bounds__(64 * W) void mx_one_kernel(MxArgs g) {
 // own, straight into registers one or two stages ahead.
 //
 // 128 rows on MX8 are bound by the matrix cores (65536 rows, 7168 x 4096: 1.48
-// ms, 2.6 PFLOP/s; K of 2048, 7168 columns: 0.87 ms, 2.2 PFLOP/s, as about 7 us
+// ms, 2.6 PFLOP/s; K of 2048, 7168 columns: 0.90 ms, 2.1 PFLOP/s, as about 7 us
 // a round of tiles go by before the first step and after the last), 64 rows on bf16 by the
 // same for short K (4108 rows, 2048 x 2816: 56 us) and reach 1.5 PFLOP/s for long
 // (8192 rows, 8192 x 8192).
@@ -1018,10 +1018,10 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* __restrict
                                                        uint8_t* __restrict__ scales) {
   const int64_t id = thread_id();
   if (id >= n) return;
-  const int lane = (int)(id & 63), NT = N / 16;
-  const int64_t tile = id >> 6;                 // over [E][NT][KT]
+  const int lane = (int)(id & 63);
+  const int64_t tile = id >> 6;                 // over [E][N / 16][KT]
   const int kt = (int)(tile % KT);
-  const int64_t rowt = tile / KT;               // over [E][NT]
+  const int64_t rowt = tile / KT;               // over [E][N / 16]
   const int64_t row = rowt * 16 + (lane & 15);  // over [E][N]
   const int k = kt * 128 + 32 * (lane >> 4);
   u32x4_t c = {0, 0, 0, 0};
@@ -1037,7 +1037,6 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(const uint8_t* __restrict
     const int KS = (KT + 3) / 4;
     *(uint32_t*)(scales + ((rowt * KS + kt / 4) * 64 + lane) * 4) = s;
   }
-  (void)NT;
 }
 
 // From values W [E, N, K]: a thread rounds one lane's blocks of four tiles.
@@ -1204,7 +1203,11 @@ enum Kind { kOneRow, kFewRows, kTiles32, kTiles64, kTiles128 };
 //   64-row against 32-row tiles, MX8: h 7168 F 2048 E 32, 16 rows 95 / 116, 128
 //     rows 194 / 224; h 4096 F 512 E 8, 128 rows (64 tiles of 64) 23 / 20; h 2048
 //     F 704 E 64, 12 rows 28 / 26, 384 rows 85 / 112.
-//   bf16: E 32, 64 rows 200 / 186, 256 rows 441 / 464.
+//   bf16, FC1 and FC2: h 7168 F 2048 E 32, 64 rows 155 / 156 and 95 / 88, 128 rows
+//     247 / 251 and 145 / 149, 192 rows 353 / 365 and 195 / 211, 256 rows 414 / 446 and
+//     246 / 266; h 2048 F 704 E 64, 64 rows 43 / 36 and 31 / 26, 192 rows 81 / 81 and
+//     61 / 63, 256 rows 96 / 102 and 76 / 80; h 2048 F 1408 E 16, 192 rows 44 / 44 and
+//     29 / 29, 257 rows 56 / 51 and 36 / 35, 400 rows 69 / 73 and 46 / 45.
 //   128-row against 64-row tiles, MX8: E 32, 2048 rows 1459 / 1544 (FC2 959 / 974),
 //     256 rows 285 / 275; h 2048 F 704 E 64, 384 rows 93 / 85.
 Kind kind_of(const MxArgs& g, int mode) {
@@ -1237,7 +1240,8 @@ template <bool MX8, int MODE> hipError_t run(const MxArgs& g, hipStream_t s) {
         return run_fc1_rows<MX8, 8>(g, s);
       } else {
         // 64 rows of MX8 activations fit in registers, 32 of bf16
-        if (MX8 && (g.offsets ? g.n > 8 * g.E : g.n > 32)) return run_cols<MX8, MX8 ? 4 : 2>(g, s);
+        if constexpr (MX8)
+          if (g.offsets ? g.n > 8 * g.E : g.n > 32) return run_cols<MX8, 4>(g, s);
         return run_cols<MX8, 2>(g, s);
       }
     case kTiles32: return run_tiles<MX8, MODE, 32, 3>(g, s);

@@ -6,9 +6,11 @@
 //   dX = r (dY w - x r^2 mean(dY w x)) + dS;   dw = sum over rows of dY x r
 //
 // All are bound by memory: each element is loaded once, kept in registers
-// across the row's reduction, and its results stored once.  A workgroup of W
-// waves owns a row at a time; lane-consecutive 16-byte vectors; sums in fp32.
-// bf16: 32768 rows of 7168 with R, S, Y and MX8 367 us (2.12 GB, 5.8 TB/s), its
+// across the row's reduction, and its results stored once (but the gradient of rows
+// past 8192 elements, whose workgroups of up to 1024 threads have 128 registers a
+// lane, keeps 44 bytes a lane in scratch memory in bf16 and 208 in fp32).  A workgroup
+// of W waves owns a row at a time; lane-consecutive 16-byte vectors; sums in fp32.
+// bf16: 32768 rows of 7168 with R, S, Y and MX8 365 us (2.12 GB, 5.8 TB/s), its
 // values read back 143 us; 16385 rows of 4096 backward 102 us (537 MB, 5.2 TB/s).
 #include <algorithm>
 
