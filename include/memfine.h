@@ -585,6 +585,139 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
                         const memfine_allocator* alloc, void* stream);
 int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chunks, int32_t mx8);
 
+/* ------------------------------------------------------------------------
+ * Attention in front of the layer.  A row holds heads of `dim` elements, one
+ * after the other; rows of queries, keys, values, their gradients and of what
+ * memfine_rope reads and writes lie ld elements apart (ld_* >= their heads times
+ * dim, a multiple of 16 bytes, at most 2^20, UNSUPPORTED beyond), so that
+ * they may be columns of one projection's output; O and dO are contiguous.
+ * Head j uses key-value head j / (heads / kv_heads).
+ *
+ * Packed sequences: sequence b is rows [d_offsets[b], d_offsets[b + 1]) of T,
+ * d_offsets int32 [seqs + 1] on the device, ascending, within [0, T] (what lies
+ * outside is neither read nor written, whatever the offsets hold); a sequence may be
+ * empty, and rows of none are left as they were.
+ *
+ * Pointers as above (16 bytes), but d_offsets, d_table, d_lengths, d_lse and
+ * d_delta's like, aligned as their elements.  dim is 64 or 128, heads at most 1024
+ * (MEMFINE_ERR_UNSUPPORTED otherwise).
+ */
+typedef struct memfine_attn {
+  int32_t heads, kv_heads;   /* heads a multiple of kv_heads                    */
+  int32_t dim;
+  int32_t dtype;             /* MEMFINE_BF16 or MEMFINE_F32                     */
+  int32_t causal;            /* 1: token i sees j <= i                          */
+  int32_t window;            /* w > 0 (causal only): and j > i - w; 0: no limit */
+  float scale;               /* of the products; finite, > 0                    */
+} memfine_attn;
+
+/*
+ * Attention over packed sequences.  Per head, over the tokens j that token i sees:
+ *   s_ij = scale q_i . k_j;  lse_i = log sum_j exp(s_ij);
+ *   O_i = sum_j exp(s_ij - lse_i) v_j
+ *   d_Q  dtype [T, heads, dim];  d_K, d_V  dtype [T, kv_heads, dim]
+ *   d_O  dtype [T, heads, dim] out;  d_lse  float [heads, T] out, may be null
+ * Products and sums in fp32; in bf16 the weights exp(.) are rounded to bf16 for
+ * the product with V (their sum is not), as the ds of the gradient for theirs.
+ * A NaN or an infinity in a row reaches any token of its sequence.
+ */
+int memfine_attn_fwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
+                     const void* d_Q, int64_t ld_q, const void* d_K, int64_t ld_k, const void* d_V,
+                     int64_t ld_v, void* d_O, float* d_lse, void* stream);
+
+/*
+ * Its gradient, from the forward's O and lse and from dO:
+ *   delta_i = dO_i . O_i;  p_ij = exp(s_ij - lse_i)
+ *   ds_ij = scale p_ij (dO_i . v_j - delta_i)
+ *   dQ_i = sum_j ds_ij k_j;  dK_j = sum_i ds_ij q_i;  dV_j = sum_i p_ij dO_i
+ * dK and dV add up over the heads that share a key-value head.  dQ, dK and dV are
+ * overwritten, rows of no sequence left as they were; they must not overlap the
+ * inputs.  Every sum has a fixed order.  Working memory (delta,
+ * memfine_attn_bwd_workspace_bytes; < 0: invalid arguments) comes from `alloc` as
+ * for the layer's calls.
+ */
+int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
+                     const void* d_Q, int64_t ld_q, const void* d_K, int64_t ld_k, const void* d_V,
+                     int64_t ld_v, const void* d_O, const float* d_lse, const void* d_dO,
+                     void* d_dQ, int64_t ld_dq, void* d_dK, int64_t ld_dk, void* d_dV,
+                     int64_t ld_dv, const memfine_allocator* alloc, void* stream);
+int64_t memfine_attn_bwd_workspace_bytes(int64_t T, const memfine_attn* a);
+
+/*
+ * Rotation by position, of rows of packed sequences (position: the row's place in
+ * its sequence), for the pairs (a, b) = (i, i + dim / 2) of every head, or with
+ * interleaved = 1 (2 i, 2 i + 1), 0 <= i < dim / 2, c and s their cosine and sine:
+ *   y_a = x_a c - x_b s;  y_b = x_b c + x_a s     (inverse = 1: -s, the gradient)
+ *   d_cos, d_sin  float [positions, dim / 2]; rows past the tables become NaN
+ *   d_X, d_Y  dtype [T, heads, dim], Y may be X (with X's ld)
+ */
+typedef struct memfine_rotary {
+  const float *d_cos, *d_sin;
+  int64_t positions;
+  int32_t interleaved;       /* 0 or 1                                          */
+} memfine_rotary;
+int memfine_rope(int64_t T, int32_t seqs, const int32_t* d_offsets, int32_t heads, int32_t dim,
+                 int32_t dtype, const memfine_rotary* r, int32_t inverse, const void* d_X,
+                 int64_t ld_x, void* d_Y, int64_t ld_y, void* stream);
+
+/*
+ * Keys and values of served sequences, in pages of `page` tokens (a power of two, 16 to
+ * 65536):
+ *   d_k, d_v    bf16 [pages, kv_heads, page, dim] when d_ks and d_vs are null, else
+ *               MX8: e4m3 bytes and scales d_ks, d_vs uint8 [pages, kv_heads,
+ *               page, dim / 32]
+ * Token t of sequence b is token t % page of page d_table[b][t / page], d_table
+ * int32 [seqs, width] on the device (width page <= 2^30), d_lengths int32 [seqs] the tokens
+ * that each sequence has (cut to [0, width page]).  Entries of the table past a sequence's
+ * last page are not used.  An entry outside [0, pages) stands for no page: nothing
+ * is written to it, and its tokens are left out of the attention.
+ */
+typedef struct memfine_cache {
+  int32_t kv_heads, dim;     /* dim 64 or 128                                   */
+  int32_t page;
+  int64_t pages;             /* 1 .. 2^31 - 1                                   */
+  void *d_k, *d_v;
+  uint8_t *d_ks, *d_vs;
+} memfine_cache;
+
+/*
+ * New tokens into the cache: d_lengths counts them already, row i of the n that
+ * sequence b brings is its token d_lengths[b] - n + i (a negative one is dropped).
+ *   d_offsets  the sequences' rows, packed as above, or null: T = seqs, row b is
+ *              sequence b's
+ *   d_K, d_V   bf16 [T, kv_heads, dim];  K is turned on its way if r is not null,
+ *              by the token's position, V is not; MX8 holds the unrounded K
+ *   d_Q        bf16 [T, heads, dim] or null (heads = 0); turned likewise into
+ *   d_R        bf16 [T, heads, dim], which may be d_Q when that is contiguous.
+ *              Rows that are dropped are left as they were.
+ * No page may be a sequence's twice, or that of two sequences that write to it.
+ */
+int memfine_kv_write(const memfine_cache* c, int64_t T, int32_t seqs, int32_t width,
+                     const int32_t* d_table, const int32_t* d_lengths, const int32_t* d_offsets,
+                     const memfine_rotary* r, const void* d_K, int64_t ld_k, const void* d_V,
+                     int64_t ld_v, int32_t heads, const void* d_Q, int64_t ld_q, void* d_R,
+                     void* stream);
+
+/*
+ * Attention of one token a sequence over its cached tokens (its own among them;
+ * with a->window, the last `window`): O_b and lse_b as memfine_attn_fwd's for the
+ * last token of sequence b.  A sequence without tokens gets zeros (lse -inf).
+ *   a      kv_heads and dim as the cache's, dtype MEMFINE_BF16; causal is not used
+ *   d_Q    bf16 [seqs, heads, dim];  d_O  bf16 [seqs, heads, dim] out
+ *   d_lse  float [seqs, heads] out, may be null
+ * What pages hold past a sequence's tokens does not matter.  Sums are formed in an order
+ * that depends on all lengths, the sizes and the device's compute units alone.
+ * Working memory (the parts of sequences that several workgroups share,
+ * memfine_attn_decode_workspace_bytes; < 0: invalid arguments) comes from `alloc` as
+ * for the layer's calls.
+ */
+int memfine_attn_decode(const memfine_attn* a, const memfine_cache* c, int32_t seqs, int32_t width,
+                        const int32_t* d_table, const int32_t* d_lengths, const void* d_Q,
+                        int64_t ld_q, void* d_O, float* d_lse, const memfine_allocator* alloc,
+                        void* stream);
+int64_t memfine_attn_decode_workspace_bytes(const memfine_attn* a, const memfine_cache* c,
+                                            int32_t seqs, int32_t width);
+
 /* Static, human-readable text for a status code. */
 const char* memfine_status_str(int status);
 
@@ -620,7 +753,12 @@ const char* memfine_status_str(int status);
 #define MEMFINE_K_MX_FC1     21 /* MX4: FC1 + SwiGLU                        */
 #define MEMFINE_K_MX_FC2     22
 #define MEMFINE_K_MX_COMBINE 23
-#define MEMFINE_K_NUM        24
+#define MEMFINE_K_ATTN_FWD   24 /* attention: flops are counted as 0 (they depend */
+#define MEMFINE_K_ATTN_BWD   25 /* on lengths that the host does not see)        */
+#define MEMFINE_K_ATTN_DECODE 26
+#define MEMFINE_K_ROPE       27
+#define MEMFINE_K_KV_WRITE   28
+#define MEMFINE_K_NUM        29
 
 typedef struct memfine_kernel_stat {
   int64_t launches;

@@ -26,7 +26,8 @@ PASS_FWD, PASS_BWD = 0, 1
 KERNELS = ["count", "dispatch", "fc1", "fc2", "combine", "fc1_recompute", "fc2_dgrad",
            "fc2_wgrad", "fc1_wgrad", "fc1_dgrad", "unpermute", "fc1_dgrad_wgrad",
            "router_fwd", "router_bwd_dx", "router_wgrad", "router_reduce", "norm_fwd", "norm_bwd",
-           "route_fwd", "route_bwd", "mx_linear", "mx_fc1", "mx_fc2", "mx_combine"]
+           "route_fwd", "route_bwd", "mx_linear", "mx_fc1", "mx_fc2", "mx_combine", "attn_fwd",
+           "attn_bwd", "attn_decode", "rope", "kv_write"]
 
 
 class MemfineError(RuntimeError):
@@ -90,6 +91,27 @@ class Gating(ctypes.Structure):
                 ("renorm", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+class Attn(ctypes.Structure):
+    """memfine_attn: heads, types and masks of an attention."""
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class Rotary(ctypes.Structure):
+    """memfine_rotary: tables of cosines and sines."""
+    _fields_ = [("d_cos", ctypes.c_void_p), ("d_sin", ctypes.c_void_p),
+                ("positions", ctypes.c_int64), ("interleaved", ctypes.c_int32)]
+
+
+class Cache(ctypes.Structure):
+    """memfine_cache: pages of keys and values.  Made by make_cache, which keeps their
+    tensors alive with it."""
+    _fields_ = [("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("pages", ctypes.c_int64), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+                ("d_ks", ctypes.c_void_p), ("d_vs", ctypes.c_void_p)]
+
+
 class KernelStat(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_int64), ("total_ms", ctypes.c_double),
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
@@ -102,6 +124,10 @@ I64P = ctypes.POINTER(ctypes.c_int64)
 SHP = ctypes.POINTER(Shape)
 ALP = ctypes.POINTER(Allocator)
 GTP = ctypes.POINTER(Gating)
+ATP = ctypes.POINTER(Attn)
+RTP = ctypes.POINTER(Rotary)
+CHP = ctypes.POINTER(Cache)
+I32, I64 = ctypes.c_int32, ctypes.c_int64
 
 _SIGS = {
     "memfine_count": (ctypes.c_int, [SHP, P, P, I64P, P]),
@@ -156,6 +182,15 @@ _SIGS = {
                                                             ctypes.c_int32, ctypes.c_int32]),
     "memfine_moe_fwd_mxw": (ctypes.c_int, [SHP, ctypes.c_int32, P, P, P, P, P, P, P, P, P, ALP, P]),
     "memfine_moe_mxw_workspace_bytes": (ctypes.c_int64, [SHP, ctypes.c_int32, ctypes.c_int32]),
+    "memfine_attn_fwd": (ctypes.c_int, [I64, I32, ATP, P, P, I64, P, I64, P, I64, P, P, P]),
+    "memfine_attn_bwd": (ctypes.c_int, [I64, I32, ATP, P, P, I64, P, I64, P, I64, P, P, P, P, I64,
+                                        P, I64, P, I64, ALP, P]),
+    "memfine_attn_bwd_workspace_bytes": (I64, [I64, ATP]),
+    "memfine_rope": (ctypes.c_int, [I64, I32, P, I32, I32, I32, RTP, I32, P, I64, P, I64, P]),
+    "memfine_kv_write": (ctypes.c_int, [CHP, I64, I32, I32, P, P, P, RTP, P, I64, P, I64, I32, P,
+                                        I64, P, P]),
+    "memfine_attn_decode": (ctypes.c_int, [ATP, CHP, I32, I32, P, P, P, I64, P, P, ALP, P]),
+    "memfine_attn_decode_workspace_bytes": (I64, [ATP, CHP, I32, I32]),
     "memfine_status_str": (ctypes.c_char_p, [ctypes.c_int]),
     "memfine_profile_begin": (ctypes.c_int, [ctypes.c_uint32]),
     "memfine_profile_end": (ctypes.c_int, [ctypes.POINTER(KernelStat)]),
@@ -772,6 +807,215 @@ def memfine_moe_mxw_workspace_bytes(shape: Shape, chunks: int, mx8: bool = False
     v = lib().memfine_moe_mxw_workspace_bytes(ctypes.byref(shape), int(chunks), int(bool(mx8)))
     if v < 0:
         raise MemfineError(int(v), "memfine_moe_mxw_workspace_bytes")
+    return int(v)
+
+
+# -------------------------------------------------------------- attention
+def make_attn(heads: int, kv_heads: int, dim: int, causal: bool = True, window: int = 0,
+              scale: Optional[float] = None, dtype: int = BF16) -> Attn:
+    """memfine_attn; scale None: dim ** -0.5."""
+    return Attn(int(heads), int(kv_heads), int(dim), int(dtype), bool(causal), int(window),
+                int(dim) ** -0.5 if scale is None else float(scale))
+
+
+def make_cache(k, v, k_scales=None, v_scales=None) -> Cache:
+    """memfine_cache of tensors [pages, kv_heads, page, dim]: bfloat16, or (MX8) uint8
+    with scales uint8 [pages, kv_heads, page, dim / 32]."""
+    torch = _torch()
+    if k is None or k.dim() != 4:
+        raise ValueError("k: expected [pages, kv_heads, page, dim]")
+    shape = tuple(k.shape)
+    dt = torch.bfloat16 if k_scales is None and v_scales is None else torch.uint8
+    held = shape[:3] + (shape[3] // 32,)
+    c = Cache(shape[1], shape[3], shape[2], shape[0], _ptr(k, shape, dt, "k"),
+              _ptr(v, shape, dt, "v"), None, None)
+    if dt == torch.uint8:
+        c.d_ks = _ptr(k_scales, held, dt, "k_scales")
+        c.d_vs = _ptr(v_scales, held, dt, "v_scales")
+    c.tensors = (k, v, k_scales, v_scales)
+    c.device = k.device
+    return c
+
+
+def _head_rows(t, T, heads, dim, dtype, name):
+    """(address, elements between rows) of rows [T, heads, dim], whose heads are
+    contiguous."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.shape != (T, heads, dim):
+        raise ValueError(f"{name}: shape {tuple(t.shape)} != expected {(T, heads, dim)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype} != expected {dtype}")
+    ld, head, one = t.stride()
+    if one != 1 or (head != dim and heads != 1):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    if not t.is_cuda:
+        if t.numel() == 0:
+            return 0, heads * dim
+        raise ValueError(f"{name} must be a device tensor")
+    return t.data_ptr(), (ld if T > 1 else heads * dim)
+
+
+def _same_device(first, stream, *others):
+    """All tensors on one device, which the call's stream belongs to: without one, the
+    current device."""
+    d = first.device
+    for t in others:
+        if t is not None and t.device != d:
+            raise ValueError(f"tensors on {d} and {t.device}")
+    if stream is None and d.type == "cuda" and d.index != _torch().cuda.current_device():
+        raise ValueError(f"tensors on {d}, which is not the current device")
+
+
+def _attn_dt(attn: Attn):
+    torch = _torch()
+    return torch.bfloat16 if attn.dtype == BF16 else torch.float32
+
+
+def _seqs(offsets):
+    if offsets is None:
+        raise ValueError("offsets is required")
+    if offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("offsets: expected [sequences + 1]")
+    return offsets.shape[0] - 1
+
+
+def memfine_attn_fwd(attn: Attn, offsets, Q, K, V, O, lse=None, stream=None) -> None:
+    """Attention over packed sequences: Q [T, heads, dim], K and V [T, kv_heads, dim]
+    (views whose rows lie apart will do), offsets int32 [sequences + 1]; into O
+    [T, heads, dim] and lse float [heads, T]."""
+    torch = _torch()
+    seqs, dt = _seqs(offsets), _attn_dt(attn)
+    H, Hk, D = attn.heads, attn.kv_heads, attn.dim
+    T = Q.shape[0] if Q is not None else 0
+    q, ldq = _head_rows(Q, T, H, D, dt, "Q")
+    k, ldk = _head_rows(K, T, Hk, D, dt, "K")
+    v, ldv = _head_rows(V, T, Hk, D, dt, "V")
+    o, s = _ptr(O, (T, H, D), dt, "O"), _opt(lse, (H, T), torch.float32, "lse")
+    _same_device(Q, stream, K, V, O, lse, offsets)
+    rc = lib().memfine_attn_fwd(
+        T, seqs, ctypes.byref(attn), _ptr(offsets, (seqs + 1,), torch.int32, "offsets"), q, ldq, k,
+        ldk, v, ldv, o, s, _stream(stream))
+    _check(rc, "memfine_attn_fwd")
+
+
+def memfine_attn_bwd(attn: Attn, offsets, Q, K, V, O, lse, dO, dQ, dK, dV, allocator=None,
+                     stream=None) -> None:
+    """Its gradient, from the forward's O and lse and dO [T, heads, dim]: dQ, dK and dV
+    as Q, K and V (views whose rows lie apart will do)."""
+    torch = _torch()
+    seqs, dt = _seqs(offsets), _attn_dt(attn)
+    H, Hk, D = attn.heads, attn.kv_heads, attn.dim
+    T = Q.shape[0] if Q is not None else 0
+    q, ldq = _head_rows(Q, T, H, D, dt, "Q")
+    k, ldk = _head_rows(K, T, Hk, D, dt, "K")
+    v, ldv = _head_rows(V, T, Hk, D, dt, "V")
+    dq, lddq = _head_rows(dQ, T, H, D, dt, "dQ")
+    dk, lddk = _head_rows(dK, T, Hk, D, dt, "dK")
+    dv, lddv = _head_rows(dV, T, Hk, D, dt, "dV")
+    o, s = _ptr(O, (T, H, D), dt, "O"), _ptr(lse, (H, T), torch.float32, "lse")
+    do = _ptr(dO, (T, H, D), dt, "dO")
+    _same_device(Q, stream, K, V, O, lse, dO, dQ, dK, dV, offsets)
+    rc = lib().memfine_attn_bwd(
+        T, seqs, ctypes.byref(attn), _ptr(offsets, (seqs + 1,), torch.int32, "offsets"), q, ldq, k,
+        ldk, v, ldv, o, s, do, dq, lddq, dk, lddk, dv, lddv, _alloc_arg(allocator), _stream(stream))
+    _check(rc, "memfine_attn_bwd")
+
+
+def memfine_attn_bwd_workspace_bytes(attn: Attn, T: int) -> int:
+    v = lib().memfine_attn_bwd_workspace_bytes(int(T), ctypes.byref(attn))
+    if v < 0:
+        raise MemfineError(int(v), "memfine_attn_bwd_workspace_bytes")
+    return int(v)
+
+
+def _rotary(cos, sin, dim, interleaved):
+    torch = _torch()
+    n, _ = _rows(cos, "cos")
+    return Rotary(_ptr(cos, (n, dim // 2), torch.float32, "cos"),
+                  _ptr(sin, (n, dim // 2), torch.float32, "sin"), n, bool(interleaved))
+
+
+def memfine_rope(offsets, cos, sin, X, Y, interleaved: bool = False, inverse: bool = False,
+                 stream=None) -> None:
+    """Turns the heads of packed rows X [T, heads, dim] by their positions into Y (which
+    may be X); cos and sin float [positions, dim / 2]; inverse: the gradient."""
+    torch = _torch()
+    seqs = _seqs(offsets)
+    if X is None or X.dim() != 3:
+        raise ValueError("X: expected [T, heads, dim]")
+    T, H, D = X.shape
+    r = _rotary(cos, sin, D, interleaved)
+    x, ldx = _head_rows(X, T, H, D, X.dtype, "X")
+    y, ldy = _head_rows(Y, T, H, D, X.dtype, "Y")
+    _same_device(X, stream, Y, cos, sin, offsets)
+    rc = lib().memfine_rope(
+        T, seqs, _ptr(offsets, (seqs + 1,), torch.int32, "offsets"), H, D, _dtype_of(X, "X"),
+        ctypes.byref(r), int(bool(inverse)), x, ldx, y, ldy, _stream(stream))
+    _check(rc, "memfine_rope")
+
+
+def _table(table, lengths):
+    """(sequences, width, addresses) of a table of pages and the sequences' lengths."""
+    torch = _torch()
+    n, width = _rows(table, "table")
+    return (n, width, _ptr(table, (n, width), torch.int32, "table"),
+            _ptr(lengths, (n,), torch.int32, "lengths"))
+
+
+def memfine_kv_write(cache: Cache, table, lengths, K, V, offsets=None, Q=None, R=None, cos=None,
+                     sin=None, interleaved: bool = False, stream=None) -> None:
+    """Rows K and V bfloat16 [T, kv_heads, dim] of new tokens into the cache, whose
+    lengths count them already; K, and Q [T, heads, dim] into R, turned by the
+    tokens' positions if cos and sin are given.  offsets None: one row a sequence."""
+    torch = _torch()
+    bf = torch.bfloat16
+    n, width, tp, lp = _table(table, lengths)
+    Hk, D = cache.kv_heads, cache.dim
+    T = K.shape[0] if K is not None else 0
+    k, ldk = _head_rows(K, T, Hk, D, bf, "K")
+    v, ldv = _head_rows(V, T, Hk, D, bf, "V")
+    if (Q is None) != (R is None):
+        raise ValueError("Q and R: both or neither")
+    H, q, ldq, rp = 0, None, 0, None
+    if Q is not None:
+        if Q.dim() != 3:
+            raise ValueError("Q: expected [T, heads, dim]")
+        H = Q.shape[1]
+        q, ldq = _head_rows(Q, T, H, D, bf, "Q")
+        rp = _ptr(R, (T, H, D), bf, "R")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin: both or neither")
+    r = None if cos is None else ctypes.byref(_rotary(cos, sin, D, interleaved))
+    op = None
+    if offsets is not None:
+        op = _ptr(offsets, (n + 1,), torch.int32, "offsets")
+    _same_device(K, stream, V, table, lengths, offsets, Q, R, cos, sin, cache)
+    rc = lib().memfine_kv_write(ctypes.byref(cache), T, n, width, tp, lp, op, r, k, ldk, v, ldv, H,
+                                q, ldq, rp, _stream(stream))
+    _check(rc, "memfine_kv_write")
+
+
+def memfine_attn_decode(attn: Attn, cache: Cache, table, lengths, Q, O, lse=None, allocator=None,
+                        stream=None) -> None:
+    """Attention of one token a sequence, Q bfloat16 [sequences, heads, dim], over the cached
+    tokens; into O alike and lse float [sequences, heads]."""
+    torch = _torch()
+    n, width, tp, lp = _table(table, lengths)
+    H, D = attn.heads, attn.dim
+    q, ldq = _head_rows(Q, n, H, D, torch.bfloat16, "Q")
+    o, s = _ptr(O, (n, H, D), torch.bfloat16, "O"), _opt(lse, (n, H), torch.float32, "lse")
+    _same_device(Q, stream, O, lse, table, lengths, cache)
+    rc = lib().memfine_attn_decode(ctypes.byref(attn), ctypes.byref(cache), n, width, tp, lp, q,
+                                   ldq, o, s, _alloc_arg(allocator), _stream(stream))
+    _check(rc, "memfine_attn_decode")
+
+
+def memfine_attn_decode_workspace_bytes(attn: Attn, cache: Cache, seqs: int, width: int) -> int:
+    v = lib().memfine_attn_decode_workspace_bytes(ctypes.byref(attn), ctypes.byref(cache),
+                                                  int(seqs), int(width))
+    if v < 0:
+        raise MemfineError(int(v), "memfine_attn_decode_workspace_bytes")
     return int(v)
 
 

@@ -19,7 +19,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmemfine.so")
 
 SOURCES = ["api.hip", "permute.hip", "combine.hip", "grouped_gemm.hip", "mact.hip", "router.hip",
-           "norm.hip", "route.hip", "mx.hip"]
+           "norm.hip", "route.hip", "mx.hip", "attn.hip", "decode.hip", "cache.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

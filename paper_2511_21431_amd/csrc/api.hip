@@ -1877,6 +1877,311 @@ int memfine_moe_fwd_mxw(const memfine_shape* shape, int32_t chunks, const void* 
   return MEMFINE_OK;
 }
 
+namespace {
+// ------------------------------------------------------------- attention
+bool aligned4(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if ((uintptr_t)p & 3) return false;
+  return true;
+}
+constexpr int64_t kMostLd = 1 << 20;   // (64 rows of floats below 2^31 bytes)
+constexpr int32_t kMostSeqs = 1 << 20;
+
+int check_heads(int32_t heads, int32_t dim) {
+  if (heads < 1 || dim < 1) return MEMFINE_ERR_INVALID_ARG;
+  return heads > 1024 || (dim != 64 && dim != 128) ? MEMFINE_ERR_UNSUPPORTED : MEMFINE_OK;
+}
+int check_attn(const memfine_attn* a) {
+  if (!a || a->kv_heads < 1 || a->heads < 1 || a->heads % a->kv_heads ||
+      (a->causal != 0 && a->causal != 1) || a->window < 0 || (a->window > 0 && !a->causal) ||
+      !(a->scale > 0.f) || !std::isfinite(a->scale))
+    return MEMFINE_ERR_INVALID_ARG;
+  if (!known_dtype(a->dtype)) return MEMFINE_ERR_UNSUPPORTED;
+  return check_heads(a->heads, a->dim);
+}
+// Rows of `width` elements, ld apart.
+int check_ld(std::initializer_list<int64_t> lds, int64_t width, int32_t dtype) {
+  for (int64_t ld : lds) {
+    if (ld < width || ld % (dtype == MEMFINE_BF16 ? 8 : 4)) return MEMFINE_ERR_INVALID_ARG;
+    if (ld > kMostLd) return MEMFINE_ERR_UNSUPPORTED;
+  }
+  return MEMFINE_OK;
+}
+int check_rows(int64_t T, int32_t seqs) {
+  if (T < 0 || seqs < 0) return MEMFINE_ERR_INVALID_ARG;
+  return T > INT32_MAX || seqs > kMostSeqs ? MEMFINE_ERR_UNSUPPORTED : MEMFINE_OK;
+}
+int check_rotary(const memfine_rotary* r) {
+  if (!r->d_cos || !r->d_sin || !aligned16({r->d_cos, r->d_sin}) || r->positions < 1 ||
+      (r->interleaved != 0 && r->interleaved != 1))
+    return MEMFINE_ERR_INVALID_ARG;
+  return MEMFINE_OK;
+}
+RopeTable rope_table(const memfine_rotary& r, int32_t inverse) {
+  return {r.d_cos, r.d_sin, r.positions, r.interleaved, inverse};
+}
+int check_cache(const memfine_cache* c, int32_t seqs, int32_t width) {
+  if (!c || c->kv_heads < 1 || c->page < 16 || (c->page & (c->page - 1)) || c->pages < 1 ||
+      seqs < 0 || width < 1 || !c->d_k || !c->d_v || (!c->d_ks) != (!c->d_vs) ||
+      !aligned16({c->d_k, c->d_v, c->d_ks, c->d_vs}))
+    return MEMFINE_ERR_INVALID_ARG;
+  if (c->page > 65536 || c->pages > INT32_MAX || seqs > kMostSeqs ||
+      (int64_t)width * c->page > (1 << 30))
+    return MEMFINE_ERR_UNSUPPORTED;
+  return check_heads(c->kv_heads, c->dim);
+}
+int log2_of(int32_t v) { return __builtin_ctz((unsigned)v); }
+
+AttnArgs attn_args(int64_t T, int32_t seqs, const memfine_attn& a) {
+  AttnArgs g = {};
+  g.T = T;
+  g.seqs = seqs;
+  g.heads = a.heads;
+  g.kv_heads = a.kv_heads;
+  g.dim = a.dim;
+  g.f32 = a.dtype == MEMFINE_F32;
+  g.causal = a.causal;
+  g.window = a.window;
+  g.scale = a.scale;
+  return g;
+}
+int check_decode(const memfine_attn* a, const memfine_cache* c, int32_t seqs, int32_t width) {
+  int rc = check_attn(a);
+  if (rc) return rc;
+  rc = check_cache(c, seqs, width);
+  if (rc) return rc;
+  if (a->kv_heads != c->kv_heads || a->dim != c->dim) return MEMFINE_ERR_INVALID_ARG;
+  return a->dtype == MEMFINE_BF16 ? MEMFINE_OK : MEMFINE_ERR_UNSUPPORTED;
+}
+DecodeArgs decode_args(const memfine_attn& a, const memfine_cache& c, int32_t seqs, int32_t width) {
+  DecodeArgs g = {};
+  g.seqs = seqs;
+  g.heads = a.heads;
+  g.kv_heads = a.kv_heads;
+  g.dim = a.dim;
+  g.group = a.heads / a.kv_heads;
+  g.tiles = (g.group + 15) / 16;
+  g.pairs = g.tiles * g.kv_heads;
+  g.window = a.window;
+  g.scale = a.scale;
+  g.k = c.d_k;
+  g.v = c.d_v;
+  g.ks = c.d_ks;
+  g.vs = c.d_vs;
+  g.pages = (int)c.pages;
+  g.page = c.page;
+  g.page_shift = log2_of(c.page);
+  g.width = width;
+  g.most = width * c.page;
+  g.cus = device_cus();
+  g.groups = decode_groups(g);
+  return g;
+}
+}  // namespace
+
+int memfine_attn_fwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
+                     const void* d_Q, int64_t ld_q, const void* d_K, int64_t ld_k, const void* d_V,
+                     int64_t ld_v, void* d_O, float* d_lse, void* stream) {
+  int rc = check_attn(a);
+  if (rc || (rc = check_rows(T, seqs)) ||
+      (rc = check_ld({ld_q}, (int64_t)a->heads * a->dim, a->dtype)) ||
+      (rc = check_ld({ld_k, ld_v}, (int64_t)a->kv_heads * a->dim, a->dtype)))
+    return rc;
+  if (T == 0 || seqs == 0) return MEMFINE_OK;
+  if (!d_offsets || !d_Q || !d_K || !d_V || !d_O || !aligned16({d_Q, d_K, d_V, d_O}) ||
+      !aligned4({d_offsets, d_lse}))
+    return MEMFINE_ERR_INVALID_ARG;
+  AttnArgs g = attn_args(T, seqs, *a);
+  if (!attn_fits(g)) return MEMFINE_ERR_UNSUPPORTED;
+  g.offsets = d_offsets;
+  g.Q = d_Q;
+  g.K = d_K;
+  g.V = d_V;
+  g.ldq = ld_q;
+  g.ldk = ld_k;
+  g.ldv = ld_v;
+  g.out = d_O;
+  g.lse = d_lse;
+  hipStream_t s = (hipStream_t)stream;
+  const double rows = (double)T * a->dim * (g.f32 ? 4 : 2);
+  KernelTimer kt(MEMFINE_K_ATTN_FWD, s, 0.0,
+                 2.0 * rows * (a->heads + a->kv_heads) + (d_lse ? 4.0 * T * a->heads : 0.0));
+  return hip_status(launch_attn_fwd(g, s));
+}
+
+int64_t memfine_attn_bwd_workspace_bytes(int64_t T, const memfine_attn* a) {
+  if (check_attn(a) || check_rows(T, 1)) return MEMFINE_ERR_INVALID_ARG;
+  return T * a->heads * 4;
+}
+
+int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
+                     const void* d_Q, int64_t ld_q, const void* d_K, int64_t ld_k, const void* d_V,
+                     int64_t ld_v, const void* d_O, const float* d_lse, const void* d_dO,
+                     void* d_dQ, int64_t ld_dq, void* d_dK, int64_t ld_dk, void* d_dV,
+                     int64_t ld_dv, const memfine_allocator* alloc, void* stream) {
+  int rc = check_attn(a);
+  if (rc || (rc = check_rows(T, seqs)) ||
+      (rc = check_ld({ld_q, ld_dq}, (int64_t)a->heads * a->dim, a->dtype)) ||
+      (rc = check_ld({ld_k, ld_v, ld_dk, ld_dv}, (int64_t)a->kv_heads * a->dim, a->dtype)))
+    return rc;
+  if (T == 0 || seqs == 0) return MEMFINE_OK;
+  if (!d_offsets || !d_Q || !d_K || !d_V || !d_O || !d_lse || !d_dO || !d_dQ || !d_dK || !d_dV ||
+      !aligned16({d_Q, d_K, d_V, d_O, d_dO, d_dQ, d_dK, d_dV}) || !aligned4({d_offsets, d_lse}))
+    return MEMFINE_ERR_INVALID_ARG;
+  AttnArgs g = attn_args(T, seqs, *a);
+  if (!attn_fits(g)) return MEMFINE_ERR_UNSUPPORTED;
+  g.offsets = d_offsets;
+  g.Q = d_Q;
+  g.K = d_K;
+  g.V = d_V;
+  g.ldq = ld_q;
+  g.ldk = ld_k;
+  g.ldv = ld_v;
+  g.O = d_O;
+  g.lse = const_cast<float*>(d_lse);
+  g.dO = d_dO;
+  g.dQ = d_dQ;
+  g.dK = d_dK;
+  g.dV = d_dV;
+  g.lddq = ld_dq;
+  g.lddk = ld_dk;
+  g.lddv = ld_dv;
+  hipStream_t s = (hipStream_t)stream;
+  const size_t bytes = (size_t)(T * a->heads * 4);
+  g.delta = (float*)ws_alloc(alloc, bytes, s);
+  if (!g.delta) return MEMFINE_ERR_OOM;
+  const double rows = (double)T * a->dim * (g.f32 ? 4 : 2);
+  hipError_t err;
+  {
+    KernelTimer kt(MEMFINE_K_ATTN_BWD, s, 0.0,
+                   4.0 * rows * (a->heads + a->kv_heads) + 4.0 * T * a->heads);
+    err = launch_attn_bwd(g, s);
+  }
+  ws_release(alloc, g.delta, bytes, s);
+  return hip_status(err);
+}
+
+int memfine_rope(int64_t T, int32_t seqs, const int32_t* d_offsets, int32_t heads, int32_t dim,
+                 int32_t dtype, const memfine_rotary* r, int32_t inverse, const void* d_X,
+                 int64_t ld_x, void* d_Y, int64_t ld_y, void* stream) {
+  if (!r || (inverse != 0 && inverse != 1)) return MEMFINE_ERR_INVALID_ARG;
+  int rc = check_heads(heads, dim);
+  if (rc) return rc;
+  if (!known_dtype(dtype)) return MEMFINE_ERR_UNSUPPORTED;
+  if ((rc = check_rows(T, seqs)) || (rc = check_ld({ld_x, ld_y}, (int64_t)heads * dim, dtype)) ||
+      (rc = check_rotary(r)))
+    return rc;
+  if (T == 0 || seqs == 0) return MEMFINE_OK;
+  if (!d_offsets || !d_X || !d_Y || !aligned16({d_X, d_Y}) || !aligned4({d_offsets}) ||
+      (d_X == d_Y && ld_x != ld_y))
+    return MEMFINE_ERR_INVALID_ARG;
+  RopeArgs g = {};
+  g.r = rope_table(*r, inverse);
+  g.T = T;
+  g.seqs = seqs;
+  g.heads = heads;
+  g.dim = dim;
+  g.f32 = dtype == MEMFINE_F32;
+  g.offsets = d_offsets;
+  g.X = d_X;
+  g.Y = d_Y;
+  g.ldx = ld_x;
+  g.ldy = ld_y;
+  hipStream_t s = (hipStream_t)stream;
+  const double n = (double)T * heads * dim;
+  KernelTimer kt(MEMFINE_K_ROPE, s, 3.0 * n, 2.0 * n * (g.f32 ? 4 : 2));
+  return hip_status(launch_rope(g, device_cus(), s));
+}
+
+int memfine_kv_write(const memfine_cache* c, int64_t T, int32_t seqs, int32_t width,
+                     const int32_t* d_table, const int32_t* d_lengths, const int32_t* d_offsets,
+                     const memfine_rotary* r, const void* d_K, int64_t ld_k, const void* d_V,
+                     int64_t ld_v, int32_t heads, const void* d_Q, int64_t ld_q, void* d_R,
+                     void* stream) {
+  int rc = check_cache(c, seqs, width);
+  if (rc || (rc = check_rows(T, seqs)) || (r && (rc = check_rotary(r)))) return rc;
+  const int64_t kv = (int64_t)c->kv_heads * c->dim;
+  if ((rc = check_ld({ld_k, ld_v}, kv, MEMFINE_BF16))) return rc;
+  if (heads < 0 || (heads == 0) != (!d_Q) || (!d_Q) != (!d_R)) return MEMFINE_ERR_INVALID_ARG;
+  if (heads > 0 && ((rc = check_heads(heads, c->dim)) ||
+                    (rc = check_ld({ld_q}, (int64_t)heads * c->dim, MEMFINE_BF16))))
+    return rc;
+  if (!d_offsets && T != seqs) return MEMFINE_ERR_INVALID_ARG;
+  if (T == 0 || seqs == 0) return MEMFINE_OK;
+  if (!d_table || !d_lengths || !d_K || !d_V || !aligned16({d_K, d_V, d_Q, d_R}) ||
+      !aligned4({d_table, d_lengths, d_offsets}) ||
+      (d_Q && d_Q == d_R && ld_q != (int64_t)heads * c->dim))
+    return MEMFINE_ERR_INVALID_ARG;
+  WriteArgs g = {};
+  if (r) g.r = rope_table(*r, 0);
+  g.T = T;
+  g.seqs = seqs;
+  g.heads = heads;
+  g.kv_heads = c->kv_heads;
+  g.dim = c->dim;
+  g.offsets = d_offsets;
+  g.table = d_table;
+  g.lengths = d_lengths;
+  g.width = width;
+  g.most = (int64_t)width * c->page;
+  g.k = c->d_k;
+  g.v = c->d_v;
+  g.ks = c->d_ks;
+  g.vs = c->d_vs;
+  g.pages = (int)c->pages;
+  g.page = c->page;
+  g.page_shift = log2_of(c->page);
+  g.K = d_K;
+  g.V = d_V;
+  g.Q = d_Q;
+  g.ldk = ld_k;
+  g.ldv = ld_v;
+  g.ldq = ld_q;
+  g.R = d_R;
+  hipStream_t s = (hipStream_t)stream;
+  const double q = (double)T * heads * c->dim, n = (double)T * kv;
+  KernelTimer kt(MEMFINE_K_KV_WRITE, s, 3.0 * (q + n),
+                 4.0 * q + 2.0 * n * (2.0 + (c->d_ks ? 1.03125 : 2.0)));
+  return hip_status(launch_kv_write(g, device_cus(), s));
+}
+
+int64_t memfine_attn_decode_workspace_bytes(const memfine_attn* a, const memfine_cache* c,
+                                            int32_t seqs, int32_t width) {
+  if (check_decode(a, c, seqs, width)) return MEMFINE_ERR_INVALID_ARG;
+  return seqs == 0 ? 0 : decode_part_floats(decode_args(*a, *c, seqs, width)) * 4;
+}
+
+int memfine_attn_decode(const memfine_attn* a, const memfine_cache* c, int32_t seqs, int32_t width,
+                        const int32_t* d_table, const int32_t* d_lengths, const void* d_Q,
+                        int64_t ld_q, void* d_O, float* d_lse, const memfine_allocator* alloc,
+                        void* stream) {
+  int rc = check_decode(a, c, seqs, width);
+  if (rc || (rc = check_ld({ld_q}, (int64_t)a->heads * a->dim, MEMFINE_BF16))) return rc;
+  if (seqs == 0) return MEMFINE_OK;
+  if (!d_table || !d_lengths || !d_Q || !d_O || !aligned16({d_Q, d_O}) ||
+      !aligned4({d_table, d_lengths, d_lse}))
+    return MEMFINE_ERR_INVALID_ARG;
+  if ((int64_t)seqs * a->heads > kMostItems / 256) return MEMFINE_ERR_UNSUPPORTED;
+  DecodeArgs g = decode_args(*a, *c, seqs, width);
+  g.table = d_table;
+  g.lengths = d_lengths;
+  g.Q = d_Q;
+  g.ldq = ld_q;
+  g.O = d_O;
+  g.lse = d_lse;
+  hipStream_t s = (hipStream_t)stream;
+  const size_t bytes = (size_t)decode_part_floats(g) * 4;
+  g.parts = (float*)ws_alloc(alloc, bytes, s);
+  if (!g.parts) return MEMFINE_ERR_OOM;
+  hipError_t err;
+  {
+    KernelTimer kt(MEMFINE_K_ATTN_DECODE, s, 0.0, 4.0 * seqs * a->heads * a->dim);
+    err = launch_decode(g, s);
+  }
+  ws_release(alloc, g.parts, bytes, s);
+  return hip_status(err);
+}
+
 int memfine_profile_begin(uint32_t mask) {
   std::lock_guard<std::mutex> lk(g_prof_mu);
   for (auto& r : g_prof) {

@@ -1,0 +1,663 @@
+// Attention over packed sequences on gfx950, forward and backward.
+//
+//   s_ij = scale q_i . k_j over the tokens j that i sees (j <= i when causal; j >
+//   i - window where there is one);  lse_i = log sum_j exp(s_ij)
+//   p_ij = exp(s_ij - lse_i);   o_i = sum_j p_ij v_j
+//   delta_i = do_i . o_i;   ds_ij = scale p_ij (do_i . v_j - delta_i)
+//   dv_j = sum_i p_ij do_i;   dq_i = sum_j ds_ij k_j;   dk_j = sum_i ds_ij q_i
+//   (dk and dv over the queries of every head that shares the key-value head)
+//
+// All products run on the matrix cores in blocks of 32 x 32 (v_mfma_f32_32x32x16
+// _bf16, or _32x32x2_f32).  A wave owns 32 columns of the transposed scores and
+// forms them from rows of the other operand in LDS, as rows: the accumulator
+// then holds, in each lane, scores of one column alone, so that a row's maximum
+// and sum need one exchange between the wave's halves, and its registers are,
+// rounded, the operand of the second product as they stand: which of the 16
+// values of a reduction step a register holds is the accumulator's choice, and
+// the other operand, read from LDS with a transposing load, follows it.
+#include <algorithm>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace memfine {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The waits before a tile's barrier: this wave's copies have landed and its reads
+// of the other stage have returned.  (A bare s_barrier: __syncthreads() adds a fence.)
+__device__ __forceinline__ void stage_barrier() {
+  __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (0 << 8) | (0 << 14));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// The larger and the sum of a lane's value and that of the lane 32 apart.
+__device__ __forceinline__ float halves_max(float v) {
+  const u32x2_t r = __builtin_bit_cast(
+      u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  const u32x2_t r = __builtin_bit_cast(
+      u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// One reduction step of the 32 x 32 products: kStep values, of which each half of
+// the wave holds half, 16 bytes a lane.
+template <typename T> struct Mma;
+template <> struct Mma<bf16_t> {
+  static constexpr int kStep = 16;
+  typedef bf16x8_t Frag;
+  __device__ __forceinline__ static void mma(const Frag& a, const Frag& b, f32x16_t& c) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  // accumulators 8 j .. 8 j + 7, rounded: rows 16 j + 8 (i / 4) + 4 hh + i % 4 of the block
+  __device__ __forceinline__ static Frag of(const f32x16_t& c, int j) {
+    u32x4_t v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack_bf16x2(c[8 * j + 2 * i], c[8 * j + 2 * i + 1]);
+    return __builtin_bit_cast(Frag, v);
+  }
+};
+template <> struct Mma<float> {
+  static constexpr int kStep = 8;
+  typedef f32x4_t Frag;
+  __device__ __forceinline__ static void mma(const Frag& a, const Frag& b, f32x16_t& c) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[s], b[s], c, 0, 0, 0);
+  }
+  // accumulators 4 j .. 4 j + 3: rows 8 j + 4 hh + i of the block
+  __device__ __forceinline__ static Frag of(const f32x16_t& c, int j) {
+    return (Frag){c[4 * j], c[4 * j + 1], c[4 * j + 2], c[4 * j + 3]};
+  }
+};
+template <typename T> using Frag = typename Mma<T>::Frag;
+// Row of accumulator i of a block.
+__device__ __forceinline__ int acc_row(int i, int hh) { return 8 * (i >> 2) + 4 * hh + (i & 3); }
+
+__device__ __forceinline__ void zero(f32x16_t& c) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) c[i] = 0.f;
+}
+
+// ------------------------------------------------------------------- tiles
+// kRows rows of D elements in LDS.  16-byte unit u of a row sits at unit u ^
+// swizzle(row): 16 consecutive rows' reads of one unit, and the reads of four
+// (bf16) consecutive rows x 32 columns by a transposing load, or of 32 columns of rows 4
+// apart (fp32), then fall on distinct banks.
+template <typename T, int D> struct Tile {
+  static constexpr int ES = sizeof(T), kPitch = D * ES, kUnits = kPitch / 16;
+  static constexpr int kRows = ES == 2 ? 64 : 32, kBytes = kRows * kPitch;
+  static constexpr int kBlocks = kRows / 32;           // blocks of 32 rows
+  static constexpr int kSteps = D / Mma<T>::kStep;     // reduction steps along a row
+  static constexpr int kDown = 32 / Mma<T>::kStep;     // reduction steps down a block of rows
+  typedef typename Mma<T>::Frag F;
+
+  __device__ __forceinline__ static int swizzle(int row) {
+    if constexpr (ES == 4) return (row & 3) | (row & 4) << 1 | (row & 8) >> 1;
+    else if constexpr (kUnits == 16) return (row & 3) << 2 | ((row >> 2) & 3);
+    else return (row & 2) << 1 | ((row >> 2) & 3);
+  }
+  // operand rows row0 .. row0 + 31, step ks of D
+  __device__ __forceinline__ static F row(const char* __restrict__ lds, int row0, int ks, int lane) {
+    const int r = row0 + (lane & 31);
+    return *(const F*)(lds + r * kPitch + (((ks * 2 + (lane >> 5)) ^ swizzle(r)) << 4));
+  }
+  // the transposed operand: its 32 rows are columns col0 .. col0 + 31, reduced over
+  // step kk of the tile's rows, in the order in which Mma::of holds them
+  __device__ __forceinline__ static F col(const char* __restrict__ lds, int col0, int kk, int lane) {
+    if constexpr (ES == 2) {
+      // lane j of each 16 supplies 4 columns of row j / 4 and gets 4 rows of column j
+      const int j = lane & 15, G = lane >> 4;
+      const int u = (col0 + (G & 1) * 16 + 4 * (j & 3)) >> 3, in = (j & 1) << 3;
+      const int r = kk * 16 + (G >> 1) * 4 + (j >> 2);
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4*)(lds + r * kPitch + ((u ^ swizzle(r)) << 4) + in));
+      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4*)(lds + (r + 8) * kPitch + ((u ^ swizzle(r + 8)) << 4) + in));
+      return __builtin_bit_cast(F, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      F x;
+      const int b = (col0 + (lane & 31)) * 4;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int r = kk * 8 + (lane >> 5) * 4 + s;
+        x[s] = *(const float*)(lds + r * kPitch + (((b >> 4) ^ swizzle(r)) << 4) + (b & 15));
+      }
+      return x;
+    }
+  }
+};
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int32_t)bytes,
+                                           0x00020000);
+}
+// `rows` rows of D elements, ld elements apart, from base on; what lies past
+// them reads zero.  (The rows of one tile: below 2^31 bytes.)
+template <typename T, int D>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const T* base, int64_t ld, int rows) {
+  return rsrc_of(base, rows > 0 ? (uint32_t)((rows - 1) * ld + D) * (uint32_t)sizeof(T) : 0u);
+}
+
+// The copy of a tile into LDS by NW waves, straight from memory.
+template <typename T, int D, int NW> struct Copy {
+  typedef Tile<T, D> L;
+  static constexpr int kPer = 1024 / L::kPitch;               // rows an instruction
+  static constexpr int kCount = L::kBytes / 1024 / NW;        // instructions a wave
+  static_assert(kCount * NW * 1024 == L::kBytes, "a tile is split evenly over the waves");
+  uint32_t voff[kCount];
+  __device__ __forceinline__ void init(int64_t ld, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) {
+      const int r = (i * NW + wave) * kPer + lane / L::kUnits;
+      voff[i] = (uint32_t)(r * ld) * L::ES + (((lane % L::kUnits) ^ L::swizzle(r)) << 4);
+    }
+  }
+  // rows from base on, `rows` of them there
+  __device__ __forceinline__ void issue(const T* base, int64_t ld, int rows, char* lds, int wave) const {
+    const __amdgpu_buffer_rsrc_t rs = rows_rsrc<T, D>(base, ld, min(rows, L::kRows));
+#pragma unroll
+    for (int i = 0; i < kCount; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + (i * NW + wave) * 1024), 16,
+                                               voff[i], 0, 0, 0);
+  }
+};
+
+// A wave's 32 rows as an operand that stays in registers.
+template <typename T, int D, int N>
+__device__ __forceinline__ void load_rows(Frag<T> (&f)[N], const T* base, int64_t ld,
+                                          int rows, int lane) {
+  const __amdgpu_buffer_rsrc_t rs = rows_rsrc<T, D>(base, ld, rows);
+  const uint32_t at = (uint32_t)((lane & 31) * ld) * (uint32_t)sizeof(T) + (lane >> 5) * 16;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    f[k] = __builtin_bit_cast(Frag<T>, __builtin_amdgcn_raw_buffer_load_b128(rs, at + k * 32, 0, 0));
+}
+
+// Transposed accumulators of 32 rows (a lane: row lane % 32), as rows of out.
+template <typename T, int D>
+__device__ __forceinline__ void store_rows(const f32x16_t (&c)[D / 32], float scale, T* out, int64_t ld,
+                                           int rows, int lane) {
+  if ((lane & 31) >= rows) return;
+  T* p = out + (lane & 31) * ld + (lane >> 5) * 4;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float f[4] = {c[b][4 * g] * scale, c[b][4 * g + 1] * scale, c[b][4 * g + 2] * scale,
+                          c[b][4 * g + 3] * scale};
+      Vec4<T>::store(p + b * 32 + g * 8, f);
+    }
+}
+
+// ------------------------------------------------------------- work to do
+// Block b of rows of the packed sequences, each cut into blocks of R.
+struct Part {
+  int begin, n;  // the sequence's first row and its length
+  int block;     // of the sequence
+};
+// Every wave looks for itself: its lanes add up the blocks of a 64th of the
+// sequences each, and the search goes on in the one that holds block b.  (Offsets
+// are cut to [0, T], so that nothing outside is touched whatever they are.)
+__device__ __forceinline__ bool locate(const int32_t* __restrict__ offsets, int seqs, int T, int R, int b,
+                                       Part& p) {
+  const int lane = threadIdx.x & 63;
+  int s0 = 0, count = seqs;
+  for (;;) {
+    const int per = (count + 63) / 64;
+    const int first = s0 + lane * per, last = min(first + per, s0 + count);
+    int n = 0, lo = 0, hi = 0;
+    if (first < last) {
+      hi = min(max(offsets[first], 0), T);
+      for (int s = first; s < last; ++s) {
+        lo = hi;
+        hi = min(max(offsets[s + 1], 0), T);
+        n += hi > lo ? (hi - lo + R - 1) / R : 0;
+      }
+    }
+    int inc = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(inc, o, 64);
+      if (lane >= o) inc += y;
+    }
+    const uint64_t past = __ballot(inc > b);
+    if (past == 0) return false;
+    const int w = __builtin_ctzll(past);
+    b -= __builtin_amdgcn_readlane(inc - n, w);
+    if (per == 1) {
+      p.begin = __builtin_amdgcn_readlane(lo, w);
+      p.n = __builtin_amdgcn_readlane(hi, w) - p.begin;
+      p.block = b;
+      return true;
+    }
+    count = min(per, s0 + count - (s0 + w * per));
+    s0 += w * per;
+  }
+}
+// Head and block of a workgroup.  Workgroups go to the 8 XCDs in turn; with a
+// multiple of 8 heads each XCD takes an eighth of them one after the other, so
+// that its L2 holds the keys and values in use.  Else all heads advance
+// together.  Blocks come in falling order (`down`: causal, the longest first).
+__device__ __forceinline__ bool work_item(int blocks, int heads, bool down, int& head, int& b) {
+  const int id = blockIdx.x;
+  if (heads % 8 == 0) {
+    const int i = id >> 3;
+    head = (id & 7) * (heads >> 3) + i / blocks;
+    b = i % blocks;
+  } else {
+    head = id % heads;
+    b = id / heads;
+  }
+  if (down) b = blocks - 1 - b;
+  return true;
+}
+
+// Which scores of a lane's own token count.
+struct Seen {
+  int lo, hi;  // tokens lo .. hi of the sequence
+};
+__device__ __forceinline__ Seen keys_of(const AttnArgs& g, int i, int n) {
+  return {g.window > 0 ? i - g.window + 1 : 0, g.causal ? min(i, n - 1) : n - 1};
+}
+__device__ __forceinline__ Seen queries_of(const AttnArgs& g, int j, int n) {
+  return {g.causal ? j : 0, g.window > 0 ? min(n - 1, j + min(g.window, n) - 1) : n - 1};
+}
+// Whether a wave's 32 own tokens from i0 on see all `rows` other tokens from r0 on.
+__device__ __forceinline__ bool see_all(const Seen& first, const Seen& last, int r0, int rows) {
+  return r0 >= max(first.lo, last.lo) && r0 + rows - 1 <= min(first.hi, last.hi);
+}
+__device__ __forceinline__ void hide(f32x16_t& c, const Seen& s, int r0, int hh, float v) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int r = r0 + acc_row(i, hh);
+    if (r < s.lo || r > s.hi) c[i] = v;
+  }
+}
+
+// ----------------------------------------------------------------- forward
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * NW) void attn_fwd_kernel(const AttnArgs g, int blocks) {
+  typedef Tile<T, D> L;
+  typedef Mma<T> M;
+  constexpr int kBlock = 32 * NW;
+  __shared__ __align__(1024) char smem[4 * L::kBytes];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hh = lane >> 5;
+  int head, b;
+  Part p;
+  if (!work_item(blocks, g.heads, g.causal, head, b) ||
+      !locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p))
+    return;
+  const int kv = head / (g.heads / g.kv_heads);
+  const int q0 = p.block * kBlock, rows = min(kBlock, p.n - q0);
+  const int i0 = q0 + 32 * w, mine = min(32, p.n - i0);
+  const T* K = (const T*)g.K + p.begin * g.ldk + kv * D;
+  const T* V = (const T*)g.V + p.begin * g.ldv + kv * D;
+
+  // the tiles that the workgroup needs, and those that this wave does
+  const Seen wg_first = keys_of(g, q0, p.n), wg_last = keys_of(g, q0 + rows - 1, p.n);
+  const int t0 = max(wg_first.lo, 0) / L::kRows, t1 = wg_last.hi / L::kRows + 1;
+  const Seen first = keys_of(g, i0, p.n), last = keys_of(g, i0 + 31, p.n);
+  const Seen own = keys_of(g, i0 + (lane & 31), p.n);
+
+  Copy<T, D, NW> ck, cv;
+  ck.init(g.ldk, w, lane);
+  cv.init(g.ldv, w, lane);
+  auto issue = [&](int t) {
+    char* st = smem + (t & 1) * 2 * L::kBytes;
+    const int64_t r = (int64_t)t * L::kRows;
+    ck.issue(K + r * g.ldk, g.ldk, p.n - (int)r, st, w);
+    cv.issue(V + r * g.ldv, g.ldv, p.n - (int)r, st + L::kBytes, w);
+  };
+  issue(t0);
+  Frag<T> q[L::kSteps];
+  load_rows<T, D>(q, (const T*)g.Q + (p.begin + i0) * g.ldq + head * D, g.ldq, mine, lane);
+
+  const float c = g.scale * kLog2e;
+  f32x16_t o[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) zero(o[i]);
+  float m = -INFINITY, l = 0.f;  // (l: of this half's tokens)
+  for (int t = t0; t < t1; ++t) {
+    stage_barrier();
+    if (t + 1 < t1) issue(t + 1);
+    const int r0 = t * L::kRows;
+    if (mine <= 0 || r0 > last.hi || r0 + L::kRows <= first.lo) continue;
+    const char* ks = smem + (t & 1) * 2 * L::kBytes;
+    const char* vs = ks + L::kBytes;
+    f32x16_t s[L::kBlocks];
+#pragma unroll
+    for (int i = 0; i < L::kBlocks; ++i) zero(s[i]);
+#pragma unroll
+    for (int k = 0; k < L::kSteps; ++k)
+#pragma unroll
+      for (int i = 0; i < L::kBlocks; ++i) M::mma(L::row(ks, 32 * i, k, lane), q[k], s[i]);
+    if (!see_all(first, last, r0, L::kRows)) {
+#pragma unroll
+      for (int i = 0; i < L::kBlocks; ++i) hide(s[i], own, r0 + 32 * i, hh, -INFINITY);
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int i = 0; i < L::kBlocks; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
+    top = halves_max(top) * c;
+    // The sums are kept relative to 2^m, m a maximum seen so far: it moves, and they are
+    // multiplied, only where a row's maximum has passed it by more than 8 (weights of up to
+    // 2^8 are as exact).
+    if (__any(top > m + 8.f)) {
+      const float now = fmaxf(m, top);
+      const float f = now == -INFINITY ? 1.f : exp2_(m - now);
+      m = now;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;  // (a row that sees nothing yet)
+#pragma unroll
+    for (int i = 0; i < L::kBlocks; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[i][e] = exp2_(fmaf(s[i][e], c, -ref));
+        l += s[i][e];
+      }
+#pragma unroll
+    for (int i = 0; i < L::kBlocks; ++i)
+#pragma unroll
+      for (int j = 0; j < L::kDown; ++j) {
+        // the weights are rounded to the values' type, the matrix core's operand (their
+        // sum is not): half a step of bf16 each, which averages out over the row
+        const Frag<T> f = M::of(s[i], j);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, i * L::kDown + j, lane), f, o[d]);
+      }
+  }
+  if (mine <= 0) return;
+  l = halves_sum(l);
+  store_rows<T, D>(o, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l, (T*)g.out + ((p.begin + i0) * (int64_t)g.heads + head) * D,
+                   (int64_t)g.heads * D, mine, lane);
+  if (g.lse && lane < mine)
+    g.lse[head * g.T + p.begin + i0 + lane] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+}
+
+// ---------------------------------------------------------------- backward
+// dq of 32 NW rows a workgroup, and their delta for the kernel below.
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * NW) void attn_dq_kernel(const AttnArgs g, int blocks) {
+  typedef Tile<T, D> L;
+  typedef Mma<T> M;
+  constexpr int kBlock = 32 * NW;
+  __shared__ __align__(1024) char smem[4 * L::kBytes];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hh = lane >> 5;
+  int head, b;
+  Part p;
+  if (!work_item(blocks, g.heads, g.causal, head, b) ||
+      !locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p))
+    return;
+  const int kv = head / (g.heads / g.kv_heads);
+  const int q0 = p.block * kBlock, rows = min(kBlock, p.n - q0);
+  const int i0 = q0 + 32 * w, mine = min(32, p.n - i0);
+  const T* K = (const T*)g.K + p.begin * g.ldk + kv * D;
+  const T* V = (const T*)g.V + p.begin * g.ldv + kv * D;
+  const Seen wg_first = keys_of(g, q0, p.n), wg_last = keys_of(g, q0 + rows - 1, p.n);
+  const int t0 = max(wg_first.lo, 0) / L::kRows, t1 = wg_last.hi / L::kRows + 1;
+  const Seen first = keys_of(g, i0, p.n), last = keys_of(g, i0 + 31, p.n);
+  const Seen own = keys_of(g, i0 + (lane & 31), p.n);
+  Copy<T, D, NW> ck, cv;
+  ck.init(g.ldk, w, lane);
+  cv.init(g.ldv, w, lane);
+  auto issue = [&](int t) {
+    char* st = smem + (t & 1) * 2 * L::kBytes;
+    const int64_t r = (int64_t)t * L::kRows;
+    ck.issue(K + r * g.ldk, g.ldk, p.n - (int)r, st, w);
+    cv.issue(V + r * g.ldv, g.ldv, p.n - (int)r, st + L::kBytes, w);
+  };
+  issue(t0);
+  Frag<T> q[L::kSteps], d_o[L::kSteps];
+  const int64_t ldo = (int64_t)g.heads * D, at = ((p.begin + i0) * (int64_t)g.heads + head) * D;
+  load_rows<T, D>(q, (const T*)g.Q + (p.begin + i0) * g.ldq + head * D, g.ldq, mine, lane);
+  load_rows<T, D>(d_o, (const T*)g.dO + at, ldo, mine, lane);
+  float delta = 0.f;
+  {
+    Frag<T> f[L::kSteps];
+    load_rows<T, D>(f, (const T*)g.O + at, ldo, mine, lane);
+#pragma unroll
+    for (int k = 0; k < L::kSteps; ++k) {
+      float x[M::kStep / 2], y[M::kStep / 2];
+      unpack16(__builtin_bit_cast(u32x4_t, f[k]), x, (T*)nullptr);
+      unpack16(__builtin_bit_cast(u32x4_t, d_o[k]), y, (T*)nullptr);
+#pragma unroll
+      for (int e = 0; e < M::kStep / 2; ++e) delta = fmaf(x[e], y[e], delta);
+    }
+  }
+  delta = halves_sum(delta);
+  const int64_t row = head * g.T + p.begin + i0;
+  float lse = INFINITY;  // (rows past the sequence, and rows that see nothing: no weights)
+  if ((lane & 31) < mine) {
+    lse = g.lse[row + (lane & 31)];
+    if (lse == -INFINITY) lse = INFINITY;
+    if (hh == 0) g.delta[row + lane] = delta;
+  }
+  const float c = g.scale * kLog2e, ref = lse * kLog2e;
+  f32x16_t a[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) zero(a[i]);
+  for (int t = t0; t < t1; ++t) {
+    stage_barrier();
+    if (t + 1 < t1) issue(t + 1);
+    const int r0 = t * L::kRows;
+    if (mine <= 0 || r0 > last.hi || r0 + L::kRows <= first.lo) continue;
+    const char* ks = smem + (t & 1) * 2 * L::kBytes;
+    const char* vs = ks + L::kBytes;
+    const bool all = see_all(first, last, r0, L::kRows);
+#pragma unroll
+    for (int i = 0; i < L::kBlocks; ++i) {
+      f32x16_t s, dp;
+      zero(s);
+      zero(dp);
+#pragma unroll
+      for (int k = 0; k < L::kSteps; ++k) {
+        M::mma(L::row(ks, 32 * i, k, lane), q[k], s);
+        M::mma(L::row(vs, 32 * i, k, lane), d_o[k], dp);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = exp2_(fmaf(s[e], c, -ref)) * (dp[e] - delta);
+      if (!all) hide(s, own, r0 + 32 * i, hh, 0.f);
+#pragma unroll
+      for (int j = 0; j < L::kDown; ++j) {
+        const Frag<T> f = M::of(s, j);  // (rounded as the forward's weights)
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) M::mma(L::col(ks, 32 * d, i * L::kDown + j, lane), f, a[d]);
+      }
+    }
+  }
+  if (mine > 0)
+    store_rows<T, D>(a, g.scale, (T*)g.dQ + (p.begin + i0) * g.lddq + head * D, g.lddq, mine, lane);
+}
+
+// dk and dv of 32 NW rows a workgroup: it goes through the queries of all heads
+// that share them, head after head, so that every sum has one order.
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * NW) void attn_dkv_kernel(const AttnArgs g, int blocks) {
+  typedef Tile<T, D> L;
+  typedef Mma<T> M;
+  constexpr int kBlock = 32 * NW;
+  // two stages of queries, dO, and their lse and delta
+  constexpr int kStage = 2 * L::kBytes;
+  __shared__ __align__(1024) char smem[2 * kStage];
+  __shared__ __align__(16) float stats[2][2][L::kRows];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hh = lane >> 5;
+  int kv, b;
+  Part p;
+  if (!work_item(blocks, g.kv_heads, false, kv, b) ||
+      !locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p))
+    return;
+  const int group = g.heads / g.kv_heads;
+  const int k0 = p.block * kBlock, rows = min(kBlock, p.n - k0);
+  const int j0 = k0 + 32 * w, mine = min(32, p.n - j0);
+  const Seen wg_first = queries_of(g, k0, p.n), wg_last = queries_of(g, k0 + rows - 1, p.n);
+  const int t0 = wg_first.lo / L::kRows, tiles = wg_last.hi / L::kRows + 1 - t0;
+  const Seen first = queries_of(g, j0, p.n), last = queries_of(g, j0 + 31, p.n);
+  const Seen own = queries_of(g, j0 + (lane & 31), p.n);
+  const int64_t ldo = (int64_t)g.heads * D;
+  Copy<T, D, NW> cq, co;
+  cq.init(g.ldq, w, lane);
+  co.init(ldo, w, lane);
+  const int total = group * tiles;
+  auto issue = [&](int x, int stage) {
+    const int head = kv * group + x / tiles, r0 = (t0 + x % tiles) * L::kRows;
+    char* st = smem + stage * kStage;
+    cq.issue((const T*)g.Q + (p.begin + r0) * g.ldq + head * D, g.ldq, p.n - r0, st, w);
+    co.issue((const T*)g.dO + ((p.begin + r0) * (int64_t)g.heads + head) * D, ldo, p.n - r0,
+             st + L::kBytes, w);
+    if (threadIdx.x < 2 * L::kRows) {
+      const int r = threadIdx.x % L::kRows, which = threadIdx.x / L::kRows;
+      const int64_t at = head * g.T + p.begin + r0 + r;
+      float v = which ? 0.f : INFINITY;
+      if (r0 + r < p.n) {
+        v = (which ? g.delta : g.lse)[at];
+        if (!which) v = v == -INFINITY ? INFINITY : v * kLog2e;
+      }
+      stats[stage][which][r] = v;
+    }
+  };
+  issue(0, 0);
+  Frag<T> k[L::kSteps], v[L::kSteps];
+  load_rows<T, D>(k, (const T*)g.K + (p.begin + j0) * g.ldk + kv * D, g.ldk, mine, lane);
+  load_rows<T, D>(v, (const T*)g.V + (p.begin + j0) * g.ldv + kv * D, g.ldv, mine, lane);
+  const float c = g.scale * kLog2e;
+  f32x16_t dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    zero(dk[i]);
+    zero(dv[i]);
+  }
+  for (int x = 0; x < total; ++x) {
+    stage_barrier();
+    if (x + 1 < total) issue(x + 1, (x + 1) & 1);
+    const int r0 = (t0 + x % tiles) * L::kRows;
+    if (mine <= 0 || r0 + L::kRows <= first.lo || r0 > last.hi) continue;
+    const char* qs = smem + (x & 1) * kStage;
+    const char* os = qs + L::kBytes;
+    const bool all = see_all(first, last, r0, L::kRows);
+#pragma unroll
+    for (int i = 0; i < L::kBlocks; ++i) {
+      f32x16_t s, dp;
+      zero(s);
+      zero(dp);
+#pragma unroll
+      for (int e = 0; e < L::kSteps; ++e) {
+        M::mma(L::row(qs, 32 * i, e, lane), k[e], s);
+        M::mma(L::row(os, 32 * i, e, lane), v[e], dp);
+      }
+      const float* lse = &stats[x & 1][0][32 * i + 4 * hh];
+      const float* del = &stats[x & 1][1][32 * i + 4 * hh];
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const f32x4_t a = *(const f32x4_t*)(lse + 2 * e);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) s[e + y] = exp2_(fmaf(s[e + y], c, -a[y]));
+      }
+      if (!all) hide(s, own, r0 + 32 * i, hh, 0.f);
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const f32x4_t a = *(const f32x4_t*)(del + 2 * e);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) dp[e + y] = s[e + y] * (dp[e + y] - a[y]);
+      }
+#pragma unroll
+      for (int j = 0; j < L::kDown; ++j) {
+        const Frag<T> f = M::of(s, j), h = M::of(dp, j);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+          M::mma(L::col(os, 32 * d, i * L::kDown + j, lane), f, dv[d]);
+          M::mma(L::col(qs, 32 * d, i * L::kDown + j, lane), h, dk[d]);
+        }
+      }
+    }
+  }
+  if (mine <= 0) return;
+  store_rows<T, D>(dk, g.scale, (T*)g.dK + (p.begin + j0) * g.lddk + kv * D, g.lddk, mine, lane);
+  store_rows<T, D>(dv, 1.f, (T*)g.dV + (p.begin + j0) * g.lddv + kv * D, g.lddv, mine, lane);
+}
+
+// Blocks of R rows of seqs sequences that share T rows, at most.
+int64_t blocks_of(int64_t T, int64_t seqs, int R) {
+  const int64_t full = std::min(seqs, T);
+  return (T + full * (R - 1)) / R;
+}
+
+// Waves of a workgroup: eight in bf16, two a SIMD, so that one multiplies while the
+// other works on its scores; four in fp32, whose operands need the registers of two.
+constexpr int kWaves = 8, kWavesF32 = 4, kDkvWaves = 4;
+
+// (The compiler leaves out host stubs of kernels that only templates launch.)
+#define MEMFINE_ATTN(T, D, NW)                                                \
+  template __global__ void attn_fwd_kernel<T, D, NW>(const AttnArgs, int);    \
+  template __global__ void attn_dq_kernel<T, D, NW>(const AttnArgs, int);     \
+  template __global__ void attn_dkv_kernel<T, D, kDkvWaves>(const AttnArgs, int);
+MEMFINE_ATTN(bf16_t, 64, kWaves)
+MEMFINE_ATTN(bf16_t, 128, kWaves)
+MEMFINE_ATTN(float, 64, kWavesF32)
+MEMFINE_ATTN(float, 128, kWavesF32)
+#undef MEMFINE_ATTN
+
+template <typename T, int D, int NW> void run_fwd(const AttnArgs& g, hipStream_t s) {
+  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW);
+  attn_fwd_kernel<T, D, NW><<<(unsigned)blocks * g.heads, 64 * NW, 0, s>>>(g, blocks);
+}
+template <typename T, int D, int NW> void run_bwd(const AttnArgs& g, hipStream_t s) {
+  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW);
+  // (writes delta, which the next one reads)
+  attn_dq_kernel<T, D, NW><<<(unsigned)blocks * g.heads, 64 * NW, 0, s>>>(g, blocks);
+  const int kb = (int)blocks_of(g.T, g.seqs, 32 * kDkvWaves);
+  attn_dkv_kernel<T, D, kDkvWaves><<<(unsigned)kb * g.kv_heads, 64 * kDkvWaves, 0, s>>>(g, kb);
+}
+
+}  // namespace
+
+bool attn_fits(const AttnArgs& g) {
+  return blocks_of(g.T, g.seqs, 32 * kDkvWaves) * g.heads <= kMostItems / (64 * kWaves);
+}
+
+hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s) {
+  if (!attn_fits(g)) return hipErrorInvalidValue;
+  if (g.f32) {
+    if (g.dim == 64) run_fwd<float, 64, kWavesF32>(g, s);
+    else run_fwd<float, 128, kWavesF32>(g, s);
+  } else {
+    if (g.dim == 64) run_fwd<bf16_t, 64, kWaves>(g, s);
+    else run_fwd<bf16_t, 128, kWaves>(g, s);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_attn_bwd(const AttnArgs& g, hipStream_t s) {
+  if (!attn_fits(g)) return hipErrorInvalidValue;
+  if (g.f32) {
+    if (g.dim == 64) run_bwd<float, 64, kWavesF32>(g, s);
+    else run_bwd<float, 128, kWavesF32>(g, s);
+  } else {
+    if (g.dim == 64) run_bwd<bf16_t, 64, kWaves>(g, s);
+    else run_bwd<bf16_t, 128, kWaves>(g, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace memfine

@@ -1,0 +1,518 @@
+// Attention of one new token a sequence over a cache of pages, on gfx950.
+//
+//   s_j = scale q . k_j over the sequence's tokens j (the last `window` of them,
+//   where there is one);  o = sum_j exp(s_j - lse) v_j,  lse = log sum_j exp(s_j)
+//
+// Bound by memory: every key and value is read once.  The tokens of all sequences
+// and key-value heads are laid end to end in steps of 128, of which each
+// workgroup takes an equal run, whatever the lengths are; runs end inside
+// sequences, whose parts (sums relative to a maximum of their own) a second
+// kernel joins in order.  A step's four waves take 32 tokens each.
+//
+// Up to 16 heads that share a key-value head are the columns of 16 x 16 products
+// on the matrix cores (v_mfma_f32_16x16x32_bf16).  Keys go from memory into
+// registers as the operand; values through LDS, from where a transposing load
+// makes them one.  The scores' accumulators, rounded, are the second product's
+// other operand as they stand: value rows are read in the order that they have.
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "kernels.h"
+#include "mx.h"
+
+namespace memfine {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kTokens = 32;              // of a wave's step
+constexpr int kStep = 4 * kTokens;       // of a workgroup's
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The largest and the sum over the lanes l, l ^ 16, l ^ 32, l ^ 48.
+template <class F> __device__ __forceinline__ float over_quarters(float v, F f) {
+  u32x2_t r = __builtin_bit_cast(
+      u32x2_t, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+  v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_bit_cast(
+      u32x2_t, __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quarters_max(float v) {
+  return over_quarters(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float quarters_sum(float v) {
+  return over_quarters(v, [](float a, float b) { return a + b; });
+}
+
+// ------------------------------------------------------------- work to do
+// A sequence's tokens that count: [lo, n), lo0 = lo cut down to a block of 16.
+struct Span {
+  int lo, lo0, n;
+};
+__device__ __forceinline__ Span span_of(const DecodeArgs& g, int b) {
+  Span s;
+  s.n = min(max(g.lengths[b], 0), g.most);
+  s.lo = g.window > 0 ? max(0, s.n - g.window) : 0;
+  s.lo0 = s.lo & ~15;
+  return s;
+}
+__device__ __forceinline__ int steps_of(const Span& s) { return (s.n - s.lo0 + kStep - 1) / kStep; }
+
+// Sum over a workgroup's 256 threads in every one, and the sum over those before
+// this one.  Ends and begins with a barrier's worth of order on `part`.
+__device__ __forceinline__ int64_t scan256(int64_t v, int64_t* part, int64_t& before) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int64_t inc = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += y;
+  }
+  __syncthreads();
+  if (lane == 63) part[w] = inc;
+  __syncthreads();
+  int64_t total = 0, head = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i < w) head += part[i];
+    total += part[i];
+  }
+  before = head + inc - v;
+  return total;
+}
+
+// Steps of all sequences, and of those before each thread's share of them
+// (sequences t per .. t per + per - 1 for thread t).
+struct Plan {
+  int64_t before;   // steps of one key-value head before this thread's sequences
+  int64_t total;    // of all sequences
+  int per;
+};
+__device__ __forceinline__ Plan plan_of(const DecodeArgs& g, int64_t* part) {
+  Plan p;
+  p.per = (g.seqs + 255) / 256;
+  int64_t v = 0;
+  const int first = threadIdx.x * p.per, last = min(first + p.per, g.seqs);
+  for (int b = first; b < last; ++b) v += steps_of(span_of(g, b));
+  p.total = scan256(v, part, p.before);
+  return p;
+}
+// Steps a workgroup takes.
+__device__ __forceinline__ int64_t share_of(const DecodeArgs& g, int64_t total) {
+  const int64_t all = total * g.pairs;
+  return std::max<int64_t>((all + g.groups - 1) / g.groups, 1);
+}
+
+// --------------------------------------------------------------- operands
+// D elements of 32 tokens, in two blocks of 16 that each lie in one page.  A
+// lane of quarter g reads token t % 16 of a block for keys.  The reduction over a
+// row goes in steps of 32 elements, of which a lane holds 8; in MX8 a 16-byte
+// load holds two steps' 8.
+template <int D, bool MX8> struct Held;
+template <int D> struct Held<D, false> {
+  static constexpr int kLoads = D / 32;  // 16-byte loads a lane and block
+  // first element of a lane's part of load i
+  __device__ __forceinline__ static int at(int i, int g) { return i * 32 + g * 8; }
+};
+template <int D> struct Held<D, true> {
+  static constexpr int kLoads = D / 64;
+  __device__ __forceinline__ static int at(int i, int g) { return i * 64 + g * 16; }
+};
+
+// Eight e4m3 values with their scale, exactly.
+__device__ __forceinline__ bf16x8_t bf16_of(uint32_t a, uint32_t b, float scale) {
+  const bf16x2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
+  const bf16x2_t p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+  const bf16x2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
+  const bf16x2_t p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+  return (bf16x8_t){p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+}
+// The conversion reads the scale's exponent field alone: byte 0 is 2^-127, 255 NaN.
+__device__ __forceinline__ float cvt_scale(uint32_t s) { return __uint_as_float(s << 23); }
+
+// Values of a wave's step in LDS: 32 rows of D bf16; 16-byte unit u of a row at u ^
+// swizzle(row), so that a transposing load's 16 rows x 16 columns spread over the banks.
+template <int D> struct Values {
+  static constexpr int kPitch = 2 * D, kBytes = kTokens * kPitch;
+  __device__ __forceinline__ static int swizzle(int row) {
+    if constexpr (D == 128) return (row & 7) << 1;
+    else return (row & 6);
+  }
+  __device__ __forceinline__ static int at(int row, int unit) {
+    return row * kPitch + ((unit ^ swizzle(row)) << 4);
+  }
+  // columns col0 .. col0 + 15 as an operand's rows: lane quarter g has tokens 4 g ..
+  // 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3, as the scores' accumulators
+  __device__ __forceinline__ static bf16x8_t col(const char* lds, int col0, int lane) {
+    const int j = lane & 15, r = (lane >> 4) * 4 + (j >> 2);
+    const int u = (col0 + 4 * (j & 3)) >> 3, in = (j & 1) << 3;
+    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + at(r, u) + in));
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + at(r + 16, u) + in));
+    return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// What a wave has in flight: keys and values of one step.
+template <int D, bool MX8> struct Loaded {
+  static constexpr int kK = 2 * Held<D, MX8>::kLoads;
+  u32x4_t k[kK], v[kK];
+  uint32_t ks[MX8 ? 2 : 1], vs[MX8 ? kK : 1];
+};
+
+// Sums of a (pair of a sequence and) key-value head's part: o relative to 2^m.
+template <int D> struct Sums {
+  f32x4_t o[D / 16];  // o^T: columns 16 i + 4 g + e of the query lane % 16
+  float m, l;         // (l: of this lane quarter's tokens)
+};
+
+template <int D, bool MX8>
+__global__ __launch_bounds__(256, 2) void decode_kernel(const DecodeArgs g) {
+  typedef Held<D, MX8> H;
+  typedef Values<D> LV;
+  constexpr int kRowBytes = MX8 ? D : 2 * D, kLoads = H::kLoads;
+  __shared__ __align__(1024) char smem[4 * LV::kBytes > 4 * 16 * (D + 4) * 4 ? 4 * LV::kBytes
+                                                                             : 4 * 16 * (D + 4) * 4];
+  __shared__ int64_t part[4];
+  __shared__ int64_t found[3];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lg = lane >> 4, col = lane & 15;
+  const Plan plan = plan_of(g, part);
+  const int64_t share = share_of(g, plan.total), end = std::min(plan.total * g.pairs, (blockIdx.x + 1) * share);
+  int64_t at = blockIdx.x * share;
+  if (at >= end) return;
+  // the sequence that holds step `at`: all pairs of a sequence follow each other
+  {
+    int64_t before = plan.before;
+    const int first = threadIdx.x * plan.per, last = min(first + plan.per, g.seqs);
+    for (int b = first; b < last; ++b) {
+      const int64_t n = steps_of(span_of(g, b));
+      if (at >= before * g.pairs && at < (before + n) * g.pairs) {
+        found[0] = b;
+        found[1] = before * g.pairs;
+      }
+      before += n;
+    }
+    __syncthreads();
+  }
+  int b = __builtin_amdgcn_readfirstlane((int)found[0]);
+  int64_t base = found[1];
+  const float c = g.scale * kLog2e;
+  char* mine = smem + w * LV::kBytes;
+  bool first_run = true;
+  for (; at < end; ++b) {
+    if (b >= g.seqs) return;  // (not reached)
+    const Span sp = span_of(g, b);
+    const int n = steps_of(sp);
+    if (n == 0) continue;
+    const int32_t* table = g.table + (int64_t)b * g.width;
+    const int64_t stop = std::min(end, base + (int64_t)n * g.pairs);
+    while (at < stop) {
+      const int pair = (int)((at - base) / n), x0 = (int)((at - base) % n);
+      const int x1 = (int)std::min<int64_t>(n, x0 + (stop - at));
+      const int kv = pair / g.tiles, h0 = kv * g.group + pair % g.tiles * 16;
+      const int heads = min(16, g.group - pair % g.tiles * 16);
+      // queries: columns; the reduction's order is that of the keys' loads
+      bf16x8_t q[D / 32];
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const bf16_t* p = (const bf16_t*)g.Q + b * g.ldq + (h0 + (col < heads ? col : 0)) * D + H::at(i, lg);
+        if constexpr (MX8) {
+          q[2 * i] = *(const bf16x8_t*)p;
+          q[2 * i + 1] = *(const bf16x8_t*)(p + 8);
+        } else {
+          q[i] = *(const bf16x8_t*)p;
+        }
+      }
+      Sums<D> a;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) a.o[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      a.m = -INFINITY;
+      a.l = 0.f;
+
+      // page of block j (16 tokens, from sp.lo0 on) of this wave's run, by lanes: two blocks a step
+      const int t_first = sp.lo0 + x0 * kStep + w * kTokens;
+      auto pages = [&](int step) {  // lane l: block l % 2 of step + l / 2
+        const int t = t_first + (step + (lane >> 1)) * kStep + (lane & 1) * 16;
+        int id = -1;
+        if (t < sp.n && step + (lane >> 1) < x1 - x0) id = table[t >> g.page_shift];
+        return (uint32_t)id < (uint32_t)g.pages ? id : -1;
+      };
+      int ids = pages(0);
+      Loaded<D, MX8> next;
+      auto load = [&](int x) {
+        const int id0 = __builtin_amdgcn_readlane(ids, (x & 31) * 2);
+        const int id1 = __builtin_amdgcn_readlane(ids, (x & 31) * 2 + 1);
+        const int t = t_first + x * kStep;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int id = h ? id1 : id0;
+          const int in = (t + 16 * h) & (g.page - 1);
+          const int64_t row = ((int64_t)max(id, 0) * g.kv_heads + kv) * g.page + in;
+          const char* kp = (const char*)g.k + row * kRowBytes + (int64_t)col * kRowBytes;
+          const char* vp = (const char*)g.v + row * kRowBytes;
+#pragma unroll
+          for (int i = 0; i < kLoads; ++i) {
+            next.k[h * kLoads + i] = *(const u32x4_t*)(kp + H::at(i, lg) * (MX8 ? 1 : 2));
+            next.v[h * kLoads + i] = *(const u32x4_t*)(vp + i * 1024 + lane * 16);
+          }
+          if constexpr (MX8) {
+            if constexpr (D == 128) next.ks[h] = *(const uint32_t*)(g.ks + (row + col) * 4);
+            else next.ks[h] = *(const uint16_t*)(g.ks + (row + col) * 2);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+              next.vs[h * kLoads + i] = g.vs[row * (D / 32) + (i * 1024 + lane * 16) / 32];
+          }
+        }
+      };
+      load(0);
+      for (int x = 0; x < x1 - x0; ++x) {
+        const Loaded<D, MX8> now = next;
+        const int t0 = t_first + x * kStep;
+        const int id0 = __builtin_amdgcn_readlane(ids, (x & 31) * 2);
+        const int id1 = __builtin_amdgcn_readlane(ids, (x & 31) * 2 + 1);
+        if (x + 1 < x1 - x0) {
+          if (((x + 1) & 31) == 0) ids = pages(x + 1);
+          load(x + 1);
+        }
+        if (id0 < 0 && id1 < 0) continue;  // (nothing of this wave's in the step)
+        // tokens of each block that count
+        const int lo0 = id0 < 0 ? 16 : sp.lo - t0, hi0 = id0 < 0 ? 0 : sp.n - t0;
+        const int lo1 = id1 < 0 ? 16 : sp.lo - t0 - 16, hi1 = id1 < 0 ? 0 : sp.n - t0 - 16;
+        const bool all = lo0 <= 0 && lo1 <= 0 && hi0 >= 16 && hi1 >= 16;
+        // values to LDS; rows that do not count are zeros (a weight of zero times what
+        // the page happens to hold there could be a NaN)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < kLoads; ++i) {
+            constexpr int kPerRow = kRowBytes / 16;
+            const int r = (i * 64 + lane) / kPerRow, u = (i * 64 + lane) % kPerRow;
+            const bool counts = all || (r >= (h ? lo1 : lo0) && r < (h ? hi1 : hi0));
+            u32x4_t v = now.v[h * kLoads + i];
+            if constexpr (MX8) {
+              const float s = cvt_scale(now.vs[h * kLoads + i]);
+              u32x4_t x0v = __builtin_bit_cast(u32x4_t, bf16_of(v[0], v[1], s));
+              u32x4_t x1v = __builtin_bit_cast(u32x4_t, bf16_of(v[2], v[3], s));
+              if (!counts) x0v = x1v = (u32x4_t){0, 0, 0, 0};
+              *(u32x4_t*)(mine + LV::at(16 * h + r, 2 * u)) = x0v;
+              *(u32x4_t*)(mine + LV::at(16 * h + r, 2 * u + 1)) = x1v;
+            } else {
+              if (!counts) v = (u32x4_t){0, 0, 0, 0};
+              *(u32x4_t*)(mine + LV::at(16 * h + r, u)) = v;
+            }
+          }
+        f32x4_t s[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          s[h] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < kLoads; ++i) {
+            const u32x4_t k = now.k[h * kLoads + i];
+            if constexpr (MX8) {
+              // elements 64 i + 16 g .. + 15: block 2 i + g / 2
+              const float sc = cvt_scale(now.ks[h] >> (8 * (2 * i + (lg >> 1))) & 255u);
+              s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(k[0], k[1], sc), q[2 * i], s[h], 0, 0, 0);
+              s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(k[2], k[3], sc), q[2 * i + 1], s[h], 0, 0, 0);
+            } else {
+              s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), q[i], s[h], 0, 0, 0);
+            }
+          }
+          if (!all) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = 4 * lg + e;
+              if (r < (h ? lo1 : lo0) || r >= (h ? hi1 : hi0)) s[h][e] = -INFINITY;
+            }
+          }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, s[h][e]);
+        top = quarters_max(top) * c;
+        // sums relative to a maximum that moves only past 2^8 (as in the prompt's kernel)
+        if (__any(top > a.m + 8.f)) {
+          const float m = fmaxf(a.m, top), f = m == -INFINITY ? 1.f : exp2_(a.m - m);
+          a.m = m;
+          a.l *= f;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a.o[i][e] *= f;
+        }
+        const float ref = a.m == -INFINITY ? 0.f : a.m;
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = exp2_(fmaf(s[e >> 2][e & 3], c, -ref));
+          a.l += p[e];
+        }
+        const bf16x8_t pw = __builtin_bit_cast(bf16x8_t, pack16(p, (bf16_t*)nullptr));
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+          a.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(LV::col(mine, 16 * i, lane), pw, a.o[i], 0, 0, 0);
+      }
+      // the four waves' sums, joined through LDS: [wave][query][D + m, l]
+      a.l = quarters_sum(a.l);
+      __syncthreads();  // (the values' LDS is free)
+      float* mem = (float*)smem;
+      constexpr int kRow = D + 4;
+      {
+        float* r = mem + (w * 16 + col) * kRow;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) *(f32x4_t*)(r + 16 * i + 4 * lg) = a.o[i];
+        if (lg == 0) {
+          r[D] = a.m;
+          r[D + 1] = a.l;
+        }
+      }
+      __syncthreads();
+      const bool whole = x0 == 0 && x1 == n;
+      float* out = g.parts + ((int64_t)blockIdx.x * 2 + (first_run ? 0 : 1)) * 16 * kRow;
+      for (int e = threadIdx.x; e < heads * (D / 4); e += 256) {
+        const int qi = e / (D / 4), d = e % (D / 4) * 4;
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, mem[(i * 16 + qi) * kRow + D]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float* r = mem + (i * 16 + qi) * kRow;
+          const float f = exp2_(r[D] - ref);
+          const f32x4_t v = *(const f32x4_t*)(r + d);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) o[y] += v[y] * f;
+          l += r[D + 1] * f;
+        }
+        if (whole) {
+          const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+          const float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+          const int64_t head = (int64_t)b * g.heads + h0 + qi;
+          Vec4<bf16_t>::store((bf16_t*)g.O + head * D + d, f);
+          if (g.lse && d == 0) g.lse[head] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+        } else {
+          *(f32x4_t*)(out + qi * kRow + d) = o;
+          if (d == 0) {
+            out[qi * kRow + D] = m;
+            out[qi * kRow + D + 1] = l;
+          }
+        }
+      }
+      __syncthreads();  // (the next part's values may overwrite the sums)
+      first_run = false;
+      at += x1 - x0;
+    }
+    base += (int64_t)n * g.pairs;
+  }
+}
+
+// Joins the parts of one head of one sequence whose steps lie in more than one
+// workgroup's run, in order; writes zeros where there is no token.
+template <int D>
+__global__ __launch_bounds__(256) void join_kernel(const DecodeArgs g) {
+  constexpr int kRow = D + 4, kAcross = 256 / (D / 4);  // (threads: D / 4 columns, kAcross parts at a time)
+  __shared__ int64_t part[4];
+  __shared__ int64_t found[1];
+  __shared__ __align__(16) float mem[kAcross][kRow];
+  const Plan plan = plan_of(g, part);
+  const int b = blockIdx.x / g.heads, head = blockIdx.x % g.heads;
+  {
+    const int first = threadIdx.x * plan.per;
+    if (b >= first && b < first + plan.per) {
+      int64_t before = plan.before;
+      for (int i = first; i < b; ++i) before += steps_of(span_of(g, i));
+      found[0] = before;
+    }
+    __syncthreads();
+  }
+  const int n = steps_of(span_of(g, b));
+  const int d = threadIdx.x % (D / 4) * 4, y = threadIdx.x / (D / 4);
+  const int64_t at = (int64_t)b * g.heads + head;
+  if (n == 0) {
+    if (y == 0) {
+      const float f[4] = {0.f, 0.f, 0.f, 0.f};
+      Vec4<bf16_t>::store((bf16_t*)g.O + at * D + d, f);
+      if (g.lse && d == 0) g.lse[at] = -INFINITY;
+    }
+    return;
+  }
+  const int kv = head / g.group, in = head % g.group;
+  const int64_t share = share_of(g, plan.total);
+  const int64_t s0 = found[0] * g.pairs + (int64_t)(kv * g.tiles + in / 16) * n, s1 = s0 + n;
+  const int64_t w0 = s0 / share, w1 = (s1 - 1) / share;
+  if (w0 == w1) return;  // one workgroup had it all
+  auto row = [&](int64_t w) {  // a run's first part is part 0
+    const int which = w == w0 && w0 * share < s0 ? 1 : 0;
+    return g.parts + ((w * 2 + which) * 16 + in % 16) * kRow;
+  };
+  float m = -INFINITY, l = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t w = w0 + y; w <= w1; w += kAcross) {
+    const float* r = row(w);
+    const f32x4_t v = *(const f32x4_t*)(r + d);
+    const float pm = r[D], pl = r[D + 1];
+    const float now = fmaxf(m, pm), ref = now == -INFINITY ? 0.f : now;
+    const float f = exp2_(m - ref), h = exp2_(pm - ref);
+    m = now;
+    l = l * f + pl * h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * f + v[e] * h;
+  }
+  *(f32x4_t*)(&mem[y][d]) = o;
+  if (d == 0) {
+    mem[y][D] = m;
+    mem[y][D + 1] = l;
+  }
+  __syncthreads();
+  if (y) return;
+  m = -INFINITY;
+  for (int i = 0; i < kAcross; ++i) m = fmaxf(m, mem[i][D]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  o = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+  for (int i = 0; i < kAcross; ++i) {
+    const float f = exp2_(mem[i][D] - ref);
+    const f32x4_t v = *(const f32x4_t*)(&mem[i][d]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += v[e] * f;
+    l += mem[i][D + 1] * f;
+  }
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  const float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  Vec4<bf16_t>::store((bf16_t*)g.O + at * D + d, f);
+  if (g.lse && d == 0) g.lse[at] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+}
+
+}  // namespace
+
+int decode_groups(const DecodeArgs& g) {
+  // all resident at once: two workgroups a CU
+  const int64_t most = (int64_t)g.seqs * g.pairs * ((g.most + kStep - 1) / kStep);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(2 * g.cus, most));
+}
+int64_t decode_part_floats(const DecodeArgs& g) { return (int64_t)decode_groups(g) * 2 * 16 * (g.dim + 4); }
+
+hipError_t launch_decode(const DecodeArgs& g, hipStream_t s) {
+  const int64_t heads = (int64_t)g.seqs * g.heads;
+  if (heads > kMostItems / 256) return hipErrorInvalidValue;
+  if (g.dim == 64) {
+    if (g.ks) decode_kernel<64, true><<<g.groups, 256, 0, s>>>(g);
+    else decode_kernel<64, false><<<g.groups, 256, 0, s>>>(g);
+    join_kernel<64><<<(unsigned)heads, 256, 0, s>>>(g);
+  } else {
+    if (g.ks) decode_kernel<128, true><<<g.groups, 256, 0, s>>>(g);
+    else decode_kernel<128, false><<<g.groups, 256, 0, s>>>(g);
+    join_kernel<128><<<(unsigned)heads, 256, 0, s>>>(g);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace memfine

@@ -266,4 +266,83 @@ hipError_t launch_mx_combine_half(const void* y, const uint8_t* ye, const int32_
                                   const float* gates, int64_t t0, int64_t tokens, int h, int k,
                                   void* Y, hipStream_t s);
 
+// Attention over packed sequences (dim 64 or 128, heads a multiple of kv_heads).
+struct AttnArgs {
+  int64_t T;                    // rows
+  int seqs, heads, kv_heads, dim;
+  int f32;                      // 1: float, 0: bf16
+  int causal, window;           // window 0: none
+  float scale;
+  const int32_t* offsets;       // [seqs + 1]: sequence b is rows [offsets[b], offsets[b + 1])
+  const void *Q, *K, *V;        // rows of heads of dim elements, ld* elements apart
+  int64_t ldq, ldk, ldv;
+  void* out;                    // forward: O [T, heads, dim]
+  float* lse;                   // [heads, T]; the forward's may be null
+  const void *O, *dO;           // backward: [T, heads, dim]
+  void *dQ, *dK, *dV;
+  int64_t lddq, lddk, lddv;
+  float* delta;                 // working memory [heads, T]
+};
+bool attn_fits(const AttnArgs& g);  // whether a launch holds that many rows and heads
+hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s);
+hipError_t launch_attn_bwd(const AttnArgs& g, hipStream_t s);
+
+// Attention of one token a sequence over a cache of pages [pages, kv_heads, page,
+// dim] of bf16, or of e4m3 with scales [pages, kv_heads, page, dim / 32].
+struct DecodeArgs {
+  int seqs, heads, kv_heads, dim;
+  int group, tiles, pairs;      // heads / kv_heads, sixteens of them, tiles kv_heads
+  int window;
+  float scale;
+  const void *k, *v;
+  const uint8_t *ks, *vs;       // null: bf16
+  int pages, page, page_shift;
+  const int32_t *table, *lengths;  // [seqs, width], [seqs]
+  int width, most;              // most: width page
+  const void* Q;                // rows of heads of dim elements, ldq apart
+  int64_t ldq;
+  void* O;                      // [seqs, heads, dim]
+  float* lse;                   // [seqs, heads] or null
+  float* parts;                 // working memory: decode_part_floats
+  int cus, groups;              // groups: decode_groups
+};
+int decode_groups(const DecodeArgs& g);
+int64_t decode_part_floats(const DecodeArgs& g);
+hipError_t launch_decode(const DecodeArgs& g, hipStream_t s);
+
+// Rotation by position: cosines and sines float [positions, dim / 2].
+struct RopeTable {
+  const float *cos, *sin;
+  int64_t positions;
+  int interleaved, inverse;
+};
+struct RopeArgs {
+  RopeTable r;
+  int64_t T;
+  int seqs, heads, dim, f32;
+  const int32_t* offsets;       // [seqs + 1]
+  const void* X;
+  void* Y;
+  int64_t ldx, ldy;
+};
+hipError_t launch_rope(const RopeArgs& g, int cus, hipStream_t s);
+// Rows into the cache (as DecodeArgs holds it): row t of sequence b with n rows
+// is its token lengths[b] - n + (t - the sequence's first row).
+struct WriteArgs {
+  RopeTable r;                  // cos null: not turned
+  int64_t T;
+  int seqs, heads, kv_heads, dim;
+  const int32_t *offsets;       // [seqs + 1], or null: row b is sequence b's only one
+  const int32_t *table, *lengths;
+  int width;
+  int64_t most;
+  void *k, *v;
+  uint8_t *ks, *vs;
+  int pages, page, page_shift;
+  const void *K, *V, *Q;        // Q with heads = 0: none
+  int64_t ldk, ldv, ldq;
+  void* R;                      // [T, heads, dim]: the turned queries
+};
+hipError_t launch_kv_write(const WriteArgs& g, int cus, hipStream_t s);
+
 }  // namespace memfine
