@@ -1943,6 +1943,7 @@ AttnArgs attn_args(int64_t T, int32_t seqs, const memfine_attn& a) {
   g.causal = a.causal;
   g.window = a.window;
   g.scale = a.scale;
+  g.parts = T > 0 ? attn_parts(g, device_cus()) : 1;
   return g;
 }
 int check_decode(const memfine_attn* a, const memfine_cache* c, int32_t seqs, int32_t width) {
@@ -2011,7 +2012,7 @@ int memfine_attn_fwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32
 
 int64_t memfine_attn_bwd_workspace_bytes(int64_t T, const memfine_attn* a) {
   if (check_attn(a) || check_rows(T, 1)) return MEMFINE_ERR_INVALID_ARG;
-  return T * a->heads * 4;
+  return attn_bwd_floats(attn_args(T, 1, *a)) * 4;
 }
 
 int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
@@ -2047,9 +2048,11 @@ int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32
   g.lddk = ld_dk;
   g.lddv = ld_dv;
   hipStream_t s = (hipStream_t)stream;
-  const size_t bytes = (size_t)(T * a->heads * 4);
-  g.delta = (float*)ws_alloc(alloc, bytes, s);
-  if (!g.delta) return MEMFINE_ERR_OOM;
+  const size_t bytes = (size_t)attn_bwd_floats(g) * 4;
+  g.sums = (float*)ws_alloc(alloc, bytes, s);  // (first: read in 16-byte pieces)
+  if (!g.sums) return MEMFINE_ERR_OOM;
+  g.top = g.sums + (g.parts > 1 ? 2 * (int64_t)g.parts * g.kv_heads * g.dim * T : 0);
+  g.delta = g.top + T * g.heads;
   const double rows = (double)T * a->dim * (g.f32 ? 4 : 2);
   hipError_t err;
   {
@@ -2057,7 +2060,7 @@ int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32
                    4.0 * rows * (a->heads + a->kv_heads) + 4.0 * T * a->heads);
     err = launch_attn_bwd(g, s);
   }
-  ws_release(alloc, g.delta, bytes, s);
+  ws_release(alloc, g.sums, bytes, s);
   return hip_status(err);
 }
 

@@ -156,21 +156,24 @@ template <typename T, int D, int NW> struct Copy {
   static constexpr int kPer = 1024 / L::kPitch;               // rows an instruction
   static constexpr int kCount = L::kBytes / 1024 / NW;        // instructions a wave
   static_assert(kCount * NW * 1024 == L::kBytes, "a tile is split evenly over the waves");
-  uint32_t voff[kCount];
+  static constexpr int kApart = kPer * NW;                    // rows between a wave's instructions
+  static constexpr int kKinds = kApart % 16 ? 2 : 1;          // (the swizzle repeats every 16 rows)
+  static_assert(kApart * kKinds % 16 == 0 || kCount <= kKinds, "rows of an instruction");
+  uint32_t voff[kKinds];  // from the instruction's first row on
   __device__ __forceinline__ void init(int64_t ld, int wave, int lane) {
 #pragma unroll
-    for (int i = 0; i < kCount; ++i) {
-      const int r = (i * NW + wave) * kPer + lane / L::kUnits;
-      voff[i] = (uint32_t)(r * ld) * L::ES + (((lane % L::kUnits) ^ L::swizzle(r)) << 4);
+    for (int i = 0; i < kKinds; ++i) {
+      const int r = wave * kPer + lane / L::kUnits;
+      voff[i] = (uint32_t)(r * ld) * L::ES + (((lane % L::kUnits) ^ L::swizzle(r + i * kApart)) << 4);
     }
   }
   // rows from base on, `rows` of them there
   __device__ __forceinline__ void issue(const T* base, int64_t ld, int rows, char* lds, int wave) const {
-    const __amdgpu_buffer_rsrc_t rs = rows_rsrc<T, D>(base, ld, min(rows, L::kRows));
 #pragma unroll
     for (int i = 0; i < kCount; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + (i * NW + wave) * 1024), 16,
-                                               voff[i], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rows_rsrc<T, D>(base + i * kApart * ld, ld, min(rows - i * kApart, kApart)),
+          (lds_void*)(lds + (i * NW + wave) * 1024), 16, voff[i % kKinds], 0, 0, 0);
   }
 };
 
@@ -246,22 +249,21 @@ __device__ __forceinline__ bool locate(const int32_t* __restrict__ offsets, int 
     s0 += w * per;
   }
 }
-// Head and block of a workgroup.  Workgroups go to the 8 XCDs in turn; with a
-// multiple of 8 heads each XCD takes an eighth of them one after the other, so
-// that its L2 holds the keys and values in use.  Else all heads advance
-// together.  Blocks come in falling order (`down`: causal, the longest first).
-__device__ __forceinline__ bool work_item(int blocks, int heads, bool down, int& head, int& b) {
+// Head and block of a workgroup.  All heads advance together through the blocks, in falling
+// order with `down`: under a causal mask the longest come first and the shortest
+// even out the end.  Workgroups go to the 8 XCDs in turn; with a multiple of 8 heads each
+// XCD has an eighth of them, neighbours, which share keys and values in its L2.
+__device__ __forceinline__ void work_item(int blocks, int heads, bool down, int& head, int& b) {
   const int id = blockIdx.x;
   if (heads % 8 == 0) {
-    const int i = id >> 3;
-    head = (id & 7) * (heads >> 3) + i / blocks;
-    b = i % blocks;
+    const int i = id >> 3, per = heads >> 3;
+    head = (id & 7) * per + i % per;
+    b = i / per;
   } else {
     head = id % heads;
     b = id / heads;
   }
   if (down) b = blocks - 1 - b;
-  return true;
 }
 
 // Which scores of a lane's own token count.
@@ -297,9 +299,8 @@ __global__ __launch_bounds__(64 * NW) void attn_fwd_kernel(const AttnArgs g, int
   const int hh = lane >> 5;
   int head, b;
   Part p;
-  if (!work_item(blocks, g.heads, g.causal, head, b) ||
-      !locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p))
-    return;
+  work_item(blocks, g.heads, g.causal, head, b);
+  if (!locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p)) return;
   const int kv = head / (g.heads / g.kv_heads);
   const int q0 = p.block * kBlock, rows = min(kBlock, p.n - q0);
   const int i0 = q0 + 32 * w, mine = min(32, p.n - i0);
@@ -395,7 +396,8 @@ __global__ __launch_bounds__(64 * NW) void attn_fwd_kernel(const AttnArgs g, int
 }
 
 // ---------------------------------------------------------------- backward
-// dq of 32 NW rows a workgroup, and their delta for the kernel below.
+// dq of 32 NW rows a workgroup, and their log2 of the weights' sum and delta for the
+// kernel below.
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(64 * NW) void attn_dq_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D> L;
@@ -406,9 +408,8 @@ __global__ __launch_bounds__(64 * NW) void attn_dq_kernel(const AttnArgs g, int 
   const int hh = lane >> 5;
   int head, b;
   Part p;
-  if (!work_item(blocks, g.heads, g.causal, head, b) ||
-      !locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p))
-    return;
+  work_item(blocks, g.heads, g.causal, head, b);
+  if (!locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p)) return;
   const int kv = head / (g.heads / g.kv_heads);
   const int q0 = p.block * kBlock, rows = min(kBlock, p.n - q0);
   const int i0 = q0 + 32 * w, mine = min(32, p.n - i0);
@@ -451,9 +452,12 @@ __global__ __launch_bounds__(64 * NW) void attn_dq_kernel(const AttnArgs g, int 
   if ((lane & 31) < mine) {
     lse = g.lse[row + (lane & 31)];
     if (lse == -INFINITY) lse = INFINITY;
-    if (hh == 0) g.delta[row + lane] = delta;
   }
   const float c = g.scale * kLog2e, ref = lse * kLog2e;
+  if (lane < mine) {
+    g.top[row + lane] = ref;
+    g.delta[row + lane] = delta;
+  }
   f32x16_t a[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) zero(a[i]);
@@ -490,25 +494,28 @@ __global__ __launch_bounds__(64 * NW) void attn_dq_kernel(const AttnArgs g, int 
     store_rows<T, D>(a, g.scale, (T*)g.dQ + (p.begin + i0) * g.lddq + head * D, g.lddq, mine, lane);
 }
 
-// dk and dv of 32 NW rows a workgroup: it goes through the queries of all heads
-// that share them, head after head, so that every sum has one order.
-template <typename T, int D, int NW>
+// dk and dv of 32 NW rows a workgroup: it goes through the queries of the heads that share
+// them, head after head, so that every sum has one order.  With several parts each takes
+// some of the heads and leaves its sums in fp32 for attn_sum_kernel.
+// kHeld: the values stay in LDS, not in registers, of which two waves a SIMD have 256 each.
+template <typename T, int D, int NW, bool kHeld>
 __global__ __launch_bounds__(64 * NW) void attn_dkv_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D> L;
   typedef Mma<T> M;
   constexpr int kBlock = 32 * NW;
-  // two stages of queries, dO, and their lse and delta
+  // two stages of queries, dO, and their rows' log2 of the sum and delta
   constexpr int kStage = 2 * L::kBytes;
-  __shared__ __align__(1024) char smem[2 * kStage];
-  __shared__ __align__(16) float stats[2][2][L::kRows];
+  __shared__ __align__(1024) char smem[2 * kStage + (kHeld ? kBlock * L::kPitch : 0)];
+  __shared__ __align__(16) float stats[2][2][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
   int kv, b;
   Part p;
-  if (!work_item(blocks, g.kv_heads, false, kv, b) ||
-      !locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p))
-    return;
+  work_item(blocks * g.parts, g.kv_heads, false, kv, b);
+  const int part = b % g.parts;
+  if (!locate(g.offsets, g.seqs, (int)g.T, kBlock, b / g.parts, p)) return;
   const int group = g.heads / g.kv_heads;
+  const int h0 = group * part / g.parts, h1 = group * (part + 1) / g.parts;
   const int k0 = p.block * kBlock, rows = min(kBlock, p.n - k0);
   const int j0 = k0 + 32 * w, mine = min(32, p.n - j0);
   const Seen wg_first = queries_of(g, k0, p.n), wg_last = queries_of(g, k0 + rows - 1, p.n);
@@ -519,35 +526,41 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_kernel(const AttnArgs g, int
   Copy<T, D, NW> cq, co;
   cq.init(g.ldq, w, lane);
   co.init(ldo, w, lane);
-  const int total = group * tiles;
+  const int total = (h1 - h0) * tiles;
   auto issue = [&](int x, int stage) {
-    const int head = kv * group + x / tiles, r0 = (t0 + x % tiles) * L::kRows;
+    const int head = kv * group + h0 + x / tiles, r0 = (t0 + x % tiles) * L::kRows;
     char* st = smem + stage * kStage;
     cq.issue((const T*)g.Q + (p.begin + r0) * g.ldq + head * D, g.ldq, p.n - r0, st, w);
     co.issue((const T*)g.dO + ((p.begin + r0) * (int64_t)g.heads + head) * D, ldo, p.n - r0,
              st + L::kBytes, w);
-    if (threadIdx.x < 2 * L::kRows) {
-      const int r = threadIdx.x % L::kRows, which = threadIdx.x / L::kRows;
-      const int64_t at = head * g.T + p.begin + r0 + r;
-      float v = which ? 0.f : INFINITY;
-      if (r0 + r < p.n) {
-        v = (which ? g.delta : g.lse)[at];
-        if (!which) v = v == -INFINITY ? INFINITY : v * kLog2e;
-      }
-      stats[stage][which][r] = v;
+    // (rows past the sequence read zero, like their dO: they add nothing)
+    if (w < 2) {
+      const float* from = (w ? g.delta : g.top) + head * g.T + p.begin + r0;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_of(from, (uint32_t)min(p.n - r0, L::kRows) * 4),
+                                               (lds_void*)stats[stage][w], 4, lane * 4, 0, 0, 0);
     }
   };
-  issue(0, 0);
-  Frag<T> k[L::kSteps], v[L::kSteps];
+  const T* V = (const T*)g.V + (p.begin + k0) * g.ldv + kv * D;
+  const char* held = smem + 2 * kStage;
+  Frag<T> k[L::kSteps], v[kHeld ? 1 : L::kSteps];
+  if constexpr (kHeld) {
+    Copy<T, D, NW> cv;
+    cv.init(g.ldv, w, lane);
+#pragma unroll
+    for (int i = 0; i < kBlock / L::kRows; ++i)
+      cv.issue(V + i * L::kRows * g.ldv, g.ldv, rows - i * L::kRows, smem + 2 * kStage + i * L::kBytes, w);
+  } else {
+    load_rows<T, D>(v, V + 32 * w * g.ldv, g.ldv, mine, lane);
+  }
   load_rows<T, D>(k, (const T*)g.K + (p.begin + j0) * g.ldk + kv * D, g.ldk, mine, lane);
-  load_rows<T, D>(v, (const T*)g.V + (p.begin + j0) * g.ldv + kv * D, g.ldv, mine, lane);
-  const float c = g.scale * kLog2e;
+  issue(0, 0);
   f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
     zero(dk[i]);
     zero(dv[i]);
   }
+  const float scale = g.scale * kLog2e;
   for (int x = 0; x < total; ++x) {
     stage_barrier();
     if (x + 1 < total) issue(x + 1, (x + 1) & 1);
@@ -556,23 +569,36 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_kernel(const AttnArgs g, int
     const char* qs = smem + (x & 1) * kStage;
     const char* os = qs + L::kBytes;
     const bool all = see_all(first, last, r0, L::kRows);
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < L::kBlocks; ++i) {
+      // (what is read from LDS is read where it is used: registers are full)
+      if constexpr (kHeld) asm volatile("" ::: "memory");
       f32x16_t s, dp;
       zero(s);
       zero(dp);
+      // (a step's operands are read while the one before it multiplies, and no earlier)
+      Frag<T> a[2], o[2], u[2];
+      auto rows_of = [&](int e) {
+        a[e & 1] = L::row(qs, 32 * i, e, lane);
+        o[e & 1] = L::row(os, 32 * i, e, lane);
+        if constexpr (kHeld) u[e & 1] = L::row(held, 32 * w, e, lane);
+      };
+      rows_of(0);
 #pragma unroll
       for (int e = 0; e < L::kSteps; ++e) {
-        M::mma(L::row(qs, 32 * i, e, lane), k[e], s);
-        M::mma(L::row(os, 32 * i, e, lane), v[e], dp);
+        if (e + 1 < L::kSteps) rows_of(e + 1);
+        M::mma(a[e & 1], k[e], s);
+        if constexpr (kHeld) M::mma(o[e & 1], u[e & 1], dp);
+        else M::mma(o[e & 1], v[e], dp);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      const float* lse = &stats[x & 1][0][32 * i + 4 * hh];
+      const float* top = &stats[x & 1][0][32 * i + 4 * hh];
       const float* del = &stats[x & 1][1][32 * i + 4 * hh];
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
-        const f32x4_t a = *(const f32x4_t*)(lse + 2 * e);
+        const f32x4_t a = *(const f32x4_t*)(top + 2 * e);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) s[e + y] = exp2_(fmaf(s[e + y], c, -a[y]));
+        for (int y = 0; y < 4; ++y) s[e + y] = exp2_(fmaf(s[e + y], scale, -a[y]));
       }
       if (!all) hide(s, own, r0 + 32 * i, hh, 0.f);
 #pragma unroll
@@ -581,20 +607,66 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_kernel(const AttnArgs g, int
 #pragma unroll
         for (int y = 0; y < 4; ++y) dp[e + y] = s[e + y] * (dp[e + y] - a[y]);
       }
+      constexpr int kCols = D / 32;
+      auto cols_of = [&](int x) {
+        o[x & 1] = L::col(os, 32 * (x % kCols), i * L::kDown + x / kCols, lane);
+        a[x & 1] = L::col(qs, 32 * (x % kCols), i * L::kDown + x / kCols, lane);
+      };
+      cols_of(0);
 #pragma unroll
       for (int j = 0; j < L::kDown; ++j) {
         const Frag<T> f = M::of(s, j), h = M::of(dp, j);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          M::mma(L::col(os, 32 * d, i * L::kDown + j, lane), f, dv[d]);
-          M::mma(L::col(qs, 32 * d, i * L::kDown + j, lane), h, dk[d]);
+        for (int d = 0; d < kCols; ++d) {
+          const int x = j * kCols + d;
+          if (x + 1 < L::kDown * kCols) cols_of(x + 1);
+          M::mma(o[x & 1], f, dv[d]);
+          M::mma(a[x & 1], h, dk[d]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
   }
   if (mine <= 0) return;
-  store_rows<T, D>(dk, g.scale, (T*)g.dK + (p.begin + j0) * g.lddk + kv * D, g.lddk, mine, lane);
-  store_rows<T, D>(dv, 1.f, (T*)g.dV + (p.begin + j0) * g.lddv + kv * D, g.lddv, mine, lane);
+  const int64_t j = p.begin + j0;
+  if (g.parts > 1) {
+    const int64_t kvd = (int64_t)g.kv_heads * D;
+    float* out = g.sums + (part * 2 * g.T + j) * kvd + kv * D;
+    store_rows<float, D>(dk, g.scale, out, kvd, mine, lane);
+    store_rows<float, D>(dv, 1.f, out + g.T * kvd, kvd, mine, lane);
+  } else {
+    store_rows<T, D>(dk, g.scale, (T*)g.dK + j * g.lddk + kv * D, g.lddk, mine, lane);
+    store_rows<T, D>(dv, 1.f, (T*)g.dV + j * g.lddv + kv * D, g.lddv, mine, lane);
+  }
+}
+
+// dK and dV from the parts' sums [parts][dK, dV][T][kv_heads dim], added in order: four
+// elements a thread, of rows that lie in a sequence.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_sum_kernel(const AttnArgs g) {
+  const int64_t kvd = (int64_t)g.kv_heads * g.dim, n = g.T * kvd / 4;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < 2 * n; i += gridDim.x * 256ll) {
+    const bool v = i >= n;
+    const int64_t at = (v ? i - n : i) * 4, row = at / kvd, col = at % kvd;
+    bool in = false;  // of a sequence (the last that begins at or before it)
+    {
+      int lo = 0, hi = g.seqs;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (g.offsets[mid] <= row) lo = mid;
+        else hi = mid;
+      }
+      in = g.offsets[lo] <= row && row < g.offsets[lo + 1];
+    }
+    if (!in) continue;
+    float f[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < g.parts; ++p) {
+      const f32x4_t x = *(const f32x4_t*)(g.sums + (p * 2 + v) * g.T * kvd + at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] += x[e];
+    }
+    Vec4<T>::store(v ? (T*)g.dV + row * g.lddv + col : (T*)g.dK + row * g.lddk + col, f);
+  }
 }
 
 // Blocks of R rows of seqs sequences that share T rows, at most.
@@ -605,35 +677,52 @@ int64_t blocks_of(int64_t T, int64_t seqs, int R) {
 
 // Waves of a workgroup: eight in bf16, two a SIMD, so that one multiplies while the
 // other works on its scores; four in fp32, whose operands need the registers of two.
-constexpr int kWaves = 8, kWavesF32 = 4, kDkvWaves = 4;
+constexpr int kWaves = 8, kWavesF32 = 4;
 
 // (The compiler leaves out host stubs of kernels that only templates launch.)
-#define MEMFINE_ATTN(T, D, NW)                                                \
-  template __global__ void attn_fwd_kernel<T, D, NW>(const AttnArgs, int);    \
-  template __global__ void attn_dq_kernel<T, D, NW>(const AttnArgs, int);     \
-  template __global__ void attn_dkv_kernel<T, D, kDkvWaves>(const AttnArgs, int);
-MEMFINE_ATTN(bf16_t, 64, kWaves)
-MEMFINE_ATTN(bf16_t, 128, kWaves)
-MEMFINE_ATTN(float, 64, kWavesF32)
-MEMFINE_ATTN(float, 128, kWavesF32)
+#define MEMFINE_ATTN(T, D, NW, HELD)                                         \
+  template __global__ void attn_fwd_kernel<T, D, NW>(const AttnArgs, int);   \
+  template __global__ void attn_dq_kernel<T, D, NW>(const AttnArgs, int);    \
+  template __global__ void attn_dkv_kernel<T, D, NW, HELD>(const AttnArgs, int);
+MEMFINE_ATTN(bf16_t, 64, kWaves, false)
+MEMFINE_ATTN(bf16_t, 128, kWaves, true)
+MEMFINE_ATTN(float, 64, kWavesF32, false)
+MEMFINE_ATTN(float, 128, kWavesF32, false)
 #undef MEMFINE_ATTN
+template __global__ void attn_sum_kernel<bf16_t>(const AttnArgs);
+template __global__ void attn_sum_kernel<float>(const AttnArgs);
 
 template <typename T, int D, int NW> void run_fwd(const AttnArgs& g, hipStream_t s) {
   const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW);
   attn_fwd_kernel<T, D, NW><<<(unsigned)blocks * g.heads, 64 * NW, 0, s>>>(g, blocks);
 }
-template <typename T, int D, int NW> void run_bwd(const AttnArgs& g, hipStream_t s) {
+template <typename T, int D, int NW, bool kHeld> void run_bwd(const AttnArgs& g, hipStream_t s) {
   const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW);
-  // (writes delta, which the next one reads)
+  // (writes top and delta, which the next one reads)
   attn_dq_kernel<T, D, NW><<<(unsigned)blocks * g.heads, 64 * NW, 0, s>>>(g, blocks);
-  const int kb = (int)blocks_of(g.T, g.seqs, 32 * kDkvWaves);
-  attn_dkv_kernel<T, D, kDkvWaves><<<(unsigned)kb * g.kv_heads, 64 * kDkvWaves, 0, s>>>(g, kb);
+  attn_dkv_kernel<T, D, NW, kHeld>
+      <<<(unsigned)blocks * g.kv_heads * g.parts, 64 * NW, 0, s>>>(g, blocks);
+  if (g.parts > 1) {
+    const int64_t n = (g.T * g.kv_heads * D / 2 + 255) / 256;
+    attn_sum_kernel<T><<<(unsigned)std::min<int64_t>(n, 8192), 256, 0, s>>>(g);
+  }
 }
 
 }  // namespace
 
+// Parts of dK and dV: a workgroup for 256 keys (fp32: 128) goes through all queries of
+// the group; where that leaves fewer than two a CU the group's heads are shared out.
+int attn_parts(const AttnArgs& g, int cus) {
+  const int64_t items = (g.T + 255) / 256 * g.kv_heads;
+  const int64_t want = (2 * (int64_t)cus + items - 1) / items;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(want, g.heads / g.kv_heads));
+}
+int64_t attn_bwd_floats(const AttnArgs& g) {
+  return (2 * g.heads + (g.parts > 1 ? 2 * (int64_t)g.parts * g.kv_heads * g.dim : 0)) * g.T;
+}
+
 bool attn_fits(const AttnArgs& g) {
-  return blocks_of(g.T, g.seqs, 32 * kDkvWaves) * g.heads <= kMostItems / (64 * kWaves);
+  return blocks_of(g.T, g.seqs, 32 * kWavesF32) * g.heads <= kMostItems / (64 * kWaves);
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s) {
@@ -651,11 +740,11 @@ hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s) {
 hipError_t launch_attn_bwd(const AttnArgs& g, hipStream_t s) {
   if (!attn_fits(g)) return hipErrorInvalidValue;
   if (g.f32) {
-    if (g.dim == 64) run_bwd<float, 64, kWavesF32>(g, s);
-    else run_bwd<float, 128, kWavesF32>(g, s);
+    if (g.dim == 64) run_bwd<float, 64, kWavesF32, false>(g, s);
+    else run_bwd<float, 128, kWavesF32, false>(g, s);
   } else {
-    if (g.dim == 64) run_bwd<bf16_t, 64, kWaves>(g, s);
-    else run_bwd<bf16_t, 128, kWaves>(g, s);
+    if (g.dim == 64) run_bwd<bf16_t, 64, kWaves, false>(g, s);
+    else run_bwd<bf16_t, 128, kWaves, true>(g, s);
   }
   return hipGetLastError();
 }

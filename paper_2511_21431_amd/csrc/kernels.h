@@ -281,8 +281,13 @@ struct AttnArgs {
   const void *O, *dO;           // backward: [T, heads, dim]
   void *dQ, *dK, *dV;
   int64_t lddq, lddk, lddv;
-  float* delta;                 // working memory [heads, T]
+  // working memory of the backward, attn_bwd_floats
+  float *top, *delta;           // [heads, T]: lse in bits, dO . O
+  float* sums;                  // parts > 1: [parts][2][T, kv_heads, dim]
+  int parts;                    // attn_parts
 };
+int attn_parts(const AttnArgs& g, int cus);
+int64_t attn_bwd_floats(const AttnArgs& g);
 bool attn_fits(const AttnArgs& g);  // whether a launch holds that many rows and heads
 hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s);
 hipError_t launch_attn_bwd(const AttnArgs& g, hipStream_t s);

@@ -61,7 +61,7 @@ def test_packed_refusals():
         assert fwd(off=N, Q=N, K=N, V=N, O=N, lse=N, **kw) == 0
         assert bwd(off=N, Q=N, dQ=N, **kw) == 0
     f = _lib.lib().memfine_attn_bwd_workspace_bytes
-    assert f(1000, ctypes.byref(attn())) == 1000 * 8 * 4 and f(0, ctypes.byref(attn())) == 0
+    assert f(1000, ctypes.byref(attn())) >= 2 * 1000 * 8 * 4 and f(0, ctypes.byref(attn())) == 0
     assert f(-1, ctypes.byref(attn())) < 0 and f(1, ctypes.byref(attn(heads=7))) < 0
 
 
