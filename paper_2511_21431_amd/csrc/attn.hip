@@ -16,6 +16,7 @@
 // values of a reduction step a register holds is the accumulator's choice, and
 // the other operand, read from LDS with a transposing load, follows it.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -188,20 +189,29 @@ __device__ __forceinline__ void load_rows(Frag<T> (&f)[N], const T* base, int64_
     f[k] = __builtin_bit_cast(Frag<T>, __builtin_amdgcn_raw_buffer_load_b128(rs, at + k * 32, 0, 0));
 }
 
-// Transposed accumulators of 32 rows (a lane: row lane % 32), as rows of out.
+// Transposed accumulators of 32 rows (a lane: row lane % 32), as rows of out.  They go
+// through the wave's own 32 rows of LDS, so that whole rows are stored (straight from the
+// accumulators a store writes 8 bytes of each of 64 lines: 8192 rows of 32 heads 27 us).
 template <typename T, int D>
 __device__ __forceinline__ void store_rows(const f32x16_t (&c)[D / 32], float scale, T* out, int64_t ld,
-                                           int rows, int lane) {
-  if ((lane & 31) >= rows) return;
-  T* p = out + (lane & 31) * ld + (lane >> 5) * 4;
+                                           int rows, char* lds, int lane) {
+  constexpr int kPitch = D * (int)sizeof(T), kUnits = kPitch / 16, kVec = Elem<T>::kVec;
+  const int r = lane & 31, hh = lane >> 5;
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const float f[4] = {c[b][4 * g] * scale, c[b][4 * g + 1] * scale, c[b][4 * g + 2] * scale,
                           c[b][4 * g + 3] * scale};
-      Vec4<T>::store(p + b * 32 + g * 8, f);
+      const int at = (b * 32 + g * 8 + hh * 4) * (int)sizeof(T);
+      Vec4<T>::store((T*)(lds + r * kPitch + (((at >> 4) ^ (r & 15) % kUnits) << 4) + (at & 15)), f);
     }
+#pragma unroll
+  for (int i = 0; i < kUnits / 2; ++i) {
+    const int row = i * (64 / kUnits) + lane / kUnits, u = lane % kUnits;
+    const u32x4_t v = *(const u32x4_t*)(lds + row * kPitch + ((u ^ (row & 15) % kUnits) << 4));
+    if (row < rows) *(u32x4_t*)(out + row * ld + u * kVec) = v;
+  }
 }
 
 // ------------------------------------------------------------- work to do
@@ -210,6 +220,18 @@ struct Part {
   int begin, n;  // the sequence's first row and its length
   int block;     // of the sequence
 };
+// Sum over the lanes up to this one, by DPP: row shifts, then each row's last lane to the next.
+template <int kCtrl, int kRows> __device__ __forceinline__ int add_dpp(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+  v = add_dpp<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  v = add_dpp<0x112, 0xf>(v);
+  v = add_dpp<0x114, 0xf>(v);
+  v = add_dpp<0x118, 0xf>(v);
+  v = add_dpp<0x142, 0xa>(v);  // row_bcast 15 into rows 1 and 3
+  return add_dpp<0x143, 0xc>(v);  // row_bcast 31 into rows 2 and 3
+}
 // Every wave looks for itself: its lanes add up the blocks of a 64th of the
 // sequences each, and the search goes on in the one that holds block b.  (Offsets
 // are cut to [0, T], so that nothing outside is touched whatever they are.)
@@ -217,37 +239,39 @@ __device__ __forceinline__ bool locate(const int32_t* __restrict__ offsets, int 
                                        Part& p) {
   const int lane = threadIdx.x & 63;
   int s0 = 0, count = seqs;
-  for (;;) {
+  while (count > 64) {
     const int per = (count + 63) / 64;
     const int first = s0 + lane * per, last = min(first + per, s0 + count);
-    int n = 0, lo = 0, hi = 0;
+    int n = 0;
     if (first < last) {
-      hi = min(max(offsets[first], 0), T);
+      int hi = min(max(offsets[first], 0), T);
       for (int s = first; s < last; ++s) {
-        lo = hi;
+        const int lo = hi;
         hi = min(max(offsets[s + 1], 0), T);
         n += hi > lo ? (hi - lo + R - 1) / R : 0;
       }
     }
-    int inc = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(inc, o, 64);
-      if (lane >= o) inc += y;
-    }
+    const int inc = wave_scan(n);
     const uint64_t past = __ballot(inc > b);
     if (past == 0) return false;
     const int w = __builtin_ctzll(past);
     b -= __builtin_amdgcn_readlane(inc - n, w);
-    if (per == 1) {
-      p.begin = __builtin_amdgcn_readlane(lo, w);
-      p.n = __builtin_amdgcn_readlane(hi, w) - p.begin;
-      p.block = b;
-      return true;
-    }
     count = min(per, s0 + count - (s0 + w * per));
     s0 += w * per;
   }
+  const int at = s0 + min(lane, count - 1);
+  int lo = offsets[at], hi = offsets[at + 1];
+  lo = min(max(lo, 0), T);
+  hi = min(max(hi, 0), T);
+  const int n = lane < count && hi > lo ? (hi - lo + R - 1) / R : 0;
+  const int inc = wave_scan(n);
+  const uint64_t past = __ballot(inc > b);
+  if (past == 0) return false;
+  const int w = __builtin_ctzll(past);
+  p.begin = __builtin_amdgcn_readlane(lo, w);
+  p.n = __builtin_amdgcn_readlane(hi, w) - p.begin;
+  p.block = b - __builtin_amdgcn_readlane(inc - n, w);
+  return true;
 }
 // Head and block of a workgroup.  All heads advance together through the blocks, in falling
 // order with `down`: under a causal mask the longest come first and the shortest
@@ -280,30 +304,41 @@ __device__ __forceinline__ Seen queries_of(const AttnArgs& g, int j, int n) {
 __device__ __forceinline__ bool see_all(const Seen& first, const Seen& last, int r0, int rows) {
   return r0 >= max(first.lo, last.lo) && r0 + rows - 1 <= min(first.hi, last.hi);
 }
+// Scores of a block of rows from r0 on that do not count become v: one bit a row, two
+// instructions a score.
 __device__ __forceinline__ void hide(f32x16_t& c, const Seen& s, int r0, int hh, float v) {
+  const int lo = s.lo - r0 - 4 * hh, hi = s.hi - r0 - 4 * hh;
+  const uint32_t to = hi < 0 ? 0u : hi >= 31 ? ~0u : (2u << hi) - 1u;
+  const uint32_t from = lo <= 0 ? ~0u : lo >= 32 ? 0u : ~0u << lo;
+  const uint32_t bits = from & to;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int r = r0 + acc_row(i, hh);
-    if (r < s.lo || r > s.hi) c[i] = v;
+    const uint32_t m = (uint32_t)((int32_t)(bits << (31 - acc_row(i, 0))) >> 31);
+    c[i] = __uint_as_float((__float_as_uint(c[i]) & m) | (__float_as_uint(v) & ~m));
   }
 }
 
 // ----------------------------------------------------------------- forward
+// NW waves of 32 queries each, which share the tiles of keys and values in LDS: heads of a
+// group, where there are groups, for the same queries (under a causal mask they
+// then need the same tiles), the rest further queries.
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void attn_fwd_kernel(const AttnArgs g, int blocks) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void attn_fwd_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D> L;
   typedef Mma<T> M;
-  constexpr int kBlock = 32 * NW;
   __shared__ __align__(1024) char smem[4 * L::kBytes];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
   int head, b;
   Part p;
-  work_item(blocks, g.heads, g.causal, head, b);
-  if (!locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p)) return;
+  // 2^share waves take the same queries for as many heads
+  const int block = 32 * NW >> g.share;
+  work_item(blocks, g.heads >> g.share, g.causal, head, b);
+  if (!locate(g.offsets, g.seqs, (int)g.T, block, b, p)) return;
+  head = (head << g.share) + (w & ((1 << g.share) - 1));
   const int kv = head / (g.heads / g.kv_heads);
-  const int q0 = p.block * kBlock, rows = min(kBlock, p.n - q0);
-  const int i0 = q0 + 32 * w, mine = min(32, p.n - i0);
+  const int q0 = p.block * block, rows = min(block, p.n - q0);
+  const int i0 = q0 + 32 * (w >> g.share), mine = min(32, p.n - i0);
   const T* K = (const T*)g.K + p.begin * g.ldk + kv * D;
   const T* V = (const T*)g.V + p.begin * g.ldv + kv * D;
 
@@ -316,13 +351,12 @@ __global__ __launch_bounds__(64 * NW) void attn_fwd_kernel(const AttnArgs g, int
   Copy<T, D, NW> ck, cv;
   ck.init(g.ldk, w, lane);
   cv.init(g.ldv, w, lane);
-  auto issue = [&](int t) {
-    char* st = smem + (t & 1) * 2 * L::kBytes;
+  auto issue = [&](int t, char* st) {
     const int64_t r = (int64_t)t * L::kRows;
     ck.issue(K + r * g.ldk, g.ldk, p.n - (int)r, st, w);
     cv.issue(V + r * g.ldv, g.ldv, p.n - (int)r, st + L::kBytes, w);
   };
-  issue(t0);
+  issue(t0, smem);
   Frag<T> q[L::kSteps];
   load_rows<T, D>(q, (const T*)g.Q + (p.begin + i0) * g.ldq + head * D, g.ldq, mine, lane);
 
@@ -331,12 +365,14 @@ __global__ __launch_bounds__(64 * NW) void attn_fwd_kernel(const AttnArgs g, int
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) zero(o[i]);
   float m = -INFINITY, l = 0.f;  // (l: of this half's tokens)
-  for (int t = t0; t < t1; ++t) {
+  // (the stage a constant: its addresses are then offsets in the reads)
+  auto tile = [&](int t, auto stage) {
+    constexpr int kAt = decltype(stage)::value * 2 * L::kBytes;
     stage_barrier();
-    if (t + 1 < t1) issue(t + 1);
+    if (t + 1 < t1) issue(t + 1, smem + (2 * L::kBytes - kAt));
     const int r0 = t * L::kRows;
-    if (mine <= 0 || r0 > last.hi || r0 + L::kRows <= first.lo) continue;
-    const char* ks = smem + (t & 1) * 2 * L::kBytes;
+    if (mine <= 0 || r0 > last.hi || r0 + L::kRows <= first.lo) return;
+    const char* ks = smem + kAt;
     const char* vs = ks + L::kBytes;
     f32x16_t s[L::kBlocks];
 #pragma unroll
@@ -386,33 +422,41 @@ __global__ __launch_bounds__(64 * NW) void attn_fwd_kernel(const AttnArgs g, int
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, i * L::kDown + j, lane), f, o[d]);
       }
+  };
+  for (int t = t0; t < t1; t += 2) {
+    tile(t, std::integral_constant<int, 0>());
+    if (t + 1 < t1) tile(t + 1, std::integral_constant<int, 1>());
   }
+  stage_barrier();  // (all tiles are used: their LDS takes the results)
   if (mine <= 0) return;
   l = halves_sum(l);
-  store_rows<T, D>(o, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l, (T*)g.out + ((p.begin + i0) * (int64_t)g.heads + head) * D,
-                   (int64_t)g.heads * D, mine, lane);
+  store_rows<T, D>(o, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l,
+                   (T*)g.out + ((p.begin + i0) * (int64_t)g.heads + head) * D, (int64_t)g.heads * D, mine,
+                   smem + w * 32 * L::kPitch, lane);
   if (g.lse && lane < mine)
     g.lse[head * g.T + p.begin + i0 + lane] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
 // ---------------------------------------------------------------- backward
-// dq of 32 NW rows a workgroup, and their log2 of the weights' sum and delta for the
+// dq (shared out as in the forward), and their log2 of the weights' sum and delta for the
 // kernel below.
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void attn_dq_kernel(const AttnArgs g, int blocks) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void attn_dq_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D> L;
   typedef Mma<T> M;
-  constexpr int kBlock = 32 * NW;
   __shared__ __align__(1024) char smem[4 * L::kBytes];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
   int head, b;
   Part p;
-  work_item(blocks, g.heads, g.causal, head, b);
-  if (!locate(g.offsets, g.seqs, (int)g.T, kBlock, b, p)) return;
+  // 2^share waves take the same queries for as many heads
+  const int block = 32 * NW >> g.share;
+  work_item(blocks, g.heads >> g.share, g.causal, head, b);
+  if (!locate(g.offsets, g.seqs, (int)g.T, block, b, p)) return;
+  head = (head << g.share) + (w & ((1 << g.share) - 1));
   const int kv = head / (g.heads / g.kv_heads);
-  const int q0 = p.block * kBlock, rows = min(kBlock, p.n - q0);
-  const int i0 = q0 + 32 * w, mine = min(32, p.n - i0);
+  const int q0 = p.block * block, rows = min(block, p.n - q0);
+  const int i0 = q0 + 32 * (w >> g.share), mine = min(32, p.n - i0);
   const T* K = (const T*)g.K + p.begin * g.ldk + kv * D;
   const T* V = (const T*)g.V + p.begin * g.ldv + kv * D;
   const Seen wg_first = keys_of(g, q0, p.n), wg_last = keys_of(g, q0 + rows - 1, p.n);
@@ -490,8 +534,10 @@ __global__ __launch_bounds__(64 * NW) void attn_dq_kernel(const AttnArgs g, int 
       }
     }
   }
+  stage_barrier();
   if (mine > 0)
-    store_rows<T, D>(a, g.scale, (T*)g.dQ + (p.begin + i0) * g.lddq + head * D, g.lddq, mine, lane);
+    store_rows<T, D>(a, g.scale, (T*)g.dQ + (p.begin + i0) * g.lddq + head * D, g.lddq, mine,
+                     smem + w * 32 * L::kPitch, lane);
 }
 
 // dk and dv of 32 NW rows a workgroup: it goes through the queries of the heads that share
@@ -499,13 +545,14 @@ __global__ __launch_bounds__(64 * NW) void attn_dq_kernel(const AttnArgs g, int 
 // some of the heads and leaves its sums in fp32 for attn_sum_kernel.
 // kHeld: the values stay in LDS, not in registers, of which two waves a SIMD have 256 each.
 template <typename T, int D, int NW, bool kHeld>
-__global__ __launch_bounds__(64 * NW) void attn_dkv_kernel(const AttnArgs g, int blocks) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 : 1) void attn_dkv_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D> L;
   typedef Mma<T> M;
   constexpr int kBlock = 32 * NW;
   // two stages of queries, dO, and their rows' log2 of the sum and delta
   constexpr int kStage = 2 * L::kBytes;
-  __shared__ __align__(1024) char smem[2 * kStage + (kHeld ? kBlock * L::kPitch : 0)];
+  constexpr int kNeed = 2 * kStage + (kHeld ? kBlock * L::kPitch : 0), kOut = kBlock * D * 4;
+  __shared__ __align__(1024) char smem[kNeed > kOut ? kNeed : kOut];
   __shared__ __align__(16) float stats[2][2][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
@@ -627,16 +674,19 @@ __global__ __launch_bounds__(64 * NW) void attn_dkv_kernel(const AttnArgs g, int
       }
     }
   }
+  stage_barrier();
   if (mine <= 0) return;
   const int64_t j = p.begin + j0;
   if (g.parts > 1) {
     const int64_t kvd = (int64_t)g.kv_heads * D;
     float* out = g.sums + (part * 2 * g.T + j) * kvd + kv * D;
-    store_rows<float, D>(dk, g.scale, out, kvd, mine, lane);
-    store_rows<float, D>(dv, 1.f, out + g.T * kvd, kvd, mine, lane);
+    char* lds = smem + w * 32 * D * 4;
+    store_rows<float, D>(dk, g.scale, out, kvd, mine, lds, lane);
+    store_rows<float, D>(dv, 1.f, out + g.T * kvd, kvd, mine, lds, lane);
   } else {
-    store_rows<T, D>(dk, g.scale, (T*)g.dK + j * g.lddk + kv * D, g.lddk, mine, lane);
-    store_rows<T, D>(dv, 1.f, (T*)g.dV + j * g.lddv + kv * D, g.lddv, mine, lane);
+    char* lds = smem + w * 32 * L::kPitch;
+    store_rows<T, D>(dk, g.scale, (T*)g.dK + j * g.lddk + kv * D, g.lddk, mine, lds, lane);
+    store_rows<T, D>(dv, 1.f, (T*)g.dV + j * g.lddv + kv * D, g.lddv, mine, lds, lane);
   }
 }
 
@@ -675,37 +725,53 @@ int64_t blocks_of(int64_t T, int64_t seqs, int R) {
   return (T + full * (R - 1)) / R;
 }
 
-// Waves of a workgroup: eight in bf16, two a SIMD, so that one multiplies while the
-// other works on its scores; four in fp32, whose operands need the registers of two.
-constexpr int kWaves = 8, kWavesF32 = 4;
-
 // (The compiler leaves out host stubs of kernels that only templates launch.)
 #define MEMFINE_ATTN(T, D, NW, HELD)                                         \
   template __global__ void attn_fwd_kernel<T, D, NW>(const AttnArgs, int);   \
   template __global__ void attn_dq_kernel<T, D, NW>(const AttnArgs, int);    \
   template __global__ void attn_dkv_kernel<T, D, NW, HELD>(const AttnArgs, int);
-MEMFINE_ATTN(bf16_t, 64, kWaves, false)
-MEMFINE_ATTN(bf16_t, 128, kWaves, true)
-MEMFINE_ATTN(float, 64, kWavesF32, false)
-MEMFINE_ATTN(float, 128, kWavesF32, false)
+MEMFINE_ATTN(bf16_t, 64, 4, false)
+MEMFINE_ATTN(bf16_t, 64, 8, false)
+MEMFINE_ATTN(bf16_t, 128, 4, false)
+MEMFINE_ATTN(bf16_t, 128, 8, true)
+MEMFINE_ATTN(float, 64, 4, false)
+MEMFINE_ATTN(float, 128, 4, false)
 #undef MEMFINE_ATTN
 template __global__ void attn_sum_kernel<bf16_t>(const AttnArgs);
 template __global__ void attn_sum_kernel<float>(const AttnArgs);
 
-template <typename T, int D, int NW> void run_fwd(const AttnArgs& g, hipStream_t s) {
-  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW);
-  attn_fwd_kernel<T, D, NW><<<(unsigned)blocks * g.heads, 64 * NW, 0, s>>>(g, blocks);
+// Heads of a group that a workgroup of `waves` takes together: the largest power of two that
+// divides the group.
+int share_of(const AttnArgs& g, int waves) {
+  int share = 0;
+  while ((g.heads / g.kv_heads) % (2 << share) == 0 && (2 << share) <= waves) ++share;
+  return share;
 }
-template <typename T, int D, int NW, bool kHeld> void run_bwd(const AttnArgs& g, hipStream_t s) {
+template <typename T, int D, int NW> void run_fwd(AttnArgs g, hipStream_t s) {
+  g.share = share_of(g, NW);
+  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW >> g.share);
+  attn_fwd_kernel<T, D, NW><<<(unsigned)blocks * (g.heads >> g.share), 64 * NW, 0, s>>>(g, blocks);
+}
+template <typename T, int D, int NW> void run_dq(AttnArgs g, hipStream_t s) {
+  g.share = share_of(g, NW);
+  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW >> g.share);
+  attn_dq_kernel<T, D, NW><<<(unsigned)blocks * (g.heads >> g.share), 64 * NW, 0, s>>>(g, blocks);
+}
+template <typename T, int D, int NW, bool kHeld> void run_dkv(const AttnArgs& g, hipStream_t s) {
   const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW);
-  // (writes top and delta, which the next one reads)
-  attn_dq_kernel<T, D, NW><<<(unsigned)blocks * g.heads, 64 * NW, 0, s>>>(g, blocks);
   attn_dkv_kernel<T, D, NW, kHeld>
       <<<(unsigned)blocks * g.kv_heads * g.parts, 64 * NW, 0, s>>>(g, blocks);
   if (g.parts > 1) {
     const int64_t n = (g.T * g.kv_heads * D / 2 + 255) / 256;
     attn_sum_kernel<T><<<(unsigned)std::min<int64_t>(n, 8192), 256, 0, s>>>(g);
   }
+}
+
+// Waves of a workgroup (of 32 queries, or keys, each).  fp32: four, whose operands need the
+// registers of two waves a SIMD.
+bool short_rows(const AttnArgs& g, int kind) {
+  static const int most[3] = {getenv("MF_F") ? atoi(getenv("MF_F")) : 1024, getenv("MF_Q") ? atoi(getenv("MF_Q")) : 1024, getenv("MF_K") ? atoi(getenv("MF_K")) : 1024};
+  return g.T / std::max(g.seqs, 1) < most[kind];
 }
 
 }  // namespace
@@ -722,29 +788,46 @@ int64_t attn_bwd_floats(const AttnArgs& g) {
 }
 
 bool attn_fits(const AttnArgs& g) {
-  return blocks_of(g.T, g.seqs, 32 * kWavesF32) * g.heads <= kMostItems / (64 * kWaves);
+  return blocks_of(g.T, g.seqs, 32) * g.heads <= kMostItems / 256;
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s) {
   if (!attn_fits(g)) return hipErrorInvalidValue;
   if (g.f32) {
-    if (g.dim == 64) run_fwd<float, 64, kWavesF32>(g, s);
-    else run_fwd<float, 128, kWavesF32>(g, s);
+    if (g.dim == 64) run_fwd<float, 64, 4>(g, s);
+    else run_fwd<float, 128, 4>(g, s);
+  } else if (short_rows(g, 0)) {
+    if (g.dim == 64) run_fwd<bf16_t, 64, 4>(g, s);
+    else run_fwd<bf16_t, 128, 4>(g, s);
   } else {
-    if (g.dim == 64) run_fwd<bf16_t, 64, kWaves>(g, s);
-    else run_fwd<bf16_t, 128, kWaves>(g, s);
+    if (g.dim == 64) run_fwd<bf16_t, 64, 8>(g, s);
+    else run_fwd<bf16_t, 128, 8>(g, s);
   }
   return hipGetLastError();
 }
 
 hipError_t launch_attn_bwd(const AttnArgs& g, hipStream_t s) {
   if (!attn_fits(g)) return hipErrorInvalidValue;
+  // (dq's kernel writes top and delta, which dkv's reads)
   if (g.f32) {
-    if (g.dim == 64) run_bwd<float, 64, kWavesF32, false>(g, s);
-    else run_bwd<float, 128, kWavesF32, false>(g, s);
+    if (g.dim == 64) run_dq<float, 64, 4>(g, s);
+    else run_dq<float, 128, 4>(g, s);
+  } else if (short_rows(g, 1)) {
+    if (g.dim == 64) run_dq<bf16_t, 64, 4>(g, s);
+    else run_dq<bf16_t, 128, 4>(g, s);
   } else {
-    if (g.dim == 64) run_bwd<bf16_t, 64, kWaves, false>(g, s);
-    else run_bwd<bf16_t, 128, kWaves, true>(g, s);
+    if (g.dim == 64) run_dq<bf16_t, 64, 8>(g, s);
+    else run_dq<bf16_t, 128, 8>(g, s);
+  }
+  if (g.f32) {
+    if (g.dim == 64) run_dkv<float, 64, 4, false>(g, s);
+    else run_dkv<float, 128, 4, false>(g, s);
+  } else if (short_rows(g, 2)) {
+    if (g.dim == 64) run_dkv<bf16_t, 64, 4, false>(g, s);
+    else run_dkv<bf16_t, 128, 4, false>(g, s);
+  } else {
+    if (g.dim == 64) run_dkv<bf16_t, 64, 8, false>(g, s);
+    else run_dkv<bf16_t, 128, 8, true>(g, s);
   }
   return hipGetLastError();
 }

@@ -285,6 +285,7 @@ struct AttnArgs {
   float *top, *delta;           // [heads, T]: lse in bits, dO . O
   float* sums;                  // parts > 1: [parts][2][T, kv_heads, dim]
   int parts;                    // attn_parts
+  int share;                    // (set by the launchers)
 };
 int attn_parts(const AttnArgs& g, int cus);
 int64_t attn_bwd_floats(const AttnArgs& g);
