@@ -466,13 +466,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
   Copy<T, D, NW> ck, cv;
   ck.init(g.ldk, w, lane);
   cv.init(g.ldv, w, lane);
-  auto issue = [&](int t) {
-    char* st = smem + (t & 1) * 2 * L::kBytes;
+  auto issue = [&](int t, char* st) {
     const int64_t r = (int64_t)t * L::kRows;
     ck.issue(K + r * g.ldk, g.ldk, p.n - (int)r, st, w);
     cv.issue(V + r * g.ldv, g.ldv, p.n - (int)r, st + L::kBytes, w);
   };
-  issue(t0);
+  issue(t0, smem);
   Frag<T> q[L::kSteps], d_o[L::kSteps];
   const int64_t ldo = (int64_t)g.heads * D, at = ((p.begin + i0) * (int64_t)g.heads + head) * D;
   load_rows<T, D>(q, (const T*)g.Q + (p.begin + i0) * g.ldq + head * D, g.ldq, mine, lane);
@@ -505,12 +504,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
   f32x16_t a[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) zero(a[i]);
-  for (int t = t0; t < t1; ++t) {
+  auto tile = [&](int t, auto stage) {  // (a constant stage, as in the forward)
+    constexpr int kAt = decltype(stage)::value * 2 * L::kBytes;
     stage_barrier();
-    if (t + 1 < t1) issue(t + 1);
+    if (t + 1 < t1) issue(t + 1, smem + (2 * L::kBytes - kAt));
     const int r0 = t * L::kRows;
-    if (mine <= 0 || r0 > last.hi || r0 + L::kRows <= first.lo) continue;
-    const char* ks = smem + (t & 1) * 2 * L::kBytes;
+    if (mine <= 0 || r0 > last.hi || r0 + L::kRows <= first.lo) return;
+    const char* ks = smem + kAt;
     const char* vs = ks + L::kBytes;
     const bool all = see_all(first, last, r0, L::kRows);
 #pragma unroll
@@ -533,6 +533,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
         for (int d = 0; d < D / 32; ++d) M::mma(L::col(ks, 32 * d, i * L::kDown + j, lane), f, a[d]);
       }
     }
+  };
+  for (int t = t0; t < t1; t += 2) {
+    tile(t, std::integral_constant<int, 0>());
+    if (t + 1 < t1) tile(t + 1, std::integral_constant<int, 1>());
   }
   stage_barrier();
   if (mine > 0)
@@ -574,8 +578,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
   cq.init(g.ldq, w, lane);
   co.init(ldo, w, lane);
   const int total = (h1 - h0) * tiles;
-  auto issue = [&](int x, int stage) {
-    const int head = kv * group + h0 + x / tiles, r0 = (t0 + x % tiles) * L::kRows;
+  int head = kv * group + h0, next = t0;  // of the tile to copy next
+  auto issue = [&](int stage) {
+    const int r0 = next * L::kRows;
     char* st = smem + stage * kStage;
     cq.issue((const T*)g.Q + (p.begin + r0) * g.ldq + head * D, g.ldq, p.n - r0, st, w);
     co.issue((const T*)g.dO + ((p.begin + r0) * (int64_t)g.heads + head) * D, ldo, p.n - r0,
@@ -585,6 +590,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
       const float* from = (w ? g.delta : g.top) + head * g.T + p.begin + r0;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_of(from, (uint32_t)min(p.n - r0, L::kRows) * 4),
                                                (lds_void*)stats[stage][w], 4, lane * 4, 0, 0, 0);
+    }
+    if (++next == t0 + tiles) {
+      next = t0;
+      ++head;
     }
   };
   const T* V = (const T*)g.V + (p.begin + k0) * g.ldv + kv * D;
@@ -600,7 +609,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
     load_rows<T, D>(v, V + 32 * w * g.ldv, g.ldv, mine, lane);
   }
   load_rows<T, D>(k, (const T*)g.K + (p.begin + j0) * g.ldk + kv * D, g.ldk, mine, lane);
-  issue(0, 0);
+  issue(0);
   f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
@@ -608,15 +617,18 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
     zero(dv[i]);
   }
   const float scale = g.scale * kLog2e;
-  for (int x = 0; x < total; ++x) {
+  int now = t0;  // the tile to use
+  auto tile = [&](int x, auto stage) {  // (a constant stage, as in the forward)
+    constexpr int kAt = decltype(stage)::value;
     stage_barrier();
-    if (x + 1 < total) issue(x + 1, (x + 1) & 1);
-    const int r0 = (t0 + x % tiles) * L::kRows;
-    if (mine <= 0 || r0 + L::kRows <= first.lo || r0 > last.hi) continue;
-    const char* qs = smem + (x & 1) * kStage;
+    const int r0 = now * L::kRows;
+    now = next;
+    if (x + 1 < total) issue(1 - kAt);
+    if (mine <= 0 || r0 + L::kRows <= first.lo || r0 > last.hi) return;
+    const char* qs = smem + kAt * kStage;
     const char* os = qs + L::kBytes;
     const bool all = see_all(first, last, r0, L::kRows);
-#pragma unroll 1
+#pragma unroll
     for (int i = 0; i < L::kBlocks; ++i) {
       // (what is read from LDS is read where it is used: registers are full)
       if constexpr (kHeld) asm volatile("" ::: "memory");
@@ -639,8 +651,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
         else M::mma(o[e & 1], v[e], dp);
         __builtin_amdgcn_sched_barrier(0);
       }
-      const float* top = &stats[x & 1][0][32 * i + 4 * hh];
-      const float* del = &stats[x & 1][1][32 * i + 4 * hh];
+      const float* top = &stats[kAt][0][32 * i + 4 * hh];
+      const float* del = &stats[kAt][1][32 * i + 4 * hh];
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
         const f32x4_t a = *(const f32x4_t*)(top + 2 * e);
@@ -673,6 +685,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
         }
       }
     }
+  };
+  for (int x = 0; x < total; x += 2) {
+    tile(x, std::integral_constant<int, 0>());
+    if (x + 1 < total) tile(x + 1, std::integral_constant<int, 1>());
   }
   stage_barrier();
   if (mine <= 0) return;
