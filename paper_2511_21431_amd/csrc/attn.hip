@@ -742,17 +742,28 @@ int64_t blocks_of(int64_t T, int64_t seqs, int R) {
 }
 
 // (The compiler leaves out host stubs of kernels that only templates launch.)
-#define MEMFINE_ATTN(T, D, NW, HELD)                                         \
-  template __global__ void attn_fwd_kernel<T, D, NW>(const AttnArgs, int);   \
-  template __global__ void attn_dq_kernel<T, D, NW>(const AttnArgs, int);    \
+#define MEMFINE_FWD(T, D, NW) template __global__ void attn_fwd_kernel<T, D, NW>(const AttnArgs, int);
+#define MEMFINE_DQ(T, D) template __global__ void attn_dq_kernel<T, D, 4>(const AttnArgs, int);
+#define MEMFINE_DKV(T, D, NW, HELD) \
   template __global__ void attn_dkv_kernel<T, D, NW, HELD>(const AttnArgs, int);
-MEMFINE_ATTN(bf16_t, 64, 4, false)
-MEMFINE_ATTN(bf16_t, 64, 8, false)
-MEMFINE_ATTN(bf16_t, 128, 4, false)
-MEMFINE_ATTN(bf16_t, 128, 8, true)
-MEMFINE_ATTN(float, 64, 4, false)
-MEMFINE_ATTN(float, 128, 4, false)
-#undef MEMFINE_ATTN
+MEMFINE_FWD(bf16_t, 64, 4)
+MEMFINE_FWD(bf16_t, 64, 8)
+MEMFINE_FWD(bf16_t, 128, 4)
+MEMFINE_FWD(bf16_t, 128, 8)
+MEMFINE_FWD(float, 64, 4)
+MEMFINE_FWD(float, 128, 4)
+MEMFINE_DQ(bf16_t, 64)
+MEMFINE_DQ(bf16_t, 128)
+MEMFINE_DQ(float, 64)
+MEMFINE_DQ(float, 128)
+MEMFINE_DKV(bf16_t, 64, 4, false)
+MEMFINE_DKV(bf16_t, 64, 8, false)
+MEMFINE_DKV(bf16_t, 128, 8, true)
+MEMFINE_DKV(float, 64, 4, false)
+MEMFINE_DKV(float, 128, 4, false)
+#undef MEMFINE_FWD
+#undef MEMFINE_DQ
+#undef MEMFINE_DKV
 template __global__ void attn_sum_kernel<bf16_t>(const AttnArgs);
 template __global__ void attn_sum_kernel<float>(const AttnArgs);
 
@@ -768,10 +779,13 @@ template <typename T, int D, int NW> void run_fwd(AttnArgs g, hipStream_t s) {
   const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW >> g.share);
   attn_fwd_kernel<T, D, NW><<<(unsigned)blocks * (g.heads >> g.share), 64 * NW, 0, s>>>(g, blocks);
 }
-template <typename T, int D, int NW> void run_dq(AttnArgs g, hipStream_t s) {
-  g.share = share_of(g, NW);
-  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW >> g.share);
-  attn_dq_kernel<T, D, NW><<<(unsigned)blocks * (g.heads >> g.share), 64 * NW, 0, s>>>(g, blocks);
+template <typename T, int D> void run_dq(AttnArgs g, hipStream_t s) {
+  // four waves, two workgroups a CU: the one's start and end lie under the other's
+  // products (64 heads of 4096 tokens in 8 groups 372 us, eight waves 389; 32 sequences of
+  // 256 tokens, 32 heads, 77 against 99)
+  g.share = share_of(g, 4);
+  const int blocks = (int)blocks_of(g.T, g.seqs, 128 >> g.share);
+  attn_dq_kernel<T, D, 4><<<(unsigned)blocks * (g.heads >> g.share), 256, 0, s>>>(g, blocks);
 }
 template <typename T, int D, int NW, bool kHeld> void run_dkv(const AttnArgs& g, hipStream_t s) {
   const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW);
@@ -783,12 +797,12 @@ template <typename T, int D, int NW, bool kHeld> void run_dkv(const AttnArgs& g,
   }
 }
 
-// Waves of a workgroup (of 32 queries, or keys, each).  fp32: four, whose operands need the
-// registers of two waves a SIMD.
-bool short_rows(const AttnArgs& g, int kind) {
-  static const int most[3] = {getenv("MF_F") ? atoi(getenv("MF_F")) : 1024, getenv("MF_Q") ? atoi(getenv("MF_Q")) : 1024, getenv("MF_K") ? atoi(getenv("MF_K")) : 1024};
-  return g.T / std::max(g.seqs, 1) < most[kind];
-}
+// Sequences so short, on average, that the starts and ends of workgroups weigh more than
+// what twice the rows save of copies: four waves, several workgroups a CU, else eight.  The
+// forward, 8192 tokens, 32 heads in 8 groups: sequences of 256 44 us against 56, of
+// 1024 105 against 113, of 2048 152 against 151, one 516 against 498.  dk and dv of 16
+// heads of 64: sequences of 668 tokens 38 us against 50, of 4096 68 against 60.
+bool short_rows(const AttnArgs& g) { return g.T < 2048 * (int64_t)g.seqs; }
 
 }  // namespace
 
@@ -812,7 +826,7 @@ hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s) {
   if (g.f32) {
     if (g.dim == 64) run_fwd<float, 64, 4>(g, s);
     else run_fwd<float, 128, 4>(g, s);
-  } else if (short_rows(g, 0)) {
+  } else if (short_rows(g)) {
     if (g.dim == 64) run_fwd<bf16_t, 64, 4>(g, s);
     else run_fwd<bf16_t, 128, 4>(g, s);
   } else {
@@ -826,24 +840,20 @@ hipError_t launch_attn_bwd(const AttnArgs& g, hipStream_t s) {
   if (!attn_fits(g)) return hipErrorInvalidValue;
   // (dq's kernel writes top and delta, which dkv's reads)
   if (g.f32) {
-    if (g.dim == 64) run_dq<float, 64, 4>(g, s);
-    else run_dq<float, 128, 4>(g, s);
-  } else if (short_rows(g, 1)) {
-    if (g.dim == 64) run_dq<bf16_t, 64, 4>(g, s);
-    else run_dq<bf16_t, 128, 4>(g, s);
+    if (g.dim == 64) {
+      run_dq<float, 64>(g, s);
+      run_dkv<float, 64, 4, false>(g, s);
+    } else {
+      run_dq<float, 128>(g, s);
+      run_dkv<float, 128, 4, false>(g, s);
+    }
+  } else if (g.dim == 64) {
+    run_dq<bf16_t, 64>(g, s);
+    if (short_rows(g)) run_dkv<bf16_t, 64, 4, false>(g, s);
+    else run_dkv<bf16_t, 64, 8, false>(g, s);
   } else {
-    if (g.dim == 64) run_dq<bf16_t, 64, 8>(g, s);
-    else run_dq<bf16_t, 128, 8>(g, s);
-  }
-  if (g.f32) {
-    if (g.dim == 64) run_dkv<float, 64, 4, false>(g, s);
-    else run_dkv<float, 128, 4, false>(g, s);
-  } else if (short_rows(g, 2)) {
-    if (g.dim == 64) run_dkv<bf16_t, 64, 4, false>(g, s);
-    else run_dkv<bf16_t, 128, 4, false>(g, s);
-  } else {
-    if (g.dim == 64) run_dkv<bf16_t, 64, 8, false>(g, s);
-    else run_dkv<bf16_t, 128, 8, true>(g, s);
+    run_dq<bf16_t, 128>(g, s);
+    run_dkv<bf16_t, 128, 8, true>(g, s);
   }
   return hipGetLastError();
 }
