@@ -832,14 +832,43 @@ def make_cache(k, v, k_scales=None, v_scales=None) -> Cache:
     if dt == torch.uint8:
         c.d_ks = _ptr(k_scales, held, dt, "k_scales")
         c.d_vs = _ptr(v_scales, held, dt, "v_scales")
-    c.tensors = (k, v, k_scales, v_scales)
-    c.device = k.device
+    c.tensors, c.on = (k, v, k_scales, v_scales), k.get_device()
+    if any(t is not None and t.get_device() != c.on for t in c.tensors):
+        raise ValueError("the cache's tensors are on several devices")
     return c
 
 
-def _head_rows(t, T, heads, dim, dtype, name):
-    """(address, elements between rows) of rows [T, heads, dim], whose heads are
-    contiguous."""
+def _device_of(t, name, stream):
+    """Index of the device that a call's tensors have to be on (this one's), and the
+    handle of its stream: without one, torch's current stream on the current device,
+    which then has to be theirs."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    d = t.get_device()
+    if d < 0 and t.numel() != 0:
+        raise ValueError(f"{name} must be a device tensor")
+    if stream is not None or d < 0:
+        return d, _stream(stream)
+    C = _torch()._C
+    if d != C._cuda_getDevice():
+        raise ValueError(f"tensors on {t.device}, which is not the current device")
+    return d, C._cuda_getCurrentRawStream(d)
+
+
+def _on(t, d, shape_tuple, dtype, name) -> int:
+    """_ptr of a tensor on device d."""
+    if t is not None and t.get_device() != d:
+        if t.numel() == 0 or not t.is_cuda:
+            return _ptr(t, shape_tuple, dtype, name)  # (empty, or refused there)
+        raise ValueError(f"{name}: tensors on device {d} and on {t.device}")
+    if t is not None and t.shape == shape_tuple and t.dtype == dtype and t.is_contiguous():
+        return t.data_ptr()
+    return _ptr(t, shape_tuple, dtype, name)
+
+
+def _head_rows(t, d, T, heads, dim, dtype, name):
+    """(address, elements between rows) of rows [T, heads, dim] on device d, whose heads
+    are contiguous."""
     if t is None:
         raise ValueError(f"{name} is required")
     if t.shape != (T, heads, dim):
@@ -849,22 +878,11 @@ def _head_rows(t, T, heads, dim, dtype, name):
     ld, head, one = t.stride()
     if one != 1 or (head != dim and heads != 1):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    if not t.is_cuda:
-        if t.numel() == 0:
-            return 0, heads * dim
-        raise ValueError(f"{name} must be a device tensor")
+    if t.get_device() != d and t.numel() != 0:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        raise ValueError(f"{name}: tensors on device {d} and on {t.device}")
     return t.data_ptr(), (ld if T > 1 else heads * dim)
-
-
-def _same_device(first, stream, *others):
-    """All tensors on one device, which the call's stream belongs to: without one, the
-    current device."""
-    d = first.device
-    for t in others:
-        if t is not None and t.device != d:
-            raise ValueError(f"tensors on {d} and {t.device}")
-    if stream is None and d.type == "cuda" and d.index != _torch().cuda.current_device():
-        raise ValueError(f"tensors on {d}, which is not the current device")
 
 
 def _attn_dt(attn: Attn):
@@ -887,15 +905,15 @@ def memfine_attn_fwd(attn: Attn, offsets, Q, K, V, O, lse=None, stream=None) -> 
     torch = _torch()
     seqs, dt = _seqs(offsets), _attn_dt(attn)
     H, Hk, D = attn.heads, attn.kv_heads, attn.dim
-    T = Q.shape[0] if Q is not None else 0
-    q, ldq = _head_rows(Q, T, H, D, dt, "Q")
-    k, ldk = _head_rows(K, T, Hk, D, dt, "K")
-    v, ldv = _head_rows(V, T, Hk, D, dt, "V")
-    o, s = _ptr(O, (T, H, D), dt, "O"), _opt(lse, (H, T), torch.float32, "lse")
-    _same_device(Q, stream, K, V, O, lse, offsets)
+    dev, st = _device_of(Q, "Q", stream)
+    T = Q.shape[0]
+    q, ldq = _head_rows(Q, dev, T, H, D, dt, "Q")
+    k, ldk = _head_rows(K, dev, T, Hk, D, dt, "K")
+    v, ldv = _head_rows(V, dev, T, Hk, D, dt, "V")
+    o, s = _on(O, dev, (T, H, D), dt, "O"), None if lse is None else _on(lse, dev, (H, T), torch.float32, "lse")
     rc = lib().memfine_attn_fwd(
-        T, seqs, ctypes.byref(attn), _ptr(offsets, (seqs + 1,), torch.int32, "offsets"), q, ldq, k,
-        ldk, v, ldv, o, s, _stream(stream))
+        T, seqs, ctypes.byref(attn), _on(offsets, dev, (seqs + 1,), torch.int32, "offsets"), q, ldq, k,
+        ldk, v, ldv, o, s, st)
     _check(rc, "memfine_attn_fwd")
 
 
@@ -906,19 +924,19 @@ def memfine_attn_bwd(attn: Attn, offsets, Q, K, V, O, lse, dO, dQ, dK, dV, alloc
     torch = _torch()
     seqs, dt = _seqs(offsets), _attn_dt(attn)
     H, Hk, D = attn.heads, attn.kv_heads, attn.dim
-    T = Q.shape[0] if Q is not None else 0
-    q, ldq = _head_rows(Q, T, H, D, dt, "Q")
-    k, ldk = _head_rows(K, T, Hk, D, dt, "K")
-    v, ldv = _head_rows(V, T, Hk, D, dt, "V")
-    dq, lddq = _head_rows(dQ, T, H, D, dt, "dQ")
-    dk, lddk = _head_rows(dK, T, Hk, D, dt, "dK")
-    dv, lddv = _head_rows(dV, T, Hk, D, dt, "dV")
-    o, s = _ptr(O, (T, H, D), dt, "O"), _ptr(lse, (H, T), torch.float32, "lse")
-    do = _ptr(dO, (T, H, D), dt, "dO")
-    _same_device(Q, stream, K, V, O, lse, dO, dQ, dK, dV, offsets)
+    dev, st = _device_of(Q, "Q", stream)
+    T = Q.shape[0]
+    q, ldq = _head_rows(Q, dev, T, H, D, dt, "Q")
+    k, ldk = _head_rows(K, dev, T, Hk, D, dt, "K")
+    v, ldv = _head_rows(V, dev, T, Hk, D, dt, "V")
+    dq, lddq = _head_rows(dQ, dev, T, H, D, dt, "dQ")
+    dk, lddk = _head_rows(dK, dev, T, Hk, D, dt, "dK")
+    dv, lddv = _head_rows(dV, dev, T, Hk, D, dt, "dV")
+    o, s = _on(O, dev, (T, H, D), dt, "O"), _on(lse, dev, (H, T), torch.float32, "lse")
+    do = _on(dO, dev, (T, H, D), dt, "dO")
     rc = lib().memfine_attn_bwd(
-        T, seqs, ctypes.byref(attn), _ptr(offsets, (seqs + 1,), torch.int32, "offsets"), q, ldq, k,
-        ldk, v, ldv, o, s, do, dq, lddq, dk, lddk, dv, lddv, _alloc_arg(allocator), _stream(stream))
+        T, seqs, ctypes.byref(attn), _on(offsets, dev, (seqs + 1,), torch.int32, "offsets"), q, ldq, k,
+        ldk, v, ldv, o, s, do, dq, lddq, dk, lddk, dv, lddv, _alloc_arg(allocator), st)
     _check(rc, "memfine_attn_bwd")
 
 
@@ -929,11 +947,13 @@ def memfine_attn_bwd_workspace_bytes(attn: Attn, T: int) -> int:
     return int(v)
 
 
-def _rotary(cos, sin, dim, interleaved):
+def _rotary(cos, sin, d, dim, interleaved):
     torch = _torch()
-    n, _ = _rows(cos, "cos")
-    return Rotary(_ptr(cos, (n, dim // 2), torch.float32, "cos"),
-                  _ptr(sin, (n, dim // 2), torch.float32, "sin"), n, bool(interleaved))
+    if cos is None or cos.dim() != 2:
+        raise ValueError("cos: expected [positions, dim / 2]")
+    shape = (cos.shape[0], dim // 2)
+    return Rotary(_on(cos, d, shape, torch.float32, "cos"), _on(sin, d, shape, torch.float32, "sin"),
+                  shape[0], bool(interleaved))
 
 
 def memfine_rope(offsets, cos, sin, X, Y, interleaved: bool = False, inverse: bool = False,
@@ -945,22 +965,29 @@ def memfine_rope(offsets, cos, sin, X, Y, interleaved: bool = False, inverse: bo
     if X is None or X.dim() != 3:
         raise ValueError("X: expected [T, heads, dim]")
     T, H, D = X.shape
-    r = _rotary(cos, sin, D, interleaved)
-    x, ldx = _head_rows(X, T, H, D, X.dtype, "X")
-    y, ldy = _head_rows(Y, T, H, D, X.dtype, "Y")
-    _same_device(X, stream, Y, cos, sin, offsets)
+    dev, st = _device_of(X, "X", stream)
+    r = _rotary(cos, sin, dev, D, interleaved)
+    x, ldx = _head_rows(X, dev, T, H, D, X.dtype, "X")
+    y, ldy = _head_rows(Y, dev, T, H, D, X.dtype, "Y")
     rc = lib().memfine_rope(
-        T, seqs, _ptr(offsets, (seqs + 1,), torch.int32, "offsets"), H, D, _dtype_of(X, "X"),
-        ctypes.byref(r), int(bool(inverse)), x, ldx, y, ldy, _stream(stream))
+        T, seqs, _on(offsets, dev, (seqs + 1,), torch.int32, "offsets"), H, D, _dtype_of(X, "X"),
+        ctypes.byref(r), int(bool(inverse)), x, ldx, y, ldy, st)
     _check(rc, "memfine_rope")
 
 
-def _table(table, lengths):
+def _table(table, lengths, d):
     """(sequences, width, addresses) of a table of pages and the sequences' lengths."""
     torch = _torch()
-    n, width = _rows(table, "table")
-    return (n, width, _ptr(table, (n, width), torch.int32, "table"),
-            _ptr(lengths, (n,), torch.int32, "lengths"))
+    if table is None or table.dim() != 2:
+        raise ValueError("table: expected [sequences, pages]")
+    n, width = shape = table.shape
+    return (n, width, _on(table, d, shape, torch.int32, "table"),
+            _on(lengths, d, (n,), torch.int32, "lengths"))
+
+
+def _cache_on(cache, d):
+    if cache.on != d and d >= 0:
+        raise ValueError(f"tensors on device {d} and a cache on {cache.on}")
 
 
 def memfine_kv_write(cache: Cache, table, lengths, K, V, offsets=None, Q=None, R=None, cos=None,
@@ -970,11 +997,12 @@ def memfine_kv_write(cache: Cache, table, lengths, K, V, offsets=None, Q=None, R
     tokens' positions if cos and sin are given.  offsets None: one row a sequence."""
     torch = _torch()
     bf = torch.bfloat16
-    n, width, tp, lp = _table(table, lengths)
-    Hk, D = cache.kv_heads, cache.dim
-    T = K.shape[0] if K is not None else 0
-    k, ldk = _head_rows(K, T, Hk, D, bf, "K")
-    v, ldv = _head_rows(V, T, Hk, D, bf, "V")
+    dev, st = _device_of(K, "K", stream)
+    _cache_on(cache, dev)
+    n, width, tp, lp = _table(table, lengths, dev)
+    Hk, D, T = cache.kv_heads, cache.dim, K.shape[0]
+    k, ldk = _head_rows(K, dev, T, Hk, D, bf, "K")
+    v, ldv = _head_rows(V, dev, T, Hk, D, bf, "V")
     if (Q is None) != (R is None):
         raise ValueError("Q and R: both or neither")
     H, q, ldq, rp = 0, None, 0, None
@@ -982,17 +1010,16 @@ def memfine_kv_write(cache: Cache, table, lengths, K, V, offsets=None, Q=None, R
         if Q.dim() != 3:
             raise ValueError("Q: expected [T, heads, dim]")
         H = Q.shape[1]
-        q, ldq = _head_rows(Q, T, H, D, bf, "Q")
-        rp = _ptr(R, (T, H, D), bf, "R")
+        q, ldq = _head_rows(Q, dev, T, H, D, bf, "Q")
+        rp = _on(R, dev, (T, H, D), bf, "R")
     if (cos is None) != (sin is None):
         raise ValueError("cos and sin: both or neither")
-    r = None if cos is None else ctypes.byref(_rotary(cos, sin, D, interleaved))
+    r = None if cos is None else ctypes.byref(_rotary(cos, sin, dev, D, interleaved))
     op = None
     if offsets is not None:
-        op = _ptr(offsets, (n + 1,), torch.int32, "offsets")
-    _same_device(K, stream, V, table, lengths, offsets, Q, R, cos, sin, cache)
+        op = _on(offsets, dev, (n + 1,), torch.int32, "offsets")
     rc = lib().memfine_kv_write(ctypes.byref(cache), T, n, width, tp, lp, op, r, k, ldk, v, ldv, H,
-                                q, ldq, rp, _stream(stream))
+                                q, ldq, rp, st)
     _check(rc, "memfine_kv_write")
 
 
@@ -1001,13 +1028,15 @@ def memfine_attn_decode(attn: Attn, cache: Cache, table, lengths, Q, O, lse=None
     """Attention of one token a sequence, Q bfloat16 [sequences, heads, dim], over the cached
     tokens; into O alike and lse float [sequences, heads]."""
     torch = _torch()
-    n, width, tp, lp = _table(table, lengths)
+    dev, st = _device_of(Q, "Q", stream)
+    _cache_on(cache, dev)
+    n, width, tp, lp = _table(table, lengths, dev)
     H, D = attn.heads, attn.dim
-    q, ldq = _head_rows(Q, n, H, D, torch.bfloat16, "Q")
-    o, s = _ptr(O, (n, H, D), torch.bfloat16, "O"), _opt(lse, (n, H), torch.float32, "lse")
-    _same_device(Q, stream, O, lse, table, lengths, cache)
+    q, ldq = _head_rows(Q, dev, n, H, D, torch.bfloat16, "Q")
+    o = _on(O, dev, (n, H, D), torch.bfloat16, "O")
+    s = None if lse is None else _on(lse, dev, (n, H), torch.float32, "lse")
     rc = lib().memfine_attn_decode(ctypes.byref(attn), ctypes.byref(cache), n, width, tp, lp, q,
-                                   ldq, o, s, _alloc_arg(allocator), _stream(stream))
+                                   ldq, o, s, _alloc_arg(allocator), st)
     _check(rc, "memfine_attn_decode")
 
 

@@ -63,49 +63,105 @@ __device__ __forceinline__ Span span_of(const DecodeArgs& g, int b) {
 }
 __device__ __forceinline__ int steps_of(const Span& s) { return (s.n - s.lo0 + kStep - 1) / kStep; }
 
-// Sum over a workgroup's 256 threads in every one, and the sum over those before
-// this one.  Ends and begins with a barrier's worth of order on `part`.
-__device__ __forceinline__ int64_t scan256(int64_t v, int64_t* part, int64_t& before) {
+// Sum over the lanes up to this one, by DPP: row shifts, then each row's last lane to the next.
+template <int kCtrl, int kRows> __device__ __forceinline__ int add_dpp(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+  v = add_dpp<0x111, 0xf>(v);
+  v = add_dpp<0x112, 0xf>(v);
+  v = add_dpp<0x114, 0xf>(v);
+  v = add_dpp<0x118, 0xf>(v);
+  v = add_dpp<0x142, 0xa>(v);
+  return add_dpp<0x143, 0xc>(v);
+}
+// a / b, in 32 bits where these hold a (all but caches of billions of tokens).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (uint64_t)a >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
+// The steps of all sequences (of one pair each), for every thread of a workgroup, and
+// the steps before some sequences.  Up to 64 sequences a wave sums them by itself;
+// more are summed by the workgroup's 256 threads, `per` to each.
+struct Plan {
+  int64_t total;
+  int64_t before;  // steps before this lane's sequence (few), or before this thread's
+  int n, per;      // few: the lane's sequence's steps
+};
+__device__ __forceinline__ bool few(const DecodeArgs& g) { return g.seqs <= 64; }
+__device__ __forceinline__ Plan plan_of(const DecodeArgs& g, int64_t* part) {
+  Plan p;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if (few(g)) {
+    p.per = 1;
+    p.n = steps_of(span_of(g, min(lane, g.seqs - 1)));
+    if (lane >= g.seqs) p.n = 0;
+    const int inc = wave_scan(p.n);  // (64 sequences of at most 2^23 steps)
+    p.total = __builtin_amdgcn_readlane(inc, 63);
+    p.before = inc - p.n;
+    return p;
+  }
+  p.per = (g.seqs + 255) / 256;
+  int64_t v = 0;
+  const int first = threadIdx.x * p.per, last = min(first + p.per, g.seqs);
+  for (int b = first; b < last; ++b) v += steps_of(span_of(g, b));
   int64_t inc = v;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int64_t y = __shfl_up(inc, o, 64);
     if (lane >= o) inc += y;
   }
-  __syncthreads();
   if (lane == 63) part[w] = inc;
   __syncthreads();
-  int64_t total = 0, head = 0;
+  p.total = 0;
+  p.before = inc - v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (i < w) head += part[i];
-    total += part[i];
+    if (i < w) p.before += part[i];
+    p.total += part[i];
   }
-  before = head + inc - v;
-  return total;
-}
-
-// Steps of all sequences, and of those before each thread's share of them
-// (sequences t per .. t per + per - 1 for thread t).
-struct Plan {
-  int64_t before;   // steps of one key-value head before this thread's sequences
-  int64_t total;    // of all sequences
-  int per;
-};
-__device__ __forceinline__ Plan plan_of(const DecodeArgs& g, int64_t* part) {
-  Plan p;
-  p.per = (g.seqs + 255) / 256;
-  int64_t v = 0;
-  const int first = threadIdx.x * p.per, last = min(first + p.per, g.seqs);
-  for (int b = first; b < last; ++b) v += steps_of(span_of(g, b));
-  p.total = scan256(v, part, p.before);
   return p;
+}
+// The sequence whose pairs' steps hold step `at` < total pairs, and the steps of those
+// before it; the same in every thread.
+__device__ __forceinline__ int sequence_at(const DecodeArgs& g, const Plan& p, int64_t at, int64_t* found,
+                                           int64_t& base) {
+  if (few(g)) {
+    const uint64_t past = __ballot((p.before + p.n) * g.pairs > at);
+    const int b = __builtin_ctzll(past);
+    base = (int64_t)__builtin_amdgcn_readlane((int)p.before, b) * g.pairs;
+    return b;
+  }
+  int64_t before = p.before;
+  const int first = threadIdx.x * p.per, last = min(first + p.per, g.seqs);
+  for (int b = first; b < last; ++b) {
+    const int64_t n = steps_of(span_of(g, b));
+    if (at >= before * g.pairs && at < (before + n) * g.pairs) {
+      found[0] = b;
+      found[1] = before * g.pairs;
+    }
+    before += n;
+  }
+  __syncthreads();
+  base = found[1];
+  return __builtin_amdgcn_readfirstlane((int)found[0]);
+}
+// The steps before sequence b.
+__device__ __forceinline__ int64_t steps_before(const DecodeArgs& g, const Plan& p, int b, int64_t* found) {
+  if (few(g)) return __builtin_amdgcn_readlane((int)p.before, b);
+  const int first = threadIdx.x * p.per;
+  if (b >= first && b < first + p.per) {
+    int64_t before = p.before;
+    for (int i = first; i < b; ++i) before += steps_of(span_of(g, i));
+    found[0] = before;
+  }
+  __syncthreads();
+  return found[0];
 }
 // Steps a workgroup takes.
 __device__ __forceinline__ int64_t share_of(const DecodeArgs& g, int64_t total) {
   const int64_t all = total * g.pairs;
-  return std::max<int64_t>((all + g.groups - 1) / g.groups, 1);
+  return std::max<int64_t>(quotient(all + g.groups - 1, g.groups), 1);
 }
 
 // --------------------------------------------------------------- operands
@@ -178,29 +234,16 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(const DecodeArgs g) {
   __shared__ __align__(1024) char smem[4 * LV::kBytes > 4 * 16 * (D + 4) * 4 ? 4 * LV::kBytes
                                                                              : 4 * 16 * (D + 4) * 4];
   __shared__ int64_t part[4];
-  __shared__ int64_t found[3];
+  __shared__ int64_t found[2];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lg = lane >> 4, col = lane & 15;
   const Plan plan = plan_of(g, part);
   const int64_t share = share_of(g, plan.total), end = std::min(plan.total * g.pairs, (blockIdx.x + 1) * share);
   int64_t at = blockIdx.x * share;
   if (at >= end) return;
-  // the sequence that holds step `at`: all pairs of a sequence follow each other
-  {
-    int64_t before = plan.before;
-    const int first = threadIdx.x * plan.per, last = min(first + plan.per, g.seqs);
-    for (int b = first; b < last; ++b) {
-      const int64_t n = steps_of(span_of(g, b));
-      if (at >= before * g.pairs && at < (before + n) * g.pairs) {
-        found[0] = b;
-        found[1] = before * g.pairs;
-      }
-      before += n;
-    }
-    __syncthreads();
-  }
-  int b = __builtin_amdgcn_readfirstlane((int)found[0]);
-  int64_t base = found[1];
+  // (all pairs of a sequence follow each other)
+  int64_t base;
+  int b = sequence_at(g, plan, at, found, base);
   const float c = g.scale * kLog2e;
   char* mine = smem + w * LV::kBytes;
   bool first_run = true;
@@ -212,7 +255,7 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(const DecodeArgs g) {
     const int32_t* table = g.table + (int64_t)b * g.width;
     const int64_t stop = std::min(end, base + (int64_t)n * g.pairs);
     while (at < stop) {
-      const int pair = (int)((at - base) / n), x0 = (int)((at - base) % n);
+      const int pair = (int)quotient(at - base, n), x0 = (int)(at - base - (int64_t)pair * n);
       const int x1 = (int)std::min<int64_t>(n, x0 + (stop - at));
       const int kv = pair / g.tiles, h0 = kv * g.group + pair % g.tiles * 16;
       const int heads = min(16, g.group - pair % g.tiles * 16);
@@ -424,15 +467,7 @@ __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs g) {
   __shared__ __align__(16) float mem[kAcross][kRow];
   const Plan plan = plan_of(g, part);
   const int b = blockIdx.x / g.heads, head = blockIdx.x % g.heads;
-  {
-    const int first = threadIdx.x * plan.per;
-    if (b >= first && b < first + plan.per) {
-      int64_t before = plan.before;
-      for (int i = first; i < b; ++i) before += steps_of(span_of(g, i));
-      found[0] = before;
-    }
-    __syncthreads();
-  }
+  const int64_t before = steps_before(g, plan, b, found);
   const int n = steps_of(span_of(g, b));
   const int d = threadIdx.x % (D / 4) * 4, y = threadIdx.x / (D / 4);
   const int64_t at = (int64_t)b * g.heads + head;
@@ -446,8 +481,8 @@ __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs g) {
   }
   const int kv = head / g.group, in = head % g.group;
   const int64_t share = share_of(g, plan.total);
-  const int64_t s0 = found[0] * g.pairs + (int64_t)(kv * g.tiles + in / 16) * n, s1 = s0 + n;
-  const int64_t w0 = s0 / share, w1 = (s1 - 1) / share;
+  const int64_t s0 = before * g.pairs + (int64_t)(kv * g.tiles + in / 16) * n, s1 = s0 + n;
+  const int64_t w0 = quotient(s0, share), w1 = quotient(s1 - 1, share);
   if (w0 == w1) return;  // one workgroup had it all
   auto row = [&](int64_t w) {  // a run's first part is part 0
     const int which = w == w0 && w0 * share < s0 ? 1 : 0;

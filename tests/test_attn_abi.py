@@ -141,7 +141,7 @@ class Device:
     """A device tensor, as far as the binding looks."""
     is_cuda = True
 
-    def __init__(self, *shape, dtype=bf, strides=None, device="cpu"):
+    def __init__(self, *shape, dtype=bf, strides=None, device="cuda:0"):
         self.shape, self.dtype, self.device = torch.Size(shape), dtype, torch.device(device)
         s = [1]
         for n in reversed(shape[1:]):
@@ -150,6 +150,9 @@ class Device:
 
     def is_contiguous(self):
         return self.whole
+
+    def get_device(self):
+        return self.device.index
 
     def stride(self):
         return self.strides
