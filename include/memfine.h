@@ -598,8 +598,8 @@ int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chun
  * outside is neither read nor written, whatever the offsets hold); a sequence may be
  * empty, and rows of none are left as they were.
  *
- * Pointers as above (16 bytes), but d_offsets, d_table, d_lengths, d_lse and
- * d_delta's like, aligned as their elements.  dim is 64 or 128, heads at most 1024
+ * Pointers as above (16 bytes), but d_offsets, d_table, d_lengths and d_lse, aligned
+ * as their elements.  dim is 64 or 128, heads at most 1024
  * (MEMFINE_ERR_UNSUPPORTED otherwise).
  */
 typedef struct memfine_attn {
@@ -632,9 +632,10 @@ int memfine_attn_fwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32
  *   dQ_i = sum_j ds_ij k_j;  dK_j = sum_i ds_ij q_i;  dV_j = sum_i p_ij dO_i
  * dK and dV add up over the heads that share a key-value head.  dQ, dK and dV are
  * overwritten, rows of no sequence left as they were; they must not overlap the
- * inputs.  Every sum has a fixed order.  Working memory (delta,
- * memfine_attn_bwd_workspace_bytes; < 0: invalid arguments) comes from `alloc` as
- * for the layer's calls.
+ * inputs.  Every sum has a fixed order, which depends on T, seqs, the heads and the
+ * device's compute units alone.  Working memory (two floats a row and head, and partial
+ * dK and dV where keys are few; at most memfine_attn_bwd_workspace_bytes, < 0: invalid
+ * arguments) comes from `alloc` as for the layer's calls.
  */
 int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
                      const void* d_Q, int64_t ld_q, const void* d_K, int64_t ld_k, const void* d_V,

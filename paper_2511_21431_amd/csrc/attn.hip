@@ -807,11 +807,16 @@ bool short_rows(const AttnArgs& g) { return g.T < 2048 * (int64_t)g.seqs; }
 }  // namespace
 
 // Parts of dK and dV: a workgroup for 256 keys (fp32: 128) goes through all queries of
-// the group; where that leaves fewer than two a CU the group's heads are shared out.
+// the group; where that leaves fewer than two a CU the group's heads are shared out, but not
+// below 4096 queries a part, under which the parts' sums cost more than the even load gives
+// (32 heads in 8 groups, without and with two parts: one sequence of 8192 tokens 2.41 ms and
+// 1.72, 8 of 1024 354 us and 409; 64 heads in 8 groups, 4096 tokens, one to four parts
+// 1.22, 0.97 and 0.91 ms with one, three and four).
 int attn_parts(const AttnArgs& g, int cus) {
-  const int64_t items = (g.T + 255) / 256 * g.kv_heads;
+  const int64_t items = (g.T + 255) / 256 * g.kv_heads, group = g.heads / g.kv_heads;
   const int64_t want = (2 * (int64_t)cus + items - 1) / items;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(want, g.heads / g.kv_heads));
+  const int64_t most = std::min(group, group * g.T / std::max(g.seqs, 1) / 4096);
+  return (int)std::max<int64_t>(1, std::min(want, most));
 }
 int64_t attn_bwd_floats(const AttnArgs& g) {
   return (2 * g.heads + (g.parts > 1 ? 2 * (int64_t)g.parts * g.kv_heads * g.dim : 0)) * g.T;
