@@ -596,7 +596,8 @@ int64_t memfine_moe_mxw_workspace_bytes(const memfine_shape* shape, int32_t chun
  * Packed sequences: sequence b is rows [d_offsets[b], d_offsets[b + 1]) of T,
  * d_offsets int32 [seqs + 1] on the device, ascending, within [0, T] (what lies
  * outside is neither read nor written, whatever the offsets hold); a sequence may be
- * empty, and rows of none are left as they were.
+ * empty, and rows of none are left as they were.  T, its sequences rounded up to 32
+ * rows, times heads is at most 2^27 for the attention (UNSUPPORTED beyond).
  *
  * Pointers as above (16 bytes), but d_offsets, d_table, d_lengths and d_lse, aligned
  * as their elements.  dim is 64 or 128, heads at most 1024

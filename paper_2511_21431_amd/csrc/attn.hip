@@ -822,8 +822,9 @@ int64_t attn_bwd_floats(const AttnArgs& g) {
   return (2 * g.heads + (g.parts > 1 ? 2 * (int64_t)g.parts * g.kv_heads * g.dim : 0)) * g.T;
 }
 
+// (blocks of 32 rows: workgroups of 512 threads for more rows, or of several heads, are fewer)
 bool attn_fits(const AttnArgs& g) {
-  return blocks_of(g.T, g.seqs, 32) * g.heads <= kMostItems / 256;
+  return blocks_of(g.T, g.seqs, 32) * g.heads <= kMostItems / 512;
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s) {

@@ -54,7 +54,8 @@ def test_packed_refusals():
     for kw in (dict(lse=N), dict(dO=N), dict(dQ=N), dict(dK=N), dict(dV=N), dict(dK=ODD), dict(lddq=64),
                dict(lddk=129), dict(lddv=120)):
         assert bwd(**kw) == INVALID, kw
-    for kw in (dict(T=2 ** 31), dict(seqs=2 ** 20 + 1), dict(ldk=2 ** 20 + 8), dict(T=2 ** 31 - 1, seqs=1)):
+    for kw in (dict(T=2 ** 31), dict(seqs=2 ** 20 + 1), dict(ldk=2 ** 20 + 8), dict(T=2 ** 31 - 1, seqs=1),
+               dict(T=2 ** 24 + 1), dict(T=2 ** 20, seqs=2 ** 20)):
         assert fwd(**kw) == bwd(**kw) == UNSUPPORTED, kw
     # nothing to do
     for kw in (dict(T=0), dict(seqs=0)):

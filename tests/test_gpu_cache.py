@@ -282,7 +282,7 @@ def check_decode(mf, p, lens, H, window=0, seed=0, tokens=None, q=None, want_lse
         if want_lse:
             fin = np.isfinite(rl)
             assert np.array_equal(gl[b][~fin], rl[~fin])
-            assert np.all(np.abs(gl[b] - rl)[fin] <= (ds + steps + 4 * U * np.abs(rl))[fin])
+            assert np.all(np.abs(gl[b][fin] - rl[fin]) <= (ds + steps)[fin] + 4 * U * np.abs(rl[fin]))
     return O, lse, dev, attn
 
 
