@@ -635,15 +635,14 @@ int memfine_attn_fwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32
  * overwritten, rows of no sequence left as they were; they must not overlap the
  * inputs.  Every sum has a fixed order, which depends on T, seqs, the heads and the
  * device's compute units alone.  Working memory (two floats a row and head, and partial
- * dK and dV where keys are few; at most memfine_attn_bwd_workspace_bytes, < 0: invalid
- * arguments) comes from `alloc` as for the layer's calls.
+ * dK and dV where keys are few: memfine_attn_bwd_workspace_bytes, < 0: invalid arguments) comes from `alloc` as for the layer's calls.
  */
 int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
                      const void* d_Q, int64_t ld_q, const void* d_K, int64_t ld_k, const void* d_V,
                      int64_t ld_v, const void* d_O, const float* d_lse, const void* d_dO,
                      void* d_dQ, int64_t ld_dq, void* d_dK, int64_t ld_dk, void* d_dV,
                      int64_t ld_dv, const memfine_allocator* alloc, void* stream);
-int64_t memfine_attn_bwd_workspace_bytes(int64_t T, const memfine_attn* a);
+int64_t memfine_attn_bwd_workspace_bytes(int64_t T, int32_t seqs, const memfine_attn* a);
 
 /*
  * Rotation by position, of rows of packed sequences (position: the row's place in

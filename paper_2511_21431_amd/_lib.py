@@ -185,7 +185,7 @@ _SIGS = {
     "memfine_attn_fwd": (ctypes.c_int, [I64, I32, ATP, P, P, I64, P, I64, P, I64, P, P, P]),
     "memfine_attn_bwd": (ctypes.c_int, [I64, I32, ATP, P, P, I64, P, I64, P, I64, P, P, P, P, I64,
                                         P, I64, P, I64, ALP, P]),
-    "memfine_attn_bwd_workspace_bytes": (I64, [I64, ATP]),
+    "memfine_attn_bwd_workspace_bytes": (I64, [I64, I32, ATP]),
     "memfine_rope": (ctypes.c_int, [I64, I32, P, I32, I32, I32, RTP, I32, P, I64, P, I64, P]),
     "memfine_kv_write": (ctypes.c_int, [CHP, I64, I32, I32, P, P, P, RTP, P, I64, P, I64, I32, P,
                                         I64, P, P]),
@@ -940,8 +940,8 @@ def memfine_attn_bwd(attn: Attn, offsets, Q, K, V, O, lse, dO, dQ, dK, dV, alloc
     _check(rc, "memfine_attn_bwd")
 
 
-def memfine_attn_bwd_workspace_bytes(attn: Attn, T: int) -> int:
-    v = lib().memfine_attn_bwd_workspace_bytes(int(T), ctypes.byref(attn))
+def memfine_attn_bwd_workspace_bytes(attn: Attn, T: int, seqs: int) -> int:
+    v = lib().memfine_attn_bwd_workspace_bytes(int(T), int(seqs), ctypes.byref(attn))
     if v < 0:
         raise MemfineError(int(v), "memfine_attn_bwd_workspace_bytes")
     return int(v)

@@ -1943,7 +1943,7 @@ AttnArgs attn_args(int64_t T, int32_t seqs, const memfine_attn& a) {
   g.causal = a.causal;
   g.window = a.window;
   g.scale = a.scale;
-  g.parts = T > 0 ? attn_parts(g, device_cus()) : 1;
+  g.parts = attn_parts(g, device_cus());
   return g;
 }
 int check_decode(const memfine_attn* a, const memfine_cache* c, int32_t seqs, int32_t width) {
@@ -2010,9 +2010,9 @@ int memfine_attn_fwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32
   return hip_status(launch_attn_fwd(g, s));
 }
 
-int64_t memfine_attn_bwd_workspace_bytes(int64_t T, const memfine_attn* a) {
-  if (check_attn(a) || check_rows(T, 1)) return MEMFINE_ERR_INVALID_ARG;
-  return attn_bwd_floats(attn_args(T, 1, *a)) * 4;
+int64_t memfine_attn_bwd_workspace_bytes(int64_t T, int32_t seqs, const memfine_attn* a) {
+  if (check_attn(a) || check_rows(T, seqs)) return MEMFINE_ERR_INVALID_ARG;
+  return T == 0 || seqs == 0 ? 0 : attn_bwd_floats(attn_args(T, seqs, *a)) * 4;
 }
 
 int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,

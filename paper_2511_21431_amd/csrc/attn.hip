@@ -16,6 +16,7 @@
 // values of a reduction step a register holds is the accumulator's choice, and
 // the other operand, read from LDS with a transposing load, follows it.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "common.h"
@@ -806,17 +807,30 @@ bool short_rows(const AttnArgs& g) { return g.T < 2048 * (int64_t)g.seqs; }
 
 }  // namespace
 
-// Parts of dK and dV: a workgroup for 256 keys (fp32: 128) goes through all queries of
-// the group; where that leaves fewer than two a CU the group's heads are shared out, but not
-// below 4096 queries a part, under which the parts' sums cost more than the even load gives
-// (32 heads in 8 groups, without and with two parts: one sequence of 8192 tokens 2.41 ms and
-// 1.72, 8 of 1024 354 us and 409; 64 heads in 8 groups, 4096 tokens, one to four parts
-// 1.22, 0.97 and 0.91 ms with one, three and four).
+// Parts that the heads of a group are shared out in for dk and dv: one workgroup's chain, all
+// queries of the group against 256 keys (fp32: 128), is the shortest time it can take, and
+// few keys leave CUs idle; but parts are written and read again.  In microseconds:
+//   tile x max(chain / parts + 4, (half the chain / parts + 4) workgroups per CU) + sums
+// (a start and an end weigh four tiles; tile: 3.5, fp32 8; sums: 6 and 16 bytes an element of
+// dk at 3 TB/s.)  32 heads in 8 groups, dim 128, without and with two parts: one sequence of
+// 8192 tokens 2.41 ms and 1.72, 8 of 1024 354 us and 409; 64 heads in 8 groups, 4096 tokens, one,
+// three and four parts 1.22, 0.97 and 0.91 ms.
 int attn_parts(const AttnArgs& g, int cus) {
-  const int64_t items = (g.T + 255) / 256 * g.kv_heads, group = g.heads / g.kv_heads;
-  const int64_t want = (2 * (int64_t)cus + items - 1) / items;
-  const int64_t most = std::min(group, group * g.T / std::max(g.seqs, 1) / 4096);
-  return (int)std::max<int64_t>(1, std::min(want, most));
+  const int group = g.heads / g.kv_heads, keys = g.f32 ? 128 : 256, rows = g.f32 ? 32 : 64;
+  const double items = (double)blocks_of(g.T, g.seqs, keys) * g.kv_heads;
+  const double mean = (double)g.T / std::max<int64_t>(std::min<int64_t>(g.seqs, g.T), 1);
+  const double chain = group * std::ceil(mean / rows);
+  int best = 1;
+  double least = 0.;
+  for (int p = 1; p <= group; p = p < group && 2 * p > group ? group : 2 * p) {
+    const double t = std::max(chain / p + 4., (.6 * chain / p + 4.) * items * p / cus) * (g.f32 ? 8. : 3.5) +
+                     (p > 1 ? 6. + p * (double)g.T * g.kv_heads * g.dim * 16. / 3e6 : 0.);
+    if (p == 1 || t < least) {
+      best = p;
+      least = t;
+    }
+  }
+  return best;
 }
 int64_t attn_bwd_floats(const AttnArgs& g) {
   return (2 * g.heads + (g.parts > 1 ? 2 * (int64_t)g.parts * g.kv_heads * g.dim : 0)) * g.T;

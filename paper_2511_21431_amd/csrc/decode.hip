@@ -457,73 +457,86 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(const DecodeArgs g) {
   }
 }
 
-// Joins the parts of one head of one sequence whose steps lie in more than one
-// workgroup's run, in order; writes zeros where there is no token.
+// One head's result from sums relative to 2^m: four columns.
+__device__ __forceinline__ void store_head(const DecodeArgs& g, int64_t at, int dim, int d, const f32x4_t& o,
+                                           float m, float l) {
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  const float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  Vec4<bf16_t>::store((bf16_t*)g.O + at * dim + d, f);
+  if (g.lse && d == 0) g.lse[at] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+}
+// Adds another part's sums.
+__device__ __forceinline__ void join(f32x4_t& o, float& m, float& l, const f32x4_t& v, float pm, float pl) {
+  const float now = fmaxf(m, pm), ref = now == -INFINITY ? 0.f : now;
+  const float f = exp2_(m - ref), h = exp2_(pm - ref);
+  m = now;
+  l = l * f + pl * h;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = o[e] * f + v[e] * h;
+}
+
+// Joins the parts of one pair of a sequence whose steps lie in more than one
+// workgroup's run, in order; writes zeros where there is no token.  Workgroup (x, y): pair
+// x, its heads y, y + gridDim.y, ...
 template <int D>
 __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs g) {
-  constexpr int kRow = D + 4, kAcross = 256 / (D / 4);  // (threads: D / 4 columns, kAcross parts at a time)
+  constexpr int kRow = D + 4, kCols = D / 4, kAcross = 256 / kCols;
   __shared__ int64_t part[4];
-  __shared__ int64_t found[1];
+  __shared__ int64_t found[2];
   __shared__ __align__(16) float mem[kAcross][kRow];
   const Plan plan = plan_of(g, part);
-  const int b = blockIdx.x / g.heads, head = blockIdx.x % g.heads;
+  const int b = blockIdx.x / g.pairs, pair = blockIdx.x % g.pairs;
   const int64_t before = steps_before(g, plan, b, found);
+  const int kv = pair / g.tiles, first = pair % g.tiles * 16, heads = min(16, g.group - first);
+  const int64_t h0 = (int64_t)b * g.heads + kv * g.group + first;
   const int n = steps_of(span_of(g, b));
-  const int d = threadIdx.x % (D / 4) * 4, y = threadIdx.x / (D / 4);
-  const int64_t at = (int64_t)b * g.heads + head;
+  const int d = threadIdx.x % kCols * 4, y = threadIdx.x / kCols;
   if (n == 0) {
-    if (y == 0) {
-      const float f[4] = {0.f, 0.f, 0.f, 0.f};
-      Vec4<bf16_t>::store((bf16_t*)g.O + at * D + d, f);
-      if (g.lse && d == 0) g.lse[at] = -INFINITY;
+    for (int h = y * gridDim.y + blockIdx.y; h < heads; h += kAcross * gridDim.y)
+      store_head(g, h0 + h, D, d, (f32x4_t){0.f, 0.f, 0.f, 0.f}, 0.f, 0.f);
+    return;
+  }
+  const int64_t share = share_of(g, plan.total);
+  const int64_t s0 = before * g.pairs + (int64_t)pair * n, s1 = s0 + n;
+  const int64_t w0 = quotient(s0, share), w1 = quotient(s1 - 1, share);
+  if (w0 == w1) return;  // one workgroup had it all
+  auto row = [&](int64_t w, int h) {  // a run's first part is part 0
+    const int which = w == w0 && w0 * share < s0 ? 1 : 0;
+    return g.parts + ((w * 2 + which) * 16 + h) * kRow;
+  };
+  if (w1 - w0 < 8) {  // few parts: a thread joins four columns of a head
+    for (int h = y * gridDim.y + blockIdx.y; h < heads; h += kAcross * gridDim.y) {
+      float m = -INFINITY, l = 0.f;
+      f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+      for (int64_t w = w0; w <= w1; ++w) {
+        const float* r = row(w, h);
+        join(o, m, l, *(const f32x4_t*)(r + d), r[D], r[D + 1]);
+      }
+      store_head(g, h0 + h, D, d, o, m, l);
     }
     return;
   }
-  const int kv = head / g.group, in = head % g.group;
-  const int64_t share = share_of(g, plan.total);
-  const int64_t s0 = before * g.pairs + (int64_t)(kv * g.tiles + in / 16) * n, s1 = s0 + n;
-  const int64_t w0 = quotient(s0, share), w1 = quotient(s1 - 1, share);
-  if (w0 == w1) return;  // one workgroup had it all
-  auto row = [&](int64_t w) {  // a run's first part is part 0
-    const int which = w == w0 && w0 * share < s0 ? 1 : 0;
-    return g.parts + ((w * 2 + which) * 16 + in % 16) * kRow;
-  };
-  float m = -INFINITY, l = 0.f;
-  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t w = w0 + y; w <= w1; w += kAcross) {
-    const float* r = row(w);
-    const f32x4_t v = *(const f32x4_t*)(r + d);
-    const float pm = r[D], pl = r[D + 1];
-    const float now = fmaxf(m, pm), ref = now == -INFINITY ? 0.f : now;
-    const float f = exp2_(m - ref), h = exp2_(pm - ref);
-    m = now;
-    l = l * f + pl * h;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = o[e] * f + v[e] * h;
+  for (int h = blockIdx.y; h < heads; h += gridDim.y) {
+    float m = -INFINITY, l = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int64_t w = w0 + y; w <= w1; w += kAcross) {
+      const float* r = row(w, h);
+      join(o, m, l, *(const f32x4_t*)(r + d), r[D], r[D + 1]);
+    }
+    *(f32x4_t*)(&mem[y][d]) = o;
+    if (d == 0) {
+      mem[y][D] = m;
+      mem[y][D + 1] = l;
+    }
+    __syncthreads();
+    if (y == 0) {
+      for (int i = 1; i < kAcross; ++i) join(o, m, l, *(const f32x4_t*)(&mem[i][d]), mem[i][D], mem[i][D + 1]);
+      store_head(g, h0 + h, D, d, o, m, l);
+    }
+    __syncthreads();
   }
-  *(f32x4_t*)(&mem[y][d]) = o;
-  if (d == 0) {
-    mem[y][D] = m;
-    mem[y][D + 1] = l;
-  }
-  __syncthreads();
-  if (y) return;
-  m = -INFINITY;
-  for (int i = 0; i < kAcross; ++i) m = fmaxf(m, mem[i][D]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  o = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-  l = 0.f;
-  for (int i = 0; i < kAcross; ++i) {
-    const float f = exp2_(mem[i][D] - ref);
-    const f32x4_t v = *(const f32x4_t*)(&mem[i][d]);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += v[e] * f;
-    l += mem[i][D + 1] * f;
-  }
-  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-  const float f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-  Vec4<bf16_t>::store((bf16_t*)g.O + at * D + d, f);
-  if (g.lse && d == 0) g.lse[at] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
 }  // namespace
@@ -536,16 +549,19 @@ int decode_groups(const DecodeArgs& g) {
 int64_t decode_part_floats(const DecodeArgs& g) { return (int64_t)decode_groups(g) * 2 * 16 * (g.dim + 4); }
 
 hipError_t launch_decode(const DecodeArgs& g, hipStream_t s) {
-  const int64_t heads = (int64_t)g.seqs * g.heads;
-  if (heads > kMostItems / 256) return hipErrorInvalidValue;
+  const int64_t pairs = (int64_t)g.seqs * g.pairs;
+  if (pairs > kMostItems / 256) return hipErrorInvalidValue;
+  // where pairs are few, a workgroup for each head
+  const int64_t y = std::max<int64_t>(1, std::min<int64_t>(std::min(16, g.group), 2 * g.cus / pairs));
+  const dim3 grid((unsigned)pairs, (unsigned)y);
   if (g.dim == 64) {
     if (g.ks) decode_kernel<64, true><<<g.groups, 256, 0, s>>>(g);
     else decode_kernel<64, false><<<g.groups, 256, 0, s>>>(g);
-    join_kernel<64><<<(unsigned)heads, 256, 0, s>>>(g);
+    join_kernel<64><<<grid, 256, 0, s>>>(g);
   } else {
     if (g.ks) decode_kernel<128, true><<<g.groups, 256, 0, s>>>(g);
     else decode_kernel<128, false><<<g.groups, 256, 0, s>>>(g);
-    join_kernel<128><<<(unsigned)heads, 256, 0, s>>>(g);
+    join_kernel<128><<<grid, 256, 0, s>>>(g);
   }
   return hipGetLastError();
 }

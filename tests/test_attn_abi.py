@@ -62,8 +62,10 @@ def test_packed_refusals():
         assert fwd(off=N, Q=N, K=N, V=N, O=N, lse=N, **kw) == 0
         assert bwd(off=N, Q=N, dQ=N, **kw) == 0
     f = _lib.lib().memfine_attn_bwd_workspace_bytes
-    assert f(1000, ctypes.byref(attn())) >= 2 * 1000 * 8 * 4 and f(0, ctypes.byref(attn())) == 0
-    assert f(-1, ctypes.byref(attn())) < 0 and f(1, ctypes.byref(attn(heads=7))) < 0
+    alone = ctypes.byref(attn(kv_heads=8))              # no shared heads: two floats a row and head
+    assert f(1000, 3, alone) == 2 * 1000 * 8 * 4 and f(0, 3, alone) == f(7, 0, alone) == 0
+    assert f(1000, 1, ctypes.byref(attn())) >= 2 * 1000 * 8 * 4
+    assert f(-1, 1, alone) < 0 and f(1, -1, alone) < 0 and f(1, 1, ctypes.byref(attn(heads=7))) < 0
 
 
 def test_rope_refusals():
