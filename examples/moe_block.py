@@ -3,8 +3,12 @@
     python examples/moe_block.py                 # a decode batch, then a few training steps
     python examples/moe_block.py --tokens 1      # one sequence
     python examples/moe_block.py --bf16          # served with bf16 activations
+    python examples/moe_block.py --context 8000  # after sequences of 8000 tokens
 
-`ServedBlock` is one block of an inference engine with its weights in MX4: the
+`ServedAttention` stands in front of a block of an inference engine: the projection
+of queries, keys and values, their rotation, the cache of pages (MX8, or bf16) and the
+attention over it, for whole prompts and then token by token; `TrainedAttention` is
+the same in training, over packed sequences.  `ServedBlock` is one block of an inference engine with its weights in MX4: the
 attention's output projection, residual and norm, routing and the experts; the
 activations of the experts are MX8 (or bf16), four library calls and the
 router's product a step.  `TrainedBlock` is the block in training, forward and
@@ -25,6 +29,106 @@ EPS = 1e-6
 
 def empty(*shape, dtype=torch.bfloat16):
     return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def tables(positions, dim, base=10000.0):
+    """Cosines and sines of the rotation, float [positions, dim / 2]."""
+    f = base ** (-torch.arange(0, dim, 2, dtype=torch.float64, device="cuda") / dim)
+    a = torch.arange(positions, dtype=torch.float64, device="cuda")[:, None] * f
+    return torch.cos(a).float(), torch.sin(a).float()
+
+
+def offsets_of(lens):
+    return torch.tensor([0, *lens], device="cuda").cumsum(0).to(torch.int32)
+
+
+class ServedAttention:
+    """Wqkv [(heads + 2 kv_heads) dim, h]: rounded to MX4 once, here.  The cache holds
+    `sequences` of up to `positions` tokens; each has the same pages for good."""
+
+    def __init__(self, Wqkv, attn, sequences, positions, page=64, mx8=True):
+        self.attn, self.H, self.Hk, self.D = attn, attn.heads, attn.kv_heads, attn.dim
+        self.N, self.h = Wqkv.shape
+        self.W = mf.memfine_mxw_quantize(Wqkv[None])
+        self.cos, self.sin = tables(positions, self.D)
+        width = -(-positions // page)
+        size = (sequences * width, self.Hk, page, self.D)
+        if mx8:
+            kv = [torch.zeros(size, dtype=torch.uint8, device="cuda") for _ in range(2)]
+            kv += [torch.zeros((*size[:3], self.D // 32), dtype=torch.uint8, device="cuda")
+                   for _ in range(2)]
+        else:
+            kv = [torch.zeros(size, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        self.cache = mf.make_cache(*kv)
+        self.table = torch.arange(sequences * width, dtype=torch.int32, device="cuda").view(sequences, width)
+        self.lengths = torch.zeros(sequences, dtype=torch.int32, device="cuda")
+        self.qkv, self.q, self.out = (empty(sequences, n) for n in (self.N, self.H * self.D, self.H * self.D))
+
+    def split(self, qkv):
+        x = qkv.view(-1, self.H + 2 * self.Hk, self.D)
+        return x[:, :self.H], x[:, self.H:self.H + self.Hk], x[:, self.H + self.Hk:]
+
+    def prompt(self, x, lens):
+        """Rows x [sum(lens), h] of one new prompt a sequence; returns [sum(lens), H D]."""
+        offsets = offsets_of(lens)
+        self.lengths.copy_(offsets[1:] - offsets[:-1])
+        qkv, out = empty(len(x), self.N), empty(len(x), self.H, self.D)
+        mf.memfine_linear_mxw(self.N, self.h, x, *self.W, qkv)
+        q, k, v = self.split(qkv)
+        both = qkv.view(len(x), -1, self.D)[:, :self.H + self.Hk]
+        mf.memfine_rope(offsets, self.cos, self.sin, both, both)
+        mf.memfine_kv_write(self.cache, self.table, self.lengths, k, v, offsets=offsets)
+        mf.memfine_attn_fwd(self.attn, offsets, q, k, v, out)
+        return out.view(len(x), -1)
+
+    def step(self, x, allocator=None):
+        """Rows x [sequences, h] of one new token a sequence; returns [sequences, H D]."""
+        self.lengths += 1
+        mf.memfine_linear_mxw(self.N, self.h, x, *self.W, self.qkv, allocator=allocator)
+        q, k, v = self.split(self.qkv)
+        shape = (len(x), self.H, self.D)
+        mf.memfine_kv_write(self.cache, self.table, self.lengths, k, v, Q=q, R=self.q.view(shape),
+                            cos=self.cos, sin=self.sin)
+        mf.memfine_attn_decode(self.attn, self.cache, self.table, self.lengths, self.q.view(shape),
+                               self.out.view(shape), allocator=allocator)
+        return self.out
+
+
+class TrainedAttention:
+    """out = attention(X Wqkv^T) Wo^T over packed sequences of lengths `lens`; the
+    gradients of both weights are float tensors."""
+
+    def __init__(self, Wqkv, Wo, attn, lens):
+        self.Wqkv, self.Wo, self.attn, self.offsets = Wqkv, Wo, attn, offsets_of(lens)
+        H, Hk, D, T = attn.heads, attn.kv_heads, attn.dim, sum(lens)
+        self.H, self.both = H, H + Hk
+        self.cos, self.sin = tables(max(lens), D)
+        self.qkv, self.dqkv = (empty(T, H + 2 * Hk, D) for _ in range(2))
+        self.o, self.lse = empty(T, H, D), empty(H, T, dtype=torch.float32)
+        self.grads = {n: torch.zeros_like(p, dtype=torch.float32) for n, p in (("Wqkv", Wqkv), ("Wo", Wo))}
+
+    def split(self, x):
+        return x[:, :self.H], x[:, self.H:self.both], x[:, self.both:]
+
+    def forward(self, X):
+        torch.matmul(X, self.Wqkv.t(), out=self.qkv.view(len(X), -1))
+        turned = self.qkv[:, :self.both]
+        mf.memfine_rope(self.offsets, self.cos, self.sin, turned, turned)
+        mf.memfine_attn_fwd(self.attn, self.offsets, *self.split(self.qkv), self.o, self.lse)
+        return self.o.view(len(X), -1) @ self.Wo.t()
+
+    def backward(self, X, dout):
+        """dX of the last forward's X; the weights' gradients are overwritten."""
+        T = len(X)
+        self.grads["Wo"].copy_(dout.t() @ self.o.view(T, -1))
+        do = (dout @ self.Wo).view(self.o.shape)
+        mf.memfine_attn_bwd(self.attn, self.offsets, *self.split(self.qkv), self.o, self.lse, do,
+                            *self.split(self.dqkv))
+        turned = self.dqkv[:, :self.both]
+        mf.memfine_rope(self.offsets, self.cos, self.sin, turned, turned, inverse=True)
+        d = self.dqkv.view(T, -1)
+        self.grads["Wqkv"].copy_(d.t() @ X)
+        return d @ self.Wqkv
 
 
 class ServedBlock:
@@ -128,6 +232,24 @@ def serve(p, gating, tokens, steps, mx8, gen):
     return start.elapsed_time(stop) / steps
 
 
+def serve_attention(h, heads, kv_heads, dim, tokens, context, steps, gen):
+    """Milliseconds a step of `tokens` sequences that have `context` tokens each."""
+    attn = mf.make_attn(heads, kv_heads, dim)
+    Wqkv = (torch.randn((heads + 2 * kv_heads) * dim, h, generator=gen, device="cuda") * h ** -0.5)
+    a = ServedAttention(Wqkv.to(torch.bfloat16), attn, tokens, context + steps + 3)
+    x = torch.randn(tokens, h, generator=gen, device="cuda").to(torch.bfloat16)
+    a.prompt(x.repeat_interleave(context, 0), [context] * tokens)
+    for _ in range(3):
+        a.step(x)
+    start, stop = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    for _ in range(steps):
+        a.step(x)
+    stop.record()
+    stop.synchronize()
+    return start.elapsed_time(stop) / steps
+
+
 def train(p, gating, tokens, steps, gen, lr=0.02):
     """Fits a fixed random map; returns the loss of every step."""
     p = {n: v for n, v in p.items() if n != "Wo"}
@@ -155,6 +277,9 @@ def main():
     a.add_argument("--ffn", type=int, default=1408)
     a.add_argument("--experts", type=int, default=64)
     a.add_argument("--topk", type=int, default=6)
+    a.add_argument("--heads", type=int, default=16)
+    a.add_argument("--kv-heads", type=int, default=4)
+    a.add_argument("--context", type=int, default=1000, help="tokens of each sequence before the step")
     a.add_argument("--bf16", action="store_true", help="bf16 activations in the served experts")
     a = a.parse_args()
     gen = torch.Generator(device="cuda").manual_seed(0)
@@ -162,6 +287,8 @@ def main():
     p = weights(gen, a.hidden, a.ffn, a.experts, a.hidden)
     ms = serve(p, gating, a.tokens, a.steps, not a.bf16, gen)
     print(f"served: {a.tokens} tokens, {'bf16' if a.bf16 else 'MX8'} activations, {ms * 1e3:.0f} us a step")
+    ms = serve_attention(a.hidden, a.heads, a.kv_heads, 128, a.tokens, a.context, a.steps, gen)
+    print(f"attention: {a.tokens} sequences of {a.context} tokens, MX8 cache, {ms * 1e3:.0f} us a step")
     losses = train(p, gating, max(a.tokens, 256), a.steps, gen)
     print(f"trained: loss {losses[0]:.4f} -> {losses[-1]:.4f} in {a.steps} steps")
 

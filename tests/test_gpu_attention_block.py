@@ -1,0 +1,118 @@
+"""The attention's calls together, as examples/moe_block.py runs them: served through the
+cache (also from a captured graph) and trained, against torch in float64 on the same
+weights."""
+import os
+import sys
+
+import pytest
+
+from gpu_harness import log, torch
+
+pytestmark = pytest.mark.gpu
+H, HK, D, HID = 8, 2, 64, 256
+
+
+@pytest.fixture(scope="module")
+def ex():
+    t = torch()
+    if not t.cuda.is_available():
+        pytest.skip("no GPU")
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import moe_block
+    return moe_block
+
+
+def draw(*shape, seed, std=1.0):
+    t = torch()
+    return (t.randn(*shape, generator=t.Generator().manual_seed(seed)) * std).to(t.bfloat16).cuda()
+
+
+def turned(x, cos, sin, first=0):
+    """Rows [n, heads, D] of one sequence in float64."""
+    t = torch()
+    c, s = (y[first:first + len(x)].double()[:, None] for y in (cos, sin))
+    a, b = x[..., :D // 2], x[..., D // 2:]
+    return t.cat([a * c - b * s, b * c + a * s], -1)
+
+
+def attention64(qkv, cos, sin):
+    """One sequence's rows [n, H + 2 HK, D] in float64, causal."""
+    t = torch()
+    qk = turned(qkv[:, :H + HK], cos, sin)
+    q = qk[:, :H].transpose(0, 1)
+    k, v = (y.transpose(0, 1).repeat_interleave(H // HK, 0) for y in (qk[:, H:], qkv[:, H + HK:]))
+    s = t.matmul(q, k.transpose(1, 2).contiguous()) * D ** -0.5
+    s = s.masked_fill(t.ones(s.shape[1:], dtype=t.bool, device=s.device).triu(1), -t.inf)
+    return t.matmul(t.softmax(s, 2), v).transpose(0, 1).reshape(len(qkv), -1)
+
+
+@pytest.mark.parametrize("mx8", (False, True), ids=("bf16", "mx8"))
+def test_served_prompt_and_steps(ex, mx8):
+    """Relative 2-norms: bf16 rounds qkv, the turned rows, weights and output by at most 2^-8
+    each, 2^-6 in all; MX8 rounds keys and values by at most 2^-4 of each, by 2^-5
+    on average over its steps, and what a score is off by enters all weights: 0.15."""
+    t = torch()
+    lens, steps = [37, 5, 100], 3
+    W = draw((H + 2 * HK) * D, HID, seed=1, std=HID ** -0.5)
+    a = ex.ServedAttention(W, ex.mf.make_attn(H, HK, D), 3, 128, page=32, mx8=mx8)
+    held = t.empty(1, *W.shape, device="cuda")
+    ex.mf.memfine_mxw_unpack(*a.W, held)
+    W64 = held[0].double()
+    rows = [draw(n + steps, HID, seed=10 + i) for i, n in enumerate(lens)]
+    want = [attention64((r.double() @ W64.t()).view(len(r), -1, D), a.cos, a.sin) for r in rows]
+
+    def off(got, ref):
+        return ((got.double() - ref).norm() / ref.norm()).item()
+    out = a.prompt(t.cat([r[:n] for r, n in zip(rows, lens)]), lens)
+    log(f"prompts, mx8={mx8}")
+    assert off(out, t.cat([w[:n] for w, n in zip(want, lens)])) <= 2 ** -6
+    eager = []
+    for i in range(steps):
+        x = t.stack([r[n + i] for r, n in zip(rows, lens)])
+        out = a.step(x)
+        log(f"step {i}")
+        assert off(out, t.stack([w[n + i] for w, n in zip(want, lens)])) <= (0.15 if mx8 else 2 ** -6)
+        eager.append((x, out.clone()))
+    # the same steps again, from a graph
+    x = t.empty_like(eager[0][0])
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        a.step(x)
+    a.lengths.copy_(t.tensor(lens))
+    for i, (xi, o) in enumerate(eager):
+        x.copy_(xi)
+        graph.replay()
+        t.cuda.synchronize()
+        log(f"replay {i}")
+        assert t.equal(a.out, o)
+
+
+def test_trained_gradients(ex):
+    """Against autograd in float64: qkv, turned rows, attention's weights and outputs, the
+    products' outputs are rounded to bf16, 2^-8 each at most: eight of them, 2^-5 of
+    the 2-norm."""
+    t = torch()
+    lens = [50, 1, 77]
+    T = sum(lens)
+    Wqkv, Wo = draw((H + 2 * HK) * D, HID, seed=1, std=HID ** -0.5), draw(HID, H * D, seed=2, std=(H * D) ** -0.5)
+    a = ex.TrainedAttention(Wqkv, Wo, ex.mf.make_attn(H, HK, D), lens)
+    X, dout = draw(T, HID, seed=3), draw(T, HID, seed=4)
+    out = a.forward(X)
+    dX = a.backward(X, dout)
+    x, w, o = (y.double().requires_grad_() for y in (X, Wqkv, Wo))
+    qkv = (x @ w.t()).view(T, -1, D)
+    ref = t.cat([attention64(q, a.cos, a.sin) for q in qkv.split(lens)]) @ o.t()
+    grads = t.autograd.grad((ref * dout.double()).sum(), (x, w, o))
+    log("trained")
+    for name, got, want in (("out", out, ref), ("dX", dX, grads[0]), ("dWqkv", a.grads["Wqkv"], grads[1]),
+                            ("dWo", a.grads["Wo"], grads[2])):
+        rel = ((got.double() - want).norm() / want.norm()).item()
+        assert rel <= 2 ** -5, (name, rel)
+
+
+def test_example_runs(ex, capsys, monkeypatch):
+    monkeypatch.setattr(sys, "argv", ["moe_block.py", "--tokens", "4", "--steps", "2", "--hidden", "256", "--ffn",
+                                      "128", "--experts", "8", "--topk", "2", "--context", "40", "--heads", "4",
+                                      "--kv-heads", "2"])
+    ex.main()
+    assert "attention: 4 sequences of 40 tokens" in capsys.readouterr().out
