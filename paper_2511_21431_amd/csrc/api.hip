@@ -1943,7 +1943,8 @@ AttnArgs attn_args(int64_t T, int32_t seqs, const memfine_attn& a) {
   g.causal = a.causal;
   g.window = a.window;
   g.scale = a.scale;
-  g.parts = attn_parts(g, device_cus());
+  g.cus = device_cus();
+  g.parts = attn_parts(g);
   return g;
 }
 int check_decode(const memfine_attn* a, const memfine_cache* c, int32_t seqs, int32_t width) {

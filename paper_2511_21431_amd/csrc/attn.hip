@@ -97,9 +97,9 @@ __device__ __forceinline__ void zero(f32x16_t& c) {
 // swizzle(row): 16 consecutive rows' reads of one unit, and the reads of four
 // (bf16) consecutive rows x 32 columns by a transposing load, or of 32 columns of rows 4
 // apart (fp32), then fall on distinct banks.
-template <typename T, int D> struct Tile {
+template <typename T, int D, int R = sizeof(T) == 2 ? 64 : 32> struct Tile {
   static constexpr int ES = sizeof(T), kPitch = D * ES, kUnits = kPitch / 16;
-  static constexpr int kRows = ES == 2 ? 64 : 32, kBytes = kRows * kPitch;
+  static constexpr int kRows = R, kBytes = kRows * kPitch;
   static constexpr int kBlocks = kRows / 32;           // blocks of 32 rows
   static constexpr int kSteps = D / Mma<T>::kStep;     // reduction steps along a row
   static constexpr int kDown = 32 / Mma<T>::kStep;     // reduction steps down a block of rows
@@ -153,8 +153,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const T* base, int64
 }
 
 // The copy of a tile into LDS by NW waves, straight from memory.
-template <typename T, int D, int NW> struct Copy {
-  typedef Tile<T, D> L;
+template <typename T, int D, int NW, class L = Tile<T, D>> struct Copy {
   static constexpr int kPer = 1024 / L::kPitch;               // rows an instruction
   static constexpr int kCount = L::kBytes / 1024 / NW;        // instructions a wave
   static_assert(kCount * NW * 1024 == L::kBytes, "a tile is split evenly over the waves");
@@ -170,7 +169,8 @@ template <typename T, int D, int NW> struct Copy {
     }
   }
   // rows from base on, `rows` of them there
-  __device__ __forceinline__ void issue(const T* base, int64_t ld, int rows, char* lds, int wave) const {
+  __device__ __forceinline__ void issue(const T* base, int64_t ld, int rows, char* lds,
+                                        int wave) const {
 #pragma unroll
     for (int i = 0; i < kCount; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -213,6 +213,22 @@ __device__ __forceinline__ void store_rows(const f32x16_t (&c)[D / 32], float sc
     const u32x4_t v = *(const u32x4_t*)(lds + row * kPitch + ((u ^ (row & 15) % kUnits) << 4));
     if (row < rows) *(u32x4_t*)(out + row * ld + u * kVec) = v;
   }
+}
+
+// Accumulators in LDS as a wave's lanes hold them, and added up: o mf + theirs of.
+template <int D>
+__device__ __forceinline__ void put_lanes(float* to, const f32x16_t (&o)[D / 32], int lane) {
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) to[(b * 16 + e) * 64 + lane] = o[b][e];
+}
+template <int D>
+__device__ __forceinline__ void add_lanes(const float* from, f32x16_t (&o)[D / 32], float mf, float of, int lane) {
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[b][e] = o[b][e] * mf + from[(b * 16 + e) * 64 + lane] * of;
 }
 
 // ------------------------------------------------------------- work to do
@@ -322,24 +338,31 @@ __device__ __forceinline__ void hide(f32x16_t& c, const Seen& s, int r0, int hh,
 // ----------------------------------------------------------------- forward
 // NW waves of 32 queries each, which share the tiles of keys and values in LDS: heads of a
 // group, where there are groups, for the same queries (under a causal mask they
-// then need the same tiles), the rest further queries.
-template <typename T, int D, int NW>
+// then need the same tiles), the rest further queries.  KS = 4, for so few queries that most
+// CUs would have none: four waves take the same queries and a quarter of each tile's keys,
+// of which there are twice as many; what they have is joined at the end, in order.
+template <typename T, int D, int NW, int KS>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void attn_fwd_kernel(const AttnArgs g, int blocks) {
-  typedef Tile<T, D> L;
+  typedef Tile<T, D, KS == 1 ? Tile<T, D>::kRows : 32 * KS> L;
+  constexpr int kOwn = L::kBlocks / KS;  // blocks of a tile that a wave takes
   typedef Mma<T> M;
-  __shared__ __align__(1024) char smem[4 * L::kBytes];
+  // (joined waves store through LDS that no other wave's sums are in)
+  constexpr int kOutPitch = KS == 1 ? L::kPitch : (D / 2 + 2) * 8;
+  constexpr int kNeed = 4 * L::kBytes, kSums = KS == 1 ? 0 : NW * (D / 2 + 2) * 256;
+  __shared__ __align__(1024) char smem[kNeed > kSums ? kNeed : kSums];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
   int head, b;
   Part p;
   // 2^share waves take the same queries for as many heads
-  const int block = 32 * NW >> g.share;
+  const int block = 32 * NW / KS >> g.share;
   work_item(blocks, g.heads >> g.share, g.causal, head, b);
   if (!locate(g.offsets, g.seqs, (int)g.T, block, b, p)) return;
-  head = (head << g.share) + (w & ((1 << g.share) - 1));
+  const int wq = w / KS, k0 = w % KS * kOwn;  // whose queries, first block of the tiles
+  head = (head << g.share) + (wq & ((1 << g.share) - 1));
   const int kv = head / (g.heads / g.kv_heads);
   const int q0 = p.block * block, rows = min(block, p.n - q0);
-  const int i0 = q0 + 32 * (w >> g.share), mine = min(32, p.n - i0);
+  const int i0 = q0 + 32 * (wq >> g.share), mine = min(32, p.n - i0);
   const T* K = (const T*)g.K + p.begin * g.ldk + kv * D;
   const T* V = (const T*)g.V + p.begin * g.ldv + kv * D;
 
@@ -349,7 +372,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
   const Seen first = keys_of(g, i0, p.n), last = keys_of(g, i0 + 31, p.n);
   const Seen own = keys_of(g, i0 + (lane & 31), p.n);
 
-  Copy<T, D, NW> ck, cv;
+  Copy<T, D, NW, L> ck, cv;
   ck.init(g.ldk, w, lane);
   cv.init(g.ldv, w, lane);
   auto issue = [&](int t, char* st) {
@@ -371,24 +394,24 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
     constexpr int kAt = decltype(stage)::value * 2 * L::kBytes;
     stage_barrier();
     if (t + 1 < t1) issue(t + 1, smem + (2 * L::kBytes - kAt));
-    const int r0 = t * L::kRows;
-    if (mine <= 0 || r0 > last.hi || r0 + L::kRows <= first.lo) return;
+    const int r0 = t * L::kRows + 32 * k0;  // of the wave's own blocks
+    if (mine <= 0 || r0 > last.hi || r0 + 32 * kOwn <= first.lo) return;
     const char* ks = smem + kAt;
     const char* vs = ks + L::kBytes;
-    f32x16_t s[L::kBlocks];
+    f32x16_t s[kOwn];
 #pragma unroll
-    for (int i = 0; i < L::kBlocks; ++i) zero(s[i]);
+    for (int i = 0; i < kOwn; ++i) zero(s[i]);
 #pragma unroll
     for (int k = 0; k < L::kSteps; ++k)
 #pragma unroll
-      for (int i = 0; i < L::kBlocks; ++i) M::mma(L::row(ks, 32 * i, k, lane), q[k], s[i]);
-    if (!see_all(first, last, r0, L::kRows)) {
+      for (int i = 0; i < kOwn; ++i) M::mma(L::row(ks, 32 * (k0 + i), k, lane), q[k], s[i]);
+    if (!see_all(first, last, r0, 32 * kOwn)) {
 #pragma unroll
-      for (int i = 0; i < L::kBlocks; ++i) hide(s[i], own, r0 + 32 * i, hh, -INFINITY);
+      for (int i = 0; i < kOwn; ++i) hide(s[i], own, r0 + 32 * i, hh, -INFINITY);
     }
     float top = s[0][0];
 #pragma unroll
-    for (int i = 0; i < L::kBlocks; ++i)
+    for (int i = 0; i < kOwn; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
     top = halves_max(top) * c;
@@ -407,21 +430,21 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
     }
     const float ref = m == -INFINITY ? 0.f : m;  // (a row that sees nothing yet)
 #pragma unroll
-    for (int i = 0; i < L::kBlocks; ++i)
+    for (int i = 0; i < kOwn; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         s[i][e] = exp2_(fmaf(s[i][e], c, -ref));
         l += s[i][e];
       }
 #pragma unroll
-    for (int i = 0; i < L::kBlocks; ++i)
+    for (int i = 0; i < kOwn; ++i)
 #pragma unroll
       for (int j = 0; j < L::kDown; ++j) {
         // the weights are rounded to the values' type, the matrix core's operand (their
         // sum is not): half a step of bf16 each, which averages out over the row
         const Frag<T> f = M::of(s[i], j);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, i * L::kDown + j, lane), f, o[d]);
+        for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, (k0 + i) * L::kDown + j, lane), f, o[d]);
       }
   };
   for (int t = t0; t < t1; t += 2) {
@@ -429,11 +452,33 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
     if (t + 1 < t1) tile(t + 1, std::integral_constant<int, 1>());
   }
   stage_barrier();  // (all tiles are used: their LDS takes the results)
+  if constexpr (KS > 1) {
+    // the lanes of the four waves hold the same queries and columns
+    float* mem = (float*)smem;
+    constexpr int kEach = (D / 2 + 2) * 64;
+    if (w % KS) {
+      put_lanes<D>(mem + w * kEach, o, lane);
+      mem[w * kEach + D / 2 * 64 + lane] = m;
+      mem[w * kEach + (D / 2 + 1) * 64 + lane] = l;
+    }
+    stage_barrier();
+    if (w % KS) return;
+#pragma unroll 1
+    for (int y = 1; y < KS; ++y) {
+      const float* from = mem + (w + y) * kEach;
+      const float om = from[D / 2 * 64 + lane], ol = from[(D / 2 + 1) * 64 + lane];
+      const float now = fmaxf(m, om), at = now == -INFINITY ? 0.f : now;
+      const float mf = exp2_(m - at), of = exp2_(om - at);
+      m = now;
+      l = l * mf + ol * of;
+      add_lanes<D>(from, o, mf, of, lane);
+    }
+  }
   if (mine <= 0) return;
   l = halves_sum(l);
   store_rows<T, D>(o, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l,
                    (T*)g.out + ((p.begin + i0) * (int64_t)g.heads + head) * D, (int64_t)g.heads * D, mine,
-                   smem + w * 32 * L::kPitch, lane);
+                   smem + w * 32 * kOutPitch, lane);
   if (g.lse && lane < mine)
     g.lse[head * g.T + p.begin + i0 + lane] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
@@ -441,30 +486,35 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
 // ---------------------------------------------------------------- backward
 // dq (shared out as in the forward), and their log2 of the weights' sum and delta for the
 // kernel below.
-template <typename T, int D, int NW>
+template <typename T, int D, int NW, int KS>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void attn_dq_kernel(const AttnArgs g, int blocks) {
-  typedef Tile<T, D> L;
+  typedef Tile<T, D, KS == 1 ? Tile<T, D>::kRows : 32 * KS> L;
+  constexpr int kOwn = L::kBlocks / KS;  // blocks of a tile that a wave takes
   typedef Mma<T> M;
-  __shared__ __align__(1024) char smem[4 * L::kBytes];
+  // (joined waves store through LDS that no other wave's sums are in)
+  constexpr int kOutPitch = KS == 1 ? L::kPitch : (D / 2 + 2) * 8;
+  constexpr int kNeed = 4 * L::kBytes, kSums = KS == 1 ? 0 : NW * (D / 2 + 2) * 256;
+  __shared__ __align__(1024) char smem[kNeed > kSums ? kNeed : kSums];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
   int head, b;
   Part p;
   // 2^share waves take the same queries for as many heads
-  const int block = 32 * NW >> g.share;
+  const int block = 32 * NW / KS >> g.share;
   work_item(blocks, g.heads >> g.share, g.causal, head, b);
   if (!locate(g.offsets, g.seqs, (int)g.T, block, b, p)) return;
-  head = (head << g.share) + (w & ((1 << g.share) - 1));
+  const int wq = w / KS, k0 = w % KS * kOwn;  // whose queries, first block of the tiles
+  head = (head << g.share) + (wq & ((1 << g.share) - 1));
   const int kv = head / (g.heads / g.kv_heads);
   const int q0 = p.block * block, rows = min(block, p.n - q0);
-  const int i0 = q0 + 32 * (w >> g.share), mine = min(32, p.n - i0);
+  const int i0 = q0 + 32 * (wq >> g.share), mine = min(32, p.n - i0);
   const T* K = (const T*)g.K + p.begin * g.ldk + kv * D;
   const T* V = (const T*)g.V + p.begin * g.ldv + kv * D;
   const Seen wg_first = keys_of(g, q0, p.n), wg_last = keys_of(g, q0 + rows - 1, p.n);
   const int t0 = max(wg_first.lo, 0) / L::kRows, t1 = wg_last.hi / L::kRows + 1;
   const Seen first = keys_of(g, i0, p.n), last = keys_of(g, i0 + 31, p.n);
   const Seen own = keys_of(g, i0 + (lane & 31), p.n);
-  Copy<T, D, NW> ck, cv;
+  Copy<T, D, NW, L> ck, cv;
   ck.init(g.ldk, w, lane);
   cv.init(g.ldv, w, lane);
   auto issue = [&](int t, char* st) {
@@ -498,7 +548,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
     if (lse == -INFINITY) lse = INFINITY;
   }
   const float c = g.scale * kLog2e, ref = lse * kLog2e;
-  if (lane < mine) {
+  if (lane < mine && w % KS == 0) {
     g.top[row + lane] = ref;
     g.delta[row + lane] = delta;
   }
@@ -509,20 +559,20 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
     constexpr int kAt = decltype(stage)::value * 2 * L::kBytes;
     stage_barrier();
     if (t + 1 < t1) issue(t + 1, smem + (2 * L::kBytes - kAt));
-    const int r0 = t * L::kRows;
-    if (mine <= 0 || r0 > last.hi || r0 + L::kRows <= first.lo) return;
+    const int r0 = t * L::kRows + 32 * k0;  // of the wave's own blocks
+    if (mine <= 0 || r0 > last.hi || r0 + 32 * kOwn <= first.lo) return;
     const char* ks = smem + kAt;
     const char* vs = ks + L::kBytes;
-    const bool all = see_all(first, last, r0, L::kRows);
+    const bool all = see_all(first, last, r0, 32 * kOwn);
 #pragma unroll
-    for (int i = 0; i < L::kBlocks; ++i) {
+    for (int i = 0; i < kOwn; ++i) {
       f32x16_t s, dp;
       zero(s);
       zero(dp);
 #pragma unroll
       for (int k = 0; k < L::kSteps; ++k) {
-        M::mma(L::row(ks, 32 * i, k, lane), q[k], s);
-        M::mma(L::row(vs, 32 * i, k, lane), d_o[k], dp);
+        M::mma(L::row(ks, 32 * (k0 + i), k, lane), q[k], s);
+        M::mma(L::row(vs, 32 * (k0 + i), k, lane), d_o[k], dp);
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = exp2_(fmaf(s[e], c, -ref)) * (dp[e] - delta);
@@ -531,7 +581,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
       for (int j = 0; j < L::kDown; ++j) {
         const Frag<T> f = M::of(s, j);  // (rounded as the forward's weights)
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) M::mma(L::col(ks, 32 * d, i * L::kDown + j, lane), f, a[d]);
+        for (int d = 0; d < D / 32; ++d) M::mma(L::col(ks, 32 * d, (k0 + i) * L::kDown + j, lane), f, a[d]);
       }
     }
   };
@@ -540,17 +590,25 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
     if (t + 1 < t1) tile(t + 1, std::integral_constant<int, 1>());
   }
   stage_barrier();
+  if constexpr (KS > 1) {
+    float* mem = (float*)smem;
+    if (w % KS) put_lanes<D>(mem + w * D / 2 * 64, a, lane);
+    stage_barrier();
+    if (w % KS) return;
+#pragma unroll 1
+    for (int y = 1; y < KS; ++y) add_lanes<D>(mem + (w + y) * D / 2 * 64, a, 1.f, 1.f, lane);
+  }
   if (mine > 0)
     store_rows<T, D>(a, g.scale, (T*)g.dQ + (p.begin + i0) * g.lddq + head * D, g.lddq, mine,
-                     smem + w * 32 * L::kPitch, lane);
+                     smem + w * 32 * kOutPitch, lane);
 }
 
 // dk and dv of 32 NW rows a workgroup: it goes through the queries of the heads that share
 // them, head after head, so that every sum has one order.  With several parts each takes
-// some of the heads and leaves its sums in fp32 for attn_sum_kernel.
+// a run of these tiles and leaves its sums in fp32 for attn_sum_kernel.
 // kHeld: the values stay in LDS, not in registers, of which two waves a SIMD have 256 each.
 template <typename T, int D, int NW, bool kHeld>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 : 1) void attn_dkv_kernel(const AttnArgs g, int blocks) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 2 : 1) void attn_dkv_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D> L;
   typedef Mma<T> M;
   constexpr int kBlock = 32 * NW;
@@ -567,7 +625,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
   const int part = b % g.parts;
   if (!locate(g.offsets, g.seqs, (int)g.T, kBlock, b / g.parts, p)) return;
   const int group = g.heads / g.kv_heads;
-  const int h0 = group * part / g.parts, h1 = group * (part + 1) / g.parts;
   const int k0 = p.block * kBlock, rows = min(kBlock, p.n - k0);
   const int j0 = k0 + 32 * w, mine = min(32, p.n - j0);
   const Seen wg_first = queries_of(g, k0, p.n), wg_last = queries_of(g, k0 + rows - 1, p.n);
@@ -578,8 +635,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
   Copy<T, D, NW> cq, co;
   cq.init(g.ldq, w, lane);
   co.init(ldo, w, lane);
-  const int total = (h1 - h0) * tiles;
-  int head = kv * group + h0, next = t0;  // of the tile to copy next
+  // the part's first tile, and how many (group tiles parts < 2^31; all in scalar registers)
+  const uint32_t run = (uint32_t)(group * tiles);
+  const int x0 = __builtin_amdgcn_readfirstlane(run * part / g.parts);
+  const int total = __builtin_amdgcn_readfirstlane(run * (part + 1) / g.parts) - x0;
+  const int skip = __builtin_amdgcn_readfirstlane(x0 / tiles);
+  int head = kv * group + skip, next = t0 + x0 - skip * tiles;  // of the tile to copy next
   auto issue = [&](int stage) {
     const int r0 = next * L::kRows;
     char* st = smem + stage * kStage;
@@ -610,7 +671,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
     load_rows<T, D>(v, V + 32 * w * g.ldv, g.ldv, mine, lane);
   }
   load_rows<T, D>(k, (const T*)g.K + (p.begin + j0) * g.ldk + kv * D, g.ldk, mine, lane);
-  issue(0);
+  int now = next;  // the tile to use
+  if (total > 0) issue(0);
   f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
@@ -618,7 +680,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
     zero(dv[i]);
   }
   const float scale = g.scale * kLog2e;
-  int now = t0;  // the tile to use
   auto tile = [&](int x, auto stage) {  // (a constant stage, as in the forward)
     constexpr int kAt = decltype(stage)::value;
     stage_barrier();
@@ -743,20 +804,26 @@ int64_t blocks_of(int64_t T, int64_t seqs, int R) {
 }
 
 // (The compiler leaves out host stubs of kernels that only templates launch.)
-#define MEMFINE_FWD(T, D, NW) template __global__ void attn_fwd_kernel<T, D, NW>(const AttnArgs, int);
-#define MEMFINE_DQ(T, D) template __global__ void attn_dq_kernel<T, D, 4>(const AttnArgs, int);
+#define MEMFINE_FWD(T, D, NW, KS) \
+  template __global__ void attn_fwd_kernel<T, D, NW, KS>(const AttnArgs, int);
+#define MEMFINE_DQ(T, D, NW, KS) \
+  template __global__ void attn_dq_kernel<T, D, NW, KS>(const AttnArgs, int);
 #define MEMFINE_DKV(T, D, NW, HELD) \
   template __global__ void attn_dkv_kernel<T, D, NW, HELD>(const AttnArgs, int);
-MEMFINE_FWD(bf16_t, 64, 4)
-MEMFINE_FWD(bf16_t, 64, 8)
-MEMFINE_FWD(bf16_t, 128, 4)
-MEMFINE_FWD(bf16_t, 128, 8)
-MEMFINE_FWD(float, 64, 4)
-MEMFINE_FWD(float, 128, 4)
-MEMFINE_DQ(bf16_t, 64)
-MEMFINE_DQ(bf16_t, 128)
-MEMFINE_DQ(float, 64)
-MEMFINE_DQ(float, 128)
+MEMFINE_FWD(bf16_t, 64, 4, 1)
+MEMFINE_FWD(bf16_t, 64, 8, 1)
+MEMFINE_FWD(bf16_t, 64, 8, 4)
+MEMFINE_FWD(bf16_t, 128, 4, 1)
+MEMFINE_FWD(bf16_t, 128, 8, 1)
+MEMFINE_FWD(bf16_t, 128, 8, 4)
+MEMFINE_FWD(float, 64, 4, 1)
+MEMFINE_FWD(float, 128, 4, 1)
+MEMFINE_DQ(bf16_t, 64, 4, 1)
+MEMFINE_DQ(bf16_t, 64, 8, 4)
+MEMFINE_DQ(bf16_t, 128, 4, 1)
+MEMFINE_DQ(bf16_t, 128, 8, 4)
+MEMFINE_DQ(float, 64, 4, 1)
+MEMFINE_DQ(float, 128, 4, 1)
 MEMFINE_DKV(bf16_t, 64, 4, false)
 MEMFINE_DKV(bf16_t, 64, 8, false)
 MEMFINE_DKV(bf16_t, 128, 8, true)
@@ -768,25 +835,22 @@ MEMFINE_DKV(float, 128, 4, false)
 template __global__ void attn_sum_kernel<bf16_t>(const AttnArgs);
 template __global__ void attn_sum_kernel<float>(const AttnArgs);
 
-// Heads of a group that a workgroup of `waves` takes together: the largest power of two that
-// divides the group.
-int share_of(const AttnArgs& g, int waves) {
+// Heads of a group that a workgroup for `sets` sets of 32 queries takes together: the largest
+// power of two that divides the group.
+int share_of(const AttnArgs& g, int sets) {
   int share = 0;
-  while ((g.heads / g.kv_heads) % (2 << share) == 0 && (2 << share) <= waves) ++share;
+  while ((g.heads / g.kv_heads) % (2 << share) == 0 && (2 << share) <= sets) ++share;
   return share;
 }
-template <typename T, int D, int NW> void run_fwd(AttnArgs g, hipStream_t s) {
-  g.share = share_of(g, NW);
-  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW >> g.share);
-  attn_fwd_kernel<T, D, NW><<<(unsigned)blocks * (g.heads >> g.share), 64 * NW, 0, s>>>(g, blocks);
+template <typename T, int D, int NW, int KS> void run_fwd(AttnArgs g, hipStream_t s) {
+  g.share = share_of(g, NW / KS);
+  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW / KS >> g.share);
+  attn_fwd_kernel<T, D, NW, KS><<<(unsigned)blocks * (g.heads >> g.share), 64 * NW, 0, s>>>(g, blocks);
 }
-template <typename T, int D> void run_dq(AttnArgs g, hipStream_t s) {
-  // four waves, two workgroups a CU: the one's start and end lie under the other's
-  // products (64 heads of 4096 tokens in 8 groups 372 us, eight waves 389; 32 sequences of
-  // 256 tokens, 32 heads, 77 against 99)
-  g.share = share_of(g, 4);
-  const int blocks = (int)blocks_of(g.T, g.seqs, 128 >> g.share);
-  attn_dq_kernel<T, D, 4><<<(unsigned)blocks * (g.heads >> g.share), 256, 0, s>>>(g, blocks);
+template <typename T, int D, int NW, int KS> void run_dq(AttnArgs g, hipStream_t s) {
+  g.share = share_of(g, NW / KS);
+  const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW / KS >> g.share);
+  attn_dq_kernel<T, D, NW, KS><<<(unsigned)blocks * (g.heads >> g.share), 64 * NW, 0, s>>>(g, blocks);
 }
 template <typename T, int D, int NW, bool kHeld> void run_dkv(const AttnArgs& g, hipStream_t s) {
   const int blocks = (int)blocks_of(g.T, g.seqs, 32 * NW);
@@ -798,6 +862,15 @@ template <typename T, int D, int NW, bool kHeld> void run_dkv(const AttnArgs& g,
   }
 }
 
+// So few sets of 32 queries (at most 4 a CU) of so long sequences that the longest ones' tiles,
+// one after the other, are the time: four waves a set, each with a quarter of the keys.  Two
+// heads of 6783 tokens 160 us with one wave, 69 with four; 16 heads in 2 groups, 2048 tokens
+// 56 and 37; 32 heads in 8 groups, 512 tokens 14.8 and 13.3, 1024 tokens 25.6 and 27.2; 8
+// sequences of 256 tokens, 8 heads 10.1 and 11.3.
+bool few_queries(const AttnArgs& g) {
+  const int64_t sets = blocks_of(g.T, g.seqs, 32) * g.heads, mean = g.T / std::max(g.seqs, 1);
+  return sets <= 4 * g.cus && mean >= 384 && mean * g.cus > 200 * sets;
+}
 // Sequences so short, on average, that the starts and ends of workgroups weigh more than
 // what twice the rows save of copies: four waves, several workgroups a CU, else eight.  The
 // forward, 8192 tokens, 32 heads in 8 groups: sequences of 256 44 us against 56, of
@@ -807,23 +880,23 @@ bool short_rows(const AttnArgs& g) { return g.T < 2048 * (int64_t)g.seqs; }
 
 }  // namespace
 
-// Parts that the heads of a group are shared out in for dk and dv: one workgroup's chain, all
-// queries of the group against 256 keys (fp32: 128), is the shortest time it can take, and
-// few keys leave CUs idle; but parts are written and read again.  In microseconds:
+// Parts that the tiles of a group's queries are shared out in for dk and dv: one workgroup's
+// chain, all queries of the group against 256 keys (fp32: 128), is the shortest time it can
+// take, and few keys leave CUs idle; but parts are written and read again.  In microseconds:
 //   tile x max(chain / parts + 4, (half the chain / parts + 4) workgroups per CU) + sums
 // (a start and an end weigh four tiles; tile: 3.5, fp32 8; sums: 6 and 16 bytes an element of
 // dk at 3 TB/s.)  32 heads in 8 groups, dim 128, without and with two parts: one sequence of
 // 8192 tokens 2.41 ms and 1.72, 8 of 1024 354 us and 409; 64 heads in 8 groups, 4096 tokens, one,
 // three and four parts 1.22, 0.97 and 0.91 ms.
-int attn_parts(const AttnArgs& g, int cus) {
+int attn_parts(const AttnArgs& g) {
   const int group = g.heads / g.kv_heads, keys = g.f32 ? 128 : 256, rows = g.f32 ? 32 : 64;
   const double items = (double)blocks_of(g.T, g.seqs, keys) * g.kv_heads;
   const double mean = (double)g.T / std::max<int64_t>(std::min<int64_t>(g.seqs, g.T), 1);
   const double chain = group * std::ceil(mean / rows);
   int best = 1;
   double least = 0.;
-  for (int p = 1; p <= group; p = p < group && 2 * p > group ? group : 2 * p) {
-    const double t = std::max(chain / p + 4., (.6 * chain / p + 4.) * items * p / cus) * (g.f32 ? 8. : 3.5) +
+  for (int p = 1; p <= 32 && p <= chain; p *= 2) {
+    const double t = std::max(chain / p + 4., (.6 * chain / p + 4.) * items * p / g.cus) * (g.f32 ? 8. : 3.5) +
                      (p > 1 ? 6. + p * (double)g.T * g.kv_heads * g.dim * 16. / 3e6 : 0.);
     if (p == 1 || t < least) {
       best = p;
@@ -844,14 +917,17 @@ bool attn_fits(const AttnArgs& g) {
 hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s) {
   if (!attn_fits(g)) return hipErrorInvalidValue;
   if (g.f32) {
-    if (g.dim == 64) run_fwd<float, 64, 4>(g, s);
-    else run_fwd<float, 128, 4>(g, s);
+    if (g.dim == 64) run_fwd<float, 64, 4, 1>(g, s);
+    else run_fwd<float, 128, 4, 1>(g, s);
+  } else if (few_queries(g)) {
+    if (g.dim == 64) run_fwd<bf16_t, 64, 8, 4>(g, s);
+    else run_fwd<bf16_t, 128, 8, 4>(g, s);
   } else if (short_rows(g)) {
-    if (g.dim == 64) run_fwd<bf16_t, 64, 4>(g, s);
-    else run_fwd<bf16_t, 128, 4>(g, s);
+    if (g.dim == 64) run_fwd<bf16_t, 64, 4, 1>(g, s);
+    else run_fwd<bf16_t, 128, 4, 1>(g, s);
   } else {
-    if (g.dim == 64) run_fwd<bf16_t, 64, 8>(g, s);
-    else run_fwd<bf16_t, 128, 8>(g, s);
+    if (g.dim == 64) run_fwd<bf16_t, 64, 8, 1>(g, s);
+    else run_fwd<bf16_t, 128, 8, 1>(g, s);
   }
   return hipGetLastError();
 }
@@ -861,18 +937,20 @@ hipError_t launch_attn_bwd(const AttnArgs& g, hipStream_t s) {
   // (dq's kernel writes top and delta, which dkv's reads)
   if (g.f32) {
     if (g.dim == 64) {
-      run_dq<float, 64>(g, s);
+      run_dq<float, 64, 4, 1>(g, s);
       run_dkv<float, 64, 4, false>(g, s);
     } else {
-      run_dq<float, 128>(g, s);
+      run_dq<float, 128, 4, 1>(g, s);
       run_dkv<float, 128, 4, false>(g, s);
     }
   } else if (g.dim == 64) {
-    run_dq<bf16_t, 64>(g, s);
+    if (few_queries(g)) run_dq<bf16_t, 64, 8, 4>(g, s);
+    else run_dq<bf16_t, 64, 4, 1>(g, s);
     if (short_rows(g)) run_dkv<bf16_t, 64, 4, false>(g, s);
     else run_dkv<bf16_t, 64, 8, false>(g, s);
   } else {
-    run_dq<bf16_t, 128>(g, s);
+    if (few_queries(g)) run_dq<bf16_t, 128, 8, 4>(g, s);
+    else run_dq<bf16_t, 128, 4, 1>(g, s);
     run_dkv<bf16_t, 128, 8, true>(g, s);
   }
   return hipGetLastError();

@@ -285,9 +285,10 @@ struct AttnArgs {
   float *top, *delta;           // [heads, T]: lse in bits, dO . O
   float* sums;                  // parts > 1: [parts][2][T, kv_heads, dim]
   int parts;                    // attn_parts
+  int cus;                      // compute units of the device
   int share;                    // (set by the launchers)
 };
-int attn_parts(const AttnArgs& g, int cus);
+int attn_parts(const AttnArgs& g);
 int64_t attn_bwd_floats(const AttnArgs& g);
 bool attn_fits(const AttnArgs& g);  // whether a launch holds that many rows and heads
 hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s);

@@ -272,17 +272,38 @@ def test_streams_graphs_and_allocator(mf):
 
 
 @pytest.mark.parametrize("dtype", ("bf16", "f32"))
-def test_parts_of_a_group(mf, dtype):
-    """Few keys, many heads to a group: its heads are shared out and their sums added."""
+def test_parts_of_the_queries(mf, dtype):
+    """Few keys and many queries to them: these are shared out and the sums added."""
     log(f"parts, {dtype}")
     c = Case(mf, [700, 0, 433], 32, 1, 64, dtype, before=3, after=2)
     c.check()
     need = mf.memfine_attn_bwd_workspace_bytes
-    each = 2 * 1138 * 64 * 4
-    parts = (need(c.attn, 1138, 3) - 2 * 1138 * 32 * 4) / each
+    parts = (need(c.attn, 1138, 3) - 2 * 1138 * 32 * 4) / (2 * 1138 * 64 * 4)
     assert parts == int(parts) and parts >= 2
-    Case(mf, [1300], 14, 2, 128, dtype).check()     # seven heads, not a power of two
-    Case(mf, [3, 1, 0, 40], 24, 1, 128, dtype).check()
+    Case(mf, [1300], 14, 2, 128, dtype).check()        # seven heads, not a power of two
+    Case(mf, [3, 1, 0, 40], 24, 1, 128, dtype).check()  # parts without a tile
+    Case(mf, [900], 1, 1, 64, dtype).check()           # one head's queries in parts
+    Case(mf, [1500, 130], 2, 2, 128, dtype, window=70).check()
+
+
+@pytest.mark.parametrize("D", (64, 128))
+@pytest.mark.parametrize("heads", [(1, 1), (6, 2), (8, 1)], ids=str)
+@pytest.mark.parametrize("kind", ("causal", "window", "all"))
+def test_few_queries(mf, heads, D, kind):
+    """Few heads of long sequences, whose keys four waves share: lengths around the tiles,
+    a short sequence beside them, rows of no sequence, large scores that grow."""
+    t = torch()
+    kw = dict(causal=kind != "all", window=200 if kind == "window" else 0)
+    log(f"few queries, {heads} {D} {kind}")
+    for lens in ([513], [1000, 7, 0, 897], [640, 385]):
+        Case(mf, lens, *heads, D, "bf16", before=2, after=1, **kw).check()
+    c = Case(mf, [800], *heads, D, "bf16", q_std=6.0, k_std=3.0, **kw)
+    c.x[:, heads[0]] *= t_ramp(800, c.x.dtype)
+    c.upload()
+    c.check()
+    O, lse = c.forward()
+    P, m = c.forward()
+    assert t.equal(O, P) and t.equal(lse, m)
 
 
 def test_gradient_against_differences(mf):
