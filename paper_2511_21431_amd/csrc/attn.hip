@@ -110,33 +110,46 @@ template <typename T, int D, int R = sizeof(T) == 2 ? 64 : 32> struct Tile {
     else if constexpr (kUnits == 16) return (row & 3) << 2 | ((row >> 2) & 3);
     else return (row & 2) << 1 | ((row >> 2) & 3);
   }
+  // What a lane's addresses begin with: further steps along a row and further columns are
+  // other units, an exclusive or; 16 rows on, the swizzle is the same.
+  struct At {
+    int row, col;
+  };
+  __device__ __forceinline__ static At at(int lane) {
+    const int r = lane & 31;
+    At x;
+    x.row = r * kPitch + (((lane >> 5) ^ swizzle(r)) << 4);
+    if constexpr (ES == 2) {
+      // lane j of each 16 supplies 4 columns of row j / 4 and gets 4 rows of column j
+      const int j = lane & 15, G = lane >> 4, q = (G >> 1) * 4 + (j >> 2);
+      x.col = q * kPitch + ((((G & 1) * 2 + ((j >> 1) & 1)) ^ swizzle(q)) << 4) + ((j & 1) << 3);
+    } else {
+      x.col = lane;
+    }
+    return x;
+  }
   // operand rows row0 .. row0 + 31, step ks of D
-  __device__ __forceinline__ static F row(const char* __restrict__ lds, int row0, int ks, int lane) {
-    const int r = row0 + (lane & 31);
-    return *(const F*)(lds + r * kPitch + (((ks * 2 + (lane >> 5)) ^ swizzle(r)) << 4));
+  __device__ __forceinline__ static F row(const char* __restrict__ lds, int row0, int ks, const At& x) {
+    return *(const F*)(lds + row0 * kPitch + (x.row ^ (ks << 5)));
   }
   // the transposed operand: its 32 rows are columns col0 .. col0 + 31, reduced over
   // step kk of the tile's rows, in the order in which Mma::of holds them
-  __device__ __forceinline__ static F col(const char* __restrict__ lds, int col0, int kk, int lane) {
+  __device__ __forceinline__ static F col(const char* __restrict__ lds, int col0, int kk, const At& x) {
     if constexpr (ES == 2) {
-      // lane j of each 16 supplies 4 columns of row j / 4 and gets 4 rows of column j
-      const int j = lane & 15, G = lane >> 4;
-      const int u = (col0 + (G & 1) * 16 + 4 * (j & 3)) >> 3, in = (j & 1) << 3;
-      const int r = kk * 16 + (G >> 1) * 4 + (j >> 2);
-      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_s16x4*)(lds + r * kPitch + ((u ^ swizzle(r)) << 4) + in));
-      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_s16x4*)(lds + (r + 8) * kPitch + ((u ^ swizzle(r + 8)) << 4) + in));
+      const int c = x.col ^ (col0 << 1);
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + kk * 16 * kPitch + c));
+      const s16x4_t hi =  // (8 rows on)
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + (kk * 16 + 8) * kPitch + (c ^ 32)));
       return __builtin_bit_cast(F, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      F x;
-      const int b = (col0 + (lane & 31)) * 4;
+      F f;
+      const int lane = x.col, b = (col0 + (lane & 31)) * 4;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const int r = kk * 8 + (lane >> 5) * 4 + s;
-        x[s] = *(const float*)(lds + r * kPitch + (((b >> 4) ^ swizzle(r)) << 4) + (b & 15));
+        f[s] = *(const float*)(lds + r * kPitch + (((b >> 4) ^ swizzle(r)) << 4) + (b & 15));
       }
-      return x;
+      return f;
     }
   }
 };
@@ -352,6 +365,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
   __shared__ __align__(1024) char smem[kNeed > kSums ? kNeed : kSums];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
+  const typename L::At lds_at = L::at(lane);
   int head, b;
   Part p;
   // 2^share waves take the same queries for as many heads
@@ -404,7 +418,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
 #pragma unroll
     for (int k = 0; k < L::kSteps; ++k)
 #pragma unroll
-      for (int i = 0; i < kOwn; ++i) M::mma(L::row(ks, 32 * (k0 + i), k, lane), q[k], s[i]);
+      for (int i = 0; i < kOwn; ++i) M::mma(L::row(ks, 32 * (k0 + i), k, lds_at), q[k], s[i]);
     if (!see_all(first, last, r0, 32 * kOwn)) {
 #pragma unroll
       for (int i = 0; i < kOwn; ++i) hide(s[i], own, r0 + 32 * i, hh, -INFINITY);
@@ -444,7 +458,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
         // sum is not): half a step of bf16 each, which averages out over the row
         const Frag<T> f = M::of(s[i], j);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, (k0 + i) * L::kDown + j, lane), f, o[d]);
+        for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, (k0 + i) * L::kDown + j, lds_at), f, o[d]);
       }
   };
   for (int t = t0; t < t1; t += 2) {
@@ -497,6 +511,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
   __shared__ __align__(1024) char smem[kNeed > kSums ? kNeed : kSums];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
+  const typename L::At lds_at = L::at(lane);
   int head, b;
   Part p;
   // 2^share waves take the same queries for as many heads
@@ -571,8 +586,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
       zero(dp);
 #pragma unroll
       for (int k = 0; k < L::kSteps; ++k) {
-        M::mma(L::row(ks, 32 * (k0 + i), k, lane), q[k], s);
-        M::mma(L::row(vs, 32 * (k0 + i), k, lane), d_o[k], dp);
+        M::mma(L::row(ks, 32 * (k0 + i), k, lds_at), q[k], s);
+        M::mma(L::row(vs, 32 * (k0 + i), k, lds_at), d_o[k], dp);
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = exp2_(fmaf(s[e], c, -ref)) * (dp[e] - delta);
@@ -581,7 +596,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
       for (int j = 0; j < L::kDown; ++j) {
         const Frag<T> f = M::of(s, j);  // (rounded as the forward's weights)
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) M::mma(L::col(ks, 32 * d, (k0 + i) * L::kDown + j, lane), f, a[d]);
+        for (int d = 0; d < D / 32; ++d) M::mma(L::col(ks, 32 * d, (k0 + i) * L::kDown + j, lds_at), f, a[d]);
       }
     }
   };
@@ -608,7 +623,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
 // a run of these tiles and leaves its sums in fp32 for attn_sum_kernel.
 // kHeld: the values stay in LDS, not in registers, of which two waves a SIMD have 256 each.
 template <typename T, int D, int NW, bool kHeld>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 2 : 1) void attn_dkv_kernel(const AttnArgs g, int blocks) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 : 1) void attn_dkv_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D> L;
   typedef Mma<T> M;
   constexpr int kBlock = 32 * NW;
@@ -619,6 +634,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 2 :
   __shared__ __align__(16) float stats[2][2][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hh = lane >> 5;
+  const typename L::At lds_at = L::at(lane);
   int kv, b;
   Part p;
   work_item(blocks * g.parts, g.kv_heads, false, kv, b);
@@ -697,12 +713,15 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 2 :
       f32x16_t s, dp;
       zero(s);
       zero(dp);
+      // (the addresses are formed where they are used, not held in registers, which are full)
+      typename L::At here = lds_at;
+      if constexpr (kHeld) asm volatile("" : "+v"(here.row), "+v"(here.col));
       // (a step's operands are read while the one before it multiplies, and no earlier)
       Frag<T> a[2], o[2], u[2];
       auto rows_of = [&](int e) {
-        a[e & 1] = L::row(qs, 32 * i, e, lane);
-        o[e & 1] = L::row(os, 32 * i, e, lane);
-        if constexpr (kHeld) u[e & 1] = L::row(held, 32 * w, e, lane);
+        a[e & 1] = L::row(qs, 32 * i, e, here);
+        o[e & 1] = L::row(os, 32 * i, e, here);
+        if constexpr (kHeld) u[e & 1] = L::row(held, 32 * w, e, here);
       };
       rows_of(0);
 #pragma unroll
@@ -730,8 +749,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 2 :
       }
       constexpr int kCols = D / 32;
       auto cols_of = [&](int x) {
-        o[x & 1] = L::col(os, 32 * (x % kCols), i * L::kDown + x / kCols, lane);
-        a[x & 1] = L::col(qs, 32 * (x % kCols), i * L::kDown + x / kCols, lane);
+        o[x & 1] = L::col(os, 32 * (x % kCols), i * L::kDown + x / kCols, here);
+        a[x & 1] = L::col(qs, 32 * (x % kCols), i * L::kDown + x / kCols, here);
       };
       cols_of(0);
 #pragma unroll
