@@ -74,22 +74,20 @@ __device__ __forceinline__ void turn(float (&x)[8], float (&y)[8], const float (
   }
 }
 
-// The 8 pairs' cosines and sines at a position; NaN past the tables.
+// The 8 pairs' cosines and sines at a position; NaN past the tables (whose first row is
+// read then: a branch around the loads keeps two of the values in memory).
 __device__ __forceinline__ void angles(const RopeTable& r, int64_t pos, int at, int dim, float (&cs)[8],
                                        float (&sn)[8]) {
-  if (pos >= r.positions) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cs[i] = sn[i] = __uint_as_float(0x7fc00000u);
-    return;
-  }
-  const int64_t row = pos * (dim / 2) + at;
+  const bool in = pos < r.positions;
+  const int64_t row = (in ? pos : 0) * (dim / 2) + at;
+  const float none = __uint_as_float(0x7fc00000u);
 #pragma unroll
   for (int i = 0; i < 8; i += 4) {
     const f32x4_t c = *(const f32x4_t*)(r.cos + row + i), s = *(const f32x4_t*)(r.sin + row + i);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      cs[i + e] = c[e];
-      sn[i + e] = r.inverse ? -s[e] : s[e];
+      cs[i + e] = in ? c[e] : none;
+      sn[i + e] = in ? (r.inverse ? -s[e] : s[e]) : none;
     }
   }
 }
