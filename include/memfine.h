@@ -635,7 +635,8 @@ int memfine_attn_fwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32
  * overwritten, rows of no sequence left as they were; they must not overlap the
  * inputs.  Every sum has a fixed order, which depends on T, seqs, the heads and the
  * device's compute units alone.  Working memory (two floats a row and head, and partial
- * dK and dV where keys are few: memfine_attn_bwd_workspace_bytes, < 0: invalid arguments) comes from `alloc` as for the layer's calls.
+ * dK and dV where keys are few: memfine_attn_bwd_workspace_bytes, < 0: invalid arguments)
+ * comes from `alloc` as for the layer's calls.
  */
 int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
                      const void* d_Q, int64_t ld_q, const void* d_K, int64_t ld_k, const void* d_V,

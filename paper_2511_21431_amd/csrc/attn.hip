@@ -15,6 +15,12 @@
 // rounded, the operand of the second product as they stand: which of the 16
 // values of a reduction step a register holds is the accumulator's choice, and
 // the other operand, read from LDS with a transposing load, follows it.
+//
+// Bound by the matrix cores where sequences are long, and by the clock that power
+// leaves them (1.7 to 1.9 GHz of 2.4 while these kernels run); next to them every score
+// costs vector instructions (exponent, sum, rounding), 40 to 50 % of the SIMDs' cycles,
+// which only another wave's products hide: two or more waves a SIMD.  Short sequences
+// are bound by a workgroup's start (offsets, queries, first tile: about 4 us) and end.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -237,7 +243,8 @@ __device__ __forceinline__ void put_lanes(float* to, const f32x16_t (&o)[D / 32]
     for (int e = 0; e < 16; ++e) to[(b * 16 + e) * 64 + lane] = o[b][e];
 }
 template <int D>
-__device__ __forceinline__ void add_lanes(const float* from, f32x16_t (&o)[D / 32], float mf, float of, int lane) {
+__device__ __forceinline__ void add_lanes(const float* from, f32x16_t (&o)[D / 32], float mf, float of,
+                                          int lane) {
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -354,8 +361,13 @@ __device__ __forceinline__ void hide(f32x16_t& c, const Seen& s, int r0, int hh,
 // then need the same tiles), the rest further queries.  KS = 4, for so few queries that most
 // CUs would have none: four waves take the same queries and a quarter of each tile's keys,
 // of which there are twice as many; what they have is joined at the end, in order.
+// Tiles of 64 keys in two stages: 64 KiB at D = 128, so that two workgroups of four or one
+// of eight waves fill a CU's registers (three stages and three workgroups spill).
+// 4096 tokens of 128 heads of 128, causal: 605 us, 909 TFLOP/s (matrix cores busy 48 % of
+// the cycles, vector 42); 12 sequences of 90 to 2000 tokens, 32 heads in 8 groups: 104 us.
 template <typename T, int D, int NW, int KS>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void attn_fwd_kernel(const AttnArgs g, int blocks) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1)
+void attn_fwd_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D, KS == 1 ? Tile<T, D>::kRows : 32 * KS> L;
   constexpr int kOwn = L::kBlocks / KS;  // blocks of a tile that a wave takes
   typedef Mma<T> M;
@@ -498,10 +510,17 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
 }
 
 // ---------------------------------------------------------------- backward
+// Two kernels, each of which forms the scores: 7 products where 5 would do with dq added up
+// in memory by atomics, whose order, and with it the result, would change from call to call.
+//
 // dq (shared out as in the forward), and their log2 of the weights' sum and delta for the
-// kernel below.
+// kernel below.  A block's ds is all that is held between its products, so that queries,
+// dO and dq stay in registers; four waves a workgroup, also for long sequences: 4096 tokens
+// of 64 heads in 8 groups, causal, 372 us, with eight waves 389; 6011 tokens of 16 heads of
+// 64 in 9 sequences 34 us.  The first runs at 1.1 PFLOP/s, its matrix cores busy for 61 %.
 template <typename T, int D, int NW, int KS>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void attn_dq_kernel(const AttnArgs g, int blocks) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1)
+void attn_dq_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D, KS == 1 ? Tile<T, D>::kRows : 32 * KS> L;
   constexpr int kOwn = L::kBlocks / KS;  // blocks of a tile that a wave takes
   typedef Mma<T> M;
@@ -621,9 +640,14 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1) void at
 // dk and dv of 32 NW rows a workgroup: it goes through the queries of the heads that share
 // them, head after head, so that every sum has one order.  With several parts each takes
 // a run of these tiles and leaves its sums in fp32 for attn_sum_kernel.
-// kHeld: the values stay in LDS, not in registers, of which two waves a SIMD have 256 each.
+// kHeld: the values stay in LDS, not in registers, of which two waves a SIMD have 256 each:
+// keys, dk and dv take 160 of them (with the values too, or 64 keys a wave, they spill).
+// 4096 tokens of 64 heads in 8 groups of 128, causal: 537 us in four parts and 23 for their
+// sum, 1.0 PFLOP/s, matrix cores busy for 55 %, vector instructions 34; 6011 tokens of 16
+// heads of 64 in 9 sequences 37 us (three waves a SIMD; two 41).
 template <typename T, int D, int NW, bool kHeld>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 : 1) void attn_dkv_kernel(const AttnArgs g, int blocks) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 : 1)
+void attn_dkv_kernel(const AttnArgs g, int blocks) {
   typedef Tile<T, D> L;
   typedef Mma<T> M;
   constexpr int kBlock = 32 * NW;
@@ -788,7 +812,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && D == 64 && NW == 4 ? 3 :
 }
 
 // dK and dV from the parts' sums [parts][dK, dV][T][kv_heads dim], added in order: four
-// elements a thread, of rows that lie in a sequence.
+// elements a thread, of rows that lie in a sequence.  Bound by memory: four parts of 4096
+// rows of 8 heads of 128, 151 MB, 23 us (6.5 TB/s, some of it out of caches).
 template <typename T>
 __global__ __launch_bounds__(256) void attn_sum_kernel(const AttnArgs g) {
   const int64_t kvd = (int64_t)g.kv_heads * g.dim, n = g.T * kvd / 4;

@@ -226,6 +226,12 @@ template <int D> struct Sums {
   float m, l;         // (l: of this lane quarter's tokens)
 };
 
+// Two workgroups a CU, all resident, with the next step's loads in flight while one is
+// multiplied: 2 x 4 waves x 16 KiB a CU (bf16, D = 128), several times what the memory's
+// latency needs.  One sequence of 131072 tokens, 8 key-value heads of 128: 92 us, 5.8 TB/s;
+// 16 of 2048, 128 heads 370 us, 5.8 TB/s; in MX8 64 of 4096 on average, pages of 16, 64
+// heads in 8 groups 108 us, 5.1 TB/s (the values' way through LDS as bf16: two writes a
+// load with conflicts on 39 % of the cycles that LDS is busy, and vector instructions for 31 %).
 template <int D, bool MX8>
 __global__ __launch_bounds__(256, 2) void decode_kernel(const DecodeArgs g) {
   typedef Held<D, MX8> H;
@@ -359,8 +365,10 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(const DecodeArgs g) {
             if constexpr (MX8) {
               // elements 64 i + 16 g .. + 15: block 2 i + g / 2
               const float sc = cvt_scale(now.ks[h] >> (8 * (2 * i + (lg >> 1))) & 255u);
-              s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(k[0], k[1], sc), q[2 * i], s[h], 0, 0, 0);
-              s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(k[2], k[3], sc), q[2 * i + 1], s[h], 0, 0, 0);
+              s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(k[0], k[1], sc), q[2 * i], s[h],
+                                                             0, 0, 0);
+              s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(k[2], k[3], sc), q[2 * i + 1], s[h],
+                                                             0, 0, 0);
             } else {
               s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), q[i], s[h], 0, 0, 0);
             }
@@ -396,6 +404,8 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(const DecodeArgs g) {
           p[e] = exp2_(fmaf(s[e >> 2][e & 3], c, -ref));
           a.l += p[e];
         }
+        // (the weights rounded to bf16, the matrix core's operand, their sum not: half a step
+        // each, which averages out over the row)
         const bf16x8_t pw = __builtin_bit_cast(bf16x8_t, pack16(p, (bf16_t*)nullptr));
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
@@ -477,7 +487,8 @@ __device__ __forceinline__ void join(f32x4_t& o, float& m, float& l, const f32x4
 
 // Joins the parts of one pair of a sequence whose steps lie in more than one
 // workgroup's run, in order; writes zeros where there is no token.  Workgroup (x, y): pair
-// x, its heads y, y + gridDim.y, ...
+// x, its heads y, y + gridDim.y, ...  Bound by latency, 4 to 5 us, which a second
+// launch needs anyway: the lengths' sums, then the parts, which lie in caches.
 template <int D>
 __global__ __launch_bounds__(256) void join_kernel(const DecodeArgs g) {
   constexpr int kRow = D + 4, kCols = D / 4, kAcross = 256 / kCols;
