@@ -561,18 +561,19 @@ void attn_dq_kernel(const AttnArgs g, int blocks) {
   const int64_t ldo = (int64_t)g.heads * D, at = ((p.begin + i0) * (int64_t)g.heads + head) * D;
   load_rows<T, D>(q, (const T*)g.Q + (p.begin + i0) * g.ldq + head * D, g.ldq, mine, lane);
   load_rows<T, D>(d_o, (const T*)g.dO + at, ldo, mine, lane);
+  // delta_i from O_i . dO_i of all the wave's rows, of which the diagonal counts: formed as dp is,
+  // step by step, so that their difference is exactly zero for a token whose output is the
+  // one value that it sees (vector instructions would add up in another order).
   float delta = 0.f;
   {
     Frag<T> f[L::kSteps];
     load_rows<T, D>(f, (const T*)g.O + at, ldo, mine, lane);
+    f32x16_t x;
+    zero(x);
 #pragma unroll
-    for (int k = 0; k < L::kSteps; ++k) {
-      float x[M::kStep / 2], y[M::kStep / 2];
-      unpack16(__builtin_bit_cast(u32x4_t, f[k]), x, (T*)nullptr);
-      unpack16(__builtin_bit_cast(u32x4_t, d_o[k]), y, (T*)nullptr);
+    for (int k = 0; k < L::kSteps; ++k) M::mma(f[k], d_o[k], x);
 #pragma unroll
-      for (int e = 0; e < M::kStep / 2; ++e) delta = fmaf(x[e], y[e], delta);
-    }
+    for (int e = 0; e < 16; ++e) delta = acc_row(e, hh) == (lane & 31) ? x[e] : delta;
   }
   delta = halves_sum(delta);
   const int64_t row = head * g.T + p.begin + i0;

@@ -306,6 +306,27 @@ def test_few_queries(mf, heads, D, kind):
     assert t.equal(O, P) and t.equal(lse, m)
 
 
+@pytest.mark.parametrize("D", (64, 128))
+@pytest.mark.parametrize("heads", [(1, 1), (6, 2), (16, 4)], ids=str)
+def test_one_visible_token_has_no_gradient_of_scores(mf, heads, D):
+    """bf16: where a token sees itself alone its weight is 1 and its output the value, so
+    that dp - delta, of equal rows summed in one order, is zero: dQ is exactly zero for a
+    sequence's first token, and dQ and dK for a window of one and sequences of one."""
+    t = torch()
+    for lens, window in (([1] * 37, 0), ([300, 1, 64], 1), ([900], 1), ([900], 0), ([5, 70, 33], 0)):
+        log(f"one visible token, {heads} {D} {lens[0]} x {len(lens)} window {window}")
+        c = Case(mf, lens, *heads, D, "bf16", window=window, before=1)
+        O, lse = c.forward()
+        d = c.backward(O, lse)
+        dQ, dK, _ = c.split(d)
+        rows = t.from_numpy(c.rows).cuda()
+        if max(lens) == 1 or window == 1:
+            assert int(t.count_nonzero(dQ[rows])) == 0 and int(t.count_nonzero(dK[rows])) == 0
+        else:
+            assert int(t.count_nonzero(dQ[c.offsets[:-1].long()])) == 0
+        c.check_backward(O, lse, d)
+
+
 def test_gradient_against_differences(mf):
     """fp32: the loss sum(O dO) along random directions; a step of e leaves a second
     difference of e^2 and rounding of about 2^-24 sum |O dO| / e."""
