@@ -361,18 +361,20 @@ __device__ __forceinline__ void hide(f32x16_t& c, const Seen& s, int r0, int hh,
 // then need the same tiles), the rest further queries.  KS = 4, for so few queries that most
 // CUs would have none: four waves take the same queries and a quarter of each tile's keys,
 // of which there are twice as many; what they have is joined at the end, in order.
-// Tiles of 32 keys in two stages, so that three workgroups of four waves share a CU
-// (D = 64: four): one starts or ends while others multiply.  Against tiles of 64, of which
-// two fit, in workgroups of four waves or, for long sequences, of eight: 8192 tokens
-// of 32 heads of 128 in 8 groups, in sequences of 256 43 us against 47, of 668 66 and 71,
-// one 515 and 514; with a window of 512 82 and 98; 4096 tokens of 128 heads 556 and 590, 990
-// TFLOP/s; heads of 64, sequences of 256 29.0 us and 29.1, of 2048 95 and 94, of 4096 164 and 166.
+// D = 128: tiles of 32 keys in two stages, so that three workgroups of four waves share a CU:
+// one starts or ends while others multiply.  Against tiles of 64, of which two fit, in
+// workgroups of four waves or, for long sequences, of eight: 8192 tokens of 32 heads in 8
+// groups, in sequences of 256 43 us against 47, of 668 66 and 71, one 515 and 514; with a window
+// of 512 82 and 98; 4096 tokens of 128 heads 549 and 575, 1.0 PFLOP/s.  D = 64: tiles of 64
+// keys, of which four fit: 8 sequences of 1024 tokens, 32 heads 56 us against 57.5 with tiles
+// of 32, two of 2048, 64 heads, not causal 146 and 160, but one of 8192, 16 heads 177 and 171.
 // (Two halves of a workgroup that multiply and exponentiate in turns, a barrier
-// between, were 2 % slower, 11 for heads of 64: power bounds both.)
+// between, were 2 % slower, 11 for heads of 64.)
 template <typename T, int D, int NW, int KS>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 || KS > 1 ? 1 : D == 128 ? 3 : 4)
 void attn_fwd_kernel(const AttnArgs g, int blocks) {
-  typedef Tile<T, D, 32 * KS> L;
+  typedef Tile<T, D, KS != 1 ? 32 * KS : D == 64 ? Tile<T, D>::kRows : 32> L;
+  constexpr int kOwn = L::kBlocks / KS;  // blocks of a tile that a wave takes
   typedef Mma<T> M;
   // (joined waves store through LDS that no other wave's sums are in)
   constexpr int kOutPitch = KS == 1 ? L::kPitch : (D / 2 + 2) * 8;
@@ -387,7 +389,7 @@ void attn_fwd_kernel(const AttnArgs g, int blocks) {
   const int block = 32 * NW / KS >> g.share;
   work_item(blocks, g.heads >> g.share, g.causal, head, b);
   if (!locate(g.offsets, g.seqs, (int)g.T, block, b, p)) return;
-  const int wq = w / KS, k0 = w % KS;  // whose queries, which block of the tiles
+  const int wq = w / KS, k0 = w % KS * kOwn;  // whose queries, first block of the tiles
   head = (head << g.share) + (wq & ((1 << g.share) - 1));
   const int kv = head / (g.heads / g.kv_heads);
   const int q0 = p.block * block, rows = min(block, p.n - q0);
@@ -423,18 +425,26 @@ void attn_fwd_kernel(const AttnArgs g, int blocks) {
     constexpr int kAt = decltype(stage)::value * 2 * L::kBytes;
     stage_barrier();
     if (t + 1 < t1) issue(t + 1, smem + (2 * L::kBytes - kAt));
-    const int r0 = t * L::kRows + 32 * k0;  // of the wave's block
-    if (mine <= 0 || r0 > last.hi || r0 + 32 <= first.lo) return;
+    const int r0 = t * L::kRows + 32 * k0;  // of the wave's own blocks
+    if (mine <= 0 || r0 > last.hi || r0 + 32 * kOwn <= first.lo) return;
     const char* ks = smem + kAt;
     const char* vs = ks + L::kBytes;
-    f32x16_t s;
-    zero(s);
+    f32x16_t s[kOwn];
 #pragma unroll
-    for (int k = 0; k < L::kSteps; ++k) M::mma(L::row(ks, 32 * k0, k, lds_at), q[k], s);
-    if (!see_all(first, last, r0, 32)) hide(s, own, r0, hh, -INFINITY);
-    float top = s[0];
+    for (int i = 0; i < kOwn; ++i) zero(s[i]);
 #pragma unroll
-    for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+    for (int k = 0; k < L::kSteps; ++k)
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) M::mma(L::row(ks, 32 * (k0 + i), k, lds_at), q[k], s[i]);
+    if (!see_all(first, last, r0, 32 * kOwn)) {
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) hide(s[i], own, r0 + 32 * i, hh, -INFINITY);
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
     top = halves_max(top) * c;
     // The sums are kept relative to 2^m, m a maximum seen so far: it moves, and they are
     // multiplied, only where a row's maximum has passed it by more than 8 (weights of up to
@@ -451,18 +461,22 @@ void attn_fwd_kernel(const AttnArgs g, int blocks) {
     }
     const float ref = m == -INFINITY ? 0.f : m;  // (a row that sees nothing yet)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      s[e] = exp2_(fmaf(s[e], c, -ref));
-      l += s[e];
-    }
+    for (int i = 0; i < kOwn; ++i)
 #pragma unroll
-    for (int j = 0; j < L::kDown; ++j) {
-      // the weights are rounded to the values' type, the matrix core's operand (their
-      // sum is not): half a step of bf16 each, which averages out over the row
-      const Frag<T> f = M::of(s, j);
+      for (int e = 0; e < 16; ++e) {
+        s[i][e] = exp2_(fmaf(s[i][e], c, -ref));
+        l += s[i][e];
+      }
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, k0 * L::kDown + j, lds_at), f, o[d]);
-    }
+    for (int i = 0; i < kOwn; ++i)
+#pragma unroll
+      for (int j = 0; j < L::kDown; ++j) {
+        // the weights are rounded to the values' type, the matrix core's operand (their
+        // sum is not): half a step of bf16 each, which averages out over the row
+        const Frag<T> f = M::of(s[i], j);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, (k0 + i) * L::kDown + j, lds_at), f, o[d]);
+      }
   };
   for (int t = t0; t < t1; t += 2) {
     tile(t, std::integral_constant<int, 0>());
@@ -847,6 +861,7 @@ int64_t blocks_of(int64_t T, int64_t seqs, int R) {
 #define MEMFINE_DKV(T, D, NW, HELD) \
   template __global__ void attn_dkv_kernel<T, D, NW, HELD>(const AttnArgs, int);
 MEMFINE_FWD(bf16_t, 64, 4, 1)
+MEMFINE_FWD(bf16_t, 64, 8, 1)
 MEMFINE_FWD(bf16_t, 64, 8, 4)
 MEMFINE_FWD(bf16_t, 128, 4, 1)
 MEMFINE_FWD(bf16_t, 128, 8, 4)
@@ -906,8 +921,10 @@ bool few_queries(const AttnArgs& g) {
   return sets <= 4 * g.cus && mean >= 384 && mean * g.cus > 200 * sets;
 }
 // Sequences so short, on average, that the starts and ends of workgroups weigh more than
-// what twice the rows save of copies: dk and dv of heads of 64 by four waves, several workgroups
-// a CU, else eight.  16 heads, sequences of 668 tokens 38 us against 50, of 4096 68 against 60.
+// what twice the rows save of copies: four waves, several workgroups a CU, else eight (heads of
+// 64).  Forward, 32 heads, sequences of 256 tokens 29 us against 30, of 1024 56 and 60, of 2048
+// 92 and 94, of 4096 178 and 165; dk and dv of 16 heads, sequences of 668 tokens 38 us against
+// 50, of 4096 68 and 60.
 bool short_rows(const AttnArgs& g) { return g.T < 2048 * (int64_t)g.seqs; }
 
 }  // namespace
@@ -955,8 +972,9 @@ hipError_t launch_attn_fwd(const AttnArgs& g, hipStream_t s) {
     if (g.dim == 64) run_fwd<bf16_t, 64, 8, 4>(g, s);
     else run_fwd<bf16_t, 128, 8, 4>(g, s);
   } else {
-    if (g.dim == 64) run_fwd<bf16_t, 64, 4, 1>(g, s);
-    else run_fwd<bf16_t, 128, 4, 1>(g, s);
+    if (g.dim == 128) run_fwd<bf16_t, 128, 4, 1>(g, s);
+    else if (short_rows(g)) run_fwd<bf16_t, 64, 4, 1>(g, s);
+    else run_fwd<bf16_t, 64, 8, 1>(g, s);
   }
   return hipGetLastError();
 }
