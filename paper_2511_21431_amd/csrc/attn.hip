@@ -17,8 +17,8 @@
 // the other operand, read from LDS with a transposing load, follows it.
 //
 // Bound by the matrix cores where sequences are long, and by the clock that power
-// leaves them (1.7 to 1.9 GHz of 2.4 while these kernels run); next to them every score
-// costs vector instructions (exponent, sum, rounding), 40 to 50 % of the SIMDs' cycles,
+// leaves them (1.6 to 1.9 GHz of 2.4 while these kernels run); next to them every score
+// costs vector instructions (exponent, sum, rounding), 35 to 60 % of the SIMDs' cycles,
 // which only another wave's products hide: two or more waves a SIMD.  Short sequences
 // are bound by a workgroup's start (offsets, queries, first tile: about 4 us) and end.
 #include <algorithm>
