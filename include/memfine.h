@@ -703,7 +703,8 @@ int memfine_kv_write(const memfine_cache* c, int64_t T, int32_t seqs, int32_t wi
 /*
  * Attention of one token a sequence over its cached tokens (its own among them;
  * with a->window, the last `window`): O_b and lse_b as memfine_attn_fwd's for the
- * last token of sequence b.  A sequence without tokens gets zeros (lse -inf).
+ * last token of sequence b, but with the weights of the product with V to 2^-16 of
+ * each.  A sequence without tokens gets zeros (lse -inf).
  *   a      kv_heads and dim as the cache's, dtype MEMFINE_BF16; causal is not used
  *   d_Q    bf16 [seqs, heads, dim];  d_O  bf16 [seqs, heads, dim] out
  *   d_lse  float [seqs, heads] out, may be null

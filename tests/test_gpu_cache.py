@@ -359,6 +359,26 @@ def test_decode_values_that_are_not_finite(mf):
         assert t.equal(P[[0, 2]], O[[0, 2]]) and t.all(t.isnan(P[1]))
 
 
+@pytest.mark.parametrize("held", ("bf16", "mx8"))
+@pytest.mark.parametrize("D", (64, 128))
+def test_decode_rounds_its_outputs_alone(mf, D, held):
+    """The weights enter as two bf16 values, 2^-16 of each off: all that is left of bf16's half
+    step is that of the output, also where a row's values cancel."""
+    t = torch()
+    lens, H = [7, 60, 300, 1500], 20
+    p = Pages(mf, lens, 2, D, 32, held, seed=D)
+    q = (t.randn(4, H, D, generator=gen(9)) * 1.5).to(t.bfloat16)
+    O = t.full((4, H, D), float("nan"), dtype=t.bfloat16, device="cuda")
+    log(f"weights of decode, {D} {held}")
+    mf.memfine_attn_decode(mf.make_attn(H, 2, D), p.cache, p.dtable, ints(lens), q.cuda(), O)
+    for b, n in enumerate(lens):
+        ref, rl, A, big = at.decode(f64(q)[b], p.tokens(0, b, n), p.tokens(1, b, n), D ** -0.5)
+        ds = U * ((D + 12) * big + 8 * np.abs(rl) + 8)
+        tol = A * (2.0 ** -16 + 2 * ds[:, None] + (n + 64) * U) + B * np.abs(ref)
+        off = np.abs(f64(O)[b] - ref) - tol
+        assert np.all(off <= 0), (n, float(off.max()), int((off > 0).sum()))
+
+
 def test_decode_growing_scores(mf):
     t = torch()
     lens = [900]
