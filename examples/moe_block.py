@@ -72,13 +72,16 @@ class ServedAttention:
         """Rows x [sum(lens), h] of one new prompt a sequence; returns [sum(lens), H D]."""
         offsets = offsets_of(lens)
         self.lengths.copy_(offsets[1:] - offsets[:-1])
-        qkv, out = empty(len(x), self.N), empty(len(x), self.H, self.D)
+        qkv, turned, out = (empty(len(x), n) for n in (self.N, self.H * self.D, self.H * self.D))
         mf.memfine_linear_mxw(self.N, self.h, x, *self.W, qkv)
         q, k, v = self.split(qkv)
-        both = qkv.view(len(x), -1, self.D)[:, :self.H + self.Hk]
-        mf.memfine_rope(offsets, self.cos, self.sin, both, both)
-        mf.memfine_kv_write(self.cache, self.table, self.lengths, k, v, offsets=offsets)
-        mf.memfine_attn_fwd(self.attn, offsets, q, k, v, out)
+        turned, out = turned.view(q.shape), out.view(q.shape)
+        # (keys go into the cache unrounded, like those of later tokens; as rows they are turned
+        # for the prompts' own attention)
+        mf.memfine_kv_write(self.cache, self.table, self.lengths, k, v, offsets=offsets, Q=q, R=turned,
+                            cos=self.cos, sin=self.sin)
+        mf.memfine_rope(offsets, self.cos, self.sin, k, k)
+        mf.memfine_attn_fwd(self.attn, offsets, turned, k, v, out)
         return out.view(len(x), -1)
 
     def step(self, x, allocator=None):

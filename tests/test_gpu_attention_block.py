@@ -87,6 +87,31 @@ def test_served_prompt_and_steps(ex, mx8):
         assert t.equal(a.out, o)
 
 
+@pytest.mark.parametrize("mx8", (False, True), ids=("bf16", "mx8"))
+def test_prompts_and_steps_cache_the_same_keys(ex, mx8):
+    """A prompt's keys and values lie in the cache bit for bit as rows that are written with the
+    tables in hand, as single tokens are: turned and rounded once."""
+    t = torch()
+    lens = [37, 5, 100]
+    W = draw((H + 2 * HK) * D, HID, seed=1, std=HID ** -0.5)
+    a, b = (ex.ServedAttention(W, ex.mf.make_attn(H, HK, D), 3, 128, page=32, mx8=mx8) for _ in range(2))
+    x = draw(sum(lens), HID, seed=5)
+    a.prompt(x, lens)
+    qkv = t.empty(len(x), a.N, dtype=t.bfloat16, device="cuda")
+    ex.mf.memfine_linear_mxw(a.N, a.h, x, *a.W, qkv)
+    _, k, v = b.split(qkv)
+    at = 0
+    for i, n in enumerate(lens):      # token by token
+        log(f"sequence {i}")
+        for j in range(n):
+            length = t.full((1,), j + 1, dtype=t.int32, device="cuda")
+            ex.mf.memfine_kv_write(b.cache, b.table[i:i + 1], length, k[at + j:at + j + 1], v[at + j:at + j + 1],
+                                   cos=b.cos, sin=b.sin)
+        at += n
+    for y, z in zip(a.cache.tensors, b.cache.tensors):
+        assert (y is None and z is None) or t.equal(y, z)
+
+
 def test_trained_gradients(ex):
     """Against autograd in float64: qkv, turned rows, attention's weights and outputs, the
     products' outputs are rounded to bf16, 2^-8 each at most: eight of them, 2^-5 of
