@@ -8,11 +8,12 @@
 `ServedAttention` stands in front of a block of an inference engine: the projection
 of queries, keys and values, their rotation, the cache of pages (MX8, or bf16) and the
 attention over it, for whole prompts and then token by token; `TrainedAttention` is
-the same in training, over packed sequences.  `ServedBlock` is one block of an inference engine with its weights in MX4: the
-attention's output projection, residual and norm, routing and the experts; the
-activations of the experts are MX8 (or bf16), four library calls and the
-router's product a step.  `TrainedBlock` is the block in training, forward and
-gradients, in bf16.  All tensors a step writes are the block's own, made once.
+the same in training, over packed sequences.  `ServedBlock` is one block of an
+inference engine with its weights in MX4: the attention's output projection, residual
+and norm, routing and the experts; the activations of the experts are MX8 (or bf16),
+four library calls and the router's product a step.  `TrainedBlock` is the block in
+training, forward and gradients, in bf16.  `ServedLayer` and `TrainedLayer` join
+attention and block.  What a step of a block writes are the block's own tensors, made once.
 """
 import argparse
 import os
@@ -212,6 +213,40 @@ class TrainedBlock:
         self.bias += rate * torch.sign(load.mean() - load)
 
 
+class ServedLayer:
+    """A decode step of norm, attention and block; w [h]: weight of the norm in front of the
+    attention."""
+
+    def __init__(self, w, attention, block):
+        self.w, self.attention, self.block = w, attention, block
+        self.y = empty(block.o.shape[0], block.h)
+
+    def step(self, added, stream, allocator=None):
+        """added [tokens, h]: what the layer before this one adds to the residual stream
+        [tokens, h], which is updated in place.  Returns what the next one adds."""
+        mf.memfine_norm_fwd(EPS, added, self.w, R=stream, S=stream, Y=self.y)
+        return self.block.step(self.attention.step(self.y, allocator), stream, allocator)
+
+
+class TrainedLayer:
+    """out = block(X + attention(X))."""
+
+    def __init__(self, attention, block):
+        self.attention, self.block = attention, block
+        self.grads = {**attention.grads, **block.grads}
+
+    def forward(self, X):
+        self.x = X + self.attention.forward(X)
+        return self.block.forward(self.x)
+
+    def backward(self, X, dout):
+        d = self.block.backward(self.x, dout)
+        return d + self.attention.backward(X, d)
+
+    def balance(self, rate=1e-3):
+        self.block.balance(rate)
+
+
 def weights(gen, h, F, E, K):
     def normal(*shape, std):
         return (torch.randn(*shape, generator=gen, device="cuda") * std).to(torch.bfloat16)
@@ -235,40 +270,54 @@ def serve(p, gating, tokens, steps, mx8, gen):
     return start.elapsed_time(stop) / steps
 
 
-def serve_attention(h, heads, kv_heads, dim, tokens, context, steps, gen):
-    """Milliseconds a step of `tokens` sequences that have `context` tokens each."""
-    attn = mf.make_attn(heads, kv_heads, dim)
-    Wqkv = (torch.randn((heads + 2 * kv_heads) * dim, h, generator=gen, device="cuda") * h ** -0.5)
-    a = ServedAttention(Wqkv.to(torch.bfloat16), attn, tokens, context + steps + 3)
-    x = torch.randn(tokens, h, generator=gen, device="cuda").to(torch.bfloat16)
-    a.prompt(x.repeat_interleave(context, 0), [context] * tokens)
+def qkv_weight(gen, attn, h):
+    n = (attn.heads + 2 * attn.kv_heads) * attn.dim
+    return (torch.randn(n, h, generator=gen, device="cuda") * h ** -0.5).to(torch.bfloat16)
+
+
+def serve_layer(p, gating, attn, tokens, context, steps, mx8, gen):
+    """Milliseconds a step of attention and block, for `tokens` sequences that have `context`
+    tokens each."""
+    h = p["w"].numel()
+    a = ServedAttention(qkv_weight(gen, attn, h), attn, tokens, context + steps + 3)
+    layer = ServedLayer(torch.ones_like(p["w"]), a, ServedBlock(**p, gating=gating, tokens=tokens, mx8=mx8))
+    stream = torch.randn(tokens, h, generator=gen, device="cuda").to(torch.bfloat16)
+    a.prompt(stream.repeat_interleave(context, 0), [context] * tokens)
+    added = torch.zeros_like(stream)
     for _ in range(3):
-        a.step(x)
+        added = layer.step(added, stream)
     start, stop = (torch.cuda.Event(enable_timing=True) for _ in range(2))
     start.record()
     for _ in range(steps):
-        a.step(x)
+        added = layer.step(added, stream)
     stop.record()
     stop.synchronize()
     return start.elapsed_time(stop) / steps
 
 
-def train(p, gating, tokens, steps, gen, lr=0.02):
-    """Fits a fixed random map; returns the loss of every step."""
-    p = {n: v for n, v in p.items() if n != "Wo"}
-    block = TrainedBlock(**p, gating=gating, tokens=tokens)
-    master = {n: p[n].float() for n in block.grads}
+def train(p, gating, tokens, steps, gen, lr=0.02, attn=None):
+    """Fits a fixed random map; returns the loss of every step.  With attn the layer
+    begins with attention over three sequences, which the tokens are split into."""
+    Wo, p = p["Wo"], {n: v for n, v in p.items() if n != "Wo"}
+    layer = TrainedBlock(**p, gating=gating, tokens=tokens)
+    if attn is not None:
+        lens = [tokens // 2, tokens // 3]
+        p["Wqkv"], p["Wo"] = qkv_weight(gen, attn, p["w"].numel()), Wo
+        layer = TrainedLayer(TrainedAttention(p["Wqkv"], Wo, attn, [*lens, tokens - sum(lens)]), layer)
+    master = {n: p[n].float() for n in layer.grads}
     X = torch.randn(tokens, p["w"].numel(), generator=gen, device="cuda").to(torch.bfloat16)
     want = torch.randn(X.shape, generator=gen, device="cuda")
     losses = []
     for _ in range(steps):
-        diff = block.forward(X).float() - want
+        diff = layer.forward(X).float() - want
         losses.append(diff.square().mean().item())
-        block.backward(X, (2 / tokens * diff).to(torch.bfloat16))
+        layer.backward(X, (2 / tokens * diff).to(torch.bfloat16))
         for n, m in master.items():
-            m -= lr * block.grads[n]
+            g = layer.grads[n]
+            # (the attention has no norm in front: its weights move by 1 % of theirs at most)
+            m -= g * (torch.clamp(0.01 * m.norm() / g.norm(), max=lr) if n in ("Wqkv", "Wo") else lr)
             p[n].copy_(m)
-        block.balance()
+        layer.balance()
     return losses
 
 
@@ -287,12 +336,13 @@ def main():
     a = a.parse_args()
     gen = torch.Generator(device="cuda").manual_seed(0)
     gating = mf.make_gating(a.experts, a.topk, score="sigmoid", groups=4, top_groups=2, scale=2.5)
-    p = weights(gen, a.hidden, a.ffn, a.experts, a.hidden)
+    attn = mf.make_attn(a.heads, a.kv_heads, 128)
+    p = weights(gen, a.hidden, a.ffn, a.experts, attn.heads * attn.dim)
     ms = serve(p, gating, a.tokens, a.steps, not a.bf16, gen)
     print(f"served: {a.tokens} tokens, {'bf16' if a.bf16 else 'MX8'} activations, {ms * 1e3:.0f} us a step")
-    ms = serve_attention(a.hidden, a.heads, a.kv_heads, 128, a.tokens, a.context, a.steps, gen)
-    print(f"attention: {a.tokens} sequences of {a.context} tokens, MX8 cache, {ms * 1e3:.0f} us a step")
-    losses = train(p, gating, max(a.tokens, 256), a.steps, gen)
+    ms = serve_layer(p, gating, attn, a.tokens, a.context, a.steps, not a.bf16, gen)
+    print(f"with attention: {a.tokens} sequences of {a.context} tokens, MX8 cache, {ms * 1e3:.0f} us a step")
+    losses = train(p, gating, max(a.tokens, 256), a.steps, gen, attn=attn)
     print(f"trained: loss {losses[0]:.4f} -> {losses[-1]:.4f} in {a.steps} steps")
 
 

@@ -135,6 +135,72 @@ def test_trained_gradients(ex):
         assert rel <= 2 ** -5, (name, rel)
 
 
+def test_layer_joins_attention_and_block(ex):
+    """Served: the same bits as its calls one after the other.  Trained: the block's gradient goes
+    through the attention and past it (a block that passes its input on, so that
+    autograd in float64 knows the rest; tolerance as above)."""
+    t = torch()
+    gen = t.Generator(device="cuda").manual_seed(4)
+    attn, tokens, E = ex.mf.make_attn(H, HK, D), 6, 16
+    p = ex.weights(gen, HID, 128, E, H * D)
+    gating = ex.mf.make_gating(E, 4, score="sigmoid", groups=4, top_groups=2, scale=2.5)
+    W = ex.qkv_weight(gen, attn, HID)
+    parts = [(ex.ServedAttention(W, attn, tokens, 64), ex.ServedBlock(**p, gating=gating, tokens=tokens))
+             for _ in range(2)]
+    w = draw(HID, seed=6)
+    layer, (a, b) = ex.ServedLayer(w, *parts[0]), parts[1]
+    x = draw(tokens * 20, HID, seed=7)
+    a.prompt(x, [20] * tokens)
+    layer.attention.prompt(x, [20] * tokens)
+    stream, added = draw(tokens, HID, seed=8), draw(tokens, HID, seed=9)
+    s2, a2 = stream.clone(), added.clone()
+    for i in range(3):
+        log(f"served layer, step {i}")
+        added = layer.step(added, stream)
+        y = t.empty_like(s2)
+        ex.mf.memfine_norm_fwd(ex.EPS, a2, w, R=s2, S=s2, Y=y)
+        a2 = b.step(a.step(y), s2)
+        assert t.equal(added, a2) and t.equal(stream, s2) and bool(t.isfinite(added.float()).all())
+
+    class Through:
+        grads = {}
+
+        def forward(self, X):
+            return X
+
+        def backward(self, X, dout):
+            return dout
+    lens = [30, 1, 40]
+    Wo = draw(HID, H * D, seed=2, std=(H * D) ** -0.5)
+    layer = ex.TrainedLayer(ex.TrainedAttention(W, Wo, attn, lens), Through())
+    X, dout = draw(sum(lens), HID, seed=3), draw(sum(lens), HID, seed=4)
+    log("trained layer")
+    out = layer.forward(X)
+    dX = layer.backward(X, dout)
+    x, w, o = (y.double().requires_grad_() for y in (X, W, Wo))
+    qkv = (x @ w.t()).view(len(X), -1, D)
+    att = layer.attention
+    ref = x + t.cat([attention64(q, att.cos, att.sin) for q in qkv.split(lens)]) @ o.t()
+    grads = t.autograd.grad((ref * dout.double()).sum(), (x, w, o))
+    for name, got, want in (("out", out, ref), ("dX", dX, grads[0]), ("dWqkv", layer.grads["Wqkv"], grads[1]),
+                            ("dWo", layer.grads["Wo"], grads[2])):
+        rel = ((got.double() - want).norm() / want.norm()).item()
+        assert rel <= 2 ** -5, (name, rel)
+
+
+def test_training_with_attention_moves_the_weights(ex):
+    t = torch()
+    gen = t.Generator(device="cuda").manual_seed(5)
+    attn, E = ex.mf.make_attn(H, HK, D), 16
+    p = ex.weights(gen, HID, 128, E, H * D)
+    before = {n: v.clone() for n, v in p.items()}
+    gating = ex.mf.make_gating(E, 4, score="sigmoid", groups=4, top_groups=2, scale=2.5)
+    log("training with attention")
+    losses = ex.train(p, gating, 101, 3, gen, lr=0.1, attn=attn)
+    assert len(losses) == 3 and all(0 < x < float("inf") for x in losses)
+    assert not any(t.equal(p[n], before[n]) for n in ("Wo", "Wr", "W1", "W2"))
+
+
 def test_example_runs(ex, capsys, monkeypatch):
     monkeypatch.setattr(sys, "argv", ["moe_block.py", "--tokens", "4", "--steps", "2", "--hidden", "256", "--ffn",
                                       "128", "--experts", "8", "--topk", "2", "--context", "40", "--heads", "4",
