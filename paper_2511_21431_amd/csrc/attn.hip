@@ -930,22 +930,28 @@ bool short_rows(const AttnArgs& g) { return g.T < 2048 * (int64_t)g.seqs; }
 }  // namespace
 
 // Parts that the tiles of a group's queries are shared out in for dk and dv: one workgroup's
-// chain, all queries of the group against 256 keys (fp32: 128), is the shortest time it can
-// take, and few keys leave CUs idle; but parts are written and read again.  In microseconds:
-//   tile x max(chain / parts + 4, (half the chain / parts + 4) workgroups per CU) + sums
-// (a start and an end weigh four tiles; tile: 3.5, fp32 8; sums: 6 and 16 bytes an element of
-// dk at 3 TB/s.)  32 heads in 8 groups, dim 128, without and with two parts: one sequence of
-// 8192 tokens 2.41 ms and 1.72, 8 of 1024 354 us and 409; 64 heads in 8 groups, 4096 tokens, one,
-// three and four parts 1.22, 0.97 and 0.91 ms.
+// chain, all queries of the group that see any of 256 keys (fp32: 128), is the shortest time
+// it can take, and few keys leave CUs idle; but parts are written and read again.  In
+// microseconds:
+//   tile x max(chain / parts + 4, (load chain / parts + 4) workgroups per CU) + sums
+// (a start and an end weigh four tiles; load: the mean chain over the longest, .6 under a
+// causal mask, 1 where a short window or no mask makes all alike; tile: 3.5, fp32 8; sums: 6
+// and 16 bytes an element of dk at 3 TB/s.)  Dim 128, the whole gradient with one, two and four
+// parts: 32 heads in 8 groups, 8192 tokens 2.33, 1.79 and 1.81 ms (two are taken), a window of
+// 128 160, 208 and 271 us (one), 4 sequences of 1024 without a mask, 4 groups 481, 311 and 248 us
+// (four); 64 heads in 8 groups, 4096 tokens 1.85, 1.18 and 0.94 ms (four), a window of 512 399,
+// 309 and 335 us (two).
 int attn_parts(const AttnArgs& g) {
   const int group = g.heads / g.kv_heads, keys = g.f32 ? 128 : 256, rows = g.f32 ? 32 : 64;
   const double items = (double)blocks_of(g.T, g.seqs, keys) * g.kv_heads;
   const double mean = (double)g.T / std::max<int64_t>(std::min<int64_t>(g.seqs, g.T), 1);
-  const double chain = group * std::ceil(mean / rows);
+  const double seen = g.window > 0 ? std::min<double>(mean, g.window) : mean;
+  const double chain = group * std::ceil(std::min(mean, seen + keys) / rows);
+  const double load = g.causal ? 1. - .4 * seen / std::max(mean, 1.) : 1.;
   int best = 1;
   double least = 0.;
   for (int p = 1; p <= 32 && p <= chain; p *= 2) {
-    const double t = std::max(chain / p + 4., (.6 * chain / p + 4.) * items * p / g.cus) * (g.f32 ? 8. : 3.5) +
+    const double t = std::max(chain / p + 4., (load * chain / p + 4.) * items * p / g.cus) * (g.f32 ? 8. : 3.5) +
                      (p > 1 ? 6. + p * (double)g.T * g.kv_heads * g.dim * 16. / 3e6 : 0.);
     if (p == 1 || t < least) {
       best = p;

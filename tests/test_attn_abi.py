@@ -68,6 +68,31 @@ def test_packed_refusals():
     assert f(-1, 1, alone) < 0 and f(1, -1, alone) < 0 and f(1, 1, ctypes.byref(attn(heads=7))) < 0
 
 
+def test_parts_of_the_gradient_follow_what_keys_are_seen_by():
+    """Working memory of the gradient: none for partial sums where a short window leaves each
+    block of keys few queries, as with no window where it is as long as the sequence, and
+    never more with a window than without."""
+    f = _lib.lib().memfine_attn_bwd_workspace_bytes
+
+    def parts(T, seqs, **kw):
+        a = attn(**kw)
+        n = f(T, seqs, ctypes.byref(a)) - 2 * T * a.heads * 4
+        each = 2 * T * a.kv_heads * a.dim * 4
+        assert n % each == 0
+        return n // each
+    big = dict(heads=32, kv_heads=8, dim=128)
+    assert parts(8192, 1, **big) == 2
+    assert parts(8192, 1, window=128, **big) == parts(8192, 1, window=1024, **big) == 0
+    assert parts(8192, 4, window=512, **big) == 0
+    assert parts(4096, 1, causal=False, **big) == 2      # (all chains alike: two fill the device)
+    for T, seqs, kw in ((8192, 1, big), (2048, 1, dict(heads=16, kv_heads=2)), (6783, 2, dict(heads=2)),
+                        (900, 1, dict(heads=8, kv_heads=1, dtype=mf.F32))):
+        kw = {**kw, "kv_heads": kw.get("kv_heads", kw["heads"])}
+        whole = parts(T, seqs, **kw)
+        assert all(parts(T, seqs, window=w, **kw) <= whole for w in (1, 64, 300, 1000, 2 ** 31 - 1))
+        assert parts(T, seqs, window=T, **kw) == whole
+
+
 def test_rope_refusals():
     def f(T=4, seqs=1, off=P, heads=3, dim=64, dtype=0, cos=P, sin=P, n=8, inter=0, inv=0, X=P, ldx=192,
           Y=P, ldy=192, null=False):
