@@ -916,9 +916,14 @@ template <typename T, int D, int NW, bool kHeld> void run_dkv(const AttnArgs& g,
 // forward of two heads of 6783 tokens 141 us with one wave, 69 with four; 16 heads in 2 groups,
 // 2048 tokens 48 and 37; 32 heads in 8 groups, 512 tokens 15.6 and 13.3, 1024 tokens 26.9 both,
 // 2048 tokens 54 and 71; 8 sequences of 256 tokens, 8 heads 10.6 and 11.2.
+// Where no mask, or a window of at most half the sequence, makes all chains alike, none is left
+// to run alone at the end, and heads of 128 are better off from two sets a CU on: 16 heads in 4
+// groups, 2048 tokens, a window of 512 18 us with one wave and 28 with four, without a mask 48 and
+// 54; 8 heads in 2 groups, a window of 512 17 and 15 (16 heads of 64: 15.5 and 14.5).
 bool few_queries(const AttnArgs& g) {
   const int64_t sets = blocks_of(g.T, g.seqs, 32) * g.heads, mean = g.T / std::max(g.seqs, 1);
-  return sets <= 4 * g.cus && mean >= 384 && mean * g.cus > 200 * sets;
+  const bool alike = !g.causal || (g.window > 0 && g.window <= mean / 2);
+  return sets <= (alike && g.dim == 128 ? 2 : 4) * g.cus && mean >= 384 && mean * g.cus > 200 * sets;
 }
 // Sequences so short, on average, that the starts and ends of workgroups weigh more than
 // what twice the rows save of copies: four waves, several workgroups a CU, else eight (heads of

@@ -54,6 +54,16 @@ def test_long_sequences(mf, lens, heads, groups, D, kind):  # noqa: F811
     check_groups(Case(mf, lens, *heads, D, "bf16", before=3, after=2, **kw), groups)
 
 
+@pytest.mark.parametrize("kind", ("window", "all", "causal"))
+@pytest.mark.parametrize("heads,groups", [((8, 2), (1,)), ((16, 4), (0, 3))], ids=str)
+def test_few_heads_around_the_rule(mf, heads, groups, kind):  # noqa: F811
+    """Two and four sets of 32 queries a compute unit: the keys are shared out among four
+    waves, or not, as mask and window say."""
+    log(f"few heads {heads} {kind}")
+    kw = dict(causal=kind != "all", window=512 if kind == "window" else 0)
+    check_groups(Case(mf, [2048], *heads, 128, "bf16", **kw), groups)
+
+
 @pytest.mark.parametrize("D", (64, 128))
 def test_long_sequences_fp32(mf, D):  # noqa: F811
     log(f"long fp32 {D}")
