@@ -633,10 +633,11 @@ int memfine_attn_fwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32
  *   dQ_i = sum_j ds_ij k_j;  dK_j = sum_i ds_ij q_i;  dV_j = sum_i p_ij dO_i
  * dK and dV add up over the heads that share a key-value head.  dQ, dK and dV are
  * overwritten, rows of no sequence left as they were; they must not overlap the
- * inputs.  Every sum has a fixed order, which depends on T, seqs, the heads and the
- * device's compute units alone.  Working memory (two floats a row and head, and partial
- * dK and dV where keys are few: memfine_attn_bwd_workspace_bytes, < 0: invalid arguments)
- * comes from `alloc` as for the layer's calls.
+ * inputs.  Every sum, here and in the forward, has a fixed order, which depends on T, seqs,
+ * what `a` holds, the sequence's own length and the device's compute units alone.  Working
+ * memory (two floats a row and head, and partial dK and dV where keys are few:
+ * memfine_attn_bwd_workspace_bytes, < 0: invalid arguments) comes from `alloc` as for the
+ * layer's calls.
  */
 int memfine_attn_bwd(int64_t T, int32_t seqs, const memfine_attn* a, const int32_t* d_offsets,
                      const void* d_Q, int64_t ld_q, const void* d_K, int64_t ld_k, const void* d_V,
@@ -684,7 +685,8 @@ typedef struct memfine_cache {
 
 /*
  * New tokens into the cache: d_lengths counts them already, row i of the n that
- * sequence b brings is its token d_lengths[b] - n + i (a negative one is dropped).
+ * sequence b brings is its token d_lengths[b] - n + i (a negative one is dropped, and one
+ * that the table's width has no page for).
  *   d_offsets  the sequences' rows, packed as above, or null: T = seqs, row b is
  *              sequence b's
  *   d_K, d_V   bf16 [T, kv_heads, dim];  K is turned on its way if r is not null,
@@ -705,7 +707,8 @@ int memfine_kv_write(const memfine_cache* c, int64_t T, int32_t seqs, int32_t wi
  * with a->window, the last `window`): O_b and lse_b as memfine_attn_fwd's for the
  * last token of sequence b, but with the weights of the product with V to 2^-16 of
  * each.  A sequence without tokens gets zeros (lse -inf).
- *   a      kv_heads and dim as the cache's, dtype MEMFINE_BF16; causal is not used
+ *   a      kv_heads and dim as the cache's, dtype MEMFINE_BF16; causal 0 and 1 are the
+ *          same here, but a window is for causal = 1 alone, as everywhere
  *   d_Q    bf16 [seqs, heads, dim];  d_O  bf16 [seqs, heads, dim] out
  *   d_lse  float [seqs, heads] out, may be null
  * What pages hold past a sequence's tokens does not matter.  Sums are formed in an order

@@ -379,6 +379,20 @@ def test_decode_rounds_its_outputs_alone(mf, D, held):
         assert np.all(off <= 0), (n, float(off.max()), int((off > 0).sum()))
 
 
+def test_decode_is_the_same_causal_or_not(mf):
+    t = torch()
+    lens = [300, 0, 77]
+    p = Pages(mf, lens, 2, 64, 32, "bf16")
+    O, lse, q, _ = check_decode(mf, p, lens, 4)
+    P, m = t.zeros_like(O), t.zeros_like(lse)
+    log("not causal")
+    mf.memfine_attn_decode(mf.make_attn(4, 2, 64, causal=False), p.cache, p.dtable, ints(lens), q[:, :4], P, m)
+    assert t.equal(P, O) and t.equal(m, lse)
+    with pytest.raises(mf.MemfineError):
+        mf.memfine_attn_decode(mf.make_attn(4, 2, 64, causal=False, window=5), p.cache, p.dtable, ints(lens),
+                               q[:, :4], P, m)
+
+
 def test_decode_growing_scores(mf):
     t = torch()
     lens = [900]
