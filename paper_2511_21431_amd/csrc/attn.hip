@@ -16,10 +16,11 @@
 // values of a reduction step a register holds is the accumulator's choice, and
 // the other operand, read from LDS with a transposing load, follows it.
 //
-// Bound by the matrix cores where sequences are long, and by the clock that power
-// leaves them (1.6 to 1.9 GHz of 2.4 while these kernels run); next to them every score
-// costs vector instructions (exponent, sum, rounding), 35 to 60 % of the SIMDs' cycles,
-// which only another wave's products hide: two or more waves a SIMD.  Short sequences
+// Bound by the matrix cores where sequences are long, and by the clock (1.7 to 1.9 GHz
+// while the long calls of heads of 128 run, 2.4 in kernels that only move data); next to
+// them every score costs vector instructions (exponent, sum, rounding), 35 to 60 % of the
+// SIMDs' cycles, which only another wave's products hide: two or more waves a SIMD (fp32 with
+// heads of 128 has one, for its registers).  Short sequences
 // are bound by a workgroup's start (offsets, queries, first tile: about 4 us) and end.
 #include <algorithm>
 #include <cmath>
@@ -310,9 +311,10 @@ __device__ __forceinline__ bool locate(const int32_t* __restrict__ offsets, int 
   p.block = b - __builtin_amdgcn_readlane(inc - n, w);
   return true;
 }
-// Head and block of a workgroup.  All heads advance together through the blocks, in falling
-// order with `down`: under a causal mask the longest come first and the shortest
-// even out the end.  Workgroups go to the 8 XCDs in turn; with a multiple of 8 heads each
+// Head and block of a workgroup.  All heads advance together through the blocks of the whole
+// batch, in falling order with `down`: under a causal mask each sequence's longest come
+// first, and the shortest of the first sequence even out the end (the longest of a first
+// sequence that is longer than the others come late).  Workgroups go to the 8 XCDs in turn; with a multiple of 8 heads each
 // XCD has an eighth of them, neighbours, which share keys and values in its L2.
 __device__ __forceinline__ void work_item(int blocks, int heads, bool down, int& head, int& b) {
   const int id = blockIdx.x;
@@ -365,7 +367,8 @@ __device__ __forceinline__ void hide(f32x16_t& c, const Seen& s, int r0, int hh,
 // one starts or ends while others multiply.  Against tiles of 64, of which two fit, in
 // workgroups of four waves or, for long sequences, of eight: 8192 tokens of 32 heads in 8
 // groups, in sequences of 256 43 us against 47, of 668 66 and 71, one 515 and 514; with a window
-// of 512 82 and 98; 4096 tokens of 128 heads 549 and 575, 1.0 PFLOP/s.  D = 64: tiles of 64
+// of 512 82 and 98; 4096 tokens of 128 heads 549 and 575 (in other runs, at other clocks, 560 to
+// 620: 0.9 to 1.0 PFLOP/s).  D = 64: tiles of 64
 // keys, of which four fit: 8 sequences of 1024 tokens, 32 heads 56 us against 57.5 with tiles
 // of 32, two of 2048, 64 heads, not causal 146 and 160, but one of 8192, 16 heads 177 and 171.
 // (Two halves of a workgroup that multiply and exponentiate in turns, a barrier
@@ -415,6 +418,8 @@ void attn_fwd_kernel(const AttnArgs g, int blocks) {
   Frag<T> q[L::kSteps];
   load_rows<T, D>(q, (const T*)g.Q + (p.begin + i0) * g.ldq + head * D, g.ldq, mine, lane);
 
+  // (in base 2: a score's factor and, in the gradient, lse are rounded once more than for a
+  // natural exponent, 2^-24 of each, beside the D roundings of the score's own sum)
   const float c = g.scale * kLog2e;
   f32x16_t o[D / 32];
 #pragma unroll
@@ -472,7 +477,9 @@ void attn_fwd_kernel(const AttnArgs g, int blocks) {
 #pragma unroll
       for (int j = 0; j < L::kDown; ++j) {
         // the weights are rounded to the values' type, the matrix core's operand (their
-        // sum is not): half a step of bf16 each, which averages out over the row
+        // sum is not): half a step of bf16 each, with which outputs are 2.1e-3 of the
+        // 2-norm off where their own rounding is 1.6e-3.  A second product with what the rounding
+        // leaves out would be half as many again, and the matrix cores are the bound.
         const Frag<T> f = M::of(s[i], j);
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) M::mma(L::col(vs, 32 * d, (k0 + i) * L::kDown + j, lds_at), f, o[d]);
@@ -521,8 +528,9 @@ void attn_fwd_kernel(const AttnArgs g, int blocks) {
 // dq (shared out as in the forward), and their log2 of the weights' sum and delta for the
 // kernel below.  A block's ds is all that is held between its products, so that queries,
 // dO and dq stay in registers; four waves a workgroup, also for long sequences: 4096 tokens
-// of 64 heads in 8 groups, causal, 372 us, with eight waves 389; 6011 tokens of 16 heads of
-// 64 in 9 sequences 34 us.  The first runs at 1.1 PFLOP/s, its matrix cores busy for 61 %.
+// of 64 heads in 8 groups, causal, 372 us, with eight waves 389 (the shortest of a run; its
+// median is 390 to 400); 6011 tokens of 16 heads of 64 in 9 sequences 34 us.  The first runs at
+// 1.0 PFLOP/s, its matrix cores busy for 61 %.
 template <typename T, int D, int NW, int KS>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 4 ? 2 : 1)
 void attn_dq_kernel(const AttnArgs g, int blocks) {
@@ -619,7 +627,8 @@ void attn_dq_kernel(const AttnArgs g, int blocks) {
       if (!all) hide(s, own, r0 + 32 * i, hh, 0.f);
 #pragma unroll
       for (int j = 0; j < L::kDown; ++j) {
-        const Frag<T> f = M::of(s, j);  // (rounded as the forward's weights)
+        // (rounded as the forward's weights, and for its reason: 2.5e-3 for 1.8e-3)
+        const Frag<T> f = M::of(s, j);
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) M::mma(L::col(ks, 32 * d, (k0 + i) * L::kDown + j, lds_at), f, a[d]);
       }
@@ -648,7 +657,7 @@ void attn_dq_kernel(const AttnArgs g, int blocks) {
 // a run of these tiles and leaves its sums in fp32 for attn_sum_kernel.
 // kHeld: the values stay in LDS, not in registers, of which two waves a SIMD have 256 each:
 // keys, dk and dv take 160 of them (with the values too, or 64 keys a wave, they spill).
-// 4096 tokens of 64 heads in 8 groups of 128, causal: 537 us in four parts and 23 for their
+// 4096 tokens of 64 heads in 8 groups of 128, causal: 543 us in four parts and 23 for their
 // sum, 1.0 PFLOP/s, matrix cores busy for 55 %, vector instructions 34; 6011 tokens of 16
 // heads of 64 in 9 sequences 37 us (three waves a SIMD; two 41).
 template <typename T, int D, int NW, bool kHeld>

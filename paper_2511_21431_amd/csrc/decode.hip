@@ -3,7 +3,8 @@
 //   s_j = scale q . k_j over the sequence's tokens j (the last `window` of them,
 //   where there is one);  o = sum_j exp(s_j - lse) v_j,  lse = log sum_j exp(s_j)
 //
-// Bound by memory: every key and value is read once.  The tokens of all sequences
+// Bound by memory: every key and value is read once for each 16 heads that share it (64 of them:
+// four times, in runs that may lie far apart).  The tokens of all sequences
 // and key-value heads are laid end to end in steps of 128, of which each
 // workgroup takes an equal run, whatever the lengths are; runs end inside
 // sequences, whose parts (sums relative to a maximum of their own) a second
@@ -228,10 +229,11 @@ template <int D> struct Sums {
 
 // Two workgroups a CU, all resident, with the next step's loads in flight while one is
 // multiplied: 2 x 4 waves x 16 KiB a CU (bf16, D = 128), several times what the memory's
-// latency needs.  One sequence of 131072 tokens, 8 key-value heads of 128: 92 us, 5.8 TB/s;
-// 16 of 2048, 128 heads 370 us, 5.8 TB/s; in MX8 64 of 4096 on average, pages of 16, 64
-// heads in 8 groups 108 us, 5.1 TB/s (the values' way through LDS as bf16: two writes a
-// load with conflicts on 39 % of the cycles that LDS is busy, and vector instructions for 31 %).
+// latency needs.  One sequence of 131072 tokens, 8 key-value heads of 128: 93.5 us, 5.7 TB/s
+// (a plain kernel that only reads: 7.1); 16 of 2048, 128 heads 377 us, 5.7 TB/s; in MX8 64 of
+// 4096 on average, pages of 16, 64 heads in 8 groups 109 us, 5.1 TB/s (the values' way through
+// LDS as bf16: two writes a load with conflicts on 39 % of the cycles that LDS is busy, and
+// vector instructions for 34 %).
 template <int D, bool MX8>
 __global__ __launch_bounds__(256, 2) void decode_kernel(const DecodeArgs g) {
   typedef Held<D, MX8> H;
